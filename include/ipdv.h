@@ -32,7 +32,15 @@
  *                               indices (the other model's top-K), which
  *                               complete the union support of Eq. (6);
  *   source_split_kl          -- the per-position values of the source-split
- *                               objective (Eqs. (6), (10), (11)).
+ *                               objective (Eqs. (6), (10), (11));
+ *   rope_window              -- rotary positions of a window's queries and keys
+ *                               (and their gradient);
+ *   kv_append_q8, kv_read_q8 -- the window quantised into an 8-bit paged cache,
+ *                               and cached rows read back;
+ *   verify_attn_q8           -- the verification stage's attention over the
+ *                               8-bit cache;
+ *   sample_logits            -- a draw per row from logits, filtered by
+ *                               temperature, top-k, top-p and min-p.
  *
  * Conventions common to every entry point:
  *   - All array arguments are DEVICE pointers owned by the caller (except the
@@ -526,6 +534,168 @@ int source_split_kl(int M, int K,
                     const int32_t* cu, int B, float* seq_loss, float* t_ratio,
                     void* hip_stream);
 
+/* Pairs of channels that rope_window turns. */
+#define IPDV_ROPE_HALF 0          /* channels p and p + rot/2 */
+#define IPDV_ROPE_INTERLEAVED 1   /* channels 2p and 2p + 1 */
+
+/* Frequencies of long contexts (ipdv_rope_inv_freq). */
+#define IPDV_ROPE_PLAIN 0    /* f_p = base^(-2p/rot) */
+#define IPDV_ROPE_LINEAR 1   /* f_p / factor: positions interpolated */
+#define IPDV_ROPE_NTK 2      /* base * factor^(rot/(rot-2)): the lowest frequency is divided by factor */
+#define IPDV_ROPE_YARN 3     /* f_p / factor where a pair turns less than beta_slow times over
+                                original_len, f_p where more than beta_fast times, a ramp over p between */
+
+/*
+ * ipdv_rope_inv_freq -- the inverse frequencies of rope_window for a head of
+ * `rot` rotary channels.  Host arithmetic in double, rounded once: inv_freq
+ * [rot/2] is a HOST array.  *rope_factor (not NULL) becomes the factor to
+ * multiply the rotation with: 0.1 ln(factor) + 1 for IPDV_ROPE_YARN, else 1.
+ *
+ * Errors: IPDV_EINVAL (null pointer, rot odd or < 2, base not > 1 and finite,
+ * factor not >= 1 and finite, unknown kind; IPDV_ROPE_NTK with rot = 2;
+ * IPDV_ROPE_YARN with original_len < 1 or not beta_fast > beta_slow > 0).
+ */
+int ipdv_rope_inv_freq(int rot, double base, int kind, double factor, int original_len,
+                       double beta_fast, double beta_slow, float* inv_freq, float* rope_factor);
+
+/*
+ * rope_window -- rotary positions.  For row i of handled sequence b (position
+ * L_b + i), every head of q and k, and every pair (x, y) of its first `rot`
+ * channels:
+ *   x' = factor (x cos a - y sin a),  y' = factor (x sin a + y cos a),
+ *   a = (L_b + i) inv_freq[pair], in double; `inverse` turns by -a
+ * (with the same factor the transposed map: the gradient of q and k from that
+ * of q' and k').  Channels from `rot` on are copied.
+ *
+ * q [T, Hq, D], k [T, Hkv, D], q_out, k_out of the same shapes (dtype).  Heads
+ * and channels are dense; *_row_stride is the number of ELEMENTS from one row
+ * to the next (>= heads * D), so that q and k may be slices of one projection's
+ * output.  q_out == q and k_out == k (with equal strides) work in place; any
+ * other overlap does not.
+ * inv_freq [rot/2] float (device); ctx_lens, cu_q, seq_ids, n_seq, max_q as in
+ * verify_attn_paged.  Rows of other sequences are neither read nor written.
+ * Requirements: 2 <= rot <= D <= 512, rot even; n_seq <= 65535.
+ *
+ * Errors: IPDV_EINVAL, IPDV_EUNSUPPORTED (dtype, D, n_seq), IPDV_EHIP.
+ */
+int rope_window(const void* q, int64_t q_row_stride, const void* k, int64_t k_row_stride,
+                void* q_out, int64_t q_out_row_stride, void* k_out, int64_t k_out_row_stride,
+                const float* inv_freq, const int32_t* ctx_lens, const int32_t* cu_q,
+                const int32_t* seq_ids, int n_seq, int max_q, int Hq, int Hkv, int D, int rot,
+                int layout, float factor, int inverse, int dtype, void* hip_stream);
+
+/*
+ * kv_append_q8 -- the window's keys and values quantised into the 8-bit cache:
+ * rows i of every handled sequence go to positions L_b + i.
+ *
+ * One row of one KV head, keys and values apart, is stored in 8-bit floats
+ * (e4m3: 4 exponent, 3 mantissa bits, no infinities, largest 448) with a
+ * power-of-two scale:
+ *   e = the least integer >= -126 with max|x| <= 448 * 2^e  (0 if all are 0)
+ *   stored = x * 2^-e rounded to nearest even; scale byte = e + 127
+ * so that a stored value stands for stored * 2^e.  A row with an entry that is
+ * not finite is stored as NaN as a whole (scale byte 255).
+ *
+ * k_new, v_new [T, Hkv, D] (dtype), *_row_stride elements from one row to the
+ *                       next (>= Hkv * D)
+ * k_pages [num_pages, Hkv, D/16, page_size, 16]  e4m3 bytes: per KV head and 16
+ *                       channels, those of each slot in turn (channel d of a
+ *                       slot at [page][g][d/16][slot][d%16])
+ * v_pages [num_pages, Hkv, D, page_size]         e4m3 bytes, channel-major
+ * scales  [num_pages, Hkv, 2, page_size]         scale bytes: keys, values
+ * page_table, ctx_lens, cu_q, seq_ids, n_seq, max_q as in verify_attn_paged.
+ * Slots of other positions are left as they are.
+ * Requirements: D in {64, 128}, page_size 16, 32 or 64; pages, scales and the
+ * rows of k_new and v_new start on 16-byte boundaries.
+ *
+ * Errors: IPDV_EINVAL, IPDV_EUNSUPPORTED (D, page_size, dtype, alignment), IPDV_EHIP.
+ */
+int kv_append_q8(const void* k_new, int64_t k_row_stride, const void* v_new, int64_t v_row_stride,
+                 void* k_pages, void* v_pages, void* scales,
+                 const int32_t* page_table, int max_pages_per_seq,
+                 const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* seq_ids,
+                 int n_seq, int max_q, int Hkv, int D, int page_size, int num_pages,
+                 int dtype, void* hip_stream);
+
+/*
+ * kv_read_q8 -- rows of the 8-bit cache as values: positions L_b + i, i < k_b,
+ * of every handled sequence to rows cu_q[b] + i of k_out and v_out [T, Hkv, D]
+ * (dense, dtype).  With ctx_lens = 0 and the cached lengths in cu_q, whole
+ * sequences.  An e4m3 value times its scale is exact in fp32, and in bf16 down
+ * to 2^-133 (below, it is rounded); rows of scale byte 255 are NaN.  The other
+ * arguments, requirements and errors are those of kv_append_q8.
+ */
+int kv_read_q8(const void* k_pages, const void* v_pages, const void* scales,
+               const int32_t* page_table, int max_pages_per_seq,
+               const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* seq_ids,
+               int n_seq, int max_q, void* k_out, void* v_out,
+               int Hkv, int D, int page_size, int num_pages, int dtype, void* hip_stream);
+
+/* Workspace bytes verify_attn_q8 needs (0 if the arguments are invalid). */
+size_t ipdv_attn_q8_workspace_size(int n_seq, int Hq, int Hkv, int D, int max_q);
+
+/*
+ * verify_attn_q8 -- verification-stage attention over the 8-bit cache: with
+ * K_j and V_j the values that positions j = 0 .. L_b + i of KV head g stand for,
+ *   out[cu_q[b]+i, h, :] = softmax_j( scale * q[cu_q[b]+i, h, :] . K_j ) . V_j
+ * as in verify_attn_paged, but the window must already be in the cache
+ * (kv_append_q8 on the same stream).  A NaN row of the cache makes the rows
+ * that see it NaN, and no others; slots behind a sequence's last position may
+ * hold anything.
+ *
+ * q [T, Hq, D] (dtype), q_row_stride elements from one row to the next (>= Hq *
+ * D); out [T, Hq, D] dense (dtype).  bf16 and fp32, D in {64, 128}.  The pages
+ * as in kv_append_q8, the other arguments as in verify_attn_paged.  q's rows,
+ * out, the pages, scales and workspace start on 16-byte boundaries.
+ * The workspace is written by the call; two calls that may overlap need one each.
+ *
+ * Errors: IPDV_EINVAL, IPDV_EUNSUPPORTED (D, page_size, dtype, alignment, sizes
+ * as in verify_attn_paged), IPDV_EWORKSPACE, IPDV_EHIP.
+ */
+int verify_attn_q8(const void* q, int64_t q_row_stride,
+                   const void* k_pages, const void* v_pages, const void* scales,
+                   const int32_t* page_table, int max_pages_per_seq,
+                   const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* seq_ids,
+                   int n_seq, int max_q, void* out,
+                   int Hq, int Hkv, int D, int page_size, int num_pages, float scale,
+                   int dtype, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Workspace bytes sample_logits needs (0 if the arguments are invalid). */
+size_t ipdv_sample_logits_workspace_size(int M, int V);
+
+/*
+ * sample_logits -- one draw per row from logits, each row with its own filters.
+ *
+ * For row m let p = softmax(l / T), and order the vocabulary by logit
+ * descending, lower index first on equal logits.  Each filter keeps a prefix:
+ *   top-k: the first top_k[m] entries                      (<= 0: off)
+ *   top-p: as many of those as it takes for their mass to reach top_p[m] times
+ *          the mass that top-k left                        (>= 1 or NaN: off)
+ *   min-p: the entries with (l - max l) / T >= ln(min_p[m]) (<= 0 or NaN: off)
+ * and the shortest, of one entry at least, is drawn from:
+ *   token[m] = the first kept index v (index order) whose cumulative kept mass
+ *              exceeds u[m] times the kept mass
+ *   logp[m]  = ln of token[m]'s share of the kept mass (optional; NULL)
+ * Entries with less than e^-31.9 of the largest probability count as of
+ * probability zero.  Masses are fp32 exponentials (relative error about 1e-7
+ * each) summed exactly; a cut or a draw closer than that to a border may fall
+ * on the border's other side.  The same call repeats bit for bit.
+ * T = 0 draws the first entry of the order.  Entries of -inf are never drawn.  A
+ * row that holds NaN or +inf, or nothing above -inf, and a row whose T is
+ * negative or NaN, gets token -1 and logp NaN.
+ *
+ * logits [M, V] (dtype), row_stride elements from one row to the next (>= V);
+ * u [M] float in [0, 1); temperature, top_p, min_p [M] float and top_k [M]
+ * int32, each NULL for off (temperature: 1).  Requirements: M >= 0, 1 <= V <=
+ * 262144, M <= 16777215; workspace on a 16-byte boundary.
+ *
+ * Errors: IPDV_EINVAL, IPDV_EUNSUPPORTED (dtype, V, M), IPDV_EWORKSPACE, IPDV_EHIP.
+ */
+int sample_logits(const void* logits, int64_t row_stride, int M, int V, const float* u,
+                  const float* temperature, const int32_t* top_k, const float* top_p,
+                  const float* min_p, int32_t* token, float* logp, int dtype,
+                  void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /*
  * Optional timing hook for profilers and benchmarks (thread-local).  While
  * set, each kernel an entry point launches is bracketed by hipEventRecord of
@@ -540,7 +710,9 @@ int source_split_kl(int M, int K,
  * combine interval), lmhead_logsoftmax_verify 3 (the hidden rows' copy into the tiled
  * layout, empty where none is made; GEMM + epilogue; merge), accept_scan 1,
  * accept_scan_rule 1, sample_takeover 1, lmhead_sample 1, lmhead_pack_w 1,
- * lmhead_logp_gather 1, source_split_kl 1 (+1 with cu).
+ * lmhead_logp_gather 1, source_split_kl 1 (+1 with cu), rope_window 1,
+ * kv_append_q8 1, kv_read_q8 1, verify_attn_q8 2 (attention, merge of cut
+ * items), sample_logits 2 (chunks, rows).
  */
 int ipdv_trace_events(void* const* events, int capacity);
 int ipdv_trace_count(void);

@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OUT = os.path.join(HERE, "libipdv.so")
 BUILD_DIR = os.path.join(HERE, "_build")
-SOURCES = ["verify_attn.hip", "lmhead.hip", "accept_scan.hip", "kl.hip", "abi.cpp"]
+SOURCES = ["verify_attn.hip", "lmhead.hip", "accept_scan.hip", "kl.hip", "rope.hip", "kv_q8.hip",
+           "attn_q8.hip", "sample_logits.hip", "abi.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -25,10 +26,10 @@ FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function", "-I", INCLUDE, "-I", CSRC,
 ]
-# Per-source code generation flags.  The attention kernel keeps its MFMA
-# accumulators in arch VGPRs (it rescales them with VALU ops every block);
+# Per-source code generation flags.  The attention kernels keep their MFMA
+# accumulators in arch VGPRs (they rescale them with VALU ops);
 # the LM-head GEMM needs AGPRs for its 256-register accumulator tile.
-EXTRA = {"verify_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for src in ("verify_attn.hip", "attn_q8.hip")}
 
 
 def _run(cmd):

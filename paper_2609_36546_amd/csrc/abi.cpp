@@ -3,6 +3,7 @@
 // include/ipdv.h.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -464,6 +465,239 @@ int source_split_kl(int M, int K, const int32_t* s_idx, const float* s_logp, con
                    kl_rev, kl_fwd, loss, overlap, cu, cu ? B : 0, seq_loss, t_ratio};
   hipError_t e = ipdv::launch_source_split_kl(L, reinterpret_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return hip_fail("source_split_kl launch", e);
+  return ok();
+}
+
+static bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+int ipdv_rope_inv_freq(int rot, double base, int kind, double factor, int original_len,
+                       double beta_fast, double beta_slow, float* inv_freq, float* rope_factor) {
+  if (!inv_freq || !rope_factor) return fail(IPDV_EINVAL, "null required pointer");
+  if (rot < 2 || rot % 2 != 0) return fail(IPDV_EINVAL, "rot=%d must be even and >= 2", rot);
+  if (!(base > 1.0) || !std::isfinite(base)) return fail(IPDV_EINVAL, "base must be > 1 and finite");
+  if (!(factor >= 1.0) || !std::isfinite(factor)) return fail(IPDV_EINVAL, "factor must be >= 1 and finite");
+  if (kind < IPDV_ROPE_PLAIN || kind > IPDV_ROPE_YARN) return fail(IPDV_EINVAL, "unknown kind %d", kind);
+  if (kind == IPDV_ROPE_NTK && rot == 2) return fail(IPDV_EINVAL, "a scaled base needs rot > 2");
+  if (kind == IPDV_ROPE_YARN && (original_len < 1 || !(beta_slow > 0.0) || !(beta_fast > beta_slow) ||
+                                 !std::isfinite(beta_fast)))
+    return fail(IPDV_EINVAL, "original_len must be >= 1 and beta_fast > beta_slow > 0");
+  if (kind == IPDV_ROPE_NTK) base *= std::pow(factor, (double)rot / (rot - 2));
+  const int n = rot / 2;
+  // the pair that makes `turns` turns over the original length
+  auto pair_of = [&](double turns) {
+    return rot * std::log(original_len / (2.0 * M_PI * turns)) / (2.0 * std::log(base));
+  };
+  double lo = 0.0, hi = 0.0;
+  if (kind == IPDV_ROPE_YARN) {
+    lo = std::max(0.0, std::floor(pair_of(beta_fast)));
+    hi = std::min(n - 1.0, std::ceil(pair_of(beta_slow)));
+  }
+  for (int p = 0; p < n; ++p) {
+    double f = std::pow(base, -2.0 * p / rot);
+    if (kind == IPDV_ROPE_LINEAR) {
+      f /= factor;
+    } else if (kind == IPDV_ROPE_YARN) {
+      const double ramp = std::min(1.0, std::max(0.0, (p - lo) / std::max(hi - lo, 1e-3)));
+      f = f / factor * ramp + f * (1.0 - ramp);
+    }
+    inv_freq[p] = (float)f;
+  }
+  *rope_factor = kind == IPDV_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
+  return ok();
+}
+
+// The batch arguments that the window calls share.
+static int window_check(int n_seq, int max_q) {
+  if (n_seq < 0) return fail(IPDV_EINVAL, "n_seq must be >= 0 (got %d)", n_seq);
+  if (max_q < 1) return fail(IPDV_EINVAL, "max_q must be >= 1 (got %d)", max_q);
+  if (n_seq > 65535) return fail(IPDV_EUNSUPPORTED, "n_seq exceeds 65535");
+  return IPDV_OK;
+}
+
+int rope_window(const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out,
+                int64_t qo_stride, void* k_out, int64_t ko_stride, const float* inv_freq,
+                const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* seq_ids, int n_seq,
+                int max_q, int Hq, int Hkv, int D, int rot, int layout, float factor, int inverse,
+                int dtype, void* hip_stream) {
+  int st = window_check(n_seq, max_q);
+  if (st != IPDV_OK) return st;
+  if (Hq < 1 || Hkv < 1 || Hq > 65535 || Hkv > 65535) return fail(IPDV_EINVAL, "bad head counts %d, %d", Hq, Hkv);
+  if (D < 1 || D > 512) return fail(IPDV_EUNSUPPORTED, "head dim D=%d not in [1, 512]", D);
+  if (rot < 2 || rot > D || rot % 2 != 0)
+    return fail(IPDV_EINVAL, "rot=%d must be even and in [2, D=%d]", rot, D);
+  if (layout != IPDV_ROPE_HALF && layout != IPDV_ROPE_INTERLEAVED)
+    return fail(IPDV_EINVAL, "unknown layout %d", layout);
+  if (!std::isfinite(factor)) return fail(IPDV_EINVAL, "factor must be finite");
+  if (dtype != IPDV_F32 && dtype != IPDV_BF16) return fail(IPDV_EUNSUPPORTED, "dtype %d", dtype);
+  const int64_t nq = (int64_t)Hq * D, nk = (int64_t)Hkv * D;
+  if (q_stride < nq || qo_stride < nq || k_stride < nk || ko_stride < nk)
+    return fail(IPDV_EINVAL, "a row stride is shorter than the row");
+  if (n_seq == 0) return ok();
+  if (!q || !k || !q_out || !k_out || !inv_freq || !ctx_lens || !cu_q)
+    return fail(IPDV_EINVAL, "null required pointer");
+  if ((q_out == q && qo_stride != q_stride) || (k_out == k && ko_stride != k_stride))
+    return fail(IPDV_EINVAL, "in place, the row strides must be equal");
+  const int size = dtype == IPDV_BF16 ? 2 : 4;
+  const bool al16 = on16(q) && on16(k) && on16(q_out) && on16(k_out) &&
+                    (q_stride | k_stride | qo_stride | ko_stride) * size % 16 == 0;
+  ipdv::RopeLaunch L{q, k, q_stride, k_stride, q_out, k_out, qo_stride, ko_stride, inv_freq,
+                     ctx_lens, cu_q, seq_ids, n_seq, max_q, Hq, Hkv, D, rot,
+                     layout == IPDV_ROPE_INTERLEAVED, inverse != 0, factor, dtype == IPDV_BF16, al16};
+  hipError_t e = ipdv::launch_rope(L, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return hip_fail("rope_window launch", e);
+  return ok();
+}
+
+// Shape and pointer checks of the calls on the 8-bit cache.
+static int q8_check(int n_seq, int max_q, int Hkv, int D, int page_size, int num_pages,
+                    int max_pages, int dtype) {
+  int st = window_check(n_seq, max_q);
+  if (st != IPDV_OK) return st;
+  if (Hkv < 1) return fail(IPDV_EINVAL, "Hkv must be >= 1 (got %d)", Hkv);
+  if (max_pages < 1) return fail(IPDV_EINVAL, "max_pages_per_seq must be >= 1 (got %d)", max_pages);
+  if (num_pages < 1) return fail(IPDV_EINVAL, "num_pages must be >= 1 (got %d)", num_pages);
+  if (D != 64 && D != 128) return fail(IPDV_EUNSUPPORTED, "head dim D=%d not in {64, 128}", D);
+  if (!is_pow2(page_size) || page_size < 16 || page_size > 64)
+    return fail(IPDV_EUNSUPPORTED, "page_size=%d not in {16, 32, 64}", page_size);
+  if ((long)n_seq * Hkv > 65535) return fail(IPDV_EUNSUPPORTED, "n_seq * Hkv exceeds 65535");
+  if (dtype != IPDV_F32 && dtype != IPDV_BF16) return fail(IPDV_EUNSUPPORTED, "dtype %d", dtype);
+  return IPDV_OK;
+}
+
+static int kv_call(const char* what, bool append, const void* k_rows, int64_t k_stride,
+                   const void* v_rows, int64_t v_stride, const void* k_pages, const void* v_pages,
+                   const void* scales, const int32_t* page_table, int max_pages,
+                   const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* seq_ids, int n_seq,
+                   int max_q, int Hkv, int D, int page_size, int num_pages, int dtype,
+                   void* hip_stream) {
+  int st = q8_check(n_seq, max_q, Hkv, D, page_size, num_pages, max_pages, dtype);
+  if (st != IPDV_OK) return st;
+  if (k_stride < (int64_t)Hkv * D || v_stride < (int64_t)Hkv * D)
+    return fail(IPDV_EINVAL, "a row stride is shorter than the row");
+  if (n_seq == 0) return ok();
+  if (!k_rows || !v_rows || !k_pages || !v_pages || !scales || !page_table || !ctx_lens || !cu_q)
+    return fail(IPDV_EINVAL, "null required pointer");
+  const int size = dtype == IPDV_BF16 ? 2 : 4;
+  if (!on16(k_rows) || !on16(v_rows) || !on16(k_pages) || !on16(v_pages) || !on16(scales) ||
+      (k_stride | v_stride) * size % 16 != 0)
+    return fail(IPDV_EUNSUPPORTED, "rows, pages and scales must start on 16-byte boundaries");
+  ipdv::KvLaunch L{};
+  L.k_in = k_rows;
+  L.v_in = v_rows;
+  L.k_out = const_cast<void*>(k_rows);
+  L.v_out = const_cast<void*>(v_rows);
+  L.k_stride = k_stride;
+  L.v_stride = v_stride;
+  L.k_pages = static_cast<uint8_t*>(const_cast<void*>(k_pages));
+  L.v_pages = static_cast<uint8_t*>(const_cast<void*>(v_pages));
+  L.scales = static_cast<uint8_t*>(const_cast<void*>(scales));
+  L.page_table = page_table;
+  L.max_pages = max_pages;
+  L.ctx_lens = ctx_lens;
+  L.cu_q = cu_q;
+  L.seq_ids = seq_ids;
+  L.n_seq = n_seq;
+  L.max_q = max_q;
+  L.Hkv = Hkv;
+  L.D = D;
+  L.page_size = page_size;
+  L.log2ps = __builtin_ctz((unsigned)page_size);
+  L.num_pages = num_pages;
+  L.dtype_bf16 = dtype == IPDV_BF16;
+  hipError_t e = ipdv::launch_kv_q8(L, append, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return hip_fail(what, e);
+  return ok();
+}
+
+int kv_append_q8(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                 void* k_pages, void* v_pages, void* scales, const int32_t* page_table,
+                 int max_pages, const int32_t* ctx_lens, const int32_t* cu_q,
+                 const int32_t* seq_ids, int n_seq, int max_q, int Hkv, int D, int page_size,
+                 int num_pages, int dtype, void* hip_stream) {
+  return kv_call("kv_append_q8 launch", true, k_new, k_stride, v_new, v_stride, k_pages, v_pages,
+                 scales, page_table, max_pages, ctx_lens, cu_q, seq_ids, n_seq, max_q, Hkv, D,
+                 page_size, num_pages, dtype, hip_stream);
+}
+
+int kv_read_q8(const void* k_pages, const void* v_pages, const void* scales,
+               const int32_t* page_table, int max_pages, const int32_t* ctx_lens,
+               const int32_t* cu_q, const int32_t* seq_ids, int n_seq, int max_q, void* k_out,
+               void* v_out, int Hkv, int D, int page_size, int num_pages, int dtype,
+               void* hip_stream) {
+  const int64_t row = (int64_t)Hkv * D;
+  return kv_call("kv_read_q8 launch", false, k_out, row, v_out, row, k_pages, v_pages, scales,
+                 page_table, max_pages, ctx_lens, cu_q, seq_ids, n_seq, max_q, Hkv, D, page_size,
+                 num_pages, dtype, hip_stream);
+}
+
+size_t ipdv_attn_q8_workspace_size(int n_seq, int Hq, int Hkv, int D, int max_q) {
+  if (attn_shape_check(n_seq, Hq, Hkv, D, max_q, 1, 16) != IPDV_OK) return 0;
+  return ipdv::attn_q8_workspace(n_seq, Hq, Hkv, D, max_q);
+}
+
+int verify_attn_q8(const void* q, int64_t q_stride, const void* k_pages, const void* v_pages,
+                   const void* scales, const int32_t* page_table, int max_pages,
+                   const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* seq_ids, int n_seq,
+                   int max_q, void* out, int Hq, int Hkv, int D, int page_size, int num_pages,
+                   float scale, int dtype, void* workspace, size_t workspace_bytes,
+                   void* hip_stream) {
+  int st = attn_shape_check(n_seq, Hq, Hkv, D, max_q, max_pages, page_size);
+  if (st != IPDV_OK) return st;
+  st = q8_check(n_seq, max_q, Hkv, D, page_size, num_pages, max_pages, dtype);
+  if (st != IPDV_OK) return st;
+  if (!std::isfinite(scale) || !(scale > 0.f)) return fail(IPDV_EINVAL, "scale must be positive and finite");
+  if (q_stride < (int64_t)Hq * D) return fail(IPDV_EINVAL, "a row stride is shorter than the row");
+  if (n_seq == 0) return ok();
+  if (!q || !k_pages || !v_pages || !scales || !page_table || !ctx_lens || !cu_q || !out)
+    return fail(IPDV_EINVAL, "null required pointer");
+  const size_t need = ipdv::attn_q8_workspace(n_seq, Hq, Hkv, D, max_q);
+  if (!workspace || workspace_bytes < need)
+    return fail(IPDV_EWORKSPACE, "workspace of %zu bytes needed (got %zu)", need,
+                workspace ? workspace_bytes : (size_t)0);
+  const int size = dtype == IPDV_BF16 ? 2 : 4;
+  if (!on16(q) || !on16(out) || !on16(k_pages) || !on16(v_pages) || !on16(scales) ||
+      !on16(workspace) || q_stride * size % 16 != 0)
+    return fail(IPDV_EUNSUPPORTED, "q's rows, out, pages, scales and workspace must start on 16-byte boundaries");
+  ipdv::AttnQ8Launch L{q, q_stride, k_pages, v_pages, scales, page_table, max_pages, ctx_lens,
+                       cu_q, seq_ids, n_seq, max_q, out, Hq, Hkv, D, page_size, num_pages, scale,
+                       dtype == IPDV_BF16, workspace};
+  hipError_t e = ipdv::launch_attn_q8(L, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return hip_fail("verify_attn_q8 launch", e);
+  return ok();
+}
+
+static int sample_shape_check(int M, int V) {
+  if (M < 0) return fail(IPDV_EINVAL, "M must be >= 0 (got %d)", M);
+  if (V < 1) return fail(IPDV_EINVAL, "V must be >= 1 (got %d)", V);
+  if (V > 262144) return fail(IPDV_EUNSUPPORTED, "V=%d exceeds 262144", V);
+  if (M > 16777215) return fail(IPDV_EUNSUPPORTED, "M too large");
+  return IPDV_OK;
+}
+
+size_t ipdv_sample_logits_workspace_size(int M, int V) {
+  if (sample_shape_check(M, V) != IPDV_OK) return 0;
+  return ipdv::sample_logits_workspace(M, V);
+}
+
+int sample_logits(const void* logits, int64_t stride, int M, int V, const float* u,
+                  const float* temperature, const int32_t* top_k, const float* top_p,
+                  const float* min_p, int32_t* token, float* logp, int dtype, void* workspace,
+                  size_t workspace_bytes, void* hip_stream) {
+  int st = sample_shape_check(M, V);
+  if (st != IPDV_OK) return st;
+  if (dtype != IPDV_F32 && dtype != IPDV_BF16) return fail(IPDV_EUNSUPPORTED, "dtype %d", dtype);
+  if (stride < V) return fail(IPDV_EINVAL, "the row stride is shorter than the row");
+  if (M == 0) return ok();
+  if (!logits || !u || !token) return fail(IPDV_EINVAL, "null required pointer");
+  const size_t need = ipdv::sample_logits_workspace(M, V);
+  if (!workspace || workspace_bytes < need)
+    return fail(IPDV_EWORKSPACE, "workspace of %zu bytes needed (got %zu)", need,
+                workspace ? workspace_bytes : (size_t)0);
+  if (!on16(workspace)) return fail(IPDV_EUNSUPPORTED, "workspace must start on a 16-byte boundary");
+  ipdv::SampleLogitsLaunch L{logits, stride, M, V, u, temperature, top_k, top_p, min_p, token, logp,
+                             dtype == IPDV_BF16, workspace};
+  hipError_t e = ipdv::launch_sample_logits(L, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return hip_fail("sample_logits launch", e);
   return ok();
 }
 

@@ -173,6 +173,89 @@ struct KlLaunch {
 
 hipError_t launch_source_split_kl(const KlLaunch& L, hipStream_t st);
 
+// ---- rotary positions ----
+struct RopeLaunch {
+  const void* q;
+  const void* k;
+  int64_t q_stride, k_stride;  // elements from one row to the next
+  void* q_out;
+  void* k_out;
+  int64_t qo_stride, ko_stride;
+  const float* inv_freq;       // [rot / 2]
+  const int32_t* ctx_lens;
+  const int32_t* cu_q;
+  const int32_t* seq_ids;
+  int n_seq, max_q, Hq, Hkv, D, rot;
+  bool interleaved, inverse;
+  float factor;
+  bool dtype_bf16;
+  bool al16;                   // every row starts on 16 bytes
+};
+
+hipError_t launch_rope(const RopeLaunch& L, hipStream_t st);
+
+// ---- the 8-bit cache ----
+struct KvLaunch {
+  const void* k_in;            // append: rows [T, Hkv, D]
+  const void* v_in;
+  void* k_out;                 // read: rows [T, Hkv, D]
+  void* v_out;
+  int64_t k_stride, v_stride;  // elements from one row to the next
+  uint8_t* k_pages;
+  uint8_t* v_pages;
+  uint8_t* scales;
+  const int32_t* page_table;
+  int max_pages;
+  const int32_t* ctx_lens;
+  const int32_t* cu_q;
+  const int32_t* seq_ids;
+  int n_seq, max_q, Hkv, D, page_size, log2ps, num_pages;
+  bool dtype_bf16;
+};
+
+hipError_t launch_kv_q8(const KvLaunch& L, bool append, hipStream_t st);
+
+struct AttnQ8Launch {
+  const void* q;
+  int64_t q_stride;
+  const void* k_pages;
+  const void* v_pages;
+  const void* scales;
+  const int32_t* page_table;
+  int max_pages;
+  const int32_t* ctx_lens;
+  const int32_t* cu_q;
+  const int32_t* seq_ids;
+  int n_seq, max_q;
+  void* out;
+  int Hq, Hkv, D, page_size, num_pages;
+  float scale;
+  bool dtype_bf16;
+  void* workspace;
+};
+
+size_t attn_q8_workspace(int n_seq, int Hq, int Hkv, int D, int max_q);
+hipError_t launch_attn_q8(const AttnQ8Launch& L, hipStream_t st);
+
+// ---- filtered draws from logits ----
+struct SampleLogitsLaunch {
+  const void* logits;          // [M, V]
+  int64_t stride;              // elements from one row to the next
+  int M, V;
+  const float* u;
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  int32_t* token;
+  float* logp;
+  bool dtype_bf16;
+  void* workspace;
+};
+
+size_t sample_logits_workspace(int M, int V);
+hipError_t launch_sample_logits(const SampleLogitsLaunch& L, hipStream_t st);
+
 // ---- verdict scan ----
 struct ScanLaunch {
   const int32_t* cu_q;

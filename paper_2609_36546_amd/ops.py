@@ -81,6 +81,28 @@ def lib() -> ctypes.CDLL:
         L.sample_takeover.argtypes = [vp, vp, ci, ci, ci, ci, vp, cs, i32p, ci, i32p, u8p, i32p,
                                       i32p, f32p, ctypes.c_int32, i32p, u8p, ci, vp]
         L.sample_takeover.restype = ci
+        i64, cd = ctypes.c_int64, ctypes.c_double
+        L.ipdv_rope_inv_freq.argtypes = [ci, cd, ci, cd, ci, cd, cd, vp, ctypes.POINTER(cf)]
+        L.ipdv_rope_inv_freq.restype = ci
+        L.rope_window.argtypes = ([vp, i64] * 4 + [f32p, i32p, i32p, i32p] + [ci] * 7 +
+                                  [cf, ci, ci, vp])
+        L.rope_window.restype = ci
+        L.kv_append_q8.argtypes = [vp, i64, vp, i64, vp, vp, vp, i32p, ci, i32p, i32p, i32p,
+                                   ci, ci, ci, ci, ci, ci, ci, vp]
+        L.kv_append_q8.restype = ci
+        L.kv_read_q8.argtypes = [vp, vp, vp, i32p, ci, i32p, i32p, i32p, ci, ci, vp, vp,
+                                 ci, ci, ci, ci, ci, vp]
+        L.kv_read_q8.restype = ci
+        L.ipdv_attn_q8_workspace_size.argtypes = [ci] * 5
+        L.ipdv_attn_q8_workspace_size.restype = cs
+        L.verify_attn_q8.argtypes = [vp, i64, vp, vp, vp, i32p, ci, i32p, i32p, i32p, ci, ci, vp,
+                                     ci, ci, ci, ci, ci, cf, ci, vp, cs, vp]
+        L.verify_attn_q8.restype = ci
+        L.ipdv_sample_logits_workspace_size.argtypes = [ci, ci]
+        L.ipdv_sample_logits_workspace_size.restype = cs
+        L.sample_logits.argtypes = [vp, i64, ci, ci, f32p, f32p, i32p, f32p, f32p, i32p, f32p, ci,
+                                    vp, cs, vp]
+        L.sample_logits.restype = ci
         L.ipdv_trace_events.argtypes = [ctypes.c_void_p, ci]
         L.ipdv_trace_events.restype = ci
         L.ipdv_trace_count.restype = ci
@@ -596,3 +618,261 @@ def lmhead_sample(hidden, W, K: int, workspace, u, token=None):
                              code, _stream(dev))
     _check("lmhead_sample", st)
     return token
+
+
+# ---------------------------------------------------------------------------
+# The 8-bit cache and what stands around it: rotary positions, the quantised
+# append and its read-back, attention over it, filtered draws from logits.
+
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_YARN = 0, 1, 2, 3
+
+
+def _need_rows(t: torch.Tensor, name: str, dtype, device, ndim: int) -> int:
+    """Like _need, but rows (dim 0) may lie further apart than they are long,
+    as in a slice of a wider projection.  Returns the row stride in elements."""
+    if isinstance(t, torch.Tensor) and t.dim() == ndim and t.shape[0] > 0 and not t.is_contiguous():
+        _need(t[0], name, dtype, device, ndim - 1)
+        if t.shape[0] > 1:
+            return t.stride(0)
+    else:
+        _need(t, name, dtype, device, ndim)
+    n = 1
+    for s in t.shape[1:]:
+        n *= s
+    return n
+
+
+def _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev):
+    _need(ctx_lens, "ctx_lens", torch.int32, dev, 1)
+    _need(cu_q, "cu_q", torch.int32, dev, 1)
+    B = ctx_lens.shape[0]
+    if cu_q.shape[0] != B + 1:
+        raise ValueError("cu_q must be [B+1]")
+    if seq_ids is not None:
+        _need(seq_ids, "seq_ids", torch.int32, dev, 1)
+        if n_seq is not None and n_seq > seq_ids.shape[0]:
+            raise ValueError("n_seq exceeds seq_ids")
+        return seq_ids.shape[0] if n_seq is None else n_seq
+    if n_seq is not None and n_seq > B:
+        raise ValueError("n_seq exceeds the batch")
+    return B if n_seq is None else n_seq
+
+
+def rope_inv_freq(rot: int, base: float = 10000.0, kind: int = ROPE_PLAIN, factor: float = 1.0,
+                  original_len: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """Inverse frequencies [rot/2] (float32, on the CPU) and the factor on the
+    rotation (see ipdv_rope_inv_freq)."""
+    out = torch.empty(max(int(rot), 2) // 2, dtype=torch.float32)
+    f = ctypes.c_float(1.0)
+    st = lib().ipdv_rope_inv_freq(int(rot), float(base), int(kind), float(factor), int(original_len),
+                                  float(beta_fast), float(beta_slow), out.data_ptr(), ctypes.byref(f))
+    _check("ipdv_rope_inv_freq", st)
+    return out, float(f.value)
+
+
+def rope_window(q, k, inv_freq, ctx_lens, cu_q, max_q: int, seq_ids=None,
+                n_seq: Optional[int] = None, layout: int = ROPE_HALF, factor: float = 1.0,
+                inverse: bool = False, q_out=None, k_out=None):
+    """Rotary positions of a window's queries and keys (see include/ipdv.h).
+
+    q [T,Hq,D], k [T,Hkv,D] (bf16 or fp32; rows may be strided), inv_freq
+    [rot/2] float32, ctx_lens [B], cu_q [B+1], seq_ids [n] int32 or None.
+    inverse=True turns back: the gradient of q and k.  q_out / k_out may be q /
+    k (in place).  Returns (q_out, k_out)."""
+    dev, dt = q.device, q.dtype
+    code = _dtype_code(dt)
+    qs = _need_rows(q, "q", dt, dev, 3)
+    ks = _need_rows(k, "k", dt, dev, 3)
+    T, Hq, D = q.shape
+    Hkv = k.shape[1]
+    if k.shape != (T, Hkv, D):
+        raise ValueError("k must be [T,Hkv,D]")
+    _need(inv_freq, "inv_freq", torch.float32, dev, 1)
+    n_seq = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
+    if q_out is None:
+        q_out = torch.empty(T, Hq, D, dtype=dt, device=dev)
+    if k_out is None:
+        k_out = torch.empty(T, Hkv, D, dtype=dt, device=dev)
+    if q_out.shape != q.shape or k_out.shape != k.shape:
+        raise ValueError("q_out and k_out must have the shapes of q and k")
+    qos = _need_rows(q_out, "q_out", dt, dev, 3)
+    kos = _need_rows(k_out, "k_out", dt, dev, 3)
+    if T == 0:
+        n_seq = 0
+    st = lib().rope_window(_ptr(q), qs, _ptr(k), ks, _ptr(q_out), qos, _ptr(k_out), kos,
+                           _ptr(inv_freq), _ptr(ctx_lens), _ptr(cu_q), _ptr(seq_ids), n_seq, max_q,
+                           Hq, Hkv, D, 2 * inv_freq.shape[0], int(layout), float(factor),
+                           int(bool(inverse)), code, _stream(dev))
+    _check("rope_window", st)
+    return q_out, k_out
+
+
+class Q8Cache:
+    """A paged 8-bit cache (see kv_append_q8 in include/ipdv.h): ``k``
+    [P,Hkv,D/16,ps,16] and ``v`` [P,Hkv,D,ps] in float8_e4m3fn, ``scale``
+    [P,Hkv,2,ps] uint8.  The three tensors are the caller's."""
+
+    def __init__(self, k, v, scale):
+        dev = k.device
+        _need(k, "k", torch.float8_e4m3fn, dev, 5)
+        _need(v, "v", torch.float8_e4m3fn, dev, 4)
+        _need(scale, "scale", torch.uint8, dev, 4)
+        P, Hkv, D, ps = v.shape
+        if k.shape != (P, Hkv, D // 16, ps, 16) or scale.shape != (P, Hkv, 2, ps) or D % 16:
+            raise ValueError("k must be [P,Hkv,D/16,ps,16], v [P,Hkv,D,ps] and scale [P,Hkv,2,ps]")
+        self.k, self.v, self.scale = k, v, scale
+        self.num_pages, self.Hkv, self.D, self.page_size = P, Hkv, D, ps
+
+    @classmethod
+    def empty(cls, num_pages: int, Hkv: int, D: int, page_size: int = 16, device="cuda"):
+        """An unwritten cache of `num_pages` pages."""
+        f8 = torch.float8_e4m3fn
+        return cls(torch.empty(num_pages, Hkv, D // 16, page_size, 16, dtype=f8, device=device),
+                   torch.empty(num_pages, Hkv, D, page_size, dtype=f8, device=device),
+                   torch.empty(num_pages, Hkv, 2, page_size, dtype=torch.uint8, device=device))
+
+    @property
+    def device(self):
+        return self.k.device
+
+
+def _q8_table(cache: Q8Cache, page_table, ctx_lens, dev):
+    if not isinstance(cache, Q8Cache):
+        raise TypeError("cache must be a Q8Cache")
+    if cache.device != dev:
+        raise ValueError(f"cache must be on {dev} (is on {cache.device})")
+    _need(page_table, "page_table", torch.int32, dev, 2)
+    if page_table.shape[0] != ctx_lens.shape[0]:
+        raise ValueError("page_table must be [B, maxp]")
+
+
+def kv_append_q8(k_new, v_new, cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int,
+                 seq_ids=None, n_seq: Optional[int] = None, validate: bool = False):
+    """Quantise the window's keys and values [T,Hkv,D] (bf16 or fp32; rows may
+    be strided) into the cache at positions ctx_lens[b] + i (see
+    include/ipdv.h).  validate=True first runs check_page_table on host copies."""
+    dev, dt = k_new.device, k_new.dtype
+    code = _dtype_code(dt)
+    ks = _need_rows(k_new, "k_new", dt, dev, 3)
+    vs = _need_rows(v_new, "v_new", dt, dev, 3)
+    n_seq = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
+    _q8_table(cache, page_table, ctx_lens, dev)
+    T = k_new.shape[0]
+    if k_new.shape != (T, cache.Hkv, cache.D) or v_new.shape != k_new.shape:
+        raise ValueError("k_new and v_new must be [T,Hkv,D] of the cache's heads")
+    if validate:
+        check_page_table(page_table, ctx_lens, cu_q, max_q, cache.page_size, cache.num_pages,
+                         seq_ids=seq_ids, n_seq=n_seq)
+    if T == 0:
+        n_seq = 0
+    st = lib().kv_append_q8(_ptr(k_new), ks, _ptr(v_new), vs, _ptr(cache.k), _ptr(cache.v),
+                            _ptr(cache.scale), _ptr(page_table), page_table.shape[1], _ptr(ctx_lens),
+                            _ptr(cu_q), _ptr(seq_ids), n_seq, max_q, cache.Hkv, cache.D,
+                            cache.page_size, cache.num_pages, code, _stream(dev))
+    _check("kv_append_q8", st)
+
+
+def kv_read_q8(cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int, rows: int, seq_ids=None,
+               n_seq: Optional[int] = None, dtype=torch.bfloat16, k_out=None, v_out=None):
+    """The values that positions ctx_lens[b] + i stand for, as rows cu_q[b] + i
+    of two [rows,Hkv,D] tensors (see include/ipdv.h); with ctx_lens zero and
+    the cached lengths in cu_q, whole sequences.  Returns (k, v)."""
+    dev = cache.device
+    code = _dtype_code(dtype)
+    n_seq = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
+    _q8_table(cache, page_table, ctx_lens, dev)
+    shape = (int(rows), cache.Hkv, cache.D)
+    k_out = torch.empty(shape, dtype=dtype, device=dev) if k_out is None else k_out
+    v_out = torch.empty(shape, dtype=dtype, device=dev) if v_out is None else v_out
+    _need(k_out, "k_out", dtype, dev, 3)
+    _need(v_out, "v_out", dtype, dev, 3)
+    if tuple(k_out.shape) != shape or tuple(v_out.shape) != shape:
+        raise ValueError("k_out and v_out must be [rows,Hkv,D]")
+    if shape[0] == 0:
+        n_seq = 0
+    st = lib().kv_read_q8(_ptr(cache.k), _ptr(cache.v), _ptr(cache.scale), _ptr(page_table),
+                          page_table.shape[1], _ptr(ctx_lens), _ptr(cu_q), _ptr(seq_ids), n_seq,
+                          max_q, _ptr(k_out), _ptr(v_out), cache.Hkv, cache.D, cache.page_size,
+                          cache.num_pages, code, _stream(dev))
+    _check("kv_read_q8", st)
+    return k_out, v_out
+
+
+def attn_q8_workspace_size(n_seq, Hq, Hkv, D, max_q) -> int:
+    return int(lib().ipdv_attn_q8_workspace_size(n_seq, Hq, Hkv, D, max_q))
+
+
+def verify_attn_q8(q, cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int, seq_ids=None,
+                   n_seq: Optional[int] = None, scale: Optional[float] = None, out=None,
+                   workspace=None):
+    """Causal GQA attention of the window rows q [T,Hq,D] (bf16 or fp32; rows
+    may be strided) over the 8-bit cache, which already holds the window (see
+    include/ipdv.h).  Returns out [T,Hq,D]."""
+    dev, dt = q.device, q.dtype
+    code = _dtype_code(dt)
+    qs = _need_rows(q, "q", dt, dev, 3)
+    n_seq = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
+    _q8_table(cache, page_table, ctx_lens, dev)
+    T, Hq, D = q.shape
+    if D != cache.D:
+        raise ValueError("q and the cache have different head dims")
+    if scale is None:
+        scale = 1.0 / math.sqrt(D)
+    if out is None:
+        out = torch.empty(T, Hq, D, dtype=dt, device=dev)
+    else:
+        _need(out, "out", dt, dev, 3)
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+    if T == 0:
+        n_seq = 0
+    if workspace is None:
+        need = attn_q8_workspace_size(n_seq, Hq, cache.Hkv, D, max_q)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    st = lib().verify_attn_q8(_ptr(q), qs, _ptr(cache.k), _ptr(cache.v), _ptr(cache.scale),
+                              _ptr(page_table), page_table.shape[1], _ptr(ctx_lens), _ptr(cu_q),
+                              _ptr(seq_ids), n_seq, max_q, _ptr(out), Hq, cache.Hkv, D,
+                              cache.page_size, cache.num_pages, float(scale), code, _ptr(workspace),
+                              workspace.numel() * workspace.element_size(), _stream(dev))
+    _check("verify_attn_q8", st)
+    return out
+
+
+def sample_logits_workspace_size(M, V) -> int:
+    return int(lib().ipdv_sample_logits_workspace_size(M, V))
+
+
+def sample_logits(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, token=None,
+                  logp=None, workspace=None):
+    """One draw per row of logits [M,V] (bf16 or fp32; rows may be strided),
+    each row with its own temperature, top_p, min_p [M] float32 and top_k [M]
+    int32 (each None for off), from uniforms u [M] float32 in [0, 1) (see
+    include/ipdv.h).  Returns (token [M] int32, logp [M] float32): the draws and
+    their log-probs among what the filters kept."""
+    dev, dt = logits.device, logits.dtype
+    code = _dtype_code(dt)
+    ls = _need_rows(logits, "logits", dt, dev, 2)
+    M, V = logits.shape
+    for t, name, d in ((u, "u", torch.float32), (temperature, "temperature", torch.float32),
+                       (top_k, "top_k", torch.int32), (top_p, "top_p", torch.float32),
+                       (min_p, "min_p", torch.float32)):
+        if t is not None or name == "u":
+            _need(t, name, d, dev, 1)
+            if t.shape[0] != M:
+                raise ValueError(f"{name} must be [M]")
+    token = torch.empty(M, dtype=torch.int32, device=dev) if token is None else token
+    logp = torch.empty(M, dtype=torch.float32, device=dev) if logp is None else logp
+    _need(token, "token", torch.int32, dev, 1)
+    _need(logp, "logp", torch.float32, dev, 1)
+    if token.shape[0] != M or logp.shape[0] != M:
+        raise ValueError("token and logp must be [M]")
+    if workspace is None:
+        workspace = torch.empty(max(sample_logits_workspace_size(M, V), 1), dtype=torch.uint8,
+                                device=dev)
+    st = lib().sample_logits(_ptr(logits), ls, M, V, _ptr(u), _ptr(temperature), _ptr(top_k),
+                             _ptr(top_p), _ptr(min_p), _ptr(token), _ptr(logp), code,
+                             _ptr(workspace), workspace.numel() * workspace.element_size(),
+                             _stream(dev))
+    _check("sample_logits", st)
+    return token, logp
