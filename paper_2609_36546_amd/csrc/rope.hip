@@ -11,49 +11,78 @@
 // Angles: position * f is exact in double (31 + 24 bits), and so is its
 // reduction to a fraction of a turn to about 1e-16 of the turns; only the
 // fraction goes to fp32.  In fp32 the angle of position 10^5 would be off by
-// 0.004.  One workgroup takes kRopeTok rows of one sequence with all their
-// heads, so an angle is computed once for Hq + Hkv uses and kept in LDS; what
-// is left is one read and one write of the data, in 16-byte pieces where the
-// pairs allow it (two pieces R/2 apart, or one piece of whole pairs).
+// 0.004.
+//
+// Bound by one read and one write of the data, moved in 16-byte pieces where
+// the pairs allow it (two pieces R/2 apart, or one piece of whole pairs).  A
+// sequence's pieces are dealt out flat over rows, heads and pieces, kPer to a
+// thread, so that a few rows of many heads fill as many workgroups as a prompt
+// does; a workgroup's rows (two or three at common head counts) have their
+// angles computed once, into LDS, while the first pieces are on their way.
 #include "common.h"
 #include "kernels.h"
 
 namespace ipdv {
 namespace {
 
-constexpr int kRopeTok = 4;
+constexpr int kPer = 2;         // pieces (pairs of pieces) per thread
 
 typedef __attribute__((__vector_size__(16))) int i32x4;
 
-template <typename DT>
-struct Piece {   // 16 bytes of a row
-  static constexpr int N = 16 / (int)sizeof(DT);
-  DT e[N];
-};
-
-template <typename DT>
-__device__ __forceinline__ Piece<DT> ld_piece(const DT* p) {
-  const i32x4 v = ld16<i32x4>(p);
-  return __builtin_bit_cast(Piece<DT>, v);
-}
-template <typename DT>
-__device__ __forceinline__ void st_piece(DT* p, const Piece<DT>& x) {
-  *reinterpret_cast<i32x4*>(p) = __builtin_bit_cast(i32x4, x);
-}
-
-// VEC: the pairs fall into whole 16-byte pieces (see launch_rope).
+// VEC: the pairs fall into whole 16-byte pieces (see launch_t).  A row's work:
+// per head `turns` units (half: a piece and its partner; interleaved: a piece
+// of N / 2 pairs; else a pair), then `pass` pieces behind them.
 template <typename DT, bool INTER, bool VEC>
-__global__ __launch_bounds__(256) void rope_kernel(RopeLaunch p) {
-  extern __shared__ float2 s_cs[];                 // [kRopeTok][R / 2] cos, sin
-  constexpr int N = VEC ? Piece<DT>::N : 1;
+__global__ __launch_bounds__(256) void rope_kernel(RopeLaunch p, int turns, int per_head) {
+  extern __shared__ float2 s_cs[];                 // [rows of the workgroup][R / 2] cos, sin
+  constexpr int N = VEC ? 16 / (int)sizeof(DT) : 1;
+  struct Raw { DT e[N]; };
   const int slot = blockIdx.y;
   const int b = p.seq_ids ? p.seq_ids[slot] : slot;
-  const int r0 = p.cu_q[b], kb = p.cu_q[b + 1] - r0;
-  const int i0 = blockIdx.x * kRopeTok;
-  if (i0 >= kb) return;
-  const int n_tok = min(kRopeTok, kb - i0);
-  const int half = p.rot / 2;
-  const int pos0 = max(p.ctx_lens[b], 0) + i0;
+  const int r0 = p.cu_q[b], kb = min(p.cu_q[b + 1] - r0, p.max_q);
+  const int half = p.rot / 2, per_row = per_head * (p.Hq + p.Hkv);
+  const long e0 = (long)blockIdx.x * (256 * kPer);
+  const long left = (long)max(kb, 0) * per_row - e0;
+  if (left <= 0) return;
+  const int t0 = (int)(e0 / per_row), in0 = (int)(e0 - (long)t0 * per_row);
+  const int n = (int)min(left, (long)(256 * kPer));
+  const int n_tok = (in0 + n - 1) / per_row + 1;
+  const int pos0 = max(p.ctx_lens[b], 0) + t0;
+
+  const DT* src[kPer];
+  DT* dst[kPer];
+  int tok[kPer], unit[kPer];
+  Raw x[kPer], y[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int at = i * 256 + (int)threadIdx.x;
+    unit[i] = -1;
+    if (at >= n) continue;
+    const int e = in0 + at;
+    tok[i] = e / per_row;
+    const int in_row = e - tok[i] * per_row;
+    int h = in_row / per_head;
+    unit[i] = in_row - h * per_head;
+    const bool is_q = h < p.Hq;
+    if (!is_q) h -= p.Hq;
+    const size_t row = (size_t)(r0 + t0 + tok[i]);
+    src[i] = reinterpret_cast<const DT*>(is_q ? p.q : p.k) + row * (is_q ? p.q_stride : p.k_stride) + (size_t)h * p.D;
+    dst[i] = reinterpret_cast<DT*>(is_q ? p.q_out : p.k_out) + row * (is_q ? p.qo_stride : p.ko_stride) + (size_t)h * p.D;
+    const int u = unit[i];
+    int cx = p.rot + (u - turns) * N, cy = -1;
+    if (u < turns) {
+      cx = INTER ? (VEC ? u * N : 2 * u) : u * N;
+      if (!INTER) cy = cx + half;
+      else if (!VEC) cy = cx + 1;
+    }
+    if constexpr (VEC) {
+      x[i] = __builtin_bit_cast(Raw, ld16<i32x4>(src[i] + cx));
+      if (cy >= 0) y[i] = __builtin_bit_cast(Raw, ld16<i32x4>(src[i] + cy));
+    } else {
+      x[i].e[0] = src[i][cx];
+      if (cy >= 0) y[i].e[0] = src[i][cy];
+    }
+  }
   for (int e = threadIdx.x; e < n_tok * half; e += 256) {
     const int t = e / half, c = e - t * half;
     double a = (double)(pos0 + t) * (double)p.inv_freq[c] * 0.15915494309189533577;   // in turns
@@ -63,67 +92,55 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeLaunch p) {
     s_cs[e] = make_float2(cs * p.factor, (p.inverse ? -sn : sn) * p.factor);
   }
   __syncthreads();
-  // A row's work: `turns` pieces (half: a piece and its partner; interleaved:
-  // one piece of N / 2 pairs, or one pair) and `pass` pieces behind them.
-  const int turns = INTER ? (VEC ? p.rot / N : half) : half / N;
-  const int pass = (p.D - p.rot) / N;
-  const int per_head = turns + pass;
-  const int per_row = per_head * (p.Hq + p.Hkv);
-  for (int e = threadIdx.x; e < n_tok * per_row; e += 256) {
-    const int t = e / per_row, in_row = e - t * per_row;
-    int h = in_row / per_head;
-    const int u = in_row - h * per_head;
-    const bool is_q = h < p.Hq;
-    if (!is_q) h -= p.Hq;
-    const size_t row = (size_t)(r0 + i0 + t);
-    const DT* src = reinterpret_cast<const DT*>(is_q ? p.q : p.k) + row * (is_q ? p.q_stride : p.k_stride) + (size_t)h * p.D;
-    DT* dst = reinterpret_cast<DT*>(is_q ? p.q_out : p.k_out) + row * (is_q ? p.qo_stride : p.ko_stride) + (size_t)h * p.D;
-    const float2* cs = s_cs + t * half;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int u = unit[i];
+    if (u < 0) continue;
+    DT* d = dst[i];
     if (u >= turns) {
-      const int c = p.rot + (u - turns) * N;
-      if constexpr (VEC) st_piece(dst + c, ld_piece(src + c));
-      else dst[c] = src[c];
-    } else if constexpr (!VEC) {
-      const int cx = INTER ? 2 * u : u, cy = INTER ? 2 * u + 1 : u + half;
-      const float x = to_f32(src[cx]), y = to_f32(src[cy]);
-      dst[cx] = from_f32<DT>(x * cs[u].x - y * cs[u].y);
-      dst[cy] = from_f32<DT>(x * cs[u].y + y * cs[u].x);
-    } else if constexpr (INTER) {
-      const int c = u * N;
-      Piece<DT> v = ld_piece(src + c);
+      d += p.rot + (u - turns) * N;
+    } else if constexpr (INTER && VEC) {
+      const float2* cs = s_cs + tok[i] * half + u * (N / 2);
 #pragma unroll
-      for (int i = 0; i < N; i += 2) {
-        const float x = to_f32(v.e[i]), y = to_f32(v.e[i + 1]);
-        const float2 w = cs[(c + i) / 2];
-        v.e[i] = from_f32<DT>(x * w.x - y * w.y);
-        v.e[i + 1] = from_f32<DT>(x * w.y + y * w.x);
+      for (int c = 0; c < N; c += 2) {
+        const float a = to_f32(x[i].e[c]), b2 = to_f32(x[i].e[c + 1]);
+        const float2 w = cs[c / 2];
+        x[i].e[c] = from_f32<DT>(a * w.x - b2 * w.y);
+        x[i].e[c + 1] = from_f32<DT>(a * w.y + b2 * w.x);
       }
-      st_piece(dst + c, v);
+      d += u * N;
     } else {
-      const int c = u * N;
-      Piece<DT> vx = ld_piece(src + c), vy = ld_piece(src + c + half);
+      const float2* cs = s_cs + tok[i] * half + u * N;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float x = to_f32(vx.e[i]), y = to_f32(vy.e[i]);
-        const float2 w = cs[c + i];
-        vx.e[i] = from_f32<DT>(x * w.x - y * w.y);
-        vy.e[i] = from_f32<DT>(x * w.y + y * w.x);
+      for (int c = 0; c < N; ++c) {
+        const float a = to_f32(x[i].e[c]), b2 = to_f32(y[i].e[c]);
+        x[i].e[c] = from_f32<DT>(a * cs[c].x - b2 * cs[c].y);
+        y[i].e[c] = from_f32<DT>(a * cs[c].y + b2 * cs[c].x);
       }
-      st_piece(dst + c, vx);
-      st_piece(dst + c + half, vy);
+      d += INTER ? 2 * u : u * N;
+      DT* d2 = d + (INTER ? 1 : half);
+      if constexpr (VEC) *reinterpret_cast<i32x4*>(d2) = __builtin_bit_cast(i32x4, y[i]);
+      else *d2 = y[i].e[0];
     }
+    if constexpr (VEC) *reinterpret_cast<i32x4*>(d) = __builtin_bit_cast(i32x4, x[i]);
+    else *d = x[i].e[0];
   }
 }
 
 template <typename DT>
 hipError_t launch_t(const RopeLaunch& L, hipStream_t st) {
-  constexpr int N = 16 / (int)sizeof(DT);
+  constexpr int W = 16 / (int)sizeof(DT);
   const bool inter = L.interleaved;
   // whole pieces: every row starts on 16 bytes, the pieces of a pair too
-  const bool vec = L.al16 && L.D % N == 0 && (inter ? L.rot % N == 0 : (L.rot / 2) % N == 0);
-  const dim3 grid((L.max_q + kRopeTok - 1) / kRopeTok, L.n_seq);
-  const size_t lds = (size_t)kRopeTok * (L.rot / 2) * sizeof(float2);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), lds, st, L); };
+  const bool vec = L.al16 && L.D % W == 0 && (inter ? L.rot % W == 0 : (L.rot / 2) % W == 0);
+  const int N = vec ? W : 1;
+  const int turns = inter ? (vec ? L.rot / N : L.rot / 2) : L.rot / 2 / N;
+  const int per_head = turns + (L.D - L.rot) / N, per_row = per_head * (L.Hq + L.Hkv);
+  constexpr int kUnits = 256 * kPer;
+  const dim3 grid((unsigned)(((long)L.max_q * per_row + kUnits - 1) / kUnits), L.n_seq);
+  // rows that a workgroup's units can touch
+  const size_t lds = (size_t)((kUnits - 2) / per_row + 2) * (L.rot / 2) * sizeof(float2);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), lds, st, L, turns, per_head); };
   if (inter) {
     if (vec) go(rope_kernel<DT, true, true>); else go(rope_kernel<DT, true, false>);
   } else {
