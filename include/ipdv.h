@@ -574,7 +574,8 @@ int ipdv_rope_inv_freq(int rot, double base, int kind, double factor, int origin
  * other overlap does not.
  * inv_freq [rot/2] float (device); ctx_lens, cu_q, seq_ids, n_seq, max_q as in
  * verify_attn_paged.  Rows of other sequences are neither read nor written.
- * Requirements: 2 <= rot <= D <= 512, rot even; n_seq <= 65535.
+ * Requirements: 2 <= rot <= D <= 512, rot even; n_seq <= 65535; max_q * (Hq +
+ * Hkv) * D < 2^32.
  *
  * Errors: IPDV_EINVAL, IPDV_EUNSUPPORTED (dtype, D, n_seq), IPDV_EHIP.
  */
@@ -605,8 +606,8 @@ int rope_window(const void* q, int64_t q_row_stride, const void* k, int64_t k_ro
  * scales  [num_pages, Hkv, 2, page_size]         scale bytes: keys, values
  * page_table, ctx_lens, cu_q, seq_ids, n_seq, max_q as in verify_attn_paged.
  * Slots of other positions are left as they are.
- * Requirements: D in {64, 128}, page_size 16, 32 or 64; pages, scales and the
- * rows of k_new and v_new start on 16-byte boundaries.
+ * Requirements: D in {64, 128}, page_size 16, 32 or 64, n_seq * Hkv <= 65535,
+ * max_q < 2^27; pages, scales and the rows of k_new and v_new start on 16-byte boundaries.
  *
  * Errors: IPDV_EINVAL, IPDV_EUNSUPPORTED (D, page_size, dtype, alignment), IPDV_EHIP.
  */
@@ -686,8 +687,8 @@ size_t ipdv_sample_logits_workspace_size(int M, int V);
  *
  * logits [M, V] (dtype), row_stride elements from one row to the next (>= V);
  * u [M] float in [0, 1); temperature, top_p, min_p [M] float and top_k [M]
- * int32, each NULL for off (temperature: 1).  Requirements: M >= 0, 1 <= V <=
- * 262144, M <= 16777215; workspace on a 16-byte boundary.
+ * int32, each NULL for off (temperature: 1).  Requirements: 0 <= M < 2^22, 1 <=
+ * V <= 262144, M * V < 2^35; workspace on a 16-byte boundary.
  *
  * Errors: IPDV_EINVAL, IPDV_EUNSUPPORTED (dtype, V, M), IPDV_EWORKSPACE, IPDV_EHIP.
  */

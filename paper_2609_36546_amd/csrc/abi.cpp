@@ -529,6 +529,8 @@ int rope_window(const void* q, int64_t q_stride, const void* k, int64_t k_stride
     return fail(IPDV_EINVAL, "unknown layout %d", layout);
   if (!std::isfinite(factor)) return fail(IPDV_EINVAL, "factor must be finite");
   if (dtype != IPDV_F32 && dtype != IPDV_BF16) return fail(IPDV_EUNSUPPORTED, "dtype %d", dtype);
+  if ((int64_t)max_q * (Hq + Hkv) >= ((int64_t)1 << 32) / D)
+    return fail(IPDV_EUNSUPPORTED, "max_q * (Hq + Hkv) * D must be below 2^32");
   const int64_t nq = (int64_t)Hq * D, nk = (int64_t)Hkv * D;
   if (q_stride < nq || qo_stride < nq || k_stride < nk || ko_stride < nk)
     return fail(IPDV_EINVAL, "a row stride is shorter than the row");
@@ -560,6 +562,7 @@ static int q8_check(int n_seq, int max_q, int Hkv, int D, int page_size, int num
   if (!is_pow2(page_size) || page_size < 16 || page_size > 64)
     return fail(IPDV_EUNSUPPORTED, "page_size=%d not in {16, 32, 64}", page_size);
   if ((long)n_seq * Hkv > 65535) return fail(IPDV_EUNSUPPORTED, "n_seq * Hkv exceeds 65535");
+  if (max_q >= 1 << 27) return fail(IPDV_EUNSUPPORTED, "max_q too large");
   if (dtype != IPDV_F32 && dtype != IPDV_BF16) return fail(IPDV_EUNSUPPORTED, "dtype %d", dtype);
   return IPDV_OK;
 }
@@ -670,7 +673,7 @@ static int sample_shape_check(int M, int V) {
   if (M < 0) return fail(IPDV_EINVAL, "M must be >= 0 (got %d)", M);
   if (V < 1) return fail(IPDV_EINVAL, "V must be >= 1 (got %d)", V);
   if (V > 262144) return fail(IPDV_EUNSUPPORTED, "V=%d exceeds 262144", V);
-  if (M > 16777215) return fail(IPDV_EUNSUPPORTED, "M too large");
+  if ((int64_t)M * V >= (int64_t)1 << 35 || M >= 1 << 22) return fail(IPDV_EUNSUPPORTED, "M too large");
   return IPDV_OK;
 }
 

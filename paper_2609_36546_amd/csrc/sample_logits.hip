@@ -14,37 +14,47 @@
 // factor of e^(1/8) in probability, and 255 bins from the maximum's down reach
 // e^-31.9 of the top probability.  What lies below is taken as of probability
 // zero (at V = 262144 all of it together is below 4e-9 of the mass, less than a
-// step of an fp32 u).  An entry adds 2^45 + round(2^30 m) to its bin, m its mass
-// against the bin's upper edge: one 64-bit LDS addition counts and sums.  Sums
-// of whole numbers do not depend on the order of the atomics, so a call repeats
-// bit for bit; m itself is an fp32 exponential of an argument within 1/8, and
-// joined sums are in double.  y is in double, for the bins to end where the
-// definition puts them.
+// step of an fp32 u).
+// An entry adds 2^45 + 2^30 m to its bin, m its mass against the bin's upper
+// edge: one 64-bit LDS addition counts and sums.  Sums of whole numbers do not
+// depend on the order of the atomics, so a call repeats bit for bit; m itself is
+// an fp32 exponential of an argument of about 1/8, and joined sums are in
+// double.  Where exactly a bin ends does not matter, but both kernels must find
+// an entry in the same one: it is the floor of y in fp32, a function of the
+// logit and T alone, and the rounding of y goes into m.
 //
-//   chunk kernel  one workgroup per 8192 entries: reads the logits once, into
+//   chunk kernel  one workgroup per 16384 entries: reads the logits once, into
 //                 registers; its histogram below its own maximum (bins are
 //                 aligned, since they are floors of y), and a list of its
-//                 topmost entries.  Bound by the read of the logits.
+//                 topmost entries.
 //   row kernel    one workgroup per row: adds the histograms up, finds the cut's
-//                 bin, orders the bin's entries (from the lists, or from the
+//                 bin, gathers the bin's entries (from the lists, or from the
 //                 logits where a list stops above the bin) and takes the cut;
 //                 then the chunk, and in it the entry, where the mass passes u.
-//                 Bound by latency: it reads the histograms and one chunk.
-// A bin of more entries than fit LDS (equal logits by the thousand) is cut by
-// selecting the digits of the logit from the top, reading the row for each.
+//                 Bound by latency, so it asks memory twice only: for all
+//                 histograms and lists at its start, which stay in registers,
+//                 and for the chunk of the draw; and its loops stay rolled
+//                 where they can (63 KB of code took 17 us even unfiltered).
+//
+// A bin of many entries (equal logits by the thousand) is narrowed by digits of
+// the entries' order numbers until 512 are left, in LDS or, where they do not
+// fit there, over the row's logits.
+#include <type_traits>
+
 #include "common.h"
 #include "kernels.h"
 
 namespace ipdv {
 namespace {
 
-constexpr int kChunk = 8192;      // entries per workgroup of the chunk kernel
+constexpr int kChunk = 16384;     // entries per workgroup of the chunk kernel
 constexpr int kBins = 256;
-constexpr int kList = 256;        // topmost entries that a chunk lists
-constexpr int kSort = 1024;       // entries of one bin that are ordered in LDS
-constexpr int kMaxChunks = 32;    // V <= 262144
+constexpr int kList = 1024;       // topmost entries that a chunk lists
+constexpr int kHold = 4096;       // entries of one bin that LDS holds
+constexpr int kSort = 512;        // entries that are ordered
+constexpr int kMaxChunks = 16;    // V <= 262144
 constexpr double kWidth = 8.0;    // bins per unit of l / T
-constexpr int kCountShift = 45;   // 8192 masses of at most 2^30 stay below
+constexpr int kCountShift = 45;   // 16384 masses of about 2^30 at most stay below
 constexpr unsigned long long kMassMask = (1ull << kCountShift) - 1;
 typedef unsigned long long u64;
 
@@ -76,6 +86,7 @@ __device__ __forceinline__ ChunkRec chunk_rec(const SampleLogitsLaunch& p, int n
 // A row's parameters; greedy (T = 0) is the top entry at temperature 1.
 struct Row {
   double width;   // y = l * width
+  float hi, lo;   // the same in two terms
   double temp;
   int k;          // 0: off
   float top_p;    // >= 1: off
@@ -88,6 +99,8 @@ __device__ __forceinline__ Row row_of(const SampleLogitsLaunch& p, int m) {
   r.bad = !(t >= 0.f);
   r.temp = t > 0.f ? (double)t : 1.0;
   r.width = kWidth / r.temp;
+  r.hi = (float)r.width;
+  r.lo = (float)(r.width - (double)r.hi);
   r.k = p.top_k ? max(p.top_k[m], 0) : 0;
   r.top_p = p.top_p ? p.top_p[m] : 1.f;
   r.min_p = p.min_p ? p.min_p[m] : 0.f;
@@ -101,19 +114,40 @@ __device__ __forceinline__ Row row_of(const SampleLogitsLaunch& p, int m) {
   return r;
 }
 
+// floor(y) of a finite logit, and what y has above it (a little outside [0, 1)
+// where fp32 has rounded y).  Products must not be contracted into the
+// differences that follow: what they were rounded to counts.
+constexpr float kFar = 16777216.f;      // from here on fp32 has no fraction left, and double takes over
+__device__ __forceinline__ float floor_near(const Row& r, float l, float* rest) {
+#pragma clang fp contract(off)
+  const float y = l * r.hi, f = floorf(y);
+  *rest = (y - f) + fmaf(l, r.lo, fmaf(l, r.hi, -y));
+  return f;
+}
+__device__ __forceinline__ double floor_y(const Row& r, float l, float* rest) {
+#pragma clang fp contract(off)
+  if (fabsf(l * r.hi) < kFar) return (double)floor_near(r, l, rest);
+  const double z = (double)l * r.width, f = floor(z);
+  *rest = (float)(z - f);
+  return f;
+}
+// 2^30 times the mass against the bin's upper edge: whole, as fp32 has 24 bits.
+__device__ __forceinline__ unsigned mass_above(float rest) {
+  constexpr float c = (float)(1.4426950408889634 / kWidth);
+  return (unsigned)fast_exp2(fmaf(rest, c, 30.f - c));
+}
+
 // Bin of a finite logit below `top` = floor(y) of the maximum, and its mass
 // against the bin's upper edge in units of 2^-30 (the last bin has none).
-__device__ __forceinline__ int classify(float l, double width, double top, unsigned* mass) {
-  const double y = (double)l * width;
-  const double d = top - floor(y);
+__device__ __forceinline__ int classify(const Row& r, float l, double top, unsigned* mass) {
+  float x;
+  const double d = top - floor_y(r, l, &x);
   if (!(d < kBins - 1)) {
     *mass = 0;
     return kBins - 1;
   }
-  const int bin = (int)d;
-  const float t = (float)(y - (top + 1.0 - bin));
-  *mass = (unsigned)rintf(fast_exp2(t * (float)(1.4426950408889634 / kWidth)) * 1073741824.f);
-  return bin;
+  *mass = mass_above(x);
+  return (int)d;
 }
 
 // Logits as unsigned numbers of the same order, and back to one of equal order.
@@ -121,108 +155,177 @@ __device__ __forceinline__ unsigned key_of(float l) {
   const unsigned u = __float_as_uint(l == 0.f ? 0.f : l);   // -0 is +0
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ float logit_of_key(unsigned key) {
+  return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
+}
 // Order of entries: logit, then the lower index.
-__device__ __forceinline__ u64 order_of(float l, int v) { return ((u64)key_of(l) << 32) | (unsigned)~v; }
+constexpr int kIndexBits = 18;
+static_assert(kMaxChunks * kChunk <= 1 << kIndexBits, "an index has 18 bits");
+__device__ __forceinline__ u64 order_of(float l, int v) {
+  return ((u64)key_of(l) << kIndexBits) | (unsigned)(((1 << kIndexBits) - 1) ^ v);
+}
+__device__ __forceinline__ float logit_of(u64 order) { return logit_of_key((unsigned)(order >> kIndexBits)); }
+__device__ __forceinline__ int index_of(u64 order) {
+  return (int)(((1 << kIndexBits) - 1) ^ (unsigned)(order & ((1 << kIndexBits) - 1)));
+}
 
 template <typename DT>
 __device__ __forceinline__ float logit(const SampleLogitsLaunch& p, int m, int v) {
   return to_f32(reinterpret_cast<const DT*>(p.logits)[(size_t)m * p.stride + v]);
 }
 
+constexpr int kThreads = 512;     // of both kernels
+constexpr int kWaves = kThreads / kWave;
+
 template <typename DT, bool VEC>
-__global__ __launch_bounds__(256) void chunk_kernel(SampleLogitsLaunch p, int n_chunks) {
+__global__ __launch_bounds__(kThreads, 6) void chunk_kernel(SampleLogitsLaunch p, int n_chunks) {
   constexpr int N = VEC ? 16 / (int)sizeof(DT) : 1;   // entries per load
-  constexpr int PER = kChunk / 256;
+  constexpr int PER = kChunk / kThreads;
   __shared__ u64 s_hist[kBins];
-  __shared__ float s_max[4];
-  __shared__ int s_bad, s_n, s_cover, s_wave[4];
+  __shared__ float s_max[kWaves], s_min[kWaves];
+  __shared__ int s_bad, s_n, s_cover, s_wave[kBins / kWave];
   const int m = blockIdx.x / n_chunks, s = blockIdx.x % n_chunks;
   const int tid = threadIdx.x, lane = lane_id(), w = tid >> 6;
   const int v0 = s * kChunk, n = min(kChunk, p.V - v0);
   const DT* src = reinterpret_cast<const DT*>(p.logits) + (size_t)m * p.stride + v0;
-  // entry i of the thread: v0 + (i / N) * 256 N + tid N + i % N
-  float x[PER];
+  // entry i of the thread: v0 + (i / N) * kThreads N + tid N + i % N; kept as it
+  // came, since bf16 takes half the registers so
+  typedef __attribute__((__vector_size__(16))) int i32x4;
+  typedef std::conditional_t<VEC, i32x4, DT> Raw;
+  Raw raw[PER / N];
 #pragma unroll
-  for (int i = 0; i < PER; i += N) {
-    const int at = (i / N) * 256 * N + tid * N;
-    if constexpr (VEC) {            // n is a multiple of N
-      if (at < n) {
-        typedef __attribute__((__vector_size__(16))) int i32x4;
-        const i32x4 raw = ld16<i32x4>(src + at);
-        const DT* e = reinterpret_cast<const DT*>(&raw);
-#pragma unroll
-        for (int c = 0; c < N; ++c) x[i + c] = to_f32(e[c]);
-      } else {
-#pragma unroll
-        for (int c = 0; c < N; ++c) x[i + c] = -INFINITY;
-      }
+  for (int i = 0; i < PER / N; ++i) {
+    const int at = (i * kThreads + tid) * N;
+    if (at < n) {                   // with VEC, n is a multiple of N
+      raw[i] = *reinterpret_cast<const Raw*>(src + at);
     } else {
-      x[i] = at < n ? to_f32(src[at]) : -INFINITY;
+      DT e[N];
+#pragma unroll
+      for (int c = 0; c < N; ++c) e[c] = from_f32<DT>(-INFINITY);
+      raw[i] = __builtin_bit_cast(Raw, e);
     }
   }
+  struct Lane { DT e[N]; };
+  // makes the compiler take the values as new: it would keep the fp32 forms of
+  // one pass for the next, in registers that it does not have
+  auto renew = [&] {
+#pragma unroll
+    for (int i = 0; i < PER / N; ++i) asm volatile("" : "+v"(raw[i]));
+  };
+  auto x = [&](int i) { return to_f32(__builtin_bit_cast(Lane, raw[i / N]).e[i % N]); };
   const Row r = row_of(p, m);
-  s_hist[tid] = 0;
+  if (tid < kBins) s_hist[tid] = 0;
   if (tid == 0) s_bad = s_n = s_cover = 0;
-  float mx = -INFINITY;
+  float mx = -INFINITY, mn = INFINITY;
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    mx = fmaxf(mx, x[i]);
-    bad |= !(x[i] < INFINITY);
+    mx = fmaxf(mx, x(i));
+    mn = fminf(mn, x(i) > -INFINITY ? x(i) : INFINITY);
+    bad |= !(x(i) < INFINITY);
   }
+  renew();
   mx = wave_max(mx);
-  if (lane == 0) s_max[w] = mx;
+  mn = -wave_max(-mn);
+  if (lane == 0) {
+    s_max[w] = mx;
+    s_min[w] = mn;
+  }
   __syncthreads();
   if (bad) s_bad = 1;
-  mx = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
-  const double top = floor((double)mx * r.width);
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    mx = fmaxf(mx, s_max[i]);
+    mn = fminf(mn, s_min[i]);
+  }
   const bool any = mx > -INFINITY && mx < INFINITY;
-  if (any) {
+  float ignore;
+  const double top = any ? floor_y(r, mx, &ignore) : -INFINITY;
+  auto add = [&](int bin, unsigned mass) {
+    __hip_atomic_fetch_add(&s_hist[bin], (1ull << kCountShift) + mass, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  };
+  const bool near = any && fmaxf(fabsf(mx), fabsf(mn)) * r.hi < kFar;
+  if (near) {                       // the same without double
+    const float ftop = (float)top;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      if (x[i] > -INFINITY) {
-        unsigned mass;
-        const int bin = classify(x[i], r.width, top, &mass);
-        __hip_atomic_fetch_add(&s_hist[bin], (1ull << kCountShift) + mass, __ATOMIC_RELAXED,
-                               __HIP_MEMORY_SCOPE_WORKGROUP);
+      float rest;
+      const float d = ftop - floor_near(r, x(i), &rest);       // infinite for -inf
+      if (d < kBins - 1) add((int)d, mass_above(rest));
+    }
+  } else if (any) {
+#pragma unroll 1
+    for (int i = 0; i < PER; ++i) {
+      float l = x(0);
+#pragma unroll
+      for (int c = 0; c < PER; ++c) l = c == i ? x(c) : l;
+      unsigned mass;
+      if (l > -INFINITY) {
+        const int bin = classify(r, l, top, &mass);
+        if (bin < kBins - 1) add(bin, mass);
       }
     }
   }
   __syncthreads();
   const ChunkRec rec = chunk_rec(p, n_chunks, m, s);
-  rec.hist[tid] = s_hist[tid];
   // The list: whole bins from the top while they fit.
-  int cum = wave_incl_scan_i((int)(s_hist[tid] >> kCountShift));
-  if (lane == kWave - 1) s_wave[w] = cum;
-  __syncthreads();
-  for (int i = 0; i < w; ++i) cum += s_wave[i];
-  if (cum <= kList) atomicAdd(&s_cover, 1);     // counts never fall, so these are the first bins
-  __syncthreads();
-  const int cover = s_cover;
-  if (any && (r.k > 0 || r.top_p < 1.f || r.min_p > 0.f)) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      // entries far below the list's end need no double to be told
-      if (x[i] > -INFINITY) {
-        unsigned mass;
-        if (classify(x[i], r.width, top, &mass) < cover) {
-          const int at = atomicAdd(&s_n, 1);
-          rec.list[at] = {x[i], v0 + (i / N) * 256 * N + tid * N + i % N};
-        }
-      }
-    }
+  int cum = 0;
+  if (tid < kBins) {
+    rec.hist[tid] = s_hist[tid];
+    cum = wave_incl_scan_i((int)(s_hist[tid] >> kCountShift));
+    if (lane == kWave - 1) s_wave[w] = cum;
   }
   __syncthreads();
-  if (tid == 0) *rec.head = {any ? top : -INFINITY, mx, s_bad, cover, s_n};
+  if (tid < kBins) {
+    for (int i = 0; i < w; ++i) cum += s_wave[i];
+    const u64 fits = __ballot(cum <= kList);    // counts never fall, so these are the first bins
+    if (lane == 0) atomicAdd(&s_cover, __popcll(fits));
+  }
+  __syncthreads();
+  const int cover = min(s_cover, kBins - 1);    // the last bin is never listed
+  if (any && cover > 0 && (r.k > 0 || r.top_p < 1.f || r.min_p > 0.f)) {
+    renew();
+    unsigned in = 0;                // bit i: entry i is listed
+    static_assert(PER <= 32, "a bit per entry");
+    if (near) {
+      const float last = (float)top - (float)cover;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        float rest;
+        in |= (floor_near(r, x(i), &rest) > last ? 1u : 0u) << i;
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < PER; ++i) {
+        float l = x(0), rest;
+#pragma unroll
+        for (int c = 0; c < PER; ++c) l = c == i ? x(c) : l;
+        in |= (l > -INFINITY && top - floor_y(r, l, &rest) < cover ? 1u : 0u) << i;
+      }
+    }
+    renew();
+    // a place for the wave's entries, then for each lane's
+    const int upto = wave_incl_scan_i(__popc(in));
+    int at = 0;
+    if (lane == kWave - 1) at = atomicAdd(&s_n, upto);
+    at = __shfl(at, kWave - 1, kWave) + upto - __popc(in);
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (in >> i & 1) rec.list[at++] = {x(i), v0 + (i / N) * kThreads * N + tid * N + i % N};
+  }
+  __syncthreads();
+  if (tid == 0) *rec.head = {top, mx, s_bad, cover, s_n};
 }
 
 // ---- the row kernel ----
 
-constexpr int kRowThreads = 512;
+constexpr double kUnitMass = 1.0 / 1073741824.0;
+constexpr int kHeldBins = kMaxChunks * kBins / kThreads;      // histogram bins of a thread
+constexpr int kHeldList = kMaxChunks * kList / kThreads;      // list entries of a thread
 
-// Sum over the threads before this one, and over all; every thread calls.
+// Sum over the threads before this one; every thread calls.
 template <typename T>
-__device__ __forceinline__ T block_scan(T v, T* s_part, T* total) {
+__device__ __forceinline__ T block_scan(T v, T* s_part) {
   const int lane = lane_id(), w = threadIdx.x >> 6;
   T incl = v;
 #pragma unroll
@@ -233,214 +336,292 @@ __device__ __forceinline__ T block_scan(T v, T* s_part, T* total) {
   __syncthreads();                  // the previous call's readers are done
   if (lane == kWave - 1) s_part[w] = incl;
   __syncthreads();
-  T before = 0, all = 0;
+  T before = 0;
 #pragma unroll
-  for (int i = 0; i < kRowThreads / kWave; ++i) {
+  for (int i = 0; i < kWaves; ++i)
     if (i < w) before += s_part[i];
-    all += s_part[i];
-  }
-  *total = all;
   return before + incl - v;
 }
 
 struct Shared {
   double edge[kBins];               // e^(-t/8): mass of bin t's upper edge
+  float edge_f[kBins];
   double before[kBins];             // mass above bin t
   int count_before[kBins];
   int count[kBins];
-  double top;                       // floor(y) of the row's maximum
-  int chunk_off[kMaxChunks];        // the chunk's top bin in the row's bins (kBins: none)
-  int chunk_cover[kMaxChunks], chunk_listed[kMaxChunks];
-  u64 list[kSort], sorted[kSort];   // order numbers of one bin's entries
+  u64 mass[kBins];
+  int off[kMaxChunks];              // the chunk's top bin in the row's bins (kBins: none)
+  int cover[kMaxChunks], listed[kMaxChunks];
   double chunk_mass[kMaxChunks];
-  u64 part_u[kRowThreads / kWave];
-  double part_d[kRowThreads / kWave];
-  int part_i[kRowThreads / kWave];
-  unsigned digit_count[256];
+  u64 in_bin[kMaxChunks];           // kept mass of the cut's bin
+  double grid[kMaxChunks][kBins + 1];   // mass by chunk and bin, the chunk's top bin first
+  u64 hold[kHold];                  // order numbers of one bin's entries
+  u64 few[kSort], sorted[kSort];
+  int rank[kSort];
+  int digit_count[256];
   u64 digit_mass[256];
-  int n, bin, found, chunk, token;
-  u64 cut, mass_in;
-  unsigned prefix;
+  u64 part_u[kWaves];
+  double part_d[kWaves];
+  int part_i[kWaves];
+  int n, bin, found, chunk, token, bad;
+  unsigned from_logits;             // chunks whose list stops above the bin looked for
+  float low, high;                  // a bin's logits: [low, high)
+  u64 cut, lo, hi, above_mass;
+  int above, left;
   double rest, all;
-  u64 digit_before_mass;
-  int digit_before;
+  double top;                       // floor(y) of the row's maximum
   float max;
-  int bad;
 };
 
-__device__ __forceinline__ float logit_of_key(unsigned key) {
-  return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
-}
-
-// What ends a prefix inside a bin: a count of entries, or a mass to be reached.
+// What ends a prefix: a count of entries, or a mass to be reached.
 struct Need {
   bool by_count;
-  int count;        // entries of the bin
-  double mass;      // mass of the row
+  int count;
+  double mass;
 };
 
-template <typename DT>
+template <typename DT, bool VEC>
 struct RowWork {
   const SampleLogitsLaunch& p;
   Shared& S;
+  const float (&hl)[kHeldList];     // the logits of the thread's list entries (NaN: none)
   const Row r;
   const int m, n_chunks, tid;
   const double top;
 
-  // The entries of a bin, into S.list; false when they do not fit.
-  __device__ bool collect(int bin) {
-    if (S.count[bin] > kSort) return false;
+  // Calls f(l, v) for the logits of the chunks in `chunks` that lie in
+  // [low, high); the next chunk's logits are on their way meanwhile.
+  template <class F>
+  __device__ void scan(unsigned chunks, float low, float high, F f) {
+    constexpr int PER = 16, N = VEC ? 16 / (int)sizeof(DT) : 1;      // a half of a chunk at a time
+    typedef __attribute__((__vector_size__(16))) int i32x4;
+    typedef std::conditional_t<VEC, i32x4, DT> Raw;
+    Raw raw[PER / N];
+    const DT* row = reinterpret_cast<const DT*>(p.logits) + (size_t)m * p.stride;
+    auto load = [&](int v0) {
+#pragma unroll
+      for (int i = 0; i < PER / N; ++i)
+        if (v0 + (i * kThreads + tid) * N < p.V) raw[i] = *reinterpret_cast<const Raw*>(row + v0 + (i * kThreads + tid) * N);
+    };
+    int half = 0, v0 = chunks ? (__ffs(chunks) - 1) * kChunk : 0;
+    if (chunks) load(v0);
+    while (chunks) {
+      const int now = v0;
+      unsigned in = 0;              // bit i: entry i lies in the range
+#pragma unroll
+      for (int i = 0; i < PER / N; ++i) {
+        const DT* e = reinterpret_cast<const DT*>(&raw[i]);
+        const bool on = now + (i * kThreads + tid) * N < p.V;
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+          const float l = to_f32(e[c]);
+          in |= (on && l >= low && l < high ? 1u : 0u) << (i * N + c);
+        }
+      }
+      half ^= 1;
+      if (!half) chunks &= chunks - 1;
+      if (chunks) {
+        v0 = (__ffs(chunks) - 1) * kChunk + half * (kChunk / 2);
+        load(v0);
+      }
+      for (; in; in &= in - 1) {    // few, and still in the cache
+        const int i = __ffs(in) - 1, v = now + (i / N * kThreads + tid) * N + i % N;
+        f(logit<DT>(p, m, v), v);
+      }
+    }
+  }
+  static_assert(kChunk == 2 * 16 * kThreads, "two halves of 16 per thread");
+
+  // The logits of a bin: S.low (the least one that is in it or above) and
+  // S.high (that of the bin above), two lanes of a search over the floats.
+  // Wave 0 calls.
+  __device__ void bounds(int bin) {
+    const int b = bin - (tid & 1);
+    const double goal = top - (double)b;
+    const unsigned most = key_of(S.max);
+    unsigned lo = key_of(-__FLT_MAX__) - 1u, hi = most;     // the floor is below the goal at lo (taken so), not at hi
+    if (b >= 0) {
+      const unsigned guess = key_of((float)(goal / r.width));
+      float x;
+      if (guess - 8u > lo && guess + 8u < hi && guess > 8u) {
+        if (floor_y(r, logit_of_key(guess - 8u), &x) < goal) lo = guess - 8u;
+        if (floor_y(r, logit_of_key(guess + 8u), &x) >= goal) hi = guess + 8u;
+      }
+      while (hi - lo > 1u) {
+        const unsigned mid = lo + (hi - lo) / 2;
+        if (floor_y(r, logit_of_key(mid), &x) >= goal) hi = mid; else lo = mid;
+      }
+    }
+    if (tid == 0) S.low = logit_of_key(hi);
+    if (tid == 1) S.high = b >= 0 ? logit_of_key(hi) : INFINITY;
+  }
+
+  // The entries of a bin, into S.hold as far as they fit, and S.low, S.high.
+  __device__ bool gather(int bin) {
     __syncthreads();
-    if (tid == 0) S.n = 0;
-    __syncthreads();
-    for (int s = 0; s < n_chunks; ++s) {
-      const int local = bin - S.chunk_off[s];
-      if (local < 0) continue;
-      const ChunkRec rec = chunk_rec(p, n_chunks, m, s);
-      if ((rec.hist[local] >> kCountShift) == 0) continue;
-      if (local < S.chunk_cover[s]) {
-        for (int i = tid; i < S.chunk_listed[s]; i += kRowThreads) put(rec.list[i].l, rec.list[i].v, bin);
-      } else {
-        const int v1 = min((s + 1) * kChunk, p.V);
-        for (int v = s * kChunk + tid; v < v1; v += kRowThreads) put(logit<DT>(p, m, v), v, bin);
+    if (tid < kWave) {
+      bounds(bin);
+      bool more = false;
+      if (tid < n_chunks) more = S.off[tid] <= bin && bin - S.off[tid] >= S.cover[tid];
+      const u64 b = __ballot(more);
+      if (tid == 0) {
+        S.from_logits = (unsigned)b;
+        S.n = 0;
       }
     }
     __syncthreads();
+    if (S.count[bin] > kHold) return false;
+    const float low = S.low, high = S.high;
+    auto put = [&](float l, int v) {
+      const int at = atomicAdd(&S.n, 1);
+      if (at < kHold) S.hold[at] = order_of(l, v);
+    };
+    unsigned in = 0;
+#pragma unroll
+    for (int i = 0; i < kHeldList; ++i) in |= (hl[i] >= low && hl[i] < high ? 1u : 0u) << i;
+    for (; in; in &= in - 1) {
+      const int i = __ffs(in) - 1;
+      const ListEntry e = chunk_rec(p, n_chunks, m, i / 2).list[tid + i % 2 * kThreads];
+      put(e.l, e.v);
+    }
+    const unsigned more = S.from_logits;
+    if (more) scan(more, low, high, put);
+    __syncthreads();
     return true;
   }
-  __device__ void put(float l, int v, int bin) {
-    unsigned mass;
-    if (l > -INFINITY && classify(l, r.width, top, &mass) == bin) {
-      const int at = atomicAdd(&S.n, 1);
-      if (at < kSort) S.list[at] = order_of(l, v);
+
+  // Calls f(order) for every entry of the gathered bin.
+  template <class F>
+  __device__ void each(bool held, F f) {
+    if (held) {
+      const int n = min(S.n, kHold);
+      for (int i = tid; i < n; i += kThreads) f(S.hold[i]);
+    } else {
+      scan((1u << n_chunks) - 1u, S.low, S.high, [&](float l, int v) { f(order_of(l, v)); });
     }
   }
   __device__ u64 mass_of(u64 order) const {
     unsigned mass;
-    classify(logit_of_key((unsigned)(order >> 32)), r.width, top, &mass);
+    classify(r, logit_of(order), top, &mass);
     return mass;
   }
 
-  // The cut of a prefix that ends in `bin` (S.cut), and the bin's mass up to
-  // it (S.mass_in).
-  __device__ void refine(int bin, Need need) {
-    if (!collect(bin)) return refine_long(bin, need);
-    const int n = min(S.n, kSort);
-    for (int i = tid; i < n; i += kRowThreads) {
-      const u64 o = S.list[i];
-      int rank = 0;
-      for (int c = 0; c < n; ++c) rank += S.list[c] > o;
-      S.sorted[rank] = o;
-    }
-    __syncthreads();
-    // two neighbouring entries per thread
-    const int i0 = 2 * tid;
-    const u64 a = i0 < n ? mass_of(S.sorted[i0]) : 0, b = i0 + 1 < n ? mass_of(S.sorted[i0 + 1]) : 0;
-    u64 all;
-    const u64 pre = block_scan<u64>(a + b, S.part_u, &all);
-    const double base = S.before[bin], e = S.edge[bin] * (1.0 / 1073741824.0);
-    const bool ka = i0 < n && (need.by_count ? i0 < need.count : i0 == 0 || base + e * (double)pre < need.mass);
-    const bool kb = i0 + 1 < n && (need.by_count ? i0 + 1 < need.count : base + e * (double)(pre + a) < need.mass);
-    int kept;
-    block_scan<int>((int)ka + (int)kb, S.part_i, &kept);
-    if (kept == 0) kept = 1;
-    if (tid == (kept - 1) / 2) {
-      const bool second = (kept - 1) & 1;
-      S.cut = S.sorted[kept - 1];
-      S.mass_in = pre + a + (second ? b : 0);
-    }
-    __syncthreads();
-  }
-
-  // The same for a bin too long for LDS: the cut's logit from its top digit
-  // down, then the index among equal logits.
-  __device__ void refine_long(int bin, Need need) {
-    const double base = S.before[bin], e = S.edge[bin] * (1.0 / 1073741824.0);
-    __syncthreads();
+  // The cut of a prefix that ends in the gathered bin: S.cut.
+  __device__ void select(int bin, bool held, Need need) {
+    const double base = S.before[bin], e = S.edge[bin] * kUnitMass;
+    const int first = S.count_before[bin];
+    // what is kept: entries with less than the need before them
+    auto before = [&](int c, u64 mass) { return need.by_count ? first + c < need.count : base + e * (double)mass < need.mass; };
     if (tid == 0) {
-      S.prefix = 0;
-      S.digit_before = 0;
-      S.digit_before_mass = 0;
+      S.lo = (u64)key_of(S.low) << kIndexBits;
+      S.hi = ((u64)key_of(S.high < INFINITY ? S.high : S.max) + (S.high < INFINITY ? 0u : 1u)) << kIndexBits;
+      S.hi -= 1;
+      S.above = 0;
+      S.above_mass = 0;
+      S.left = S.count[bin];
     }
-    for (int shift = 24; shift >= 0; shift -= 8) {
+    __syncthreads();
+    while (S.left > kSort) {        // by the highest digit in which lo and hi differ
+      const u64 lo = S.lo, hi = S.hi;
+      const int shift = max(0, 56 - __clzll((long long)(lo ^ hi)));
       if (tid < 256) {
         S.digit_count[tid] = 0;
         S.digit_mass[tid] = 0;
       }
+      if (tid == 0) S.found = -1;
       __syncthreads();
-      const unsigned prefix = S.prefix;
-      for (int v = tid; v < p.V; v += kRowThreads) {
-        const float l = logit<DT>(p, m, v);
-        unsigned mass;
-        if (l > -INFINITY && classify(l, r.width, top, &mass) == bin) {
-          const unsigned key = key_of(l);
-          if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) {
-            atomicAdd(&S.digit_count[(key >> shift) & 255], 1u);
-            __hip_atomic_fetch_add(&S.digit_mass[(key >> shift) & 255], (u64)mass, __ATOMIC_RELAXED,
-                                   __HIP_MEMORY_SCOPE_WORKGROUP);
-          }
-        }
-      }
+      each(held, [&](u64 o) {
+        if (o < lo || o > hi) return;
+        const int d = (int)(o >> shift) & 255;
+        atomicAdd(&S.digit_count[d], 1);
+        __hip_atomic_fetch_add(&S.digit_mass[d], mass_of(o), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      });
       __syncthreads();
-      if (tid == 0) {
-        int lowest = 0;                                 // the last digit that occurs ends it if none before does
-        while (lowest < 255 && S.digit_count[lowest] == 0) ++lowest;
-        int cnt = S.digit_before, at = 255;
-        u64 mass = S.digit_before_mass;
-        for (; at > lowest; --at) {
-          if (S.digit_count[at] == 0) continue;
-          if (need.by_count ? cnt + (int)S.digit_count[at] >= need.count
-                            : base + e * (double)(mass + S.digit_mass[at]) >= need.mass)
-            break;
-          cnt += S.digit_count[at];
-          mass += S.digit_mass[at];
-        }
-        S.prefix = prefix | ((unsigned)at << shift);
-        S.digit_before = cnt;
-        S.digit_before_mass = mass;
-        S.n = (int)S.digit_count[at];                   // after the last digit: the equal logits
+      const int d = 255 - tid;      // from the top
+      const int c = tid < 256 ? S.digit_count[d] : 0;
+      const u64 w = tid < 256 ? S.digit_mass[d] : 0;
+      const int c0 = block_scan<int>(c, S.part_i);
+      const u64 w0 = block_scan<u64>(w, S.part_u);
+      if (c > 0 && (c0 == 0 || before(S.above + c0, S.above_mass + w0))) atomicMax(&S.found, tid);
+      __syncthreads();
+      const int a = S.above;
+      const u64 am = S.above_mass;
+      __syncthreads();
+      if (tid == S.found) {
+        S.above = a + c0;
+        S.above_mass = am + w0;
+        S.left = c;
+        const u64 low = (((lo >> shift) & ~255ull) | (u64)d) << shift;
+        S.lo = max(low, lo);
+        S.hi = min(low + ((1ull << shift) - 1), hi);
       }
       __syncthreads();
     }
-    const unsigned key = S.prefix;
-    const int ties = S.n;
-    const u64 w = mass_of((u64)key << 32);
-    int keep = ties;                                    // the first `keep` of them by index
-    if (need.by_count) {
-      keep = need.count - S.digit_before;
-    } else {
-      const double left = need.mass - (base + e * (double)S.digit_before_mass), one = e * (double)w;
-      if (one > 0.0 && left < one * ties) keep = (int)ceil(left / one);
+    // order what is left: every entry's rank, counted by as many threads as there are for it
+    if (tid == 0) S.n = min(S.n, kHold);
+    S.rank[tid] = 0;
+    if (tid == 0) S.found = 0;
+    __syncthreads();
+    const u64 lo = S.lo, hi = S.hi;
+    each(held, [&](u64 o) {
+      if (o < lo || o > hi) return;
+      const int at = atomicAdd(&S.found, 1);
+      if (at < kSort) S.few[at] = o;
+    });
+    __syncthreads();
+    const int n = min(S.found, kSort);
+    const int span = n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : kSort;
+    const int mine = tid & (span - 1);
+    if (mine < n) {
+      const u64 o = S.few[mine];
+      int rank = 0;
+      for (int c = tid / span; c < n; c += kThreads / span) rank += S.few[c] > o;
+      atomicAdd(&S.rank[mine], rank);
     }
-    keep = max(1, min(keep, ties));
-    // the index of the keep-th: threads take neighbouring entries, so that counts are in index order
-    int seen = 0;
-    for (int v0 = 0; v0 < p.V; v0 += 8 * kRowThreads) {
-      int mine = 0;
-      const int a = v0 + 8 * tid, b = min(a + 8, p.V);
-      for (int v = a; v < b; ++v) mine += key_of(logit<DT>(p, m, v)) == key;
-      int all;
-      const int pre = seen + block_scan<int>(mine, S.part_i, &all);
-      if (pre < keep && keep <= pre + mine) {
-        int c = pre;
-        for (int v = a; v < b; ++v)
-          if (key_of(logit<DT>(p, m, v)) == key && ++c == keep) {
-            S.cut = ((u64)key << 32) | (unsigned)~v;
-            S.mass_in = S.digit_before_mass + (u64)keep * w;
-          }
-      }
-      seen += all;
-      if (seen >= keep) break;
-    }
+    __syncthreads();
+    if (tid < n) S.sorted[S.rank[tid]] = S.few[tid];
+    __syncthreads();
+    const u64 o = tid < n ? S.sorted[tid] : 0, w = tid < n ? mass_of(o) : 0;
+    const u64 pre = S.above_mass + block_scan<u64>(w, S.part_u);
+    const bool here = tid < n && (tid == 0 || before(S.above + tid, pre));
+    const bool next = tid + 1 < n && before(S.above + tid + 1, pre + w);
+    if (here && !next) S.cut = o;
+    __syncthreads();
+  }
+
+  // What the chunks keep of the gathered bin, given the cut: S.in_bin.
+  __device__ void record(bool held, u64 cut) {
+    if (tid < kMaxChunks) S.in_bin[tid] = 0;
+    __syncthreads();
+    each(held, [&](u64 o) {
+      if (o >= cut)
+        __hip_atomic_fetch_add(&S.in_bin[index_of(o) / kChunk], mass_of(o), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    });
     __syncthreads();
   }
 };
 
-template <typename DT>
-__global__ __launch_bounds__(kRowThreads) void row_kernel(SampleLogitsLaunch p, int n_chunks) {
+template <typename DT, bool VEC>
+__global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int n_chunks) {
   __shared__ Shared S;
-  const int m = blockIdx.x, tid = threadIdx.x;
+  const int m = blockIdx.x, tid = threadIdx.x, lane = lane_id(), w = tid >> 6;
+  const int t = tid & (kBins - 1), side = tid / kBins;
+  // everything that the row is known by: bins t of every other chunk, list entries tid + j kThreads of all
+  u64 hist[kHeldBins];
+  float hl[kHeldList];
+#pragma unroll
+  for (int i = 0; i < kHeldBins; ++i) {
+    hist[i] = 0;
+    if (2 * i + side < n_chunks) hist[i] = chunk_rec(p, n_chunks, m, 2 * i + side).hist[t];
+  }
   const Row r = row_of(p, m);
+  const double u = (double)p.u[m];
+  const bool filtered = r.k > 0 || r.top_p < 1.f || r.min_p > 0.f;
+  if (filtered) {
+#pragma unroll
+    for (int i = 0; i < kHeldList; ++i)
+      if (i / 2 < n_chunks) hl[i] = chunk_rec(p, n_chunks, m, i / 2).list[tid + i % 2 * kThreads].l;
+  }
   if (tid < kWave) {                // a lane per chunk
     double ct = -INFINITY;
     float cm = -INFINITY;
@@ -450,22 +631,27 @@ __global__ __launch_bounds__(kRowThreads) void row_kernel(SampleLogitsLaunch p, 
       ct = h.floor_max;
       cm = h.max;
       bad |= h.bad != 0;
-      S.chunk_cover[tid] = h.covered;
-      S.chunk_listed[tid] = h.listed;
+      S.cover[tid] = h.covered;
+      S.listed[tid] = h.listed;
     }
     double all = ct;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) all = fmax(all, __shfl_xor(all, o, kWave));
+    for (int o = kMaxChunks / 2; o > 0; o >>= 1) all = fmax(all, __shfl_xor(all, o, kWave));
+    all = __shfl(all, 0, kWave);
     const float mx = wave_max(cm);
-    if (tid < n_chunks) S.chunk_off[tid] = all - ct < kBins ? (int)(all - ct) : kBins;
+    if (tid < n_chunks) S.off[tid] = all - ct < kBins ? (int)(all - ct) : kBins;
     bad = __any(bad) || !(mx > -INFINITY);
     if (tid == 0) {
       S.max = mx;
       S.top = all;
       S.bad = bad;
-      S.found = 0;
-      S.bin = -1;
     }
+  }
+  if (tid < kBins) {
+    S.edge[t] = exp(-(double)t / kWidth);
+    S.edge_f[t] = (float)(S.edge[t] * kUnitMass);
+    S.mass[t] = 0;
+    S.count[t] = 0;
   }
   __syncthreads();
   if (S.bad) {
@@ -477,210 +663,183 @@ __global__ __launch_bounds__(kRowThreads) void row_kernel(SampleLogitsLaunch p, 
   }
   const double top = S.top;
   const float mx = S.max;
-  // The row's bins: each half of the threads adds up every other chunk's.
-  int count = 0;
-  u64 mass_u = 0;
-  {
-    const int t = tid & (kBins - 1);
-#pragma unroll 4
-    for (int s = tid / kBins; s < n_chunks; s += kRowThreads / kBins) {
-      const int local = t - S.chunk_off[s];
-      const u64 h = chunk_rec(p, n_chunks, m, s).hist[max(local, 0)];
-      count += local >= 0 ? (int)(h >> kCountShift) : 0;
-      mass_u += local >= 0 ? h & kMassMask : 0;
-    }
-    if (tid >= kBins) {
-      S.list[t] = mass_u;
-      S.count[t] = count;
-    }
-    __syncthreads();
-    if (tid < kBins) {
-      mass_u += S.list[t];
-      count += S.count[t];
-      if (t == kBins - 1) count = 0, mass_u = 0;     // taken as of probability zero
-      S.edge[t] = exp(-(double)t / kWidth);
+  // The row's bins; below the last one nothing counts.
+#pragma unroll
+  for (int i = 0; i < kHeldBins; ++i) {
+    const int s = 2 * i + side;
+    if (s >= n_chunks) continue;
+    const int g = t + S.off[s];
+    S.grid[s][t] = g < kBins ? (double)(hist[i] & kMassMask) * S.edge[g] : 0.0;
+    if (filtered && g < kBins - 1 && hist[i]) {
+      atomicAdd(&S.count[g], (int)(hist[i] >> kCountShift));
+      __hip_atomic_fetch_add(&S.mass[g], hist[i] & kMassMask, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
   }
-  const double unit = 1.0 / 1073741824.0;
-  const double mass = tid < kBins ? (double)mass_u * S.edge[tid] * unit : 0.0;
-  double total;
-  int n_all;
-  const double mass_before = block_scan<double>(mass, S.part_d, &total);
-  const int count_before = block_scan<int>(tid < kBins ? count : 0, S.part_i, &n_all);
-  if (tid < kBins) {
-    S.before[tid] = mass_before;
-    S.count_before[tid] = count_before;
-    S.count[tid] = count;
-  }
-  __syncthreads();
-
-  RowWork<DT> work{p, S, r, m, n_chunks, tid, top};
   u64 cut = 0;                      // everything is at or above it
-  double kept = total;              // mass of the kept entries
-  if (r.k > 0 && r.k < n_all) {     // otherwise nothing that counts is cut
-    if (tid < kBins && count_before < r.k && count_before + count >= r.k) S.bin = tid;
+  int bin_cut = kBins - 1;          // bins before it are kept whole, of later ones nothing
+  if (filtered) {
+#pragma unroll
+    for (int i = 0; i < kHeldList; ++i)       // told from what was there before by the list's length
+      if (i / 2 >= n_chunks || tid + i % 2 * kThreads >= S.listed[i / 2]) hl[i] = __uint_as_float(0x7fc00000u);
     __syncthreads();
-    const int bin = S.bin;
-    work.refine(bin, {true, r.k - S.count_before[bin], 0.0});
-    cut = S.cut;
-    kept = S.before[bin] + S.edge[bin] * unit * (double)S.mass_in;
+    const int count = tid < kBins ? S.count[t] : 0;
+    const double mass = tid < kBins ? (double)S.mass[t] * S.edge[t] * kUnitMass : 0.0;
+    const double mass_before = block_scan<double>(mass, S.part_d);
+    const int count_before = block_scan<int>(count, S.part_i);
+    if (tid < kBins) {
+      S.before[t] = mass_before;
+      S.count_before[t] = count_before;
+    }
+    if (tid == kBins - 1) S.all = mass_before;         // the last bin has none
     __syncthreads();
-  }
-  if (r.top_p < 1.f) {
-    const double need = (double)r.top_p * kept;
-    if (tid == 0) S.bin = -1;
-    __syncthreads();
-    // the bin where the mass reaches the need; of nothing, the first
-    if (tid < kBins && count > 0 && mass_before + mass >= need && (mass_before < need || count_before == 0))
-      S.bin = tid;
-    __syncthreads();
-    const int bin = S.bin;
-    if (bin >= 0) {
-      work.refine(bin, {false, 0, need});
-      if (S.cut > cut) cut = S.cut;
+    RowWork<DT, VEC> work{p, S, hl, r, m, n_chunks, tid, top};
+    double kept = S.all;            // mass of what the filters so far leave
+    bool held = false;
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {             // top-k, top-p, min-p
+      if (pass == 0 ? r.k == 0 : pass == 1 ? r.top_p == 1.f : r.min_p == 0.f) continue;
+      const Need need{pass == 0, r.k, (double)r.top_p * kept};
+      u64 bound = 0;
+      if (pass == 2) {              // min-p's cut is the least logit that passes
+        const double x = log((double)r.min_p), least = (double)mx + (x < 0.0 ? x * r.temp : 0.0);
+        float l = (float)least;
+        if ((double)l < least) l = nextafterf(l, INFINITY);
+        bound = l > -INFINITY ? (u64)key_of(l) << kIndexBits : 0;
+        if (bound <= cut) continue;
+      }
+      if (tid == 0) S.bin = -1;
       __syncthreads();
-    }
-  }
-  // min-p's cut is a logit; the top entry always stays
-  double least = -INFINITY;
-  if (r.min_p > 0.f) least = log((double)r.min_p);
-  // Mass that each chunk keeps: whole bins from its histogram; entry by entry
-  // in the cut's bin, or in three around min-p's bound (its bin is known to
-  // one, since the bound itself is rounded).
-  int bin_cut = kBins - 1;          // bins before it are kept whole
-  int bin_end = kBins - 1;          // nothing is kept from here on
-  if (cut) {
-    unsigned ignore;
-    bin_cut = classify(logit_of_key((unsigned)(cut >> 32)), r.width, top, &ignore);
-    bin_end = bin_cut + 1;
-  }
-  if (r.min_p > 0.f) {
-    const double d = top - floor(((double)mx + r.temp * least) * r.width) - 1.0;
-    const int b = d < 0 ? 0 : d < kBins - 1 ? (int)d : kBins - 1;
-    bin_cut = min(bin_cut, b);
-    bin_end = min(bin_end, b + 3);
-  }
-  auto keeps = [&](float l, int v) {
-    return l > -INFINITY && order_of(l, v) >= cut &&
-           (r.min_p == 0.f || ((double)l - (double)mx) / r.temp >= least);
-  };
-  const int lane = lane_id(), w = tid >> 6;
-  for (int s = w; s < n_chunks; s += kRowThreads / kWave) {
-    const ChunkRec rec = chunk_rec(p, n_chunks, m, s);
-    const int off = S.chunk_off[s];
-    double sum = 0.0;
-    for (int g = off + lane; g < bin_cut; g += kWave)
-      sum += (double)(rec.hist[g - off] & kMassMask) * S.edge[g];
-    u64 some[3] = {0, 0, 0};
-    auto add = [&](float l, int v) {
-      if (!(l > -INFINITY)) return;
-      unsigned ms;
-      const int g = classify(l, r.width, top, &ms) - bin_cut;
-      if (g >= 0 && g < 3 && keeps(l, v)) {
-        if (g == 0) some[0] += ms;
-        else if (g == 1) some[1] += ms;
-        else some[2] += ms;
+      if (pass == 2) {
+        unsigned ignore;
+        if (tid == 0) S.bin = classify(r, logit_of(bound), top, &ignore);
+      } else if (count > 0 && (pass == 0 ? count_before < r.k && count_before + count >= r.k
+                                         : mass_before + mass >= need.mass &&
+                                               (mass_before < need.mass || count_before == 0))) {
+        S.bin = tid;                // where the need is met; a need of nothing, in the first
       }
-    };
-    if (bin_cut < bin_end && off < bin_end) {
-      if (min(bin_end, kBins - 1) - off <= S.chunk_cover[s]) {
-        for (int i = lane; i < S.chunk_listed[s]; i += kWave) add(rec.list[i].l, rec.list[i].v);
-      } else {
-        const int v1 = min((s + 1) * kChunk, p.V);
-        for (int v = s * kChunk + lane; v < v1; v += kWave) add(logit<DT>(p, m, v), v);
-      }
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      sum += __shfl_xor(sum, o, kWave);
-#pragma unroll
-      for (int i = 0; i < 3; ++i) some[i] += __shfl_xor(some[i], o, kWave);
-    }
-    if (lane == 0) {
-#pragma unroll
-      for (int i = 0; i < 3; ++i)
-        if (bin_cut + i < kBins) sum += (double)some[i] * S.edge[bin_cut + i];
-      S.chunk_mass[s] = sum * unit;
+      __syncthreads();
+      const int bin = S.bin;
+      if (bin < 0 || bin == kBins - 1) continue;       // nothing that counts is cut
+      if (bin != bin_cut) held = work.gather(bin);
+      if (pass < 2) work.select(bin, held, need);
+      cut = pass < 2 ? S.cut : bound;                  // at or above the last one
+      work.record(held, cut);
+      bin_cut = bin;
+      u64 in = 0;
+      for (int s = 0; s < n_chunks; ++s) in += S.in_bin[s];
+      kept = S.before[bin] + S.edge[bin] * kUnitMass * (double)in;
     }
   }
   __syncthreads();
-  if (tid == 0) {
-    double all = 0.0;
-    for (int s = 0; s < n_chunks; ++s) all += S.chunk_mass[s];
-    const double goal = (double)p.u[m] * all;
-    double at = 0.0;
-    int pick = -1, last = 0;
-    for (int s = 0; s < n_chunks && pick < 0; ++s) {
-      if (S.chunk_mass[s] > 0.0) {
-        last = s;
-        if (at + S.chunk_mass[s] > goal) pick = s;
-        else at += S.chunk_mass[s];
-      }
+  {
+    constexpr int PART = kThreads / kMaxChunks;        // threads of a chunk
+    const int s = tid / PART, c = tid % PART;
+    double sum = 0.0;
+    if (s < n_chunks)
+      for (int b = c; b < bin_cut - S.off[s]; b += PART) sum += S.grid[s][b];
+#pragma unroll
+    for (int o = PART / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+    if (c == 0) {
+      if (bin_cut < kBins - 1 && s < n_chunks) sum += (double)S.in_bin[s] * S.edge[bin_cut];
+      S.chunk_mass[s] = sum * kUnitMass;
     }
-    if (pick < 0) {                 // u at or above 1
-      pick = last;
-      at -= S.chunk_mass[last];
+  }
+  __syncthreads();
+  if (w == 0) {                     // the chunk where the mass passes u
+    const double mine = lane < kMaxChunks ? S.chunk_mass[lane] : 0.0;
+    double incl = mine;
+#pragma unroll
+    for (int o = 1; o < kMaxChunks; o <<= 1) {
+      const double up = __shfl_up(incl, o, kWave);
+      if (lane >= o) incl += up;
     }
-    S.chunk = pick;
-    S.rest = goal - at;
-    S.all = all;
-    S.token = -1;
+    const double all = __shfl(incl, kMaxChunks - 1, kWave);
+    const double goal = u * all;
+    const u64 some = __ballot(mine > 0.0);
+    u64 hit = __ballot(mine > 0.0 && incl > goal);
+    if (hit == 0) hit = 1ull << (63 - __clzll((long long)(some | 1)));      // u at or above 1: the last
+    const int pick = __ffsll((long long)hit) - 1;
+    if (lane == pick) {
+      S.chunk = pick;
+      S.rest = goal - (incl - mine);
+      S.all = all;
+      S.token = -1;
+      S.found = 0;
+    }
   }
   __syncthreads();
   // The entry: threads take neighbouring entries of the chunk.
-  constexpr int PER = kChunk / kRowThreads;
-  const int v0 = S.chunk * kChunk + tid * PER, v1 = min(v0 + PER, p.V);
+  constexpr int PER = kChunk / kThreads;
+  const int v0 = S.chunk * kChunk + tid * PER;
   const double goal = S.rest;
-  double mine = 0.0;
-  int last = -1;
   float x[PER];
+  if (VEC && v0 + PER <= p.V) {
+    constexpr int N = 16 / (int)sizeof(DT);
+    typedef __attribute__((__vector_size__(16))) int i32x4;
+    const DT* src = reinterpret_cast<const DT*>(p.logits) + (size_t)m * p.stride + v0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int v = v0 + i;
-    x[i] = v < v1 ? logit<DT>(p, m, v) : -INFINITY;
-    if (keeps(x[i], v)) {
-      unsigned ms;
-      const int g = classify(x[i], r.width, top, &ms);
-      mine += (double)ms * S.edge[g] * unit;
-      if (ms) last = v;
+    for (int i = 0; i < PER; i += N) {
+      const i32x4 raw = ld16<i32x4>(src + i);
+      const DT* e = reinterpret_cast<const DT*>(&raw);
+#pragma unroll
+      for (int c = 0; c < N; ++c) x[i + c] = to_f32(e[c]);
     }
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) x[i] = v0 + i < p.V ? logit<DT>(p, m, v0 + i) : -INFINITY;
   }
-  double all;
-  const double pre = block_scan<double>(mine, S.part_d, &all);
-  if (mine > 0.0 && pre <= goal && pre + mine > goal) {
-    double c = pre;
-    int tok = last;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int v = v0 + i;
-      if (keeps(x[i], v)) {
-        unsigned ms;
-        const int g = classify(x[i], r.width, top, &ms);
-        const double c1 = c + (double)ms * S.edge[g] * unit;
-        if (c <= goal && c1 > goal && v <= tok) tok = v;
-        c = c1;
-      }
+  const float l_cut = cut ? logit_of(cut) : -__FLT_MAX__;
+  const int v_cut = cut ? index_of(cut) : p.V;
+  // mass of a kept entry
+  const bool near = fabs(top) < 0.5 * kFar;            // then whatever is not far below is near
+  const float ftop = (float)top;
+  auto weight = [&](float l, int v) -> float {
+    if (!(l > l_cut || (l == l_cut && v <= v_cut))) return 0.f;
+    if (near) {
+      float rest;
+      const float d = ftop - floor_near(r, l, &rest);
+      return d < kBins - 1 ? (float)mass_above(rest) * S.edge_f[(int)d] : 0.f;
     }
-    S.token = tok;
+    unsigned ms;
+    const int g = classify(r, l, top, &ms);
+    return (float)ms * S.edge_f[g];
+  };
+  float part = 0.f;                 // a thread's share in fp32: off by 2^-24 of little
+  if (near) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) part += weight(x[i], v0 + i);
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < PER; ++i)
+      if (v0 + i < p.V) part += weight(logit<DT>(p, m, v0 + i), v0 + i);
+  }
+  const double mine = (double)part;
+  const double pre = block_scan<double>(mine, S.part_d);
+  if (mine > 0.0) {
+    atomicMax(&S.found, tid + 1);
+    if (pre <= goal && pre + mine > goal) S.token = tid;
   }
   __syncthreads();
-  if (S.token < 0) {                // rounding, or u at or above 1: the last entry with a mass
-    if (last >= 0) atomicMax(&S.found, last + 1);
-    __syncthreads();
-    if (tid == 0) S.token = S.found - 1;
-    __syncthreads();
-  }
-  if (tid == 0) {
-    const int tok = S.token;
-    p.token[m] = tok;
-    if (p.logp) {
-      float lp = __uint_as_float(0x7fc00000u);
-      if (tok >= 0) {
-        unsigned ms;
-        const int g = classify(logit<DT>(p, m, tok), r.width, top, &ms);
-        lp = (float)log((double)ms * S.edge[g] * unit / S.all);
-      }
-      p.logp[m] = lp;
+  // One thread has it; rounding, or u at or above 1, leave it to the last that
+  // holds some.  A lane per entry finds which.
+  if (tid == (S.token >= 0 ? S.token : S.found - 1)) S.rest = goal - pre;
+  __syncthreads();
+  if (w == 0) {
+    static_assert(PER <= kWave, "a lane per entry");
+    const int v = S.chunk * kChunk + max(S.token >= 0 ? S.token : S.found - 1, 0) * PER + lane;
+    const double one = lane < PER && v < p.V ? (double)weight(logit<DT>(p, m, v), v) : 0.0;
+    double incl = one;
+#pragma unroll
+    for (int o = 1; o < PER; o <<= 1) {
+      const double up = __shfl_up(incl, o, kWave);
+      if (lane >= o) incl += up;
+    }
+    const u64 some = __ballot(one > 0.0);
+    u64 hit = __ballot(one > 0.0 && incl > S.rest);
+    if (hit == 0) hit = 1ull << (63 - __clzll((long long)(some | 1)));
+    if (lane == __ffsll((long long)hit) - 1) {
+      p.token[m] = v;
+      if (p.logp) p.logp[m] = (float)log(one / S.all);
     }
   }
 }
@@ -696,17 +855,20 @@ hipError_t launch_sample_logits(const SampleLogitsLaunch& L, hipStream_t st) {
   const int size = L.dtype_bf16 ? 2 : 4;
   const bool vec = ((uintptr_t)L.logits & 15) == 0 && L.stride * size % 16 == 0 && (size_t)L.V * size % 16 == 0;
   trace_begin(st);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(L.M * nc), dim3(256), 0, st, L, nc); };
+  auto go = [&](auto kernel, int n) { hipLaunchKernelGGL(kernel, dim3(n), dim3(kThreads), 0, st, L, nc); };
   if (L.dtype_bf16) {
-    if (vec) go(chunk_kernel<bf16, true>); else go(chunk_kernel<bf16, false>);
+    if (vec) go(chunk_kernel<bf16, true>, L.M * nc); else go(chunk_kernel<bf16, false>, L.M * nc);
   } else {
-    if (vec) go(chunk_kernel<float, true>); else go(chunk_kernel<float, false>);
+    if (vec) go(chunk_kernel<float, true>, L.M * nc); else go(chunk_kernel<float, false>, L.M * nc);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   trace_mark(st);
-  if (L.dtype_bf16) hipLaunchKernelGGL(row_kernel<bf16>, dim3(L.M), dim3(kRowThreads), 0, st, L, nc);
-  else hipLaunchKernelGGL(row_kernel<float>, dim3(L.M), dim3(kRowThreads), 0, st, L, nc);
+  if (L.dtype_bf16) {
+    if (vec) go(row_kernel<bf16, true>, L.M); else go(row_kernel<bf16, false>, L.M);
+  } else {
+    if (vec) go(row_kernel<float, true>, L.M); else go(row_kernel<float, false>, L.M);
+  }
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   trace_mark(st);

@@ -631,6 +631,13 @@ ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_YARN = 0, 1, 2, 3
 def _need_rows(t: torch.Tensor, name: str, dtype, device, ndim: int) -> int:
     """Like _need, but rows (dim 0) may lie further apart than they are long,
     as in a slice of a wider projection.  Returns the row stride in elements."""
+    try:
+        if t.is_cuda and t.dtype is dtype and t.device == device and isinstance(t, torch.Tensor):
+            size, step = t.shape, t.stride()
+            if len(size) == ndim and size[0] > 1 and step[-1] == 1 and (ndim == 2 or step[1] == size[2]):
+                return step[0]        # a stride shorter than the row is refused by the library
+    except AttributeError:
+        pass                          # not a tensor: named below
     if isinstance(t, torch.Tensor) and t.dim() == ndim and t.shape[0] > 0 and not t.is_contiguous():
         _need(t[0], name, dtype, device, ndim - 1)
         if t.shape[0] > 1:
