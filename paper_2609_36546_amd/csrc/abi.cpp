@@ -563,6 +563,7 @@ static int q8_check(int n_seq, int max_q, int Hkv, int D, int page_size, int num
     return fail(IPDV_EUNSUPPORTED, "page_size=%d not in {16, 32, 64}", page_size);
   if ((long)n_seq * Hkv > 65535) return fail(IPDV_EUNSUPPORTED, "n_seq * Hkv exceeds 65535");
   if (max_q >= 1 << 27) return fail(IPDV_EUNSUPPORTED, "max_q too large");
+  if ((int64_t)num_pages * Hkv >= (int64_t)1 << 31) return fail(IPDV_EUNSUPPORTED, "num_pages * Hkv exceeds 2^31 - 1");
   if (dtype != IPDV_F32 && dtype != IPDV_BF16) return fail(IPDV_EUNSUPPORTED, "dtype %d", dtype);
   return IPDV_OK;
 }

@@ -19,22 +19,34 @@
 // two PV steps: P never leaves the lane.  Key channels are dealt to the k-steps
 // the same way, 16 bytes of a key row at a time.
 //
-// Precision.  An e4m3 value times a power of two is exact in bf16, so keys and
-// values enter the bf16 products without a rounding: the key's scale in the
-// conversion, the value's in the probability.  Queries are bf16 already; fp32
-// queries, and the fp32 call's probabilities, are split into three bf16 terms
-// (24 bits), which makes their products exact to fp32 as well.  The bf16 call
-// rounds its probabilities to bf16 once, as the bf16 cache's attention does.
+// Precision.  The bf16 call's scores: a query's channels become two e4m3
+// numbers each, the first with the scale of the largest, the second what that
+// leaves (8 bits in all, as bf16 has, down to 2^-22 of the largest), and
+// the keys go into the scaled fp8 products as they lie in the cache, with their
+// own scale: nothing is rounded or converted on the way.  Values times
+// probabilities: an e4m3 value is exact in bf16, its scale goes into the
+// probability, which is rounded to bf16 once, as the bf16 cache's attention
+// does.  The fp32 call: keys and values exact in bf16 (the key's scale in the
+// conversion), queries and probabilities split into three bf16 terms (24 bits).
 // Sums and the running maximum are fp32.
 //
-// Work split.  All blocks of all items (an item: one row group of one
-// (sequence, KV head)) form one line, cut into as many equal spans as there are
-// workgroups, so that ragged contexts, single sequences and long prompts all
-// fill the chip.  A workgroup's four waves are RG row groups x KS key parts: up
-// to 64 rows KS = 4 (each wave its own keys, every byte read and converted
-// once), more rows share their keys through the vector cache.  Items cut by a
-// span's end leave partial results, merged by a second kernel.
+// Work split.  All steps (a step: the keys that a workgroup takes at once) of
+// all items (an item: one row group of one (sequence, KV head)) form one line,
+// cut into as many equal spans as there are workgroups, so that ragged contexts,
+// single sequences and long prompts all fill the chip.  Items cut by a span's
+// end leave partial results, merged by a second kernel.
+//
+// A workgroup's four waves are RG row groups of QT tiles x KS = 4 / RG key parts,
+// merged in LDS at an item's end; plan_of has the choice.  With one row group
+// (attn_q8_keys_kernel) every wave streams keys of its own, straight into
+// registers.  With more (attn_q8_rows_kernel) the groups share their keys through
+// LDS, filled by direct-to-LDS loads that run a step ahead through the span,
+// across its items.  (Through the vector cache instead, 64 windows of eight over
+// 1024 to 8192 tokens, 32 heads on 4, took 121 us where this takes 93: a second
+// request for a line that is still on its way holds the cache up.)
+//
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "kernels.h"
@@ -45,6 +57,12 @@ namespace {
 
 constexpr int kBlk = 64;                // keys per block
 constexpr float kRescaleSlack = 8.0f;   // log2 units a stale running max may lag
+
+// The item that a span begins in.
+struct SpanHead {
+  long first;          // where it begins on the line (the last entry: the line's length)
+  int steps, slot, g, r;
+};
 
 struct Q8Params {
   const void* q;
@@ -57,16 +75,16 @@ struct Q8Params {
   const int32_t* cu_q;
   const int32_t* seq_ids;
   void* out;
-  long* head;          // [0] the line's length, then the first block of every item
+  struct SpanHead* span;   // [grid + 1]: what every span begins in; the last: the line's length
   float* part_o;       // [2 * grid][item rows][D]
   float* part_ml;      // [2 * grid][item rows][2]: maximum, sum
-  int max_pages, Hq, Hkv, G, log2ps, num_pages, n_seq, max_q;
-  int n_rg;            // items per (sequence, KV head) at most
-  int rg;              // row groups per workgroup: 1, 2 or 4
+  int max_pages, Hq, Hkv, G, log2g, log2ps, num_pages, n_seq, max_q;   // log2g: of G, or -1
   float scale_log2;
 };
 
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+
+typedef __attribute__((__vector_size__(8 * sizeof(int)))) int i32x8;
 
 // Eight e4m3 values times 2^e, exact.
 __device__ __forceinline__ bf16x8 cvt8(unsigned lo, unsigned hi, float scale) {
@@ -77,32 +95,96 @@ __device__ __forceinline__ bf16x8 cvt8(unsigned lo, unsigned hi, float scale) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// One block of 64 keys as a lane holds it.
+// Values that do not change while a kernel runs, at addresses all lanes share:
+// scalar loads, which do not queue behind the vector loads of keys and values.
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+__device__ __forceinline__ ScalarInts scalar(const int32_t* p) { return (ScalarInts)(uintptr_t)p; }
+
+// (page, head) of the four units of a block, looked up a block ahead.
+struct Units {
+  int p0, p1, p2, p3;
+  __device__ __forceinline__ void look_up(const Q8Params& a, ScalarInts pt, int t0, int g) {
+    auto at = [&](int i) {
+      return min(max(pt[min((t0 + 16 * i) >> a.log2ps, a.max_pages - 1)], 0), a.num_pages - 1) * a.Hkv + g;
+    };
+    p0 = at(0);
+    p1 = at(1);
+    p2 = at(2);
+    p3 = at(3);
+  }
+  __device__ __forceinline__ unsigned of(int u) const {
+    const int q0 = p0, q1 = p1, q2 = p2, q3 = p3;   // by value: a choice between variables would go through memory
+    const int lo = u & 1 ? q1 : q0, hi = u & 1 ? q3 : q2;
+    return (unsigned)(u & 2 ? hi : lo);
+  }
+};
+
+// One block of 64 keys in registers.
 template <int D> struct Block {
   uint4 k[4][D / 64];   // key tile t: 16 channels of one key per load
   uint4 v[D / 16];      // channel tile: one channel's 16 slots of unit j
   uint4 ks, vs;         // scale bytes: the lane's key unit (c16 / 4), its value unit (j)
+  __device__ __forceinline__ uint4 key(int t, int h) const { return k[t][h]; }
+  __device__ __forceinline__ uint4 val(int dt) const { return v[dt]; }
+  __device__ __forceinline__ uint4 key_scales() const { return ks; }
+  __device__ __forceinline__ uint4 val_scales() const { return vs; }
 };
 
+// The same block in LDS: every load of 1 KB as the wave that asked for it has
+// its lanes, so that the same lane of any wave reads its 16 bytes back; behind
+// them the scale bytes of the four units, keys then values.
+template <int D> struct LdsBlock {
+  static constexpr int kKeys = 4 * (D / 64), kVals = D / 16, kLoads = kKeys + kVals;
+  static constexpr int kBytes = (kLoads + 1) * kWave * 16;
+  const char* at;
+  __device__ __forceinline__ uint4 get(int i) const {
+    return *reinterpret_cast<const uint4*>(at + i * (kWave * 16) + lane_id() * 16);
+  }
+  __device__ __forceinline__ uint4 scales(int i) const {
+    return *reinterpret_cast<const uint4*>(at + kLoads * (kWave * 16) + i * 16);
+  }
+  __device__ __forceinline__ uint4 key(int t, int h) const { return get(4 * h + t); }
+  __device__ __forceinline__ uint4 val(int dt) const { return get(kKeys + dt); }
+  __device__ __forceinline__ uint4 key_scales() const { return scales((lane_id() & 15) >> 2); }
+  __device__ __forceinline__ uint4 val_scales() const { return scales(4 + (lane_id() >> 4)); }
+};
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+// A barrier for what goes through LDS, which leaves loads under way.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" : : : "memory");
+}
+
+
 template <int D>
-__device__ __forceinline__ void load_block(const Q8Params& a, Block<D>& f, int t0, int g, const int* pt_row) {
+__device__ __forceinline__ void load_keys(const Q8Params& a, Block<D>& f, int t0, const Units& units) {
   const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
-  const int ps = 1 << a.log2ps;
-  const int ku = t0 + 16 * (c16 >> 2), vu = t0 + 16 * j;
-  const int kpg = min(max(pt_row[min(ku >> a.log2ps, a.max_pages - 1)], 0), a.num_pages - 1);
-  const int vpg = min(max(pt_row[min(vu >> a.log2ps, a.max_pages - 1)], 0), a.num_pages - 1);
-  const size_t kh = (size_t)kpg * a.Hkv + g, vh = (size_t)vpg * a.Hkv + g;
-  const int ks0 = ku & (ps - 1), vs0 = vu & (ps - 1);
-  const uint8_t* kb = a.k_pages + kh * D * ps + (size_t)(ks0 + (c16 & 3)) * 16;
+  const int ps = 1 << a.log2ps, ks0 = (t0 + 16 * (c16 >> 2)) & (ps - 1);
+  const unsigned kh = units.of(c16 >> 2);
+  const uint8_t* kb = a.k_pages + ((unsigned long)kh * (unsigned)(D * ps) + (unsigned)((ks0 + (c16 & 3) + j * ps) * 16));
 #pragma unroll
-  for (int h = 0; h < D / 64; ++h)
+  for (int h = 0; h < D / 64; ++h) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) f.k[t][h] = ld16<uint4>(kb + ((4 * h + j) * ps + 4 * t) * 16);
-  const uint8_t* vb = a.v_pages + vh * D * ps + vs0;
+    for (int t = 0; t < 4; ++t) f.k[t][h] = ld16<uint4>(kb + 64 * t);
+    kb += 64 * ps;
+  }
+  f.ks = ld16<uint4>(a.scales + ((unsigned long)kh * (unsigned)(2 * ps) + (unsigned)ks0));
+}
+template <int D>
+__device__ __forceinline__ void load_values(const Q8Params& a, Block<D>& f, int t0, const Units& units) {
+  const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
+  const int ps = 1 << a.log2ps, vs0 = (t0 + 16 * j) & (ps - 1);
+  const unsigned vh = units.of(j);
+  const uint8_t* vb = a.v_pages + ((unsigned long)vh * (unsigned)(D * ps) + (unsigned)(vs0 + c16 * ps));
+  int tile = 16 * ps;                 // a step that the compiler cannot see through: it would keep the
+  asm("" : "+s"(tile));               // multiples in registers that it does not have
 #pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt) f.v[dt] = ld16<uint4>(vb + (16 * dt + c16) * ps);
-  f.ks = ld16<uint4>(a.scales + kh * 2 * ps + ks0);
-  f.vs = ld16<uint4>(a.scales + vh * 2 * ps + ps + vs0);
+  for (int dt = 0; dt < D / 16; ++dt) {
+    f.v[dt] = ld16<uint4>(vb);
+    vb += tile;
+  }
+  f.vs = ld16<uint4>(a.scales + ((unsigned long)vh * (unsigned)(2 * ps) + (unsigned)(ps + vs0)));
 }
 
 __device__ __forceinline__ unsigned word(const uint4& v, int i) {
@@ -118,50 +200,120 @@ template <int NS> __device__ __forceinline__ void split(float x, __bf16 (&t)[NS]
   }
 }
 
+// The lane's queries: fp32 ones in NS = 3 bf16 terms, bf16 ones in two e4m3
+// terms, 32 channels (D = 64: 16, and 16 zeros), with the row's scale bytes.
 template <int D, int QT, int NS> struct Queries { bf16x8 q[NS][QT][D / 32]; };
+template <int D, int QT> struct Queries<D, QT, 1> {
+  i32x8 hi[QT], lo[QT];
+  int e_hi[QT], e_lo[QT];
+};
+// 16 values of a lane from channel tile h: D / 64 such tiles make up its share.
+template <int D, int QT>
+__device__ __forceinline__ void split_e4m3(Queries<D, QT, 1>& Q, int q, const bf16x8 (&x)[D / 32]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m = fmaxf(m, fabsf((float)x[i][k]));
+  m = fmaxf(m, lane_xor16(m));
+  m = fmaxf(m, lane_xor32(m));
+  // the scale that kv_q8 would take, but no less than 2^-122: the second's is 2^-4 of it
+  const unsigned u = __float_as_uint(m);
+  int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u);
+  e = min(max(e, -122), 120);                 // a query that is not finite stays so
+  const float down = __uint_as_float((unsigned)(127 - e) << 23);
+  Q.e_hi[q] = e + 127;
+  Q.e_lo[q] = e + 123;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    int hi = 0, lo = 0;
+    if (i < D / 16) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const float a = (float)x[i >> 1][4 * (i & 1) + 2 * p] * down, b = (float)x[i >> 1][4 * (i & 1) + 2 * p + 1] * down;
+        hi = p ? __builtin_amdgcn_cvt_pk_fp8_f32(a, b, hi, true) : __builtin_amdgcn_cvt_pk_fp8_f32(a, b, hi, false);
+        const auto v = p ? __builtin_amdgcn_cvt_pk_f32_fp8(hi, true) : __builtin_amdgcn_cvt_pk_f32_fp8(hi, false);
+        const float ra = (a - v[0]) * 16.f, rb = (b - v[1]) * 16.f;
+        lo = p ? __builtin_amdgcn_cvt_pk_fp8_f32(ra, rb, lo, true) : __builtin_amdgcn_cvt_pk_fp8_f32(ra, rb, lo, false);
+      }
+    }
+    Q.hi[q][i] = hi;
+    Q.lo[q][i] = lo;
+  }
+}
 
-// TAIL: some row of the wave does not see every key of the block.
-template <int D, int QT, int NS, bool TAIL>
-__device__ __forceinline__ void attend(const Block<D>& f, const Queries<D, QT, NS>& Q, float c, int t0, int n_lim,
-                                       const int (&qlimit)[QT], floatx4 (&acc)[QT][D / 16], float (&m_run)[QT],
-                                       float (&l_run)[QT]) {
-  const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
-  floatx4 s[QT][4];
+// Scores of a block: s[q][t][e] of the lane's row of tile q against unit j, slot
+// 4 t + e.
+template <int D, int QT, int NS, class B>
+__device__ __forceinline__ void scores(const B& f, const Queries<D, QT, NS>& Q, floatx4 (&s)[QT][4]) {
+  const int c16 = lane_id() & 15;
+  const uint4 kscale = f.key_scales();
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
 #pragma unroll
     for (int q = 0; q < QT; ++q) s[q][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-    const float ksc = __uint_as_float(((word(f.ks, t) >> (8 * (c16 & 3))) & 255u) << 23);
+    const unsigned kbyte = (word(kscale, t) >> (8 * (c16 & 3))) & 255u;
+    if constexpr (NS == 1) {
+      i32x8 kf = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-    for (int h = 0; h < D / 64; ++h)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const bf16x8 kf = cvt8(x ? f.k[t][h].z : f.k[t][h].x, x ? f.k[t][h].w : f.k[t][h].y, ksc);
-#pragma unroll
-        for (int n = 0; n < NS; ++n)
-#pragma unroll
-          for (int q = 0; q < QT; ++q)
-            s[q][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, Q.q[n][q][2 * h + x], s[q][t], 0, 0, 0);
+      for (int h = 0; h < D / 64; ++h) {
+        const uint4 w = f.key(t, h);
+        kf[4 * h + 0] = (int)w.x;
+        kf[4 * h + 1] = (int)w.y;
+        kf[4 * h + 2] = (int)w.z;
+        kf[4 * h + 3] = (int)w.w;
       }
+#pragma unroll
+      for (int q = 0; q < QT; ++q)
+        s[q][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, Q.lo[q], s[q][t], 0, 0, 0, (int)kbyte, 0, Q.e_lo[q]);
+#pragma unroll
+      for (int q = 0; q < QT; ++q)
+        s[q][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kf, Q.hi[q], s[q][t], 0, 0, 0, (int)kbyte, 0, Q.e_hi[q]);
+    } else {
+      const float ksc = __uint_as_float(kbyte << 23);
+#pragma unroll
+      for (int h = 0; h < D / 64; ++h) {
+        const uint4 kq = f.key(t, h);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const bf16x8 kf = cvt8(x ? kq.z : kq.x, x ? kq.w : kq.y, ksc);
+#pragma unroll
+          for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int q = 0; q < QT; ++q)
+              s[q][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, Q.q[n][q][2 * h + x], s[q][t], 0, 0, 0);
+        }
+      }
+    }
   }
-  // s[q][t][e]: the lane's row of tile q against unit j, slot 4 t + e
-  const int u0 = t0 + 16 * j;
-  float bm[QT];
+}
+
+// The block's probabilities and values.  `tail`: some row of the wave does not
+// see every key of the block.
+template <int D, int QT, int NS, class B>
+__device__ __forceinline__ void attend(const B& f, floatx4 (&s)[QT][4], float c, bool tail, int t0, int n_keys,
+                                       const int (&qlimit)[QT], floatx4 (&acc)[QT][D / 16], float (&m_run)[QT],
+                                       float (&l_run)[QT]) {
+  const int u0 = t0 + 16 * (lane_id() >> 4);          // unit j's first position
+  if (tail) {
+#pragma unroll
+    for (int q = 0; q < QT; ++q)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (u0 + i >= qlimit[q]) s[q][i >> 2][i & 3] = -INFINITY;
+  }
+  float bm[QT], m_use[QT];
+  bool rescale = false;
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
     bm[q] = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (TAIL && u0 + i >= qlimit[q]) s[q][i >> 2][i & 3] = -INFINITY;
-      bm[q] = fmaxf(bm[q], s[q][i >> 2][i & 3]);
-    }
+    for (int i = 0; i < 16; ++i) bm[q] = fmaxf(bm[q], s[q][i >> 2][i & 3]);
   }
 #pragma unroll
   for (int q = 0; q < QT; ++q) bm[q] = fmaxf(bm[q], lane_xor16(bm[q]));
 #pragma unroll
   for (int q = 0; q < QT; ++q) bm[q] = fmaxf(bm[q], lane_xor32(bm[q]));
-  float m_use[QT];
-  bool rescale = false;
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
     const float bx = bm[q] * c, m_old = m_run[q];
@@ -180,41 +332,51 @@ __device__ __forceinline__ void attend(const Block<D>& f, const Queries<D, QT, N
       for (int dt = 0; dt < D / 16; ++dt) acc[q][dt] *= alpha;
     }
   }
+  bf16x8 pf[NS][QT][2];
+  const uint4 vscale = f.val_scales();
 #pragma unroll
-  for (int st = 0; st < 2; ++st) {       // slots 8 st .. 8 st + 7 of unit j
-    bf16x8 pf[NS][QT];
-    float vsc[8];
+  for (int i = 0; i < 16; ++i) {           // slot i of unit j
+    const float vsc = __uint_as_float(((word(vscale, i >> 2) >> (8 * (i & 3))) & 255u) << 23);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      vsc[i] = scale_value((word(f.vs, 2 * st + (i >> 2)) >> (8 * (i & 3))) & 255u);
+    for (int q = 0; q < QT; ++q) {
+      const float p = fast_exp2(fmaf(s[q][i >> 2][i & 3], c, -m_use[q]));
+      l_run[q] += p;
+      __bf16 t[NS];
+      split<NS>(p * vsc, t);
+#pragma unroll
+      for (int n = 0; n < NS; ++n) pf[n][q][i >> 3][i & 7] = t[n];
+    }
+  }
+  if (tail) {
+    // An unseen key's scale byte may be anything, a later row's that of NaN
+    // (infinite here, and times its zero bytes NaN); bytes behind the last key
+    // may be NaN.
 #pragma unroll
     for (int q = 0; q < QT; ++q)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float p = fast_exp2(fmaf(s[q][2 * st + (i >> 2)][i & 3], c, -m_use[q]));
-        l_run[q] += p;
-        // an unseen key's scale may be anything, a later row's may be NaN
-        float pv = p * vsc[i];
-        if (TAIL && u0 + 8 * st + i >= qlimit[q]) pv = 0.f;
-        __bf16 t[NS];
-        split<NS>(pv, t);
+      for (int i = 0; i < 16; ++i)
 #pragma unroll
-        for (int n = 0; n < NS; ++n) pf[n][q][i] = t[n];
-      }
+        for (int n = 0; n < NS; ++n)
+          if (u0 + i >= qlimit[q]) pf[n][q][i >> 3][i & 7] = static_cast<__bf16>(0.f);
+  }
 #pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) {
-      unsigned lo = st ? f.v[dt].z : f.v[dt].x, hi = st ? f.v[dt].w : f.v[dt].y;
-      if (TAIL) {                        // bytes behind the last key may be NaN
-        const int live = n_lim - (u0 + 8 * st);
-        lo = live >= 4 ? lo : live <= 0 ? 0u : lo & ((1u << (8 * live)) - 1u);
-        hi = live >= 8 ? hi : live <= 4 ? 0u : hi & ((1u << (8 * (live - 4))) - 1u);
-      }
-      const bf16x8 vf = cvt8(lo, hi, 1.0f);
+  for (int dt = 0; dt < D / 16; ++dt) {
+    uint4 w = f.val(dt);
+    if (tail) {
+      auto live = [&](unsigned x, int at) {  // the bytes of slots at .. at + 3
+        const int n = n_keys - (u0 + at);
+        return n >= 4 ? x : n <= 0 ? 0u : x & ((1u << (8 * n)) - 1u);
+      };
+      w = make_uint4(live(w.x, 0), live(w.y, 4), live(w.z, 8), live(w.w, 12));
+    }
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {       // slots 8 st .. 8 st + 7 of unit j
+      const bf16x8 vf = cvt8(st ? w.z : w.x, st ? w.w : w.y, 1.0f);
 #pragma unroll
       for (int n = 0; n < NS; ++n)
 #pragma unroll
         for (int q = 0; q < QT; ++q)
-          acc[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][q], acc[q][dt], 0, 0, 0);
+          acc[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][q][st], acc[q][dt], 0, 0, 0);
     }
   }
 }
@@ -234,42 +396,77 @@ __device__ __forceinline__ Seq seq_of(const Q8Params& a, int slot, int item_rows
   s.n_rg = (s.rows + item_rows - 1) / item_rows;
   return s;
 }
-// Blocks of row group r: up to the last key that its last row sees.
-__device__ __forceinline__ int item_blocks(const Q8Params& a, const Seq& s, int r, int item_rows) {
-  const int last = min((r + 1) * item_rows, s.rows) - 1;
-  return (s.L + last / a.G + kBlk) / kBlk;
+// The same where all lanes ask for one slot: scalar loads.
+__device__ __forceinline__ Seq same_seq_of(const Q8Params& a, int slot, int item_rows) {
+  Seq s;
+  s.b = a.seq_ids ? scalar(a.seq_ids)[slot] : slot;
+  s.L = max(scalar(a.ctx_lens)[s.b], 0);
+  s.r0 = scalar(a.cu_q)[s.b];
+  s.kb = min(max(scalar(a.cu_q)[s.b + 1] - s.r0, 0), a.max_q);
+  s.rows = s.kb * a.G;
+  s.n_rg = (s.rows + item_rows - 1) / item_rows;
+  return s;
 }
-__device__ __forceinline__ long head_blocks(const Q8Params& a, const Seq& s, int item_rows) {
+// Window row of a packed row.
+__device__ __forceinline__ int pos_of(const Q8Params& a, int row) { return a.log2g >= 0 ? row >> a.log2g : row / a.G; }
+// Steps (of `step` keys) of row group r: up to the last key that its last row sees.
+__device__ __forceinline__ int item_steps(const Q8Params& a, const Seq& s, int r, int item_rows, int step) {
+  const int last = min((r + 1) * item_rows, s.rows) - 1;
+  return (int)((unsigned)(s.L + pos_of(a, last) + step) / (unsigned)step);
+}
+__device__ __forceinline__ long head_steps(const Q8Params& a, const Seq& s, int item_rows, int step) {
   long n = 0;
-  for (int r = 0; r < s.n_rg; ++r) n += item_blocks(a, s, r, item_rows);
+  for (int r = 0; r < s.n_rg; ++r) n += item_steps(a, s, r, item_rows, step);
   return n;
 }
 __device__ __forceinline__ long span_start(long total, long n, long w) { return w * total / n; }
-// Spans in use: no more than there are groups of `parts` blocks.
+// Spans in use: no more than there are groups of `parts` steps.
 __device__ __forceinline__ long spans(long total, int parts, int grid) {
   const long n = (total + parts - 1) / parts;
   return n < grid ? (n > 0 ? n : 1) : grid;
 }
 
-template <typename DT, int D, int QT>
-__global__ __launch_bounds__(256) void attn_q8_kernel(Q8Params a) {
-  constexpr int NS = sizeof(DT) == 2 ? 1 : 3;
-  constexpr int WR = 16 * QT;                       // rows of a wave
-  typedef floatx4 Acc[QT][D / 16][kWave];
-  __shared__ __attribute__((aligned(16))) char s_acc[2 * sizeof(Acc)];
-  __shared__ float s_ml[2][2][WR];
-  __shared__ long s_sum[4];
-  __shared__ long s_at[2];                          // the span's first slot, and its offset there
-  const int tid = threadIdx.x, wv = tid >> 6, lane = lane_id();
-  const int c16 = lane & 15, j = lane >> 4;
-  const int RG = a.rg, KS = 4 / RG, rg = wv % RG, ks = wv / RG;
-  const int item_rows = RG * WR;
+// A place on the line: an item, and where on the line it begins.
+struct Place {
+  int slot, g, r, steps;
+  long first;
+  Seq sq;
+};
+__device__ __forceinline__ bool next_item(const Q8Params& a, Place& c, int item_rows, int step) {
+  c.first += c.steps;
+  if (++c.r == c.sq.n_rg) {
+    c.r = 0;
+    if (++c.g == a.Hkv) {
+      c.g = 0;
+      do {
+        if (++c.slot >= a.n_seq) return false;
+        c.sq = same_seq_of(a, c.slot, item_rows);
+      } while (c.sq.n_rg == 0);
+    }
+  }
+  c.steps = item_steps(a, c.sq, c.r, item_rows, step);
+  return true;
+}
 
-  // Every workgroup adds up the whole line: a thread takes neighbouring slots.
-  const int per = (a.n_seq + 255) / 256;
+// The workgroup's span [*from, *to) of the line, and the item that it begins in.
+// Every workgroup adds up the whole line, a thread neighbouring slots.  False
+// when it has no span.
+template <int THREADS>
+__device__ __forceinline__ bool find_span(const Q8Params& a, int item_rows, int step, int parts, long* from, long* to,
+                                          Place& c) {
+  __shared__ long s_sum[THREADS / kWave];
+  __shared__ long s_at[2];                          // the span's first slot, and where it begins
+  constexpr int kKept = 1024;
+  __shared__ int s_steps[kKept];                    // a head's steps, of the first slots
+  const int tid = threadIdx.x, lane = lane_id(), wv = tid >> 6;
+  const int per = (a.n_seq + THREADS - 1) / THREADS;
   const int sl0 = min(tid * per, a.n_seq), sl1 = min(sl0 + per, a.n_seq);
   long mine = 0;
-  for (int i = sl0; i < sl1; ++i) mine += a.Hkv * head_blocks(a, seq_of(a, i, item_rows), item_rows);
+  for (int i = sl0; i < sl1; ++i) {
+    const long n = head_steps(a, seq_of(a, i, item_rows), item_rows, step);
+    if (i < kKept) s_steps[i] = (int)min(n, 0x7fffffffl);
+    mine += a.Hkv * n;
+  }
   long incl = mine;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
@@ -280,59 +477,73 @@ __global__ __launch_bounds__(256) void attn_q8_kernel(Q8Params a) {
   __syncthreads();
   long before = 0, total = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < THREADS / kWave; ++i) {
     if (i < wv) before += s_sum[i];
     total += s_sum[i];
   }
-  if (blockIdx.x == 0 && tid == 0) a.head[0] = total;
-  const long n_span = spans(total, KS, gridDim.x);
-  if (blockIdx.x >= n_span || total == 0) return;
-  const long sp0 = span_start(total, n_span, blockIdx.x), sp1 = span_start(total, n_span, blockIdx.x + 1);
-  {
-    const long e0 = before + incl - mine;
-    if (sp0 >= e0 && sp0 < e0 + mine) {
-      long at = e0;
-      for (int i = sl0; i < sl1; ++i) {
-        const long n = a.Hkv * head_blocks(a, seq_of(a, i, item_rows), item_rows);
-        if (sp0 < at + n) {
-          s_at[0] = i;
-          s_at[1] = at;
-          break;
-        }
-        at += n;
+  if (blockIdx.x == 0 && tid == 0) a.span[gridDim.x].first = total;
+  const long n = spans(total, parts, gridDim.x);
+  if (blockIdx.x >= n || total == 0) return false;
+  const long p0 = span_start(total, n, blockIdx.x), p1 = span_start(total, n, blockIdx.x + 1);
+  const long e0 = before + incl - mine;
+  if (p0 >= e0 && p0 < e0 + mine) {
+    long at = e0;
+    for (int i = sl0; i < sl1; ++i) {
+      long k = i < kKept ? s_steps[i] : 0x7fffffff;
+      if (k == 0x7fffffff) k = head_steps(a, seq_of(a, i, item_rows), item_rows, step);
+      k *= a.Hkv;
+      if (p0 < at + k) {
+        s_at[0] = i;
+        s_at[1] = at;
+        break;
       }
+      at += k;
     }
   }
   __syncthreads();
-  int slot = (int)s_at[0];
-  long item0 = s_at[1];                             // the item's first block on the line
-  Seq sq = seq_of(a, slot, item_rows);
-  int g, r = 0;
-  {
-    const long hb = head_blocks(a, sq, item_rows);
-    g = (int)((sp0 - item0) / hb);
-    item0 += g * hb;
+  // the same for all lanes, and known to be
+  auto uniform = [](long x) {
+    return (long)(((unsigned long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) |
+                  (unsigned)__builtin_amdgcn_readfirstlane((int)x));
+  };
+  *from = uniform(p0);
+  *to = uniform(p1);
+  c.slot = __builtin_amdgcn_readfirstlane((int)s_at[0]);
+  c.first = uniform(s_at[1]);
+  c.sq = same_seq_of(a, c.slot, item_rows);
+  long hb = c.slot < kKept ? s_steps[c.slot] : 0x7fffffff;
+  if (hb == 0x7fffffff) hb = head_steps(a, c.sq, item_rows, step);
+  hb = uniform(hb);
+  c.g = (int)((*from - c.first) / hb);
+  c.first += c.g * hb;
+  c.r = 0;
+  c.steps = item_steps(a, c.sq, 0, item_rows, step);
+  while (c.first + c.steps <= *from) {
+    c.first += c.steps;
+    c.steps = item_steps(a, c.sq, ++c.r, item_rows, step);
   }
-  int nb = item_blocks(a, sq, 0, item_rows);
-  while (item0 + nb <= sp0) {
-    item0 += nb;
-    nb = item_blocks(a, sq, ++r, item_rows);
-  }
+  if (tid == 0) a.span[blockIdx.x] = {c.first, c.steps, c.slot, c.g, c.r};
+  return true;
+}
 
-  for (long pos = sp0; pos < sp1;) {
-    const int jb0 = (int)(pos - item0), jb1 = (int)min((long)nb, sp1 - item0);
-    const bool whole = jb0 == 0 && jb1 == nb;
-    if (jb0 == 0 && tid == 0) a.head[1 + ((long)slot * a.Hkv + g) * a.n_rg + r] = item0;
-    // ---- the wave's rows and keys ----
-    const int pr0 = r * item_rows + rg * WR;
-    const int* pt_row = a.page_table + (size_t)sq.b * a.max_pages;
-    int qlimit[QT];
-#pragma unroll
-    for (int q = 0; q < QT; ++q) qlimit[q] = sq.L + min(pr0 + 16 * q + c16, sq.rows - 1) / a.G + 1;
-    const int n_keys = sq.L + (min(pr0 + WR, sq.rows) - 1) / a.G + 1;   // keys that some row sees
-    const int all_see = sq.L + pr0 / a.G + 1;                     // keys below are seen by every row
-    floatx4 acc[QT][D / 16];
-    float m_run[QT], l_run[QT];
+// What a wave holds of its 16 QT rows while it walks their keys.
+template <typename DT, int D, int QT>
+struct Rows {
+  static constexpr int NS = sizeof(DT) == 2 ? 1 : 3;
+  floatx4 acc[QT][D / 16];
+  float m_run[QT], l_run[QT];
+  Queries<D, QT, NS> Q;
+  int qlimit[QT];
+  int pr0;         // first packed row of the item's (sequence, head)
+  int n_keys;      // keys that some row sees
+  int all_see;     // keys below are seen by every row
+
+  __device__ __forceinline__ void begin(const Q8Params& a, const Place& c, int first_row) {
+    const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
+    const Seq& sq = c.sq;
+    pr0 = first_row;
+    n_keys = pr0 < sq.rows ? sq.L + pos_of(a, min(pr0 + 16 * QT, sq.rows) - 1) + 1 : 0;
+    all_see = sq.L + pos_of(a, pr0) + 1;
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
       m_run[q] = -INFINITY;
@@ -340,183 +551,363 @@ __global__ __launch_bounds__(256) void attn_q8_kernel(Q8Params a) {
 #pragma unroll
       for (int dt = 0; dt < D / 16; ++dt) acc[q][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
-    if (pr0 < sq.rows) {
-      Queries<D, QT, NS> Q;
+    if (n_keys == 0) return;
 #pragma unroll
-      for (int q = 0; q < QT; ++q) {
-        const int pr = pr0 + 16 * q + c16;
-        const bool on = pr < sq.rows;
-        const int i = on ? pr / a.G : 0, hl = on ? pr - i * a.G : 0;
-        const DT* qr = reinterpret_cast<const DT*>(a.q) + (size_t)(sq.r0 + i) * a.q_stride + (size_t)(g * a.G + hl) * D;
+    for (int q = 0; q < QT; ++q) {
+      const int pr = pr0 + 16 * q + c16;
+      qlimit[q] = sq.L + pos_of(a, min(pr, sq.rows - 1)) + 1;
+      const int row = min(pr, sq.rows - 1), i = pos_of(a, row), hl = row - i * a.G;      // rows behind the last: its copies
+      const DT* qr = reinterpret_cast<const DT*>(a.q) + (size_t)(sq.r0 + i) * a.q_stride + (size_t)(c.g * a.G + hl) * D;
+      if constexpr (NS == 1) {
+        bf16x8 x[D / 32];
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) x[i] = ld16<bf16x8>(qr + 16 * (4 * (i >> 1) + j) + 8 * (i & 1));
+        split_e4m3<D, QT>(Q, q, x);
+      } else {
 #pragma unroll
         for (int x = 0; x < D / 32; ++x) {
           const DT* p = qr + 16 * (4 * (x >> 1) + j) + 8 * (x & 1);
-          if constexpr (NS == 1) {
-            Q.q[0][q][x] = ld16<bf16x8>(p);
-          } else {
-            const floatx4 lo = ld16<floatx4>(p), hi = ld16<floatx4>(p + 4);
+          const floatx4 lo = ld16<floatx4>(p), hi = ld16<floatx4>(p + 4);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              __bf16 t[NS];
-              split<NS>(e < 4 ? lo[e & 3] : hi[e & 3], t);
+          for (int e = 0; e < 8; ++e) {
+            __bf16 t[NS];
+            split<NS>(e < 4 ? lo[e & 3] : hi[e & 3], t);
 #pragma unroll
-              for (int n = 0; n < NS; ++n) Q.q[n][q][x][e] = t[n];
-            }
+            for (int n = 0; n < NS; ++n) Q.q[n][q][x][e] = t[n];
           }
         }
       }
-      const int part = (jb1 - jb0 + KS - 1) / KS;
-      const int b0 = jb0 + ks * part;
-      const int b1 = min(min(b0 + part, jb1), (n_keys + kBlk - 1) / kBlk);
-      for (int n = b0; n < b1; ++n) {
-        Block<D> f;
-        load_block<D>(a, f, n * kBlk, g, pt_row);
-        if ((n + 1) * kBlk <= all_see)
-          attend<D, QT, NS, false>(f, Q, a.scale_log2, n * kBlk, n_keys, qlimit, acc, m_run, l_run);
-        else
-          attend<D, QT, NS, true>(f, Q, a.scale_log2, n * kBlk, n_keys, qlimit, acc, m_run, l_run);
+    }
+    // The compiler counts its own loads only: the queries have to be here before
+    // others are under way, or their wait, inside the walk, would be for those too.
+#pragma unroll
+    for (int q = 0; q < QT; ++q) {
+      if constexpr (NS == 1) {
+        asm volatile("" : "+v"(Q.hi[q]), "+v"(Q.lo[q]));
+      } else {
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+          for (int x = 0; x < D / 32; ++x) asm volatile("" : "+v"(Q.q[n][q][x]));
       }
     }
+  }
+
+  template <class B>
+  __device__ __forceinline__ void block(const Q8Params& a, const B& f, int t0) {
+    if (t0 >= n_keys) return;
+    floatx4 s[QT][4];
+    scores<D, QT, NS>(f, Q, s);
+    attend<D, QT, NS>(f, s, a.scale_log2, t0 + kBlk > all_see, t0, n_keys, qlimit, acc, m_run, l_run);
+  }
+
+  // The lanes' sums joined: l_run is the row's from here on.
+  __device__ __forceinline__ void join_lanes() {
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
       l_run[q] += lane_xor16(l_run[q]);
       l_run[q] += lane_xor32(l_run[q]);
     }
-    // ---- the key parts of a row group, merged in halves ----
-    for (int half = KS / 2; half > 0; half >>= 1) {
-      if (ks >= half && ks < 2 * half) {
-        Acc& buf = *reinterpret_cast<Acc*>(s_acc + ((ks - half) * RG + rg) * sizeof(Acc));
+  }
+
+  // One tile to LDS, and one from there merged in: sizeof(floatx4) * (D / 16) *
+  // 64 bytes and 32 floats.
+  __device__ __forceinline__ void give(int q, floatx4* buf, float* ml) const {
+    const int lane = lane_id();
 #pragma unroll
-        for (int q = 0; q < QT; ++q) {
-#pragma unroll
-          for (int dt = 0; dt < D / 16; ++dt) buf[q][dt][lane] = acc[q][dt];
-          if (j == 0) {
-            s_ml[(ks - half) * RG + rg][0][16 * q + c16] = m_run[q];
-            s_ml[(ks - half) * RG + rg][1][16 * q + c16] = l_run[q];
-          }
-        }
-      }
-      __syncthreads();
-      if (ks < half) {
-        const Acc& buf = *reinterpret_cast<const Acc*>(s_acc + (ks * RG + rg) * sizeof(Acc));
-#pragma unroll
-        for (int q = 0; q < QT; ++q) {
-          const float m2 = s_ml[ks * RG + rg][0][16 * q + c16], l2 = s_ml[ks * RG + rg][1][16 * q + c16];
-          const float m = fmaxf(m_run[q], m2), mu = m == -INFINITY ? 0.f : m;
-          const float x = fast_exp2(m_run[q] - mu), y = fast_exp2(m2 - mu);
-          m_run[q] = m;
-          l_run[q] = l_run[q] * x + l2 * y;
-#pragma unroll
-          for (int dt = 0; dt < D / 16; ++dt) acc[q][dt] = acc[q][dt] * x + buf[q][dt][lane] * y;
-        }
-      }
-      __syncthreads();
+    for (int dt = 0; dt < D / 16; ++dt) buf[dt * kWave + lane] = acc[q][dt];
+    if (lane < 16) {
+      ml[lane] = m_run[q];
+      ml[16 + lane] = l_run[q];
     }
-    if (ks == 0) {
-      const long ps = 2 * (long)blockIdx.x + (item0 >= sp0 ? 1 : 0);
+  }
+  __device__ __forceinline__ void take(int q, const floatx4* buf, const float* ml) {
+    const int lane = lane_id(), c16 = lane & 15;
+    const float m2 = ml[c16], l2 = ml[16 + c16];
+    const float m = fmaxf(m_run[q], m2), mu = m == -INFINITY ? 0.f : m;
+    const float x = fast_exp2(m_run[q] - mu), y = fast_exp2(m2 - mu);
+    m_run[q] = m;
+    l_run[q] = l_run[q] * x + l2 * y;
 #pragma unroll
-      for (int q = 0; q < QT; ++q) {
-        const int pr = pr0 + 16 * q + c16;
-        if (pr >= sq.rows) continue;
-        if (whole) {
-          const int i = pr / a.G, hl = pr - i * a.G;
-          DT* o = reinterpret_cast<DT*>(a.out) + ((size_t)(sq.r0 + i) * a.Hq + g * a.G + hl) * D + 4 * j;
-          const float inv = 1.f / l_run[q];
+    for (int dt = 0; dt < D / 16; ++dt) acc[q][dt] = acc[q][dt] * x + buf[dt * kWave + lane] * y;
+  }
+
+  // The item's rows to the output, or its part of them to the partial results.
+  __device__ __forceinline__ void finish(const Q8Params& a, const Place& c, bool whole, size_t part_row) const {
+    const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
+    const Seq& sq = c.sq;
 #pragma unroll
-          for (int dt = 0; dt < D / 16; ++dt) {
-            const floatx4 v = acc[q][dt] * inv;
-            if constexpr (NS == 1) {
-              bf16x4 w;
+    for (int q = 0; q < QT; ++q) {
+      const int pr = pr0 + 16 * q + c16;
+      if (pr >= sq.rows) continue;
+      if (whole) {
+        const int i = pos_of(a, pr), hl = pr - i * a.G;
+        DT* o = reinterpret_cast<DT*>(a.out) + ((size_t)(sq.r0 + i) * a.Hq + c.g * a.G + hl) * D + 4 * j;
+        const float inv = 1.f / l_run[q];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) w[e] = static_cast<bf16>(v[e]);
-              *reinterpret_cast<bf16x4*>(o + 16 * dt) = w;
-            } else {
-              *reinterpret_cast<floatx4*>(o + 16 * dt) = v;
-            }
+        for (int dt = 0; dt < D / 16; ++dt) {
+          const floatx4 v = acc[q][dt] * inv;
+          if constexpr (NS == 1) {
+            bf16x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = static_cast<bf16>(v[e]);
+            *reinterpret_cast<bf16x4*>(o + 16 * dt) = w;
+          } else {
+            *reinterpret_cast<floatx4*>(o + 16 * dt) = v;
           }
-        } else {
-          const size_t row = (size_t)ps * item_rows + rg * WR + 16 * q + c16;
+        }
+      } else {
+        const size_t row = part_row + 16 * q + c16;
 #pragma unroll
-          for (int dt = 0; dt < D / 16; ++dt)
-            *reinterpret_cast<floatx4*>(a.part_o + row * D + 16 * dt + 4 * j) = acc[q][dt];
-          if (j == 0) {
-            a.part_ml[2 * row] = m_run[q];
-            a.part_ml[2 * row + 1] = l_run[q];
-          }
+        for (int dt = 0; dt < D / 16; ++dt)
+          *reinterpret_cast<floatx4*>(a.part_o + row * D + 16 * dt + 4 * j) = acc[q][dt];
+        if (j == 0) {
+          a.part_ml[2 * row] = m_run[q];
+          a.part_ml[2 * row + 1] = l_run[q];
         }
       }
     }
-    // ---- the next item ----
-    pos = item0 + jb1;
-    if (pos >= sp1) break;
-    item0 += nb;
-    if (++r == sq.n_rg) {
-      r = 0;
-      if (++g == a.Hkv) {
-        g = 0;
-        do {                                         // blocks are left, so a slot with rows follows
-          if (++slot >= a.n_seq) return;
-          sq = seq_of(a, slot, item_rows);
-        } while (sq.n_rg == 0);
+  }
+};
+
+// One row group: the four waves take parts of the span's keys.
+template <typename DT, int D>
+__global__ __launch_bounds__(256, 2) void attn_q8_keys_kernel(Q8Params a) {
+  constexpr int QT = 1, kItem = 16 * QT, kTile = (D / 16) * kWave;   // of floatx4
+  __shared__ floatx4 s_acc[2][kTile];
+  __shared__ float s_ml[2][32];
+  const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  long sp0, sp1;
+  Place c;
+  if (!find_span<256>(a, kItem, kBlk, 4, &sp0, &sp1, c)) return;
+  for (long pos = sp0; pos < sp1;) {
+    const int j0 = (int)(pos - c.first), j1 = (int)min((long)c.steps, sp1 - c.first);
+    Rows<DT, D, QT> R;
+    R.begin(a, c, c.r * kItem);
+    const int part = (j1 - j0 + 3) / 4, b0 = j0 + wv * part;
+    const int b1 = min(min(b0 + part, j1), (R.n_keys + kBlk - 1) / kBlk);
+    const ScalarInts pt = scalar(a.page_table + (size_t)c.sq.b * a.max_pages);
+    // the next keys are asked for once the scores have used theirs, the next
+    // values once the products have: they are under way in the same registers
+    if (b0 < b1) {
+      Block<D> f;
+      Units units;
+      units.look_up(a, pt, b0 * kBlk, c.g);
+      load_keys<D>(a, f, b0 * kBlk, units);
+      load_values<D>(a, f, b0 * kBlk, units);
+      units.look_up(a, pt, (b0 + 1) * kBlk, c.g);
+      for (int n = b0; n < b1; ++n) {
+        floatx4 s[QT][4];
+        scores<D, QT, Rows<DT, D, QT>::NS>(f, R.Q, s);
+        const bool more = n + 1 < b1;
+        __builtin_amdgcn_sched_barrier(0);          // or the loads move up, into registers of their own
+        if (more) load_keys<D>(a, f, (n + 1) * kBlk, units);
+        __builtin_amdgcn_sched_barrier(0);
+        attend<D, QT, Rows<DT, D, QT>::NS>(f, s, a.scale_log2, (n + 1) * kBlk > R.all_see, n * kBlk, R.n_keys, R.qlimit,
+                                           R.acc, R.m_run, R.l_run);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) load_values<D>(a, f, (n + 1) * kBlk, units);
+        units.look_up(a, pt, (n + 2) * kBlk, c.g);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    nb = item_blocks(a, sq, r, item_rows);
+    R.join_lanes();
+#pragma unroll
+    for (int q = 0; q < QT; ++q)
+#pragma unroll
+      for (int half = 2; half > 0; half >>= 1) {
+        if (wv >= half && wv < 2 * half) R.give(q, s_acc[wv - half], s_ml[wv - half]);
+        __syncthreads();
+        if (wv < half) R.take(q, s_acc[wv], s_ml[wv]);
+        __syncthreads();
+      }
+    if (wv == 0) R.finish(a, c, j0 == 0 && j1 == c.steps, (size_t)(2 * blockIdx.x + (c.first >= sp0 ? 1 : 0)) * kItem);
+    pos = c.first + j1;
+    if (pos < sp1 && !next_item(a, c, kItem, kBlk)) return;
   }
 }
 
-// Merges the partial results of an item that a span's end has cut.  A thread
-// takes four channels of a row.
-template <typename DT, int D>
-__global__ __launch_bounds__(256) void attn_q8_combine_kernel(Q8Params a, int item_rows, int parts, int grid) {
-  const int r = blockIdx.x, slot = blockIdx.y / a.Hkv, g = blockIdx.y % a.Hkv;
-  const Seq sq = seq_of(a, slot, item_rows);
-  if (r >= sq.n_rg) return;
-  const long total = a.head[0];
-  const long n_span = spans(total, parts, grid);
-  const long s0 = a.head[1 + ((long)slot * a.Hkv + g) * a.n_rg + r];
-  const long s1 = s0 + item_blocks(a, sq, r, item_rows);
-  const long w0 = ((s0 + 1) * n_span - 1) / total, w1 = (s1 * n_span - 1) / total;
-  if (w0 == w1) return;
-  const long first = 2 * w0 + 1;                     // w0 holds the item's start, the others continue it
-  const int rows = min(item_rows, sq.rows - r * item_rows);
-  for (int e = threadIdx.x; e < rows * (D / 4); e += 256) {
-    const int row = e / (D / 4), d = 4 * (e % (D / 4));
-    float m = -INFINITY;
-    for (long w = w0; w <= w1; ++w)
-      m = fmaxf(m, a.part_ml[2 * ((size_t)(w == w0 ? first : 2 * w) * item_rows + row)]);
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-    const float mu = m == -INFINITY ? 0.f : m;
-    for (long w = w0; w <= w1; ++w) {
-      const size_t at = (size_t)(w == w0 ? first : 2 * w) * item_rows + row;
-      const float x = fast_exp2(a.part_ml[2 * at] - mu);
-      l += x * a.part_ml[2 * at + 1];
-      o += x * ld16<floatx4>(a.part_o + at * D + d);
-    }
-    const int pr = r * item_rows + row, i = pr / a.G, hl = pr - i * a.G;
-    DT* out = reinterpret_cast<DT*>(a.out) + ((size_t)(sq.r0 + i) * a.Hq + g * a.G + hl) * D + d;
-    const float inv = 1.f / l;
+// RG row groups x KS parts of a step's keys.  A step's blocks, one per part, are
+// asked for kDepth - 1 steps ahead by the waves of their part together; the
+// barrier of a step makes them all arrive, and frees the stage that the step
+// before has used.
+template <typename DT, int D, int QT, int RG>
+__global__ __launch_bounds__(256, 2) void attn_q8_rows_kernel(Q8Params a) {
+  constexpr int KS = 4 / RG, kStep = KS * kBlk, WR = 16 * QT, kItem = RG * WR;
+  constexpr int kDepth = KS == 2 ? 2 : 3;                       // two workgroups per CU
+  typedef LdsBlock<D> B;
+  constexpr int kStage = KS * B::kBytes;
+  constexpr int NL = B::kLoads / RG + 1;                        // loads of a wave per step
+  constexpr int kTile = (D / 16) * kWave;
+  static_assert(KS == 1 || kStage >= RG * (kTile * 16 + 128), "a merge fits the stage that its item has left");
+  __shared__ __attribute__((aligned(16))) char s_ring[kDepth * kStage];
+  const int tid = threadIdx.x, lane = lane_id(), c16 = lane & 15, j = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wv % RG, part = wv / RG;
+  long sp0, sp1;
+  Place c;
+  if (!find_span<256>(a, kItem, kStep, 2, &sp0, &sp1, c)) return;
+
+  // ---- the loads' place, ahead of the computation's ----
+  Place e = c;
+  int ej = (int)(sp0 - c.first);
+  int left = (int)min(sp1 - sp0, 0x7fffffffl);      // steps not asked for yet
+  const int ps = 1 << a.log2ps;
+  Units units;
+  auto look_up = [&]() __attribute__((always_inline)) {
+    units.look_up(a, scalar(a.page_table + (size_t)e.sq.b * a.max_pages), ej * kStep + part * kBlk, e.g);
+  };
+  int fill = 0;                                     // the next stage to fill
+  auto issue = [&]() __attribute__((always_inline)) {
+    const int t0 = ej * kStep + part * kBlk;
+    char* stage = s_ring + fill * kStage + part * B::kBytes;
+    const int ku = c16 >> 2, su = lane & 3;
+    const uint8_t* kb = a.k_pages + ((unsigned long)units.of(ku) * (unsigned)(D * ps) +
+                                     (unsigned)((((t0 + 16 * ku) & (ps - 1)) + (c16 & 3) + j * ps) * 16));
+    const uint8_t* vb = a.v_pages + ((unsigned long)units.of(j) * (unsigned)(D * ps) +
+                                     (unsigned)(((t0 + 16 * j) & (ps - 1)) + c16 * ps));
+    const uint8_t* sb = a.scales + ((unsigned long)units.of(su) * (unsigned)(2 * ps) +
+                                    (unsigned)(((t0 + 16 * su) & (ps - 1)) + (lane & 4 ? ps : 0)));
 #pragma unroll
-    for (int c = 0; c < 4; ++c) out[c] = from_f32<DT>(o[c] * inv);
+    for (int i = 0; i < NL - 1; ++i) {
+      const int n = rg + RG * i;
+      dma16(n < B::kKeys ? kb + (4 * (n >> 2) * ps + 4 * (n & 3)) * 16 : vb + 16 * (n - B::kKeys) * ps,
+            stage + n * kWave * 16);
+    }
+    dma16(sb, stage + B::kLoads * kWave * 16);
+    fill = fill + 1 == kDepth ? 0 : fill + 1;
+    if (--left > 0) {
+      if (++ej == e.steps) {
+        ej = 0;
+        if (!next_item(a, e, kItem, kStep)) left = 0;
+      }
+      if (left > 0) look_up();
+    }
+  };
+  look_up();
+#pragma unroll 1
+  for (int i = 0; i < kDepth - 1 && left > 0; ++i) issue();
+
+  int use = 0;                                      // the next stage to use
+  for (long pos = sp0; pos < sp1;) {
+    const int j0 = (int)(pos - c.first), j1 = (int)min((long)c.steps, sp1 - c.first);
+    Rows<DT, D, QT> R;
+    R.begin(a, c, c.r * kItem + rg * WR);
+    char* stage = nullptr;
+    for (int n = j0; n < j1; ++n, ++pos) {
+      // steps behind this one that are under way: kDepth - 2, or fewer at the span's end
+      if (kDepth == 2 || pos + 1 >= sp1) wait_loads<0>(); else wait_loads<NL>();
+      lds_barrier();
+      if (left > 0) issue();
+      stage = s_ring + use * kStage;
+      const B f{stage + part * B::kBytes};
+      R.block(a, f, n * kStep + part * kBlk);
+      use = use + 1 == kDepth ? 0 : use + 1;
+    }
+    R.join_lanes();
+    if constexpr (KS == 2) {                        // in the stage that was used last: the next to be filled
+      floatx4* buf = reinterpret_cast<floatx4*>(stage) + rg * kTile;
+      float* ml = reinterpret_cast<float*>(stage + RG * kTile * 16) + rg * 32;
+#pragma unroll
+      for (int q = 0; q < QT; ++q) {
+        lds_barrier();
+        if (part) R.give(q, buf, ml);
+        lds_barrier();
+        if (!part) R.take(q, buf, ml);
+      }
+    }
+    if (part == 0)
+      R.finish(a, c, j0 == 0 && j1 == c.steps, (size_t)(2 * blockIdx.x + (c.first >= sp0 ? 1 : 0)) * kItem + rg * WR);
+    if (pos < sp1 && !next_item(a, c, kItem, kStep)) break;
+  }
+  wait_loads<0>();                                  // none may land after the workgroup has gone
+}
+
+// Merges the partial results of the items that a span's end has cut: 16 rows per
+// workgroup, of the item that span blockIdx.y + 1 is the first to continue.  The
+// pieces' weights first, a wave per row; then a thread takes four channels of a
+// row, with few rows of every second or fourth piece.
+constexpr int kMergeRows = 16;
+template <typename DT, int D>
+__global__ __launch_bounds__(256) void attn_q8_merge_kernel(Q8Params a, int item_rows, int parts, int grid) {
+  extern __shared__ float s_w[];                     // [kMergeRows][pieces]
+  __shared__ floatx4 s_o[256];
+  __shared__ float s_inv[kMergeRows];
+  const long total = a.span[grid].first;
+  const long n_span = spans(total, parts, grid);
+  if (blockIdx.y + 1 >= n_span) return;
+  const SpanHead item = a.span[blockIdx.y + 1];
+  const long w0 = blockIdx.y;
+  if (item.first >= span_start(total, n_span, w0 + 1) || item.first < span_start(total, n_span, w0)) return;
+  const Seq sq = same_seq_of(a, item.slot, item_rows);
+  const int r = item.r, g = item.g, row0 = blockIdx.x * kMergeRows;
+  const int rows = min(kMergeRows, sq.rows - r * item_rows - row0);
+  if (rows <= 0) return;
+  const long w1 = ((item.first + item.steps) * n_span - 1) / total;
+  const int n = (int)(w1 - w0) + 1;                  // pieces
+  // w0 holds the item's start, the others continue it
+  auto row_at = [&](int i, int row) { return (size_t)(i ? 2 * (w0 + i) : 2 * w0 + 1) * item_rows + row0 + row; };
+  const int lane = lane_id(), tid = threadIdx.x;
+  for (int row = tid >> 6; row < rows; row += 4) {
+    float m = -INFINITY;
+    for (int i = lane; i < n; i += kWave) {
+      s_w[row * n + i] = a.part_ml[2 * row_at(i, row)];
+      m = fmaxf(m, s_w[row * n + i]);
+    }
+    m = wave_max(m);
+    m = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    for (int i = lane; i < n; i += kWave) {
+      const float x = fast_exp2(s_w[row * n + i] - m);
+      s_w[row * n + i] = x;
+      l += x * a.part_ml[2 * row_at(i, row) + 1];
+    }
+    l = wave_sum(l);
+    if (lane == 0) s_inv[row] = 1.f / l;
+  }
+  __syncthreads();
+  const int units = rows * (D / 4);
+  const int split = units <= 64 ? 4 : units <= 128 ? 2 : 1;
+  const int team = 256 / split, part = tid / team;
+  auto sum = [&](int e) {
+    const int row = e / (D / 4), d = 4 * (e % (D / 4));
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int i = part; i < n; i += split) o += s_w[row * n + i] * ld16<floatx4>(a.part_o + row_at(i, row) * D + d);
+    return o;
+  };
+  auto put = [&](int e, const floatx4& o) {
+    const int row = e / (D / 4), d = 4 * (e % (D / 4));
+    const int pr = r * item_rows + row0 + row, i = pos_of(a, pr), hl = pr - i * a.G;
+    DT* out = reinterpret_cast<DT*>(a.out) + ((size_t)(sq.r0 + i) * a.Hq + g * a.G + hl) * D + d;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) out[c] = from_f32<DT>(o[c] * s_inv[row]);
+  };
+  if (split == 1) {
+    for (int e = tid; e < units; e += 256) put(e, sum(e));
+    return;
+  }
+  const int e = tid % team;
+  if (e < units) s_o[tid] = sum(e);
+  __syncthreads();
+  if (part == 0 && e < units) {
+    floatx4 o = s_o[tid];
+    for (int x = 1; x < split; ++x) o += s_o[tid + x * team];
+    put(e, o);
   }
 }
 
 struct Q8Plan {
-  int qt, rg, n_rg, grid;
+  int qt, rg;          // tiles per wave, row groups
+  int item_rows, parts, grid;      // parts: steps per span at least
 };
 Q8Plan plan_of(int n_seq, int Hq, int Hkv, int max_q, bool bf16) {
   Q8Plan p;
   const long rows = (long)max_q * (Hq / Hkv);
-  if (bf16) {
-    p.qt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    p.rg = rows <= 64 ? 1 : rows <= 128 ? 2 : 4;
-  } else {                      // three terms per query: fewer rows fit the registers
-    p.qt = rows <= 16 ? 1 : 2;
-    p.rg = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-  }
-  const int item = 16 * p.qt * p.rg;
-  p.n_rg = (int)((rows + item - 1) / item);
-  p.grid = device_cus();
+  p.qt = bf16 && rows > 32 ? 2 : 1;                 // fp32, three terms per query: no registers for two tiles
+  p.rg = rows <= 16 ? 1 : rows <= 32 * p.qt ? 2 : 4;
+  p.item_rows = 16 * p.qt * p.rg;
+  p.parts = p.rg == 1 ? 4 : 2;
+  p.grid = 2 * device_cus();                        // as many as are resident
   return p;
 }
 
@@ -526,8 +917,8 @@ size_t attn_q8_workspace(int n_seq, int Hq, int Hkv, int D, int max_q) {
   size_t most = 0;              // either type
   for (const bool b : {false, true}) {
     const Q8Plan p = plan_of(n_seq, Hq, Hkv, max_q, b);
-    const size_t rows = 2 * (size_t)p.grid * 16 * p.qt * p.rg;
-    const size_t n = rows * (D + 2) * 4 + 8 * (1 + (size_t)n_seq * Hkv * p.n_rg);
+    const size_t rows = 2 * (size_t)p.grid * p.item_rows;
+    const size_t n = rows * (D + 2) * 4 + (p.grid + 1) * sizeof(SpanHead);
     most = std::max(most, (n + 255) / 256 * 256);
   }
   return most;
@@ -535,8 +926,7 @@ size_t attn_q8_workspace(int n_seq, int Hq, int Hkv, int D, int max_q) {
 
 hipError_t launch_attn_q8(const AttnQ8Launch& L, hipStream_t st) {
   const Q8Plan pl = plan_of(L.n_seq, L.Hq, L.Hkv, L.max_q, L.dtype_bf16);
-  const int item_rows = 16 * pl.qt * pl.rg;
-  const size_t rows = 2 * (size_t)pl.grid * item_rows;
+  const size_t rows = 2 * (size_t)pl.grid * pl.item_rows;
   Q8Params p{};
   p.q = L.q;
   p.q_stride = L.q_stride;
@@ -550,48 +940,46 @@ hipError_t launch_attn_q8(const AttnQ8Launch& L, hipStream_t st) {
   p.out = L.out;
   p.part_o = (float*)L.workspace;
   p.part_ml = p.part_o + rows * L.D;
-  p.head = (long*)(p.part_ml + 2 * rows);
+  p.span = (SpanHead*)(p.part_ml + 2 * rows);
   p.max_pages = L.max_pages;
   p.Hq = L.Hq;
   p.Hkv = L.Hkv;
   p.G = L.Hq / L.Hkv;
+  p.log2g = (p.G & (p.G - 1)) ? -1 : __builtin_ctz(p.G);
   p.log2ps = __builtin_ctz(L.page_size);
   p.num_pages = L.num_pages;
   p.n_seq = L.n_seq;
   p.max_q = L.max_q;
-  p.n_rg = pl.n_rg;
-  p.rg = pl.rg;
   p.scale_log2 = L.scale * 1.4426950408889634f;
   trace_begin(st);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(pl.grid), dim3(256), 0, st, p); };
+  auto pick = [&](auto dt, auto dim) {
+    using DT = decltype(dt);
+    constexpr int D = decltype(dim)::value, QT = sizeof(DT) == 2 ? 2 : 1;
+    if (pl.rg == 1) go(attn_q8_keys_kernel<DT, D>);
+    else if (pl.rg == 2 && pl.qt == 1) go(attn_q8_rows_kernel<DT, D, 1, 2>);
+    else if (pl.rg == 2) go(attn_q8_rows_kernel<DT, D, QT, 2>);
+    else go(attn_q8_rows_kernel<DT, D, QT, 4>);
+  };
+  typedef std::integral_constant<int, 64> D64;
+  typedef std::integral_constant<int, 128> D128;
   if (L.dtype_bf16) {
-    if (L.D == 128) {
-      if (pl.qt == 1) go(attn_q8_kernel<bf16, 128, 1>);
-      else if (pl.qt == 2) go(attn_q8_kernel<bf16, 128, 2>);
-      else go(attn_q8_kernel<bf16, 128, 4>);
-    } else {
-      if (pl.qt == 1) go(attn_q8_kernel<bf16, 64, 1>);
-      else if (pl.qt == 2) go(attn_q8_kernel<bf16, 64, 2>);
-      else go(attn_q8_kernel<bf16, 64, 4>);
-    }
+    if (L.D == 128) pick(bf16(), D128()); else pick(bf16(), D64());
   } else {
-    if (L.D == 128) {
-      if (pl.qt == 1) go(attn_q8_kernel<float, 128, 1>); else go(attn_q8_kernel<float, 128, 2>);
-    } else {
-      if (pl.qt == 1) go(attn_q8_kernel<float, 64, 1>); else go(attn_q8_kernel<float, 64, 2>);
-    }
+    if (L.D == 128) pick(float(), D128()); else pick(float(), D64());
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   trace_mark(st);
-  const dim3 cgrid(pl.n_rg, L.n_seq * L.Hkv);
+  const dim3 cgrid(pl.item_rows / kMergeRows, pl.grid - 1);
+  const size_t lds = (size_t)kMergeRows * pl.grid * 4;      // no item has more pieces than there are spans
   auto merge = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, cgrid, dim3(256), 0, st, p, item_rows, 4 / pl.rg, pl.grid);
+    hipLaunchKernelGGL(kernel, cgrid, dim3(256), lds, st, p, pl.item_rows, pl.parts, pl.grid);
   };
   if (L.dtype_bf16) {
-    if (L.D == 128) merge(attn_q8_combine_kernel<bf16, 128>); else merge(attn_q8_combine_kernel<bf16, 64>);
+    if (L.D == 128) merge(attn_q8_merge_kernel<bf16, 128>); else merge(attn_q8_merge_kernel<bf16, 64>);
   } else {
-    if (L.D == 128) merge(attn_q8_combine_kernel<float, 128>); else merge(attn_q8_combine_kernel<float, 64>);
+    if (L.D == 128) merge(attn_q8_merge_kernel<float, 128>); else merge(attn_q8_merge_kernel<float, 64>);
   }
   e = hipGetLastError();
   if (e != hipSuccess) return e;
