@@ -125,9 +125,7 @@ template <int D> struct Block {
   uint4 v[D / 16];      // channel tile: one channel's 16 slots of unit j
   uint4 ks, vs;         // scale bytes: the lane's key unit (c16 / 4), its value unit (j)
   __device__ __forceinline__ uint4 key(int t, int h) const { return k[t][h]; }
-  __device__ __forceinline__ uint4 val(int dt) const { return v[dt]; }
   __device__ __forceinline__ uint4 key_scales() const { return ks; }
-  __device__ __forceinline__ uint4 val_scales() const { return vs; }
 };
 
 // The same block in LDS: every load of 1 KB as the wave that asked for it has
@@ -290,8 +288,8 @@ __device__ __forceinline__ void scores(const B& f, const Queries<D, QT, NS>& Q, 
 
 // The block's probabilities and values.  `tail`: some row of the wave does not
 // see every key of the block.
-template <int D, int QT, int NS, class B>
-__device__ __forceinline__ void attend(const B& f, floatx4 (&s)[QT][4], float c, bool tail, int t0, int n_keys,
+template <int D, int QT, int NS>
+__device__ __forceinline__ void attend(uint4 (&v)[D / 16], uint4 vscale, floatx4 (&s)[QT][4], float c, bool tail, int t0, int n_keys,
                                        const int (&qlimit)[QT], floatx4 (&acc)[QT][D / 16], float (&m_run)[QT],
                                        float (&l_run)[QT]) {
   const int u0 = t0 + 16 * (lane_id() >> 4);          // unit j's first position
@@ -301,6 +299,13 @@ __device__ __forceinline__ void attend(const B& f, floatx4 (&s)[QT][4], float c,
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (u0 + i >= qlimit[q]) s[q][i >> 2][i & 3] = -INFINITY;
+    auto live = [&](unsigned x, int at) {             // the bytes of slots at .. at + 3: behind the last key may be NaN
+      const int n = n_keys - (u0 + at);
+      return n >= 4 ? x : n <= 0 ? 0u : x & ((1u << (8 * n)) - 1u);
+    };
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt)
+      v[dt] = make_uint4(live(v[dt].x, 0), live(v[dt].y, 4), live(v[dt].z, 8), live(v[dt].w, 12));
   }
   float bm[QT], m_use[QT];
   bool rescale = false;
@@ -333,7 +338,6 @@ __device__ __forceinline__ void attend(const B& f, floatx4 (&s)[QT][4], float c,
     }
   }
   bf16x8 pf[NS][QT][2];
-  const uint4 vscale = f.val_scales();
 #pragma unroll
   for (int i = 0; i < 16; ++i) {           // slot i of unit j
     const float vsc = __uint_as_float(((word(vscale, i >> 2) >> (8 * (i & 3))) & 255u) << 23);
@@ -349,26 +353,20 @@ __device__ __forceinline__ void attend(const B& f, floatx4 (&s)[QT][4], float c,
   }
   if (tail) {
     // An unseen key's scale byte may be anything, a later row's that of NaN
-    // (infinite here, and times its zero bytes NaN); bytes behind the last key
-    // may be NaN.
+    // (infinite here, and times its zero bytes NaN).
+    int u1 = u0;
+    asm("" : "+v"(u1));                    // compare again: the masks above would be kept, in 2 x 16 QT registers
 #pragma unroll
     for (int q = 0; q < QT; ++q)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
 #pragma unroll
         for (int n = 0; n < NS; ++n)
-          if (u0 + i >= qlimit[q]) pf[n][q][i >> 3][i & 7] = static_cast<__bf16>(0.f);
+          if (u1 + i >= qlimit[q]) pf[n][q][i >> 3][i & 7] = static_cast<__bf16>(0.f);
   }
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) {
-    uint4 w = f.val(dt);
-    if (tail) {
-      auto live = [&](unsigned x, int at) {  // the bytes of slots at .. at + 3
-        const int n = n_keys - (u0 + at);
-        return n >= 4 ? x : n <= 0 ? 0u : x & ((1u << (8 * n)) - 1u);
-      };
-      w = make_uint4(live(w.x, 0), live(w.y, 4), live(w.z, 8), live(w.w, 12));
-    }
+    const uint4 w = v[dt];
 #pragma unroll
     for (int st = 0; st < 2; ++st) {       // slots 8 st .. 8 st + 7 of unit j
       const bf16x8 vf = cvt8(st ? w.z : w.x, st ? w.w : w.y, 1.0f);
@@ -409,6 +407,10 @@ __device__ __forceinline__ Seq same_seq_of(const Q8Params& a, int slot, int item
 }
 // Window row of a packed row.
 __device__ __forceinline__ int pos_of(const Q8Params& a, int row) { return a.log2g >= 0 ? row >> a.log2g : row / a.G; }
+__device__ __forceinline__ ScalarInts pages_of(const Q8Params& a, int slot) {
+  const int b = a.seq_ids ? scalar(a.seq_ids)[slot] : slot;
+  return scalar(a.page_table + (size_t)b * a.max_pages);
+}
 // Steps (of `step` keys) of row group r: up to the last key that its last row sees.
 __device__ __forceinline__ int item_steps(const Q8Params& a, const Seq& s, int r, int item_rows, int step) {
   const int last = min((r + 1) * item_rows, s.rows) - 1;
@@ -426,34 +428,37 @@ __device__ __forceinline__ long spans(long total, int parts, int grid) {
   return n < grid ? (n > 0 ? n : 1) : grid;
 }
 
-// A place on the line: an item, and where on the line it begins.
+// A place on the line: an item, and where on the line it begins.  Its sequence is
+// read again where it is needed: two places' would take the scalar registers that
+// the walk needs.
 struct Place {
   int slot, g, r, steps;
   long first;
-  Seq sq;
 };
 __device__ __forceinline__ bool next_item(const Q8Params& a, Place& c, int item_rows, int step) {
   c.first += c.steps;
-  if (++c.r == c.sq.n_rg) {
+  Seq sq = same_seq_of(a, c.slot, item_rows);
+  if (++c.r == sq.n_rg) {
     c.r = 0;
     if (++c.g == a.Hkv) {
       c.g = 0;
       do {
         if (++c.slot >= a.n_seq) return false;
-        c.sq = same_seq_of(a, c.slot, item_rows);
-      } while (c.sq.n_rg == 0);
+        sq = same_seq_of(a, c.slot, item_rows);
+      } while (sq.n_rg == 0);
     }
   }
-  c.steps = item_steps(a, c.sq, c.r, item_rows, step);
+  c.steps = item_steps(a, sq, c.r, item_rows, step);
   return true;
 }
 
-// The workgroup's span [*from, *to) of the line, and the item that it begins in.
+// The workgroup's span [*from, *to) of the line, its number, and the item that it
+// begins in.
 // Every workgroup adds up the whole line, a thread neighbouring slots.  False
 // when it has no span.
 template <int THREADS>
-__device__ __forceinline__ bool find_span(const Q8Params& a, int item_rows, int step, int parts, long* from, long* to,
-                                          Place& c) {
+__device__ __forceinline__ bool find_span(const Q8Params& a, int item_rows, int step, int parts, int* span,
+                                          long* from, long* to, Place& c) {
   __shared__ long s_sum[THREADS / kWave];
   __shared__ long s_at[2];                          // the span's first slot, and where it begins
   constexpr int kKept = 1024;
@@ -483,8 +488,12 @@ __device__ __forceinline__ bool find_span(const Q8Params& a, int item_rows, int 
   }
   if (blockIdx.x == 0 && tid == 0) a.span[gridDim.x].first = total;
   const long n = spans(total, parts, gridDim.x);
-  if (blockIdx.x >= n || total == 0) return false;
-  const long p0 = span_start(total, n, blockIdx.x), p1 = span_start(total, n, blockIdx.x + 1);
+  // Neighbouring spans to one XCD (workgroups go to the 8 XCDs in turn): a
+  // prompt's items of one head then find its keys in one L2.
+  const int each = (int)((n + 7) / 8), w = (int)(blockIdx.x & 7) * each + (int)(blockIdx.x >> 3);
+  *span = w;
+  if ((int)(blockIdx.x >> 3) >= each || w >= n || total == 0) return false;
+  const long p0 = span_start(total, n, w), p1 = span_start(total, n, w + 1);
   const long e0 = before + incl - mine;
   if (p0 >= e0 && p0 < e0 + mine) {
     long at = e0;
@@ -510,19 +519,19 @@ __device__ __forceinline__ bool find_span(const Q8Params& a, int item_rows, int 
   *to = uniform(p1);
   c.slot = __builtin_amdgcn_readfirstlane((int)s_at[0]);
   c.first = uniform(s_at[1]);
-  c.sq = same_seq_of(a, c.slot, item_rows);
+  const Seq sq = same_seq_of(a, c.slot, item_rows);
   long hb = c.slot < kKept ? s_steps[c.slot] : 0x7fffffff;
-  if (hb == 0x7fffffff) hb = head_steps(a, c.sq, item_rows, step);
+  if (hb == 0x7fffffff) hb = head_steps(a, sq, item_rows, step);
   hb = uniform(hb);
   c.g = (int)((*from - c.first) / hb);
   c.first += c.g * hb;
   c.r = 0;
-  c.steps = item_steps(a, c.sq, 0, item_rows, step);
+  c.steps = item_steps(a, sq, 0, item_rows, step);
   while (c.first + c.steps <= *from) {
     c.first += c.steps;
-    c.steps = item_steps(a, c.sq, ++c.r, item_rows, step);
+    c.steps = item_steps(a, sq, ++c.r, item_rows, step);
   }
-  if (tid == 0) a.span[blockIdx.x] = {c.first, c.steps, c.slot, c.g, c.r};
+  if (tid == 0) a.span[w] = {c.first, c.steps, c.slot, c.g, c.r};
   return true;
 }
 
@@ -540,7 +549,7 @@ struct Rows {
 
   __device__ __forceinline__ void begin(const Q8Params& a, const Place& c, int first_row) {
     const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
-    const Seq& sq = c.sq;
+    const Seq sq = same_seq_of(a, c.slot, 16 * QT);
     pr0 = first_row;
     n_keys = pr0 < sq.rows ? sq.L + pos_of(a, min(pr0 + 16 * QT, sq.rows) - 1) + 1 : 0;
     all_see = sq.L + pos_of(a, pr0) + 1;
@@ -598,7 +607,10 @@ struct Rows {
     if (t0 >= n_keys) return;
     floatx4 s[QT][4];
     scores<D, QT, NS>(f, Q, s);
-    attend<D, QT, NS>(f, s, a.scale_log2, t0 + kBlk > all_see, t0, n_keys, qlimit, acc, m_run, l_run);
+    uint4 v[D / 16];                 // asked for now, for they take their time from LDS
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) v[dt] = f.val(dt);
+    attend<D, QT, NS>(v, f.val_scales(), s, a.scale_log2, t0 + kBlk > all_see, t0, n_keys, qlimit, acc, m_run, l_run);
   }
 
   // The lanes' sums joined: l_run is the row's from here on.
@@ -635,7 +647,7 @@ struct Rows {
   // The item's rows to the output, or its part of them to the partial results.
   __device__ __forceinline__ void finish(const Q8Params& a, const Place& c, bool whole, size_t part_row) const {
     const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
-    const Seq& sq = c.sq;
+    const Seq sq = same_seq_of(a, c.slot, 16 * QT);
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
       const int pr = pr0 + 16 * q + c16;
@@ -678,15 +690,16 @@ __global__ __launch_bounds__(256, 2) void attn_q8_keys_kernel(Q8Params a) {
   __shared__ float s_ml[2][32];
   const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   long sp0, sp1;
+  int span;
   Place c;
-  if (!find_span<256>(a, kItem, kBlk, 4, &sp0, &sp1, c)) return;
+  if (!find_span<256>(a, kItem, kBlk, 4, &span, &sp0, &sp1, c)) return;
   for (long pos = sp0; pos < sp1;) {
     const int j0 = (int)(pos - c.first), j1 = (int)min((long)c.steps, sp1 - c.first);
     Rows<DT, D, QT> R;
     R.begin(a, c, c.r * kItem);
     const int part = (j1 - j0 + 3) / 4, b0 = j0 + wv * part;
     const int b1 = min(min(b0 + part, j1), (R.n_keys + kBlk - 1) / kBlk);
-    const ScalarInts pt = scalar(a.page_table + (size_t)c.sq.b * a.max_pages);
+    const ScalarInts pt = pages_of(a, c.slot);
     // the next keys are asked for once the scores have used theirs, the next
     // values once the products have: they are under way in the same registers
     if (b0 < b1) {
@@ -703,7 +716,7 @@ __global__ __launch_bounds__(256, 2) void attn_q8_keys_kernel(Q8Params a) {
         __builtin_amdgcn_sched_barrier(0);          // or the loads move up, into registers of their own
         if (more) load_keys<D>(a, f, (n + 1) * kBlk, units);
         __builtin_amdgcn_sched_barrier(0);
-        attend<D, QT, Rows<DT, D, QT>::NS>(f, s, a.scale_log2, (n + 1) * kBlk > R.all_see, n * kBlk, R.n_keys, R.qlimit,
+        attend<D, QT, Rows<DT, D, QT>::NS>(f.v, f.vs, s, a.scale_log2, (n + 1) * kBlk > R.all_see, n * kBlk, R.n_keys, R.qlimit,
                                            R.acc, R.m_run, R.l_run);
         __builtin_amdgcn_sched_barrier(0);
         if (more) load_values<D>(a, f, (n + 1) * kBlk, units);
@@ -721,7 +734,7 @@ __global__ __launch_bounds__(256, 2) void attn_q8_keys_kernel(Q8Params a) {
         if (wv < half) R.take(q, s_acc[wv], s_ml[wv]);
         __syncthreads();
       }
-    if (wv == 0) R.finish(a, c, j0 == 0 && j1 == c.steps, (size_t)(2 * blockIdx.x + (c.first >= sp0 ? 1 : 0)) * kItem);
+    if (wv == 0) R.finish(a, c, j0 == 0 && j1 == c.steps, (size_t)(2 * span + (c.first >= sp0 ? 1 : 0)) * kItem);
     pos = c.first + j1;
     if (pos < sp1 && !next_item(a, c, kItem, kBlk)) return;
   }
@@ -744,8 +757,9 @@ __global__ __launch_bounds__(256, 2) void attn_q8_rows_kernel(Q8Params a) {
   const int tid = threadIdx.x, lane = lane_id(), c16 = lane & 15, j = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wv % RG, part = wv / RG;
   long sp0, sp1;
+  int span;
   Place c;
-  if (!find_span<256>(a, kItem, kStep, 2, &sp0, &sp1, c)) return;
+  if (!find_span<256>(a, kItem, kStep, 2, &span, &sp0, &sp1, c)) return;
 
   // ---- the loads' place, ahead of the computation's ----
   Place e = c;
@@ -753,8 +767,9 @@ __global__ __launch_bounds__(256, 2) void attn_q8_rows_kernel(Q8Params a) {
   int left = (int)min(sp1 - sp0, 0x7fffffffl);      // steps not asked for yet
   const int ps = 1 << a.log2ps;
   Units units;
+  ScalarInts pt = pages_of(a, e.slot);
   auto look_up = [&]() __attribute__((always_inline)) {
-    units.look_up(a, scalar(a.page_table + (size_t)e.sq.b * a.max_pages), ej * kStep + part * kBlk, e.g);
+    units.look_up(a, pt, ej * kStep + part * kBlk, e.g);
   };
   int fill = 0;                                     // the next stage to fill
   auto issue = [&]() __attribute__((always_inline)) {
@@ -779,6 +794,7 @@ __global__ __launch_bounds__(256, 2) void attn_q8_rows_kernel(Q8Params a) {
       if (++ej == e.steps) {
         ej = 0;
         if (!next_item(a, e, kItem, kStep)) left = 0;
+        else pt = pages_of(a, e.slot);
       }
       if (left > 0) look_up();
     }
@@ -816,7 +832,7 @@ __global__ __launch_bounds__(256, 2) void attn_q8_rows_kernel(Q8Params a) {
       }
     }
     if (part == 0)
-      R.finish(a, c, j0 == 0 && j1 == c.steps, (size_t)(2 * blockIdx.x + (c.first >= sp0 ? 1 : 0)) * kItem + rg * WR);
+      R.finish(a, c, j0 == 0 && j1 == c.steps, (size_t)(2 * span + (c.first >= sp0 ? 1 : 0)) * kItem + rg * WR);
     if (pos < sp1 && !next_item(a, c, kItem, kStep)) break;
   }
   wait_loads<0>();                                  // none may land after the workgroup has gone
