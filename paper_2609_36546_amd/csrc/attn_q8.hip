@@ -33,8 +33,10 @@
 // Work split.  All steps (a step: the keys that a workgroup takes at once) of
 // all items (an item: one row group of one (sequence, KV head)) form one line,
 // cut into as many equal spans as there are workgroups, so that ragged contexts,
-// single sequences and long prompts all fill the chip.  Items cut by a span's
-// end leave partial results, merged by a second kernel.
+// single sequences and long contexts all fill the chip.  Items cut by a span's
+// end leave partial results, merged by a second kernel.  Where no item is longer
+// than a span (prompts), nothing is cut: the items are dealt out whole, the
+// longest row groups first and every second round backwards.
 //
 // A workgroup's four waves are RG row groups of QT tiles x KS = 4 / RG key parts,
 // merged in LDS at an item's end; plan_of has the choice.  With one row group
@@ -428,82 +430,167 @@ __device__ __forceinline__ long spans(long total, int parts, int grid) {
   return n < grid ? (n > 0 ? n : 1) : grid;
 }
 
-// A place on the line: an item, and where on the line it begins.  Its sequence is
-// read again where it is needed: two places' would take the scalar registers that
-// the walk needs.
-struct Place {
-  int slot, g, r, steps;
-  long first;
+// A workgroup's way along its items: the present one's steps j .. end.  Its
+// sequence is read again where it is needed: two walks' would take the scalar
+// registers that the computation needs.
+template <bool DEALT> struct Walk {            // along a span of the line
+  int slot, g, r, steps, j, end;
+  int span, len;       // the span's number, and its steps
+  int first;           // where the item begins, counted from the span's start
+  __device__ __forceinline__ bool whole() const { return j == 0 && end == steps; }
+  // of the item's part, which no more than two items of a span have
+  __device__ __forceinline__ int part() const { return 2 * span + (first >= 0 ? 1 : 0); }
 };
-__device__ __forceinline__ bool next_item(const Q8Params& a, Place& c, int item_rows, int step) {
+template <> struct Walk<true> {                // whole items, dealt out
+  int slot, g, r, end;
+  static constexpr int j = 0;
+  int round, places, n_sg;   // places for items in all, and in a row group: (sequence, KV head)s, a multiple of 8
+  __device__ __forceinline__ bool whole() const { return true; }
+  __device__ __forceinline__ int part() const { return 0; }
+};
+
+// The next item with steps for this workgroup; false at the end.
+template <int ITEM, int STEP>
+__device__ __forceinline__ bool advance(const Q8Params& a, Walk<false>& c) {
+  if (c.first + c.end >= c.len) return false;
   c.first += c.steps;
-  Seq sq = same_seq_of(a, c.slot, item_rows);
+  Seq sq = same_seq_of(a, c.slot, ITEM);
   if (++c.r == sq.n_rg) {
     c.r = 0;
     if (++c.g == a.Hkv) {
       c.g = 0;
       do {
         if (++c.slot >= a.n_seq) return false;
-        sq = same_seq_of(a, c.slot, item_rows);
+        sq = same_seq_of(a, c.slot, ITEM);
       } while (sq.n_rg == 0);
     }
   }
-  c.steps = item_steps(a, sq, c.r, item_rows, step);
+  c.steps = item_steps(a, sq, c.r, ITEM, STEP);
+  c.j = 0;
+  c.end = min(c.steps, c.len - c.first);
   return true;
 }
-
-// The workgroup's span [*from, *to) of the line, its number, and the item that it
-// begins in.
-// Every workgroup adds up the whole line, a thread neighbouring slots.  False
-// when it has no span.
-template <int THREADS>
-__device__ __forceinline__ bool find_span(const Q8Params& a, int item_rows, int step, int parts, int* span,
-                                          long* from, long* to, Place& c) {
-  __shared__ long s_sum[THREADS / kWave];
-  __shared__ long s_at[2];                          // the span's first slot, and where it begins
-  constexpr int kKept = 1024;
-  __shared__ int s_steps[kKept];                    // a head's steps, of the first slots
-  const int tid = threadIdx.x, lane = lane_id(), wv = tid >> 6;
-  const int per = (a.n_seq + THREADS - 1) / THREADS;
-  const int sl0 = min(tid * per, a.n_seq), sl1 = min(sl0 + per, a.n_seq);
-  long mine = 0;
-  for (int i = sl0; i < sl1; ++i) {
-    const long n = head_steps(a, seq_of(a, i, item_rows), item_rows, step);
-    if (i < kKept) s_steps[i] = (int)min(n, 0x7fffffffl);
-    mine += a.Hkv * n;
+// A round deals every workgroup a place.  Workgroups go to the 8 XCDs in turn, and
+// so do the places: a head's items all go to one XCD, which has its keys in L2.
+template <int ITEM, int STEP>
+__device__ __forceinline__ bool advance(const Q8Params& a, Walk<true>& c) {
+  const int x = blockIdx.x & 7, i = blockIdx.x >> 3, n = gridDim.x >> 3;
+  for (;;) {
+    const int base = ++c.round * (int)gridDim.x;
+    if (base >= c.places) return false;
+    const int k = base + (c.round & 1 ? n - 1 - i : i) * 8 + x;
+    const int back = k / c.n_sg, sg = k - back * c.n_sg;
+    if (k >= c.places || sg >= a.n_seq * a.Hkv) continue;
+    c.r = c.places / c.n_sg - 1 - back;
+    c.slot = sg / a.Hkv;
+    c.g = sg - c.slot * a.Hkv;
+    const Seq sq = same_seq_of(a, c.slot, ITEM);
+    if (c.r >= sq.n_rg) continue;
+    c.end = item_steps(a, sq, c.r, ITEM, STEP);
+    return true;
   }
-  long incl = mine;
+}
+
+// The line as a workgroup knows it: every one adds it all up, a thread
+// neighbouring slots.
+struct Line {
+  static constexpr int kKept = 1024;
+  int steps[kKept];    // a head's steps, of the first slots
+  long sum[4], at[2];
+  int most[4], most_rg[4];
+};
+struct Share {         // a thread's
+  int sl0, sl1;        // its slots
+  long at, len;        // where they begin, and their steps
+};
+
+// Returns whether the items are dealt out whole.  The merge reads the line's length
+// (0: nothing is cut) and every span's first item.
+template <int ITEM, int STEP, bool MAY_DEAL>
+__device__ __forceinline__ bool add_up(const Q8Params& a, Line& line, Share& mine, long& total, int& places) {
+  const int tid = threadIdx.x, lane = lane_id(), wv = tid >> 6;
+  const int per = (a.n_seq + 255) / 256;
+  mine.sl0 = min(tid * per, a.n_seq);
+  mine.sl1 = min(mine.sl0 + per, a.n_seq);
+  mine.len = 0;
+  int most = 0, most_rg = 0;                        // an item's steps, and a head's items
+  for (int i = mine.sl0; i < mine.sl1; ++i) {
+    const Seq sq = seq_of(a, i, ITEM);
+    const long n = head_steps(a, sq, ITEM, STEP);
+    if (i < Line::kKept) line.steps[i] = (int)min(n, 0x7fffffffl);
+    mine.len += a.Hkv * n;
+    if (MAY_DEAL && sq.n_rg > 0) {
+      most = max(most, item_steps(a, sq, sq.n_rg - 1, ITEM, STEP));
+      most_rg = max(most_rg, sq.n_rg);
+    }
+  }
+  long incl = mine.len;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
     const long up = __shfl_up(incl, o, kWave);
     if (lane >= o) incl += up;
   }
-  if (lane == kWave - 1) s_sum[wv] = incl;
+  if (lane == kWave - 1) line.sum[wv] = incl;
   __syncthreads();
-  long before = 0, total = 0;
+  total = 0;
+  mine.at = incl - mine.len;
 #pragma unroll
-  for (int i = 0; i < THREADS / kWave; ++i) {
-    if (i < wv) before += s_sum[i];
-    total += s_sum[i];
+  for (int i = 0; i < 4; ++i) {
+    if (i < wv) mine.at += line.sum[i];
+    total += line.sum[i];
   }
-  if (blockIdx.x == 0 && tid == 0) a.span[gridDim.x].first = total;
+  bool dealt = false;
+  if (MAY_DEAL && total >= gridDim.x) {             // the same for all threads
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      most = max(most, __shfl_xor(most, o, kWave));
+      most_rg = max(most_rg, __shfl_xor(most_rg, o, kWave));
+    }
+    if (lane == 0) {
+      line.most[wv] = most;
+      line.most_rg[wv] = most_rg;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      most = max(most, line.most[i]);
+      most_rg = max(most_rg, line.most_rg[i]);
+    }
+    const long n = (long)((a.n_seq * a.Hkv + 7) & ~7) * most_rg;
+    dealt = (gridDim.x & 7) == 0 && (long)most * gridDim.x <= total && n < 1 << 30;
+    places = __builtin_amdgcn_readfirstlane((int)n);
+    dealt = __builtin_amdgcn_readfirstlane((int)dealt) != 0;
+  }
+  if (blockIdx.x == 0 && tid == 0) a.span[gridDim.x].first = dealt ? 0 : total;
+  return dealt;
+}
+
+// Where the workgroup's walk begins; false when it has none.
+template <int ITEM, int STEP>
+__device__ __forceinline__ bool begin_walk(const Q8Params& a, int places, Walk<true>& c) {
+  c.round = -1;
+  c.places = places;
+  c.n_sg = (a.n_seq * a.Hkv + 7) & ~7;
+  return advance<ITEM, STEP>(a, c);
+}
+template <int ITEM, int STEP>
+__device__ __forceinline__ bool begin_walk(const Q8Params& a, Line& line, const Share& mine, long total, int parts,
+                                           Walk<false>& c) {
   const long n = spans(total, parts, gridDim.x);
   // Neighbouring spans to one XCD (workgroups go to the 8 XCDs in turn): a
   // prompt's items of one head then find its keys in one L2.
   const int each = (int)((n + 7) / 8), w = (int)(blockIdx.x & 7) * each + (int)(blockIdx.x >> 3);
-  *span = w;
   if ((int)(blockIdx.x >> 3) >= each || w >= n || total == 0) return false;
   const long p0 = span_start(total, n, w), p1 = span_start(total, n, w + 1);
-  const long e0 = before + incl - mine;
-  if (p0 >= e0 && p0 < e0 + mine) {
-    long at = e0;
-    for (int i = sl0; i < sl1; ++i) {
-      long k = i < kKept ? s_steps[i] : 0x7fffffff;
-      if (k == 0x7fffffff) k = head_steps(a, seq_of(a, i, item_rows), item_rows, step);
+  if (p0 >= mine.at && p0 < mine.at + mine.len) {
+    long at = mine.at;
+    for (int i = mine.sl0; i < mine.sl1; ++i) {
+      long k = i < Line::kKept ? line.steps[i] : 0x7fffffff;
+      if (k == 0x7fffffff) k = head_steps(a, seq_of(a, i, ITEM), ITEM, STEP);
       k *= a.Hkv;
       if (p0 < at + k) {
-        s_at[0] = i;
-        s_at[1] = at;
+        line.at[0] = i;
+        line.at[1] = at;
         break;
       }
       at += k;
@@ -515,23 +602,27 @@ __device__ __forceinline__ bool find_span(const Q8Params& a, int item_rows, int 
     return (long)(((unsigned long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) |
                   (unsigned)__builtin_amdgcn_readfirstlane((int)x));
   };
-  *from = uniform(p0);
-  *to = uniform(p1);
-  c.slot = __builtin_amdgcn_readfirstlane((int)s_at[0]);
-  c.first = uniform(s_at[1]);
-  const Seq sq = same_seq_of(a, c.slot, item_rows);
-  long hb = c.slot < kKept ? s_steps[c.slot] : 0x7fffffff;
-  if (hb == 0x7fffffff) hb = head_steps(a, sq, item_rows, step);
+  c.span = __builtin_amdgcn_readfirstlane(w);
+  const long from = uniform(p0);
+  c.len = __builtin_amdgcn_readfirstlane((int)(p1 - p0));
+  c.slot = __builtin_amdgcn_readfirstlane((int)line.at[0]);
+  long first = uniform(line.at[1]);
+  const Seq sq = same_seq_of(a, c.slot, ITEM);
+  long hb = c.slot < Line::kKept ? line.steps[c.slot] : 0x7fffffff;
+  if (hb == 0x7fffffff) hb = head_steps(a, sq, ITEM, STEP);
   hb = uniform(hb);
-  c.g = (int)((*from - c.first) / hb);
-  c.first += c.g * hb;
+  c.g = (int)((from - first) / hb);
+  first += c.g * hb;
   c.r = 0;
-  c.steps = item_steps(a, sq, 0, item_rows, step);
-  while (c.first + c.steps <= *from) {
-    c.first += c.steps;
-    c.steps = item_steps(a, sq, ++c.r, item_rows, step);
+  c.steps = item_steps(a, sq, 0, ITEM, STEP);
+  while (first + c.steps <= from) {
+    first += c.steps;
+    c.steps = item_steps(a, sq, ++c.r, ITEM, STEP);
   }
-  if (tid == 0) a.span[w] = {c.first, c.steps, c.slot, c.g, c.r};
+  c.first = (int)(first - from);
+  c.j = -c.first;
+  c.end = min(c.steps, c.len - c.first);
+  if (threadIdx.x == 0) a.span[c.span] = {first, c.steps, c.slot, c.g, c.r};
   return true;
 }
 
@@ -547,7 +638,8 @@ struct Rows {
   int n_keys;      // keys that some row sees
   int all_see;     // keys below are seen by every row
 
-  __device__ __forceinline__ void begin(const Q8Params& a, const Place& c, int first_row) {
+  template <class W>
+  __device__ __forceinline__ void begin(const Q8Params& a, const W& c, int first_row) {
     const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
     const Seq sq = same_seq_of(a, c.slot, 16 * QT);
     pr0 = first_row;
@@ -645,9 +737,12 @@ struct Rows {
   }
 
   // The item's rows to the output, or its part of them to the partial results.
-  __device__ __forceinline__ void finish(const Q8Params& a, const Place& c, bool whole, size_t part_row) const {
+  template <class W>
+  __device__ __forceinline__ void finish(const Q8Params& a, const W& c, int item_rows, int row0) const {
     const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
     const Seq sq = same_seq_of(a, c.slot, 16 * QT);
+    const bool whole = c.whole();
+    const size_t part_row = (size_t)c.part() * item_rows + row0;
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
       const int pr = pr0 + 16 * q + c16;
@@ -689,12 +784,15 @@ __global__ __launch_bounds__(256, 2) void attn_q8_keys_kernel(Q8Params a) {
   __shared__ floatx4 s_acc[2][kTile];
   __shared__ float s_ml[2][32];
   const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  long sp0, sp1;
-  int span;
-  Place c;
-  if (!find_span<256>(a, kItem, kBlk, 4, &span, &sp0, &sp1, c)) return;
-  for (long pos = sp0; pos < sp1;) {
-    const int j0 = (int)(pos - c.first), j1 = (int)min((long)c.steps, sp1 - c.first);
+  __shared__ Line s_line;
+  Share mine;
+  long total;
+  int places;
+  add_up<kItem, kBlk, false>(a, s_line, mine, total, places);
+  Walk<false> c;
+  if (!begin_walk<kItem, kBlk>(a, s_line, mine, total, 4, c)) return;
+  do {
+    const int j0 = c.j, j1 = c.end;
     Rows<DT, D, QT> R;
     R.begin(a, c, c.r * kItem);
     const int part = (j1 - j0 + 3) / 4, b0 = j0 + wv * part;
@@ -734,37 +832,35 @@ __global__ __launch_bounds__(256, 2) void attn_q8_keys_kernel(Q8Params a) {
         if (wv < half) R.take(q, s_acc[wv], s_ml[wv]);
         __syncthreads();
       }
-    if (wv == 0) R.finish(a, c, j0 == 0 && j1 == c.steps, (size_t)(2 * span + (c.first >= sp0 ? 1 : 0)) * kItem);
-    pos = c.first + j1;
-    if (pos < sp1 && !next_item(a, c, kItem, kBlk)) return;
-  }
+    if (wv == 0) R.finish(a, c, kItem, 0);
+  } while (advance<kItem, kBlk>(a, c));
 }
 
 // RG row groups x KS parts of a step's keys.  A step's blocks, one per part, are
 // asked for kDepth - 1 steps ahead by the waves of their part together; the
 // barrier of a step makes them all arrive, and frees the stage that the step
 // before has used.
-template <typename DT, int D, int QT, int RG>
-__global__ __launch_bounds__(256, 2) void attn_q8_rows_kernel(Q8Params a) {
-  constexpr int KS = 4 / RG, kStep = KS * kBlk, WR = 16 * QT, kItem = RG * WR;
-  constexpr int kDepth = KS == 2 ? 2 : 3;                       // two workgroups per CU
+template <int D, int QT, int RG> struct Ring {
+  static constexpr int KS = 4 / RG, kStep = KS * kBlk, kItem = RG * 16 * QT;
+  static constexpr int kDepth = KS == 2 ? 2 : 3;                // two workgroups per CU
+  static constexpr int kStage = KS * LdsBlock<D>::kBytes;
+};
+template <typename DT, int D, int QT, int RG, class W>
+__device__ __forceinline__ void walk_rows(const Q8Params& a, W c, char* s_ring) {
+  typedef Ring<D, QT, RG> G;
+  constexpr int KS = G::KS, kStep = G::kStep, WR = 16 * QT, kItem = G::kItem, kDepth = G::kDepth, kStage = G::kStage;
   typedef LdsBlock<D> B;
-  constexpr int kStage = KS * B::kBytes;
   constexpr int NL = B::kLoads / RG + 1;                        // loads of a wave per step
   constexpr int kTile = (D / 16) * kWave;
   static_assert(KS == 1 || kStage >= RG * (kTile * 16 + 128), "a merge fits the stage that its item has left");
-  __shared__ __attribute__((aligned(16))) char s_ring[kDepth * kStage];
   const int tid = threadIdx.x, lane = lane_id(), c16 = lane & 15, j = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wv % RG, part = wv / RG;
-  long sp0, sp1;
-  int span;
-  Place c;
-  if (!find_span<256>(a, kItem, kStep, 2, &span, &sp0, &sp1, c)) return;
 
-  // ---- the loads' place, ahead of the computation's ----
-  Place e = c;
-  int ej = (int)(sp0 - c.first);
-  int left = (int)min(sp1 - sp0, 0x7fffffffl);      // steps not asked for yet
+  // ---- the loads' walk, ahead of the computation's ----
+  W e = c;
+  int ej = c.j;
+  bool more = true;                                 // steps to ask for
+  int ahead = 0;                                    // steps asked for and not used yet
   const int ps = 1 << a.log2ps;
   Units units;
   ScalarInts pt = pages_of(a, e.slot);
@@ -790,30 +886,28 @@ __global__ __launch_bounds__(256, 2) void attn_q8_rows_kernel(Q8Params a) {
     }
     dma16(sb, stage + B::kLoads * kWave * 16);
     fill = fill + 1 == kDepth ? 0 : fill + 1;
-    if (--left > 0) {
-      if (++ej == e.steps) {
-        ej = 0;
-        if (!next_item(a, e, kItem, kStep)) left = 0;
-        else pt = pages_of(a, e.slot);
-      }
-      if (left > 0) look_up();
+    ++ahead;
+    if (++ej == e.end) {
+      more = advance<kItem, kStep>(a, e);
+      ej = e.j;
+      if (more) pt = pages_of(a, e.slot);
     }
+    if (more) look_up();
   };
   look_up();
 #pragma unroll 1
-  for (int i = 0; i < kDepth - 1 && left > 0; ++i) issue();
+  for (int i = 0; i < kDepth - 1 && more; ++i) issue();
 
   int use = 0;                                      // the next stage to use
-  for (long pos = sp0; pos < sp1;) {
-    const int j0 = (int)(pos - c.first), j1 = (int)min((long)c.steps, sp1 - c.first);
+  do {
     Rows<DT, D, QT> R;
     R.begin(a, c, c.r * kItem + rg * WR);
     char* stage = nullptr;
-    for (int n = j0; n < j1; ++n, ++pos) {
-      // steps behind this one that are under way: kDepth - 2, or fewer at the span's end
-      if (kDepth == 2 || pos + 1 >= sp1) wait_loads<0>(); else wait_loads<NL>();
+    for (int n = c.j; n < c.end; ++n) {
+      // steps behind this one that are under way: kDepth - 2, or fewer at the walk's end
+      if (kDepth == 2 || --ahead == 0) wait_loads<0>(); else wait_loads<NL>();
       lds_barrier();
-      if (left > 0) issue();
+      if (more) issue();
       stage = s_ring + use * kStage;
       const B f{stage + part * B::kBytes};
       R.block(a, f, n * kStep + part * kBlk);
@@ -831,11 +925,26 @@ __global__ __launch_bounds__(256, 2) void attn_q8_rows_kernel(Q8Params a) {
         if (!part) R.take(q, buf, ml);
       }
     }
-    if (part == 0)
-      R.finish(a, c, j0 == 0 && j1 == c.steps, (size_t)(2 * span + (c.first >= sp0 ? 1 : 0)) * kItem + rg * WR);
-    if (pos < sp1 && !next_item(a, c, kItem, kStep)) break;
-  }
+    if (part == 0) R.finish(a, c, kItem, rg * WR);
+  } while (advance<kItem, kStep>(a, c));
   wait_loads<0>();                                  // none may land after the workgroup has gone
+}
+
+template <typename DT, int D, int QT, int RG>
+__global__ __launch_bounds__(256, 2) void attn_q8_rows_kernel(Q8Params a) {
+  typedef Ring<D, QT, RG> G;
+  __shared__ __attribute__((aligned(16))) char s_ring[G::kDepth * G::kStage];
+  __shared__ Line s_line;
+  Share mine;
+  long total;
+  int places;
+  if (add_up<G::kItem, G::kStep, true>(a, s_line, mine, total, places)) {
+    Walk<true> c;
+    if (begin_walk<G::kItem, G::kStep>(a, places, c)) walk_rows<DT, D, QT, RG>(a, c, s_ring);
+  } else {
+    Walk<false> c;
+    if (begin_walk<G::kItem, G::kStep>(a, s_line, mine, total, 2, c)) walk_rows<DT, D, QT, RG>(a, c, s_ring);
+  }
 }
 
 // Merges the partial results of the items that a span's end has cut: 16 rows per
