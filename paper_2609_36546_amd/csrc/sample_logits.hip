@@ -25,19 +25,18 @@
 //
 //   chunk kernel  one workgroup per 16384 entries: reads the logits once, into
 //                 registers; its histogram below its own maximum (bins are
-//                 aligned, since they are floors of y), and a list of its
-//                 topmost entries.
+//                 aligned, since they are floors of y), and its topmost
+//                 entries, bin by bin, as far as a cut may lie.
 //   row kernel    one workgroup per row: adds the histograms up, finds the cut's
-//                 bin, gathers the bin's entries (from the lists, or from the
-//                 logits where a list stops above the bin) and takes the cut;
+//                 bin, takes the bin's entries from the lists (or from the
+//                 logits where a list stops above the bin) and in them the cut;
 //                 then the chunk, and in it the entry, where the mass passes u.
-//                 Bound by latency, so it asks memory twice only: for all
-//                 histograms and lists at its start, which stay in registers,
-//                 and for the chunk of the draw; and its loops stay rolled
-//                 where they can (63 KB of code took 17 us even unfiltered).
+//                 Bound by latency, so all histograms are asked for at its start
+//                 and stay in registers, and its loops stay rolled where they
+//                 can (63 KB of code took 17 us even unfiltered).
 //
 // A bin of many entries (equal logits by the thousand) is narrowed by digits of
-// the entries' order numbers until 512 are left, in LDS or, where they do not
+// the entries' order numbers until 256 are left, in LDS or, where they do not
 // fit there, over the row's logits.
 #include <type_traits>
 
@@ -49,9 +48,9 @@ namespace {
 
 constexpr int kChunk = 16384;     // entries per workgroup of the chunk kernel
 constexpr int kBins = 256;
-constexpr int kList = 1024;       // topmost entries that a chunk lists
+constexpr int kList = 2048;       // topmost entries that a chunk lists
 constexpr int kHold = 4096;       // entries of one bin that LDS holds
-constexpr int kSort = 512;        // entries that are ordered
+constexpr int kSort = 256;        // entries that are ordered
 constexpr int kMaxChunks = 16;    // V <= 262144
 constexpr double kWidth = 8.0;    // bins per unit of l / T
 constexpr int kCountShift = 45;   // 16384 masses of about 2^30 at most stay below
@@ -62,25 +61,22 @@ struct ChunkHead {
   double floor_max;   // floor(y) of the chunk's maximum, -inf without a finite logit
   float max;
   int bad;            // holds NaN or +inf
-  int covered;        // bins that the list holds whole, from the chunk's top bin
-  int listed;
+  int covered;        // bins that the list holds, from the chunk's top bin
 };
-struct ListEntry {
-  float l;
-  int v;
-};
-constexpr size_t kChunkBytes = kBins * sizeof(u64) + kList * sizeof(ListEntry) + 64;
+constexpr size_t kChunkBytes = kBins * (sizeof(u64) + sizeof(int)) + kList * sizeof(u64) + 64;
 static_assert(sizeof(ChunkHead) <= 64, "chunk record");
 
 struct ChunkRec {
   u64* hist;
-  ListEntry* list;
+  u64* list;          // order numbers, bin by bin
+  int* start;         // [kBins]: where a bin's begin
   ChunkHead* head;
 };
 __device__ __forceinline__ ChunkRec chunk_rec(const SampleLogitsLaunch& p, int n_chunks, int m, int s) {
   char* at = reinterpret_cast<char*>(p.workspace) + ((size_t)m * n_chunks + s) * kChunkBytes;
-  return {reinterpret_cast<u64*>(at), reinterpret_cast<ListEntry*>(at + kBins * sizeof(u64)),
-          reinterpret_cast<ChunkHead*>(at + kBins * sizeof(u64) + kList * sizeof(ListEntry))};
+  u64* hist = reinterpret_cast<u64*>(at);
+  int* start = reinterpret_cast<int*>(hist + kBins + kList);
+  return {hist, hist + kBins, start, reinterpret_cast<ChunkHead*>(start + kBins)};
 }
 
 // A row's parameters; greedy (T = 0) is the top entry at temperature 1.
@@ -183,7 +179,7 @@ __global__ __launch_bounds__(kThreads, 6) void chunk_kernel(SampleLogitsLaunch p
   constexpr int PER = kChunk / kThreads;
   __shared__ u64 s_hist[kBins];
   __shared__ float s_max[kWaves], s_min[kWaves];
-  __shared__ int s_bad, s_n, s_cover, s_wave[kBins / kWave];
+  __shared__ int s_bad, s_cover, s_wave[kBins / kWave], s_at[kBins];
   const int m = blockIdx.x / n_chunks, s = blockIdx.x % n_chunks;
   const int tid = threadIdx.x, lane = lane_id(), w = tid >> 6;
   const int v0 = s * kChunk, n = min(kChunk, p.V - v0);
@@ -215,7 +211,7 @@ __global__ __launch_bounds__(kThreads, 6) void chunk_kernel(SampleLogitsLaunch p
   auto x = [&](int i) { return to_f32(__builtin_bit_cast(Lane, raw[i / N]).e[i % N]); };
   const Row r = row_of(p, m);
   if (tid < kBins) s_hist[tid] = 0;
-  if (tid == 0) s_bad = s_n = s_cover = 0;
+  if (tid == 0) s_bad = s_cover = 0;
   float mx = -INFINITY, mn = INFINITY;
   bool bad = false;
 #pragma unroll
@@ -268,60 +264,69 @@ __global__ __launch_bounds__(kThreads, 6) void chunk_kernel(SampleLogitsLaunch p
   }
   __syncthreads();
   const ChunkRec rec = chunk_rec(p, n_chunks, m, s);
-  // The list: whole bins from the top while they fit.
-  int cum = 0;
+  // The list: whole bins from the top while they fit, and while a cut may lie in
+  // them: in none behind k entries, and in none that far below the maximum that
+  // min-p lets nothing pass (with top-k and top-p both, top-k's cut counts first).
+  int cum = 0, count = 0;
   if (tid < kBins) {
     rec.hist[tid] = s_hist[tid];
-    cum = wave_incl_scan_i((int)(s_hist[tid] >> kCountShift));
+    count = (int)(s_hist[tid] >> kCountShift);
+    cum = wave_incl_scan_i(count);
     if (lane == kWave - 1) s_wave[w] = cum;
   }
   __syncthreads();
   if (tid < kBins) {
     for (int i = 0; i < w; ++i) cum += s_wave[i];
-    const u64 fits = __ballot(cum <= kList);    // counts never fall, so these are the first bins
-    if (lane == 0) atomicAdd(&s_cover, __popcll(fits));
+    s_at[tid] = rec.start[tid] = cum - count;
+    bool fits = cum <= kList;
+    if (r.k > 0) fits &= cum - count < r.k;
+    if (r.min_p > 0.f && !(r.k > 0 && r.top_p < 1.f)) fits &= (float)tid <= 2.f - (float)kWidth * __logf(r.min_p);
+    const u64 first = __ballot(fits);             // all three hold for the first bins
+    if (lane == 0) atomicAdd(&s_cover, __popcll(first));
   }
   __syncthreads();
-  const int cover = min(s_cover, kBins - 1);    // the last bin is never listed
-  if (any && cover > 0 && (r.k > 0 || r.top_p < 1.f || r.min_p > 0.f)) {
-    renew();
-    unsigned in = 0;                // bit i: entry i is listed
-    static_assert(PER <= 32, "a bit per entry");
-    if (near) {
-      const float last = (float)top - (float)cover;
+  const bool filtered = r.k > 0 || r.top_p < 1.f || r.min_p > 0.f;
+  const int cover = any && filtered ? min(s_cover, kBins - 1) : 0;    // the last bin is never listed
+  if (tid == 0) *rec.head = {top, mx, s_bad, cover};
+  if (cover == 0) return;
+  auto place = [&](int bin) { return atomicAdd(&s_at[bin], 1); };
+  renew();
+  if (near) {
+    const float ftop = (float)top, end = (float)cover;
+    constexpr int AT = 8;           // places asked for at a time
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
+    for (int i0 = 0; i0 < PER; i0 += AT) {
+      int at[AT];
+#pragma unroll
+      for (int i = 0; i < AT; ++i) {
         float rest;
-        in |= (floor_near(r, x(i), &rest) > last ? 1u : 0u) << i;
+        const float d = ftop - floor_near(r, x(i0 + i), &rest);
+        at[i] = -1;
+        if (d < end) at[i] = place((int)d);
       }
-    } else {
-#pragma unroll 1
-      for (int i = 0; i < PER; ++i) {
-        float l = x(0), rest;
 #pragma unroll
-        for (int c = 0; c < PER; ++c) l = c == i ? x(c) : l;
-        in |= (l > -INFINITY && top - floor_y(r, l, &rest) < cover ? 1u : 0u) << i;
+      for (int i = 0; i < AT; ++i) {
+        const int e = i0 + i;
+        if (at[i] >= 0) rec.list[at[i]] = order_of(x(e), v0 + (e / N) * kThreads * N + tid * N + e % N);
       }
     }
-    renew();
-    // a place for the wave's entries, then for each lane's
-    const int upto = wave_incl_scan_i(__popc(in));
-    int at = 0;
-    if (lane == kWave - 1) at = atomicAdd(&s_n, upto);
-    at = __shfl(at, kWave - 1, kWave) + upto - __popc(in);
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < PER; ++i) {
+      float l = x(0), rest;
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (in >> i & 1) rec.list[at++] = {x(i), v0 + (i / N) * kThreads * N + tid * N + i % N};
+      for (int c = 0; c < PER; ++c) l = c == i ? x(c) : l;
+      if (!(l > -INFINITY)) continue;
+      const double d = top - floor_y(r, l, &rest);
+      if (d < cover) rec.list[place((int)d)] = order_of(l, v0 + (i / N) * kThreads * N + tid * N + i % N);
+    }
   }
-  __syncthreads();
-  if (tid == 0) *rec.head = {top, mx, s_bad, cover, s_n};
 }
 
 // ---- the row kernel ----
 
 constexpr double kUnitMass = 1.0 / 1073741824.0;
 constexpr int kHeldBins = kMaxChunks * kBins / kThreads;      // histogram bins of a thread
-constexpr int kHeldList = kMaxChunks * kList / kThreads;      // list entries of a thread
 
 // Sum over the threads before this one; every thread calls.
 template <typename T>
@@ -351,7 +356,8 @@ struct Shared {
   int count[kBins];
   u64 mass[kBins];
   int off[kMaxChunks];              // the chunk's top bin in the row's bins (kBins: none)
-  int cover[kMaxChunks], listed[kMaxChunks];
+  int cover[kMaxChunks];
+  int start[kMaxChunks][kBins];     // where a chunk's list has its bin t
   double chunk_mass[kMaxChunks];
   u64 in_bin[kMaxChunks];           // kept mass of the cut's bin
   double grid[kMaxChunks][kBins + 1];   // mass by chunk and bin, the chunk's top bin first
@@ -384,7 +390,6 @@ template <typename DT, bool VEC>
 struct RowWork {
   const SampleLogitsLaunch& p;
   Shared& S;
-  const float (&hl)[kHeldList];     // the logits of the thread's list entries (NaN: none)
   const Row r;
   const int m, n_chunks, tid;
   const double top;
@@ -456,36 +461,45 @@ struct RowWork {
     if (tid == 1) S.high = b >= 0 ? logit_of_key(hi) : INFINITY;
   }
 
-  // The entries of a bin, into S.hold as far as they fit, and S.low, S.high.
+  // The entries of a bin into S.hold; false if they do not fit there.  Where the
+  // logits are read for them, or they are too many to be ordered at once, the
+  // bin's bounds too: S.low, S.high.
   __device__ bool gather(int bin) {
+    const bool fit = S.count[bin] <= kHold;
     __syncthreads();
     if (tid < kWave) {
-      bounds(bin);
       bool more = false;
       if (tid < n_chunks) more = S.off[tid] <= bin && bin - S.off[tid] >= S.cover[tid];
       const u64 b = __ballot(more);
+      if (b || S.count[bin] > kSort) bounds(bin);
       if (tid == 0) {
         S.from_logits = (unsigned)b;
         S.n = 0;
       }
     }
     __syncthreads();
-    if (S.count[bin] > kHold) return false;
-    const float low = S.low, high = S.high;
-    auto put = [&](float l, int v) {
-      const int at = atomicAdd(&S.n, 1);
-      if (at < kHold) S.hold[at] = order_of(l, v);
-    };
-    unsigned in = 0;
-#pragma unroll
-    for (int i = 0; i < kHeldList; ++i) in |= (hl[i] >= low && hl[i] < high ? 1u : 0u) << i;
-    for (; in; in &= in - 1) {
-      const int i = __ffs(in) - 1;
-      const ListEntry e = chunk_rec(p, n_chunks, m, i / 2).list[tid + i % 2 * kThreads];
-      put(e.l, e.v);
+    if (!fit) return false;
+    constexpr int PART = kThreads / kMaxChunks;        // threads of a chunk
+    const int s = tid / PART, c = tid % PART;
+    int first = 0, n = 0;
+    if (s < n_chunks) {
+      const int b = bin - S.off[s];
+      if (b >= 0 && b < S.cover[s]) {                  // the last bin is never covered
+        first = S.start[s][b];
+        n = S.start[s][b + 1] - first;
+      }
     }
+    int at = 0;
+    if (c == 0 && n) at = atomicAdd(&S.n, n);
+    at = __shfl(at, lane_id() & ~(PART - 1), kWave);
+    const u64* list = chunk_rec(p, n_chunks, m, s).list + first;
+    for (int i = c; i < n; i += PART) S.hold[at + i] = list[i];
     const unsigned more = S.from_logits;
-    if (more) scan(more, low, high, put);
+    if (more)
+      scan(more, S.low, S.high, [&](float l, int v) {
+        const int to = atomicAdd(&S.n, 1);
+        if (to < kHold) S.hold[to] = order_of(l, v);
+      });
     __syncthreads();
     return true;
   }
@@ -513,9 +527,13 @@ struct RowWork {
     // what is kept: entries with less than the need before them
     auto before = [&](int c, u64 mass) { return need.by_count ? first + c < need.count : base + e * (double)mass < need.mass; };
     if (tid == 0) {
-      S.lo = (u64)key_of(S.low) << kIndexBits;
-      S.hi = ((u64)key_of(S.high < INFINITY ? S.high : S.max) + (S.high < INFINITY ? 0u : 1u)) << kIndexBits;
-      S.hi -= 1;
+      S.lo = 0;
+      S.hi = ~0ull;
+      if (S.count[bin] > kSort) {
+        S.lo = (u64)key_of(S.low) << kIndexBits;
+        S.hi = ((u64)key_of(S.high < INFINITY ? S.high : S.max) + (S.high < INFINITY ? 0u : 1u)) << kIndexBits;
+        S.hi -= 1;
+      }
       S.above = 0;
       S.above_mass = 0;
       S.left = S.count[bin];
@@ -559,7 +577,7 @@ struct RowWork {
     }
     // order what is left: every entry's rank, counted by as many threads as there are for it
     if (tid == 0) S.n = min(S.n, kHold);
-    S.rank[tid] = 0;
+    if (tid < kSort) S.rank[tid] = 0;
     if (tid == 0) S.found = 0;
     __syncthreads();
     const u64 lo = S.lo, hi = S.hi;
@@ -570,7 +588,8 @@ struct RowWork {
     });
     __syncthreads();
     const int n = min(S.found, kSort);
-    const int span = n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : kSort;
+    int span = 64;
+    while (span < n) span *= 2;
     const int mine = tid & (span - 1);
     if (mine < n) {
       const u64 o = S.few[mine];
@@ -606,9 +625,9 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
   __shared__ Shared S;
   const int m = blockIdx.x, tid = threadIdx.x, lane = lane_id(), w = tid >> 6;
   const int t = tid & (kBins - 1), side = tid / kBins;
-  // everything that the row is known by: bins t of every other chunk, list entries tid + j kThreads of all
+  // everything that the row is known by: bins t of every other chunk
   u64 hist[kHeldBins];
-  float hl[kHeldList];
+  int start[kHeldBins];
 #pragma unroll
   for (int i = 0; i < kHeldBins; ++i) {
     hist[i] = 0;
@@ -619,8 +638,8 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
   const bool filtered = r.k > 0 || r.top_p < 1.f || r.min_p > 0.f;
   if (filtered) {
 #pragma unroll
-    for (int i = 0; i < kHeldList; ++i)
-      if (i / 2 < n_chunks) hl[i] = chunk_rec(p, n_chunks, m, i / 2).list[tid + i % 2 * kThreads].l;
+    for (int i = 0; i < kHeldBins; ++i)
+      if (2 * i + side < n_chunks) start[i] = chunk_rec(p, n_chunks, m, 2 * i + side).start[t];
   }
   if (tid < kWave) {                // a lane per chunk
     double ct = -INFINITY;
@@ -632,7 +651,6 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
       cm = h.max;
       bad |= h.bad != 0;
       S.cover[tid] = h.covered;
-      S.listed[tid] = h.listed;
     }
     double all = ct;
 #pragma unroll
@@ -679,8 +697,8 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
   int bin_cut = kBins - 1;          // bins before it are kept whole, of later ones nothing
   if (filtered) {
 #pragma unroll
-    for (int i = 0; i < kHeldList; ++i)       // told from what was there before by the list's length
-      if (i / 2 >= n_chunks || tid + i % 2 * kThreads >= S.listed[i / 2]) hl[i] = __uint_as_float(0x7fc00000u);
+    for (int i = 0; i < kHeldBins; ++i)
+      if (2 * i + side < n_chunks) S.start[2 * i + side][t] = start[i];
     __syncthreads();
     const int count = tid < kBins ? S.count[t] : 0;
     const double mass = tid < kBins ? (double)S.mass[t] * S.edge[t] * kUnitMass : 0.0;
@@ -692,26 +710,30 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
     }
     if (tid == kBins - 1) S.all = mass_before;         // the last bin has none
     __syncthreads();
-    RowWork<DT, VEC> work{p, S, hl, r, m, n_chunks, tid, top};
+    RowWork<DT, VEC> work{p, S, r, m, n_chunks, tid, top};
     double kept = S.all;            // mass of what the filters so far leave
     bool held = false;
+    u64 bound = 0;                  // min-p's cut is the least logit that passes
+    int bin_min = kBins - 1;
+    if (r.min_p > 0.f) {
+      const double x = log((double)r.min_p), least = (double)mx + (x < 0.0 ? x * r.temp : 0.0);
+      float l = (float)least;
+      if ((double)l < least) l = nextafterf(l, INFINITY);
+      if (l > -INFINITY) {
+        unsigned ignore;
+        bound = (u64)key_of(l) << kIndexBits;
+        bin_min = classify(r, logit_of(bound), top, &ignore);
+      }
+    }
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {             // top-k, top-p, min-p
       if (pass == 0 ? r.k == 0 : pass == 1 ? r.top_p == 1.f : r.min_p == 0.f) continue;
       const Need need{pass == 0, r.k, (double)r.top_p * kept};
-      u64 bound = 0;
-      if (pass == 2) {              // min-p's cut is the least logit that passes
-        const double x = log((double)r.min_p), least = (double)mx + (x < 0.0 ? x * r.temp : 0.0);
-        float l = (float)least;
-        if ((double)l < least) l = nextafterf(l, INFINITY);
-        bound = l > -INFINITY ? (u64)key_of(l) << kIndexBits : 0;
-        if (bound <= cut) continue;
-      }
+      if (pass == 2 && bound <= cut) continue;
       if (tid == 0) S.bin = -1;
       __syncthreads();
       if (pass == 2) {
-        unsigned ignore;
-        if (tid == 0) S.bin = classify(r, logit_of(bound), top, &ignore);
+        if (tid == 0) S.bin = bin_min;
       } else if (count > 0 && (pass == 0 ? count_before < r.k && count_before + count >= r.k
                                          : mass_before + mass >= need.mass &&
                                                (mass_before < need.mass || count_before == 0))) {
@@ -720,6 +742,7 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
       __syncthreads();
       const int bin = S.bin;
       if (bin < 0 || bin == kBins - 1) continue;       // nothing that counts is cut
+      if (pass < 2 && bin > bin_min && (pass == 1 || r.top_p == 1.f)) continue;      // min-p cuts above it
       if (bin != bin_cut) held = work.gather(bin);
       if (pass < 2) work.select(bin, held, need);
       cut = pass < 2 ? S.cut : bound;                  // at or above the last one
