@@ -948,19 +948,21 @@ __global__ __launch_bounds__(256, 2) void attn_q8_rows_kernel(Q8Params a) {
 }
 
 // Merges the partial results of the items that a span's end has cut: 16 rows per
-// workgroup, of the item that span blockIdx.y + 1 is the first to continue.  The
-// pieces' weights first, a wave per row; then a thread takes four channels of a
-// row, with few rows of every second or fourth piece.
-constexpr int kMergeRows = 16;
+// workgroup, of the item that span blockIdx.y + 1 is the first to continue.  A
+// thread takes four channels of a row: of few pieces all at once, which it weighs
+// itself; of more, once the pieces' weights have been found, 16 lanes per row, and
+// with few rows every second or fourth of them.
+constexpr int kMergeRows = 16, kFewPieces = 4;
 template <typename DT, int D>
 __global__ __launch_bounds__(256) void attn_q8_merge_kernel(Q8Params a, int item_rows, int parts, int grid) {
+  static_assert(kMergeRows == 256 / 16, "16 lanes per row");
   extern __shared__ float s_w[];                     // [kMergeRows][pieces]
   __shared__ floatx4 s_o[256];
   __shared__ float s_inv[kMergeRows];
   const long total = a.span[grid].first;
+  const SpanHead item = a.span[blockIdx.y + 1];      // asked for together; not looked at where no span has written it
   const long n_span = spans(total, parts, grid);
   if (blockIdx.y + 1 >= n_span) return;
-  const SpanHead item = a.span[blockIdx.y + 1];
   const long w0 = blockIdx.y;
   if (item.first >= span_start(total, n_span, w0 + 1) || item.first < span_start(total, n_span, w0)) return;
   const Seq sq = same_seq_of(a, item.slot, item_rows);
@@ -971,26 +973,76 @@ __global__ __launch_bounds__(256) void attn_q8_merge_kernel(Q8Params a, int item
   const int n = (int)(w1 - w0) + 1;                  // pieces
   // w0 holds the item's start, the others continue it
   auto row_at = [&](int i, int row) { return (size_t)(i ? 2 * (w0 + i) : 2 * w0 + 1) * item_rows + row0 + row; };
-  const int lane = lane_id(), tid = threadIdx.x;
-  for (int row = tid >> 6; row < rows; row += 4) {
-    float m = -INFINITY;
-    for (int i = lane; i < n; i += kWave) {
-      s_w[row * n + i] = a.part_ml[2 * row_at(i, row)];
-      m = fmaxf(m, s_w[row * n + i]);
+  const int tid = threadIdx.x;
+  const int units = rows * (D / 4);
+  auto put = [&](int e, const floatx4& o, float inv) {
+    const int row = e / (D / 4), d = 4 * (e % (D / 4));
+    const int pr = r * item_rows + row0 + row, i = pos_of(a, pr), hl = pr - i * a.G;
+    DT* out = reinterpret_cast<DT*>(a.out) + ((size_t)(sq.r0 + i) * a.Hq + g * a.G + hl) * D + d;
+    typedef DT __attribute__((ext_vector_type(4))) Four;
+    Four w;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) w[c] = from_f32<DT>(o[c] * inv);
+    *reinterpret_cast<Four*>(out) = w;
+  };
+  if (n <= kFewPieces) {
+    constexpr int PER = 2;          // units of a thread at a time
+    for (int e0 = tid; e0 < units; e0 += PER * 256) {
+      floatx4 o[PER][kFewPieces];
+      float2 ml[PER][kFewPieces];
+#pragma unroll
+      for (int u = 0; u < PER; ++u) {
+        const int e = min(e0 + 256 * u, units - 1), row = e / (D / 4), d = 4 * (e % (D / 4));
+#pragma unroll
+        for (int i = 0; i < kFewPieces; ++i)
+          if (i < n) {
+            const size_t at = row_at(i, row);
+            o[u][i] = ld16<floatx4>(a.part_o + at * D + d);
+            ml[u][i] = *reinterpret_cast<const float2*>(a.part_ml + 2 * at);
+          }
+      }
+#pragma unroll
+      for (int u = 0; u < PER; ++u) {
+        if (e0 + 256 * u >= units) continue;
+        float m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int i = 0; i < kFewPieces; ++i)
+          if (i < n) m = fmaxf(m, ml[u][i].x);
+        m = m == -INFINITY ? 0.f : m;
+        floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kFewPieces; ++i)
+          if (i < n) {
+            const float x = fast_exp2(ml[u][i].x - m);
+            l += x * ml[u][i].y;
+            sum += x * o[u][i];
+          }
+        put(e0 + 256 * u, sum, 1.f / l);
+      }
     }
-    m = wave_max(m);
-    m = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    for (int i = lane; i < n; i += kWave) {
-      const float x = fast_exp2(s_w[row * n + i] - m);
-      s_w[row * n + i] = x;
-      l += x * a.part_ml[2 * row_at(i, row) + 1];
+    return;
+  }
+  if (const int row = tid >> 4; row < rows) {
+    const int c = tid & 15;
+    float m = -INFINITY, l = 0.f;
+    for (int i = c; i < n; i += 16) {
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * row_at(i, row));
+      s_w[row * n + i] = ml.x;
+      const float m2 = fmaxf(m, ml.x), mu = m2 == -INFINITY ? 0.f : m2;
+      l = l * fast_exp2(m - mu) + ml.y * fast_exp2(ml.x - mu);
+      m = m2;
     }
-    l = wave_sum(l);
-    if (lane == 0) s_inv[row] = 1.f / l;
+    float all = m;
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) all = fmaxf(all, __shfl_xor(all, o, kWave));
+    all = all == -INFINITY ? 0.f : all;
+    l *= fast_exp2(m - all);
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) l += __shfl_xor(l, o, kWave);
+    for (int i = c; i < n; i += 16) s_w[row * n + i] = fast_exp2(s_w[row * n + i] - all);
+    if (c == 0) s_inv[row] = 1.f / l;
   }
   __syncthreads();
-  const int units = rows * (D / 4);
   const int split = units <= 64 ? 4 : units <= 128 ? 2 : 1;
   const int team = 256 / split, part = tid / team;
   auto sum = [&](int e) {
@@ -1000,15 +1052,8 @@ __global__ __launch_bounds__(256) void attn_q8_merge_kernel(Q8Params a, int item
     for (int i = part; i < n; i += split) o += s_w[row * n + i] * ld16<floatx4>(a.part_o + row_at(i, row) * D + d);
     return o;
   };
-  auto put = [&](int e, const floatx4& o) {
-    const int row = e / (D / 4), d = 4 * (e % (D / 4));
-    const int pr = r * item_rows + row0 + row, i = pos_of(a, pr), hl = pr - i * a.G;
-    DT* out = reinterpret_cast<DT*>(a.out) + ((size_t)(sq.r0 + i) * a.Hq + g * a.G + hl) * D + d;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) out[c] = from_f32<DT>(o[c] * s_inv[row]);
-  };
   if (split == 1) {
-    for (int e = tid; e < units; e += 256) put(e, sum(e));
+    for (int e = tid; e < units; e += 256) put(e, sum(e), s_inv[e / (D / 4)]);
     return;
   }
   const int e = tid % team;
@@ -1017,7 +1062,7 @@ __global__ __launch_bounds__(256) void attn_q8_merge_kernel(Q8Params a, int item
   if (part == 0 && e < units) {
     floatx4 o = s_o[tid];
     for (int x = 1; x < split; ++x) o += s_o[tid + x * team];
-    put(e, o);
+    put(e, o, s_inv[e / (D / 4)]);
   }
 }
 
