@@ -296,11 +296,19 @@ __device__ __forceinline__ void attend(uint4 (&v)[D / 16], uint4 vscale, floatx4
                                        float (&l_run)[QT]) {
   const int u0 = t0 + 16 * (lane_id() >> 4);          // unit j's first position
   if (tail) {
+    asm volatile("");                // a branch: else every block is masked, 250 of 600 instructions
+    // An unseen key's scale byte may be anything, a later row's that of NaN
+    // (infinite here, and times a probability of zero NaN): the rows that see
+    // such a key get the NaN here, and the scale is taken out.
 #pragma unroll
-    for (int q = 0; q < QT; ++q)
+    for (int i = 0; i < 16; ++i) {
+      const unsigned w = word(vscale, i >> 2), at = 255u << (8 * (i & 3));
+      const bool odd = (w & at) == at;
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (u0 + i >= qlimit[q]) s[q][i >> 2][i & 3] = -INFINITY;
+      for (int q = 0; q < QT; ++q)
+        s[q][i >> 2][i & 3] = u0 + i >= qlimit[q] ? -INFINITY : odd ? __uint_as_float(0x7fc00000u) : s[q][i >> 2][i & 3];
+      (i < 4 ? vscale.x : i < 8 ? vscale.y : i < 12 ? vscale.z : vscale.w) = odd ? w & ~at : w;
+    }
     auto live = [&](unsigned x, int at) {             // the bytes of slots at .. at + 3: behind the last key may be NaN
       const int n = n_keys - (u0 + at);
       return n >= 4 ? x : n <= 0 ? 0u : x & ((1u << (8 * n)) - 1u);
@@ -352,19 +360,6 @@ __device__ __forceinline__ void attend(uint4 (&v)[D / 16], uint4 vscale, floatx4
 #pragma unroll
       for (int n = 0; n < NS; ++n) pf[n][q][i >> 3][i & 7] = t[n];
     }
-  }
-  if (tail) {
-    // An unseen key's scale byte may be anything, a later row's that of NaN
-    // (infinite here, and times its zero bytes NaN).
-    int u1 = u0;
-    asm("" : "+v"(u1));                    // compare again: the masks above would be kept, in 2 x 16 QT registers
-#pragma unroll
-    for (int q = 0; q < QT; ++q)
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-#pragma unroll
-        for (int n = 0; n < NS; ++n)
-          if (u1 + i >= qlimit[q]) pf[n][q][i >> 3][i & 7] = static_cast<__bf16>(0.f);
   }
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) {
