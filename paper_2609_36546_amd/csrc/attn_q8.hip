@@ -34,9 +34,9 @@
 // all items (an item: one row group of one (sequence, KV head)) form one line,
 // cut into as many equal spans as there are workgroups, so that ragged contexts,
 // single sequences and long contexts all fill the chip.  Items cut by a span's
-// end leave partial results, merged by a second kernel.  Where no item is longer
-// than a span (prompts), nothing is cut: the items are dealt out whole, the
-// longest row groups first and every second round backwards.
+// end leave partial results, merged by a second kernel.  Where whole items can be
+// dealt out about as evenly (prompts), nothing is cut: the longest first, every
+// second round backwards.
 //
 // A workgroup's four waves are RG row groups of QT tiles x KS = 4 / RG key parts,
 // merged in LDS at an item's end; plan_of has the choice.  With one row group
@@ -439,7 +439,8 @@ template <bool DEALT> struct Walk {            // along a span of the line
 template <> struct Walk<true> {                // whole items, dealt out
   int slot, g, r, end;
   static constexpr int j = 0;
-  int round, places, n_sg;   // places for items in all, and in a row group: (sequence, KV head)s, a multiple of 8
+  int round, rounds;
+  const int* list;           // the rounds' items
   __device__ __forceinline__ bool whole() const { return true; }
   __device__ __forceinline__ int part() const { return 0; }
 };
@@ -465,25 +466,14 @@ __device__ __forceinline__ bool advance(const Q8Params& a, Walk<false>& c) {
   c.end = min(c.steps, c.len - c.first);
   return true;
 }
-// A round deals every workgroup a place.  Workgroups go to the 8 XCDs in turn, and
-// so do the places: a head's items all go to one XCD, which has its keys in L2.
 template <int ITEM, int STEP>
 __device__ __forceinline__ bool advance(const Q8Params& a, Walk<true>& c) {
-  const int x = blockIdx.x & 7, i = blockIdx.x >> 3, n = gridDim.x >> 3;
-  for (;;) {
-    const int base = ++c.round * (int)gridDim.x;
-    if (base >= c.places) return false;
-    const int k = base + (c.round & 1 ? n - 1 - i : i) * 8 + x;
-    const int back = k / c.n_sg, sg = k - back * c.n_sg;
-    if (k >= c.places || sg >= a.n_seq * a.Hkv) continue;
-    c.r = c.places / c.n_sg - 1 - back;
-    c.slot = sg / a.Hkv;
-    c.g = sg - c.slot * a.Hkv;
-    const Seq sq = same_seq_of(a, c.slot, ITEM);
-    if (c.r >= sq.n_rg) continue;
-    c.end = item_steps(a, sq, c.r, ITEM, STEP);
-    return true;
-  }
+  if (++c.round >= c.rounds) return false;
+  c.slot = __builtin_amdgcn_readfirstlane(c.list[3 * c.round]);
+  c.g = __builtin_amdgcn_readfirstlane(c.list[3 * c.round + 1]);
+  c.r = __builtin_amdgcn_readfirstlane(c.list[3 * c.round + 2]);
+  c.end = item_steps(a, same_seq_of(a, c.slot, ITEM), c.r, ITEM, STEP);
+  return true;
 }
 
 // The line as a workgroup knows it: every one adds it all up, a thread
@@ -492,32 +482,29 @@ struct Line {
   static constexpr int kKept = 1024;
   int steps[kKept];    // a head's steps, of the first slots
   long sum[4], at[2];
-  int most[4], most_rg[4];
+  int part[4];
 };
 struct Share {         // a thread's
   int sl0, sl1;        // its slots
   long at, len;        // where they begin, and their steps
+  int most;            // the longest item's
 };
 
-// Returns whether the items are dealt out whole.  The merge reads the line's length
-// (0: nothing is cut) and every span's first item.
-template <int ITEM, int STEP, bool MAY_DEAL>
-__device__ __forceinline__ bool add_up(const Q8Params& a, Line& line, Share& mine, long& total, int& places) {
+// The line's length, of which the merge reads the last: 0 where nothing is cut.
+template <int ITEM, int STEP>
+__device__ __forceinline__ long add_up(const Q8Params& a, Line& line, Share& mine) {
   const int tid = threadIdx.x, lane = lane_id(), wv = tid >> 6;
   const int per = (a.n_seq + 255) / 256;
   mine.sl0 = min(tid * per, a.n_seq);
   mine.sl1 = min(mine.sl0 + per, a.n_seq);
   mine.len = 0;
-  int most = 0, most_rg = 0;                        // an item's steps, and a head's items
+  mine.most = 0;
   for (int i = mine.sl0; i < mine.sl1; ++i) {
     const Seq sq = seq_of(a, i, ITEM);
     const long n = head_steps(a, sq, ITEM, STEP);
     if (i < Line::kKept) line.steps[i] = (int)min(n, 0x7fffffffl);
     mine.len += a.Hkv * n;
-    if (MAY_DEAL && sq.n_rg > 0) {
-      most = max(most, item_steps(a, sq, sq.n_rg - 1, ITEM, STEP));
-      most_rg = max(most_rg, sq.n_rg);
-    }
+    if (sq.n_rg > 0) mine.most = max(mine.most, item_steps(a, sq, sq.n_rg - 1, ITEM, STEP));
   }
   long incl = mine.len;
 #pragma unroll
@@ -527,47 +514,140 @@ __device__ __forceinline__ bool add_up(const Q8Params& a, Line& line, Share& min
   }
   if (lane == kWave - 1) line.sum[wv] = incl;
   __syncthreads();
-  total = 0;
+  long total = 0;
   mine.at = incl - mine.len;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (i < wv) mine.at += line.sum[i];
     total += line.sum[i];
   }
-  bool dealt = false;
-  if (MAY_DEAL && total >= gridDim.x) {             // the same for all threads
+  if (blockIdx.x == 0 && tid == 0) a.span[gridDim.x].first = total;
+  return total;
+}
+
+// Sum over the threads before this one; every thread calls.
+__device__ __forceinline__ int threads_before(int v, int (&part)[4], int* all = nullptr) {
+  const int lane = lane_id(), wv = threadIdx.x >> 6;
+  int incl = v;
 #pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      most = max(most, __shfl_xor(most, o, kWave));
-      most_rg = max(most_rg, __shfl_xor(most_rg, o, kWave));
-    }
-    if (lane == 0) {
-      line.most[wv] = most;
-      line.most_rg[wv] = most_rg;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      most = max(most, line.most[i]);
-      most_rg = max(most_rg, line.most_rg[i]);
-    }
-    const long n = (long)((a.n_seq * a.Hkv + 7) & ~7) * most_rg;
-    dealt = (gridDim.x & 7) == 0 && (long)most * gridDim.x <= total && n < 1 << 30;
-    places = __builtin_amdgcn_readfirstlane((int)n);
-    dealt = __builtin_amdgcn_readfirstlane((int)dealt) != 0;
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int up = __shfl_up(incl, o, kWave);
+    if (lane >= o) incl += up;
   }
-  if (blockIdx.x == 0 && tid == 0) a.span[gridDim.x].first = dealt ? 0 : total;
-  return dealt;
+  __syncthreads();                                  // the previous call's readers are done
+  if (lane == kWave - 1) part[wv] = incl;
+  __syncthreads();
+  int before = 0, sum = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    before += i < wv ? part[i] : 0;
+    sum += part[i];
+  }
+  if (all) *all = sum;
+  return before + incl - v;
+}
+
+// Items dealt out whole, by falling length in classes of 2^shift steps (256 of
+// them at most; within a class by slot, head and row group).  A round gives every
+// workgroup one; neighbours in that order, which are a head's, go to one XCD.
+struct Deal {
+  static constexpr int kRounds = 16, kClasses = 256;
+  int above[kClasses + 1];   // items of longer classes
+  int list[3 * kRounds];
+};
+// First row group of at least s steps.
+__device__ __forceinline__ int first_of(const Q8Params& a, const Seq& sq, int s, int item_rows, int step) {
+  const long x = (long)(s - 1) * step - sq.L;
+  if (x <= 0) return 0;
+  const long need = x * a.G + 1;
+  return need > sq.rows ? sq.n_rg : (int)((need + item_rows - 1) / item_rows) - 1;
+}
+// Returns whether dealing out is worth it, and if so this workgroup's walk.
+template <int ITEM, int STEP>
+__device__ __forceinline__ bool deal(const Q8Params& a, Line& line, Deal& d, const Share& mine, long total, Walk<true>& c) {
+  const int grid = gridDim.x, tid = threadIdx.x, lane = lane_id();
+  if (total < grid || (long)a.n_seq * a.Hkv > (long)Deal::kRounds * grid) return false;
+  // the longest item
+  int most = mine.most;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) most = max(most, __shfl_xor(most, o, kWave));
+  __syncthreads();
+  if (lane == 0) line.part[tid >> 6] = most;
+  d.above[tid] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) most = max(most, line.part[i]);
+  // Cutting costs its partial results, written and read: about 3 steps for 32 rows
+  // of an item; less where there are few.  Measured, cut / dealt: prompts of 512 to
+  // 1024 tokens, 32 heads on 4, eight of them 163 / 115 us, four 108 / 70; windows
+  // of 8 over 1000 tokens, 64 of them (half of the workgroups with an item) 41 / 48;
+  // of 128 over 2000 to 4000, eight of them 103 / 181.
+  const float mean = (float)((double)total / grid), limit = mean + fminf(0.8f * mean, (float)(ITEM * kBlk * 3 / (32 * STEP)));
+  if ((float)most > limit) return false;
+  int shift = 0;
+  while ((most - 1) >> shift >= Deal::kClasses) ++shift;
+  // the classes' items of one head; a slot's row groups to `team` threads
+  int team = 1;
+  while (team < kWave && 2 * team * a.n_seq <= 256) team *= 2;
+  for (int i = tid / team; i < a.n_seq; i += 256 / team) {
+    const Seq sq = seq_of(a, i, ITEM);
+    for (int r = tid & (team - 1); r < sq.n_rg; r += team)
+      atomicAdd(&d.above[(most - item_steps(a, sq, r, ITEM, STEP)) >> shift], 1);
+  }
+  __syncthreads();
+  const int n = d.above[tid] * a.Hkv;
+  int items;
+  const int before = threads_before(n, line.part, &items);
+  if (items > Deal::kRounds * grid) return false;   // then the cuts cost little
+  d.above[tid] = before;
+  if (tid == 0) d.above[Deal::kClasses] = items;
+  __syncthreads();
+  // A lane looks up one place: of this workgroup, of the round's first and of its last.
+  const int xcd = grid & 7 ? blockIdx.x : (blockIdx.x & 7) * (grid >> 3) + (blockIdx.x >> 3);
+  const int round = lane / 3, who = lane % 3, p = who == 0 ? xcd : who == 1 ? 0 : grid - 1;
+  const int k = round * grid + (round & 1 ? grid - 1 - p : p);
+  int cls = 0, hi = Deal::kClasses;                 // above[cls] <= k < above[hi]
+  while (hi - cls > 1) {
+    const int mid = (cls + hi) / 2;
+    if (d.above[mid] <= k) cls = mid; else hi = mid;
+  }
+  const bool is = round < Deal::kRounds && k < items;
+  const float load = is ? (float)(most - (cls << shift)) : 0.f;
+  const float worst = fmaxf(wave_sum(who == 1 ? load : 0.f), wave_sum(who == 2 ? load : 0.f));
+  if (!(worst <= limit)) return false;
+  c.rounds = __popcll(__ballot(is && who == 0));
+  for (int i = 0; i < c.rounds; ++i) {
+    const int ci = __shfl(cls, 3 * i, kWave), ki = __shfl(k, 3 * i, kWave);
+    const int s_hi = most - (ci << shift), s_lo = max(s_hi - (1 << shift) + 1, 1);
+    int have = 0;
+    for (int sl = mine.sl0; sl < mine.sl1; ++sl) {
+      const Seq sq = seq_of(a, sl, ITEM);
+      have += (first_of(a, sq, s_hi + 1, ITEM, STEP) - first_of(a, sq, s_lo, ITEM, STEP)) * a.Hkv;
+    }
+    int at = ki - d.above[ci] - threads_before(have, line.part);
+    if (at >= 0 && at < have) {
+      for (int sl = mine.sl0; sl < mine.sl1; ++sl) {
+        const Seq sq = seq_of(a, sl, ITEM);
+        const int r0 = first_of(a, sq, s_lo, ITEM, STEP), m = first_of(a, sq, s_hi + 1, ITEM, STEP) - r0;
+        if (at < m * a.Hkv) {
+          d.list[3 * i] = sl;
+          d.list[3 * i + 1] = at / m;
+          d.list[3 * i + 2] = r0 + at % m;
+          break;
+        }
+        at -= m * a.Hkv;
+      }
+    }
+  }
+  if (blockIdx.x == 0 && tid == 0) a.span[grid].first = 0;
+  __syncthreads();
+  c.rounds = __builtin_amdgcn_readfirstlane(c.rounds);
+  c.round = -1;
+  c.list = d.list;
+  return true;
 }
 
 // Where the workgroup's walk begins; false when it has none.
-template <int ITEM, int STEP>
-__device__ __forceinline__ bool begin_walk(const Q8Params& a, int places, Walk<true>& c) {
-  c.round = -1;
-  c.places = places;
-  c.n_sg = (a.n_seq * a.Hkv + 7) & ~7;
-  return advance<ITEM, STEP>(a, c);
-}
 template <int ITEM, int STEP>
 __device__ __forceinline__ bool begin_walk(const Q8Params& a, Line& line, const Share& mine, long total, int parts,
                                            Walk<false>& c) {
@@ -781,9 +861,7 @@ __global__ __launch_bounds__(256, 2) void attn_q8_keys_kernel(Q8Params a) {
   const int tid = threadIdx.x, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   __shared__ Line s_line;
   Share mine;
-  long total;
-  int places;
-  add_up<kItem, kBlk, false>(a, s_line, mine, total, places);
+  const long total = add_up<kItem, kBlk>(a, s_line, mine);
   Walk<false> c;
   if (!begin_walk<kItem, kBlk>(a, s_line, mine, total, 4, c)) return;
   do {
@@ -930,15 +1008,15 @@ __global__ __launch_bounds__(256, 2) void attn_q8_rows_kernel(Q8Params a) {
   typedef Ring<D, QT, RG> G;
   __shared__ __attribute__((aligned(16))) char s_ring[G::kDepth * G::kStage];
   __shared__ Line s_line;
+  __shared__ Deal s_deal;
   Share mine;
-  long total;
-  int places;
-  if (add_up<G::kItem, G::kStep, true>(a, s_line, mine, total, places)) {
-    Walk<true> c;
-    if (begin_walk<G::kItem, G::kStep>(a, places, c)) walk_rows<DT, D, QT, RG>(a, c, s_ring);
-  } else {
-    Walk<false> c;
-    if (begin_walk<G::kItem, G::kStep>(a, s_line, mine, total, 2, c)) walk_rows<DT, D, QT, RG>(a, c, s_ring);
+  const long total = add_up<G::kItem, G::kStep>(a, s_line, mine);
+  Walk<true> items;
+  Walk<false> span;
+  if (deal<G::kItem, G::kStep>(a, s_line, s_deal, mine, total, items)) {
+    if (advance<G::kItem, G::kStep>(a, items)) walk_rows<DT, D, QT, RG>(a, items, s_ring);
+  } else if (begin_walk<G::kItem, G::kStep>(a, s_line, mine, total, 2, span)) {
+    walk_rows<DT, D, QT, RG>(a, span, s_ring);
   }
 }
 
