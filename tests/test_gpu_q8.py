@@ -250,6 +250,73 @@ def test_many_sequences_some_handled_strided_queries():
             assert (o == 7).all()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("heads,longest", [((16, 4), 320), ((16, 16), 200), ((15, 5), 260)])
+def test_prompts_of_many_lengths(dt, heads, longest):
+    """Enough work for every workgroup, in row groups of very different lengths; every second prompt in another order."""
+    rng = np.random.default_rng(longest)
+    windows = [(0, int(n)) for n in rng.integers(1, longest, 36)] + [(0, 0), (0, longest), (17, 3), (0, longest)]
+    Hq, Hkv = heads
+    c, table, ctx, cu, pt, dctx, dcu = pool(windows, Hkv, 64, 16)
+    kv = fill(c, table, ctx, cu, pt, 5)
+    q = torch.randn(int(cu[-1]), Hq, 64, generator=torch.Generator().manual_seed(6)).to(dt)
+    ids = rng.permutation(len(windows)).astype(np.int32)
+    for some in (ids, ids[:29]):
+        out = torch.full((int(cu[-1]), Hq, 64), 7.0, dtype=dt, device="cuda")
+        ops.verify_attn_q8(q.cuda(), c, pt, dctx, dcu, longest, seq_ids=torch.from_numpy(some).cuda(), out=out)
+        for b, (K, V) in enumerate(kv):
+            o = out[cu[b]: cu[b + 1]]
+            if b not in some:
+                assert (o == 7).all()
+            elif len(o) and (some is ids or b % 4 == 0):
+                check_rows(o, ref.attention(f64(q[cu[b]: cu[b + 1]]), K, V, int(ctx[b]), 0.125), dt)
+
+
+@pytest.mark.gpu
+def test_long_contexts_of_shared_pages():
+    """512 sequences that share one long prefix's pages, of many lengths: items of more than 256 steps."""
+    B, k, Hq, Hkv, D, ps = 512, 5, 32, 2, 64, 64
+    n = 16800
+    c, table, ctx, cu, pt, _, _ = pool([(n - 1, 1)], Hkv, D, ps)
+    (K, V), = fill(c, table, ctx, cu, pt, 5)
+    L = np.random.default_rng(1).integers(16300, n - k, B).astype(np.int32)
+    g = torch.Generator().manual_seed(6)
+    q = (2 * torch.randn(B * k, Hq, D, generator=g)).to(BF16).cuda()
+    out = ops.verify_attn_q8(q, c, pt.expand(B, -1).contiguous(), torch.from_numpy(L).cuda(),
+                             torch.arange(0, B * k + 1, k, dtype=torch.int32).cuda(), k)
+    Kd, Vd = torch.from_numpy(K).cuda(), torch.from_numpy(V).cuda()
+    pos = torch.arange(n, device="cuda")
+    for b in range(0, B, 5):
+        for h in range(Hkv):
+            rows = q[b * k: (b + 1) * k, h * 16: (h + 1) * 16].double().reshape(k * 16, D)
+            s = rows @ Kd[:, h].T.contiguous() * D ** -0.5
+            s[pos[None] > int(L[b]) + torch.arange(k, device="cuda").repeat_interleave(16)[:, None]] = -float("inf")
+            want = torch.softmax(s, 1) @ Vd[:, h].contiguous()
+            check_rows(out[b * k: (b + 1) * k, h * 16: (h + 1) * 16], want.view(k, 16, D).cpu().numpy(), BF16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Hq,D", [(8, 64), (2, 128)])
+def test_nan_rows_inside_a_tile(Hq, D):
+    """A value row that is not a number between rows of one tile, before and behind a block's end."""
+    for at in (5, 33, 59):
+        windows = [(70, 60), (20, 3)]
+        c, table, ctx, cu, pt, dctx, dcu = pool(windows, 2, D, 16)
+        kv = fill(c, table, ctx, cu, pt, 9)
+        k, v = rows_of(windows, 2, D, BF16, 3), rows_of(windows, 2, D, BF16, 4)
+        v[at, 1, 7] = float("nan")
+        ops.kv_append_q8(k.cuda(), v.cuda(), c, pt, dctx, dcu, 60)
+        q = torch.randn(63, Hq, D, generator=torch.Generator().manual_seed(2)).to(BF16)
+        out = f64(ops.verify_attn_q8(q.cuda(), c, pt, dctx, dcu, 60))
+        nan = np.isnan(out)
+        assert nan[at:60, Hq // 2:].all() and not nan[:at].any() and not nan[:60, : Hq // 2].any() and not nan[60:].any()
+        K, V = kv[0][0].copy(), kv[0][1].copy()
+        K[70:130], V[70:130] = ref.quantise(f64(k[:60]))[0], ref.quantise(f64(v[:60]))[0]
+        want = ref.attention(f64(q[:at]), K[: 70 + at], V[: 70 + at], 70, D ** -0.5)
+        check_rows(torch.from_numpy(out[:at]), want, BF16)
+
+
 # --- refusals (no GPU) ---
 
 def c_kv(read=False, **kw):

@@ -99,6 +99,24 @@ def test_masked_rows():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("many", [300, 2500, 5000])
+def test_cuts_in_crowded_bins(dt, many):
+    """A cut among `many` entries within a small step of one another, of which one
+    part of the vocabulary holds a few, another most, and a third none."""
+    V = 50000
+    g = torch.Generator().manual_seed(many)
+    l = torch.full((6, V), -20.0) + torch.randn(6, V, generator=g)
+    crowd = torch.cat([torch.randperm(16000, generator=g)[:100], 32768 + torch.randperm(16000, generator=g)[: many - 100]])
+    l[:, crowd] = 2.0 + 0.05 * torch.randn(6, many, generator=g)
+    l[:, 40] = 6.0
+    l = l.to(dt)
+    for f in (dict(k=many // 2), dict(k=many), dict(k=many // 3, p=0.6), dict(p=0.5), dict(p=0.97), dict(p=0.6, m=0.0183),
+              dict(k=many - 50, m=0.019), dict(k=many - 50, p=0.9, m=0.0178)):
+        check(l, uniforms(6), **f)
+
+
+@pytest.mark.gpu
 def test_odd_temperatures():
     l = gauss(6, 3001, F32)
     token, logp = call(l, 0.5, T=[-1.0, float("nan"), 0.0, INF, 1e-30, 1e30])
