@@ -650,6 +650,11 @@ def _need_rows(t: torch.Tensor, name: str, dtype, device, ndim: int) -> int:
     return n
 
 
+def _need_workspace(t, dev):
+    if not (isinstance(t, torch.Tensor) and t.device == dev and t.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+
+
 def _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev):
     _need(ctx_lens, "ctx_lens", torch.int32, dev, 1)
     _need(cu_q, "cu_q", torch.int32, dev, 1)
@@ -697,14 +702,19 @@ def rope_window(q, k, inv_freq, ctx_lens, cu_q, max_q: int, seq_ids=None,
         raise ValueError("k must be [T,Hkv,D]")
     _need(inv_freq, "inv_freq", torch.float32, dev, 1)
     n_seq = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
+    qos, kos = Hq * D, Hkv * D
     if q_out is None:
         q_out = torch.empty(T, Hq, D, dtype=dt, device=dev)
+    else:
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+        qos = _need_rows(q_out, "q_out", dt, dev, 3)
     if k_out is None:
         k_out = torch.empty(T, Hkv, D, dtype=dt, device=dev)
-    if q_out.shape != q.shape or k_out.shape != k.shape:
-        raise ValueError("q_out and k_out must have the shapes of q and k")
-    qos = _need_rows(q_out, "q_out", dt, dev, 3)
-    kos = _need_rows(k_out, "k_out", dt, dev, 3)
+    else:
+        if k_out.shape != k.shape:
+            raise ValueError("k_out must have k's shape")
+        kos = _need_rows(k_out, "k_out", dt, dev, 3)
     if T == 0:
         n_seq = 0
     st = lib().rope_window(_ptr(q), qs, _ptr(k), ks, _ptr(q_out), qos, _ptr(k_out), kos,
@@ -790,12 +800,13 @@ def kv_read_q8(cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int, rows: int
     n_seq = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
     _q8_table(cache, page_table, ctx_lens, dev)
     shape = (int(rows), cache.Hkv, cache.D)
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        if t is not None:
+            _need(t, name, dtype, dev, 3)
+            if t.shape != shape:
+                raise ValueError(f"{name} must be [rows,Hkv,D]")
     k_out = torch.empty(shape, dtype=dtype, device=dev) if k_out is None else k_out
     v_out = torch.empty(shape, dtype=dtype, device=dev) if v_out is None else v_out
-    _need(k_out, "k_out", dtype, dev, 3)
-    _need(v_out, "v_out", dtype, dev, 3)
-    if tuple(k_out.shape) != shape or tuple(v_out.shape) != shape:
-        raise ValueError("k_out and v_out must be [rows,Hkv,D]")
     if shape[0] == 0:
         n_seq = 0
     st = lib().kv_read_q8(_ptr(cache.k), _ptr(cache.v), _ptr(cache.scale), _ptr(page_table),
@@ -837,6 +848,8 @@ def verify_attn_q8(q, cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int, se
     if workspace is None:
         need = attn_q8_workspace_size(n_seq, Hq, cache.Hkv, D, max_q)
         workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    else:
+        _need_workspace(workspace, dev)
     st = lib().verify_attn_q8(_ptr(q), qs, _ptr(cache.k), _ptr(cache.v), _ptr(cache.scale),
                               _ptr(page_table), page_table.shape[1], _ptr(ctx_lens), _ptr(cu_q),
                               _ptr(seq_ids), n_seq, max_q, _ptr(out), Hq, cache.Hkv, D,
@@ -868,15 +881,18 @@ def sample_logits(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
             _need(t, name, d, dev, 1)
             if t.shape[0] != M:
                 raise ValueError(f"{name} must be [M]")
+    for t, name, d in ((token, "token", torch.int32), (logp, "logp", torch.float32)):
+        if t is not None:
+            _need(t, name, d, dev, 1)
+            if t.shape[0] != M:
+                raise ValueError(f"{name} must be [M]")
     token = torch.empty(M, dtype=torch.int32, device=dev) if token is None else token
     logp = torch.empty(M, dtype=torch.float32, device=dev) if logp is None else logp
-    _need(token, "token", torch.int32, dev, 1)
-    _need(logp, "logp", torch.float32, dev, 1)
-    if token.shape[0] != M or logp.shape[0] != M:
-        raise ValueError("token and logp must be [M]")
     if workspace is None:
         workspace = torch.empty(max(sample_logits_workspace_size(M, V), 1), dtype=torch.uint8,
                                 device=dev)
+    else:
+        _need_workspace(workspace, dev)
     st = lib().sample_logits(_ptr(logits), ls, M, V, _ptr(u), _ptr(temperature), _ptr(top_k),
                              _ptr(top_p), _ptr(min_p), _ptr(token), _ptr(logp), code,
                              _ptr(workspace), workspace.numel() * workspace.element_size(),

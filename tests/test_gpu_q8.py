@@ -374,3 +374,15 @@ def test_workspace_query():
 def test_cache_object_checks_its_tensors():
     with pytest.raises(ValueError):
         ops.Q8Cache.empty(2, 1, 64, 16, device="cpu")
+
+
+@pytest.mark.gpu
+def test_a_workspace_elsewhere_is_refused():
+    c, _, _, cu, pt, dctx, dcu = pool([(3, 2)], 2, 64, 16)
+    q = torch.zeros(2, 4, 64, dtype=BF16, device="cuda")
+    ws = torch.empty(2 * ops.attn_q8_workspace_size(1, 4, 2, 64, 2), dtype=torch.uint8)
+    for bad in (ws, ws.cuda()[::2]):
+        with pytest.raises(ValueError):
+            ops.verify_attn_q8(q, c, pt, dctx, dcu, 2, workspace=bad)
+        with pytest.raises(ValueError):
+            ops.sample_logits(torch.zeros(1, 50, device="cuda"), torch.zeros(1, device="cuda"), workspace=bad)
