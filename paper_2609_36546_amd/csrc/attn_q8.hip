@@ -361,6 +361,7 @@ __device__ __forceinline__ void attend(uint4 (&v)[D / 16], uint4 vscale, floatx4
       for (int n = 0; n < NS; ++n) pf[n][q][i >> 3][i & 7] = t[n];
     }
   }
+  __builtin_amdgcn_s_setprio(1);           // matrix work before the other wave's softmax: eight prompts 105 to 98 us
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) {
     const uint4 w = v[dt];
@@ -374,6 +375,7 @@ __device__ __forceinline__ void attend(uint4 (&v)[D / 16], uint4 vscale, floatx4
           acc[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][q][st], acc[q][dt], 0, 0, 0);
     }
   }
+  __builtin_amdgcn_s_setprio(0);
 }
 
 // ---- the line of blocks ----
