@@ -607,7 +607,8 @@ int rope_window(const void* q, int64_t q_row_stride, const void* k, int64_t k_ro
  * page_table, ctx_lens, cu_q, seq_ids, n_seq, max_q as in verify_attn_paged.
  * Slots of other positions are left as they are.
  * Requirements: D in {64, 128}, page_size 16, 32 or 64, n_seq * Hkv <= 65535,
- * max_q < 2^27; pages, scales and the rows of k_new and v_new start on 16-byte boundaries.
+ * num_pages * Hkv < 2^31, max_q < 2^27; pages, scales and the rows of k_new and
+ * v_new start on 16-byte boundaries.
  *
  * Errors: IPDV_EINVAL, IPDV_EUNSUPPORTED (D, page_size, dtype, alignment), IPDV_EHIP.
  */

