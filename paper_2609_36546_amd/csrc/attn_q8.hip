@@ -1152,17 +1152,17 @@ struct Q8Plan {
   int item_rows, parts, grid;      // parts: steps per span at least
 };
 // Row groups share the keys that they load, and leave fewer parts of them to
-// merge; but where rows are few they are copies, and their work is wasted.  Measured
-// at rg = 1 / 2 / 4 (32 heads on 4, D = 128; 64 windows over 1024 to 8192 tokens;
-// us): 8 rows 66 / 66 / 76, 32 rows 102 / 76 / 86, 64 rows 182 / 97 / 94, and eight
-// prompts 455 / 199 / 100.  Two tiles share a key's conversion: qt = 1 / 2 takes
-// 111 / 97 at 64 rows, 76 / 87 at 32 (half of the second tile's rows), and 124 / 100
-// for the prompts.
+// merge; but where rows are few they are copies, and their work is wasted.  Two
+// tiles per wave share a key's conversion, and halve the waves that a row count
+// fills.  Measured (32 heads on 4, D = 128; 64 windows over 1024 to 8192 tokens;
+// us) at rg = 1 / 2 / 4 with one tile: 8 rows 66 / 66 / 76, 32 rows 102 / 76 / 86,
+// 64 rows 182 / 111 / 97; with two at rg = 2: 64 rows 106; at rg = 4, one tile / two:
+// 128 rows 101 / 92, eight prompts 124 / 100.
 Q8Plan plan_of(int n_seq, int Hq, int Hkv, int max_q, bool bf16) {
   Q8Plan p;
   const long rows = (long)max_q * (Hq / Hkv);
-  p.qt = bf16 && rows > 32 ? 2 : 1;                 // fp32, three terms per query: no registers for two tiles
-  p.rg = rows <= 16 ? 1 : rows <= 32 * p.qt ? 2 : 4;
+  p.qt = bf16 && rows > 64 ? 2 : 1;                 // fp32, three terms per query: no registers for two tiles
+  p.rg = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   p.item_rows = 16 * p.qt * p.rg;
   p.parts = p.rg == 1 ? 4 : 2;
   p.grid = 2 * device_cus();                        // as many as are resident
@@ -1215,8 +1215,8 @@ hipError_t launch_attn_q8(const AttnQ8Launch& L, hipStream_t st) {
     using DT = decltype(dt);
     constexpr int D = decltype(dim)::value, QT = sizeof(DT) == 2 ? 2 : 1;
     if (pl.rg == 1) go(attn_q8_keys_kernel<DT, D>);
-    else if (pl.rg == 2 && pl.qt == 1) go(attn_q8_rows_kernel<DT, D, 1, 2>);
-    else if (pl.rg == 2) go(attn_q8_rows_kernel<DT, D, QT, 2>);
+    else if (pl.rg == 2) go(attn_q8_rows_kernel<DT, D, 1, 2>);
+    else if (pl.qt == 1) go(attn_q8_rows_kernel<DT, D, 1, 4>);
     else go(attn_q8_rows_kernel<DT, D, QT, 4>);
   };
   typedef std::integral_constant<int, 64> D64;
