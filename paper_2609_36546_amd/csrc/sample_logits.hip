@@ -36,7 +36,7 @@
 //                 can (63 KB of code took 17 us even unfiltered).
 //
 // At V = 151936: one fp32 row takes 6 us and 13 unfiltered, 8 and 17 with top-p
-// 0.9; 64 bf16 rows 11 and 13, and 19 and 18.  The chunk kernel is bound by its
+// 0.9; 64 bf16 rows 11 and 13, and 18 and 17.  The chunk kernel is bound by its
 // vector instructions (about 25 an entry) and LDS atomics, the row kernel by the
 // latency of some ten dependent steps.  Lists that were not in bin order had to be
 // searched, and ended higher: a mixed batch of 64 took 58 us where this takes 38.
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kThreads, 6) void chunk_kernel(SampleLogitsLaunch p
   constexpr int N = VEC ? 16 / (int)sizeof(DT) : 1;   // entries per load
   constexpr int PER = kChunk / kThreads;
   __shared__ u64 s_hist[kBins];
-  __shared__ float s_max[kWaves], s_min[kWaves];
+  __shared__ float s_max[kWaves];
   __shared__ int s_bad, s_cover, s_wave[kBins / kWave], s_at[kBins];
   const int m = blockIdx.x / n_chunks, s = blockIdx.x % n_chunks;
   const int tid = threadIdx.x, lane = lane_id(), w = tid >> 6;
@@ -218,35 +218,28 @@ __global__ __launch_bounds__(kThreads, 6) void chunk_kernel(SampleLogitsLaunch p
   const Row r = row_of(p, m);
   if (tid < kBins) s_hist[tid] = 0;
   if (tid == 0) s_bad = s_cover = 0;
-  float mx = -INFINITY, mn = INFINITY;
+  float mx = -INFINITY;
   bool bad = false;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    mx = fmaxf(mx, x(i));
-    mn = fminf(mn, x(i) > -INFINITY ? x(i) : INFINITY);
-    bad |= !(x(i) < INFINITY);
+  for (int i = 0; i < PER; i += 2) {
+    mx = fmaxf(mx, fmaxf(x(i), x(i + 1)));
+    bad |= __builtin_isunordered(x(i), x(i + 1));
   }
   renew();
   mx = wave_max(mx);
-  mn = -wave_max(-mn);
-  if (lane == 0) {
-    s_max[w] = mx;
-    s_min[w] = mn;
-  }
+  if (lane == 0) s_max[w] = mx;
   __syncthreads();
   if (bad) s_bad = 1;
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    mx = fmaxf(mx, s_max[i]);
-    mn = fminf(mn, s_min[i]);
-  }
+  for (int i = 0; i < kWaves; ++i) mx = fmaxf(mx, s_max[i]);
+  if (mx == INFINITY) s_bad = 1;
   const bool any = mx > -INFINITY && mx < INFINITY;
   float ignore;
   const double top = any ? floor_y(r, mx, &ignore) : -INFINITY;
   auto add = [&](int bin, unsigned mass) {
     __hip_atomic_fetch_add(&s_hist[bin], (1ull << kCountShift) + mass, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
   };
-  const bool near = any && fmaxf(fabsf(mx), fabsf(mn)) * r.hi < kFar;
+  const bool near = any && fabs(top) < 0.5 * kFar;      // whatever is not far below is near then
   if (near) {                       // the same without double
     const float ftop = (float)top;
 #pragma unroll
@@ -295,36 +288,41 @@ __global__ __launch_bounds__(kThreads, 6) void chunk_kernel(SampleLogitsLaunch p
   const int cover = any && filtered ? min(s_cover, kBins - 1) : 0;    // the last bin is never listed
   if (tid == 0) *rec.head = {top, mx, s_bad, cover};
   if (cover == 0) return;
-  auto place = [&](int bin) { return atomicAdd(&s_at[bin], 1); };
   renew();
+  const float ftop = (float)top;
+  unsigned in = 0;                  // bit i: entry i is listed
+  static_assert(PER <= 32, "a bit per entry");
   if (near) {
-    const float ftop = (float)top, end = (float)cover;
-    constexpr int AT = 8;           // places asked for at a time
+    const float least = ftop - (float)(cover - 1);       // floor(y) >= this, a whole number, where y is
 #pragma unroll
-    for (int i0 = 0; i0 < PER; i0 += AT) {
-      int at[AT];
-#pragma unroll
-      for (int i = 0; i < AT; ++i) {
-        float rest;
-        const float d = ftop - floor_near(r, x(i0 + i), &rest);
-        at[i] = -1;
-        if (d < end) at[i] = place((int)d);
-      }
-#pragma unroll
-      for (int i = 0; i < AT; ++i) {
-        const int e = i0 + i;
-        if (at[i] >= 0) rec.list[at[i]] = order_of(x(e), v0 + (e / N) * kThreads * N + tid * N + e % N);
-      }
-    }
+    for (int i = 0; i < PER; ++i) in |= (x(i) * r.hi >= least ? 1u : 0u) << i;
   } else {
 #pragma unroll 1
     for (int i = 0; i < PER; ++i) {
       float l = x(0), rest;
 #pragma unroll
       for (int c = 0; c < PER; ++c) l = c == i ? x(c) : l;
-      if (!(l > -INFINITY)) continue;
-      const double d = top - floor_y(r, l, &rest);
-      if (d < cover) rec.list[place((int)d)] = order_of(l, v0 + (i / N) * kThreads * N + tid * N + i % N);
+      in |= (l > -INFINITY && top - floor_y(r, l, &rest) < cover ? 1u : 0u) << i;
+    }
+  }
+  // Few, so a rolled loop, which cannot choose among registers: the cache still has them.
+  constexpr int AT = 4;
+  while (__any(in != 0)) {
+    int v[AT];
+    float l[AT];
+#pragma unroll
+    for (int k = 0; k < AT; ++k) {
+      const int i = __ffs(in) - 1;
+      v[k] = in ? (i / N * kThreads + tid) * N + i % N : -1;
+      in &= in - 1;
+      if (v[k] >= 0) l[k] = to_f32(src[v[k]]);
+    }
+#pragma unroll
+    for (int k = 0; k < AT; ++k) {
+      if (v[k] < 0) continue;
+      float rest;
+      const int bin = near ? (int)(ftop - floor_near(r, l[k], &rest)) : (int)(top - floor_y(r, l[k], &rest));
+      rec.list[atomicAdd(&s_at[bin], 1)] = order_of(l[k], v0 + v[k]);
     }
   }
 }
