@@ -50,9 +50,9 @@
 // What bounds it, in bf16 at D = 128: one token each of 64 sequences of 1024 to
 // 8192 tokens, 16 heads on 8, the bytes (609 MB in 120 us, the rate of a copy);
 // windows of eight, 32 heads on 4, the vector instructions beside the loads (313
-// MB in 95 us, of which the loads alone take 62 and the merge 10); prompts, the
+// MB in 94 us, of which the loads alone take 62 and the merge 10); prompts, the
 // vector instructions of softmax and conversion, about 430 per 64 keys and 32 rows
-// beside 48 matrix ones (eight of 512 to 1024 tokens in 98 us, 413 TFLOP/s).
+// beside 48 matrix ones (eight of 512 to 1024 tokens in 94 us, 430 TFLOP/s).
 #include <algorithm>
 #include <type_traits>
 
