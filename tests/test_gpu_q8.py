@@ -274,6 +274,96 @@ def test_prompts_of_many_lengths(dt, heads, longest):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("Hq,Hkv,most", [(1, 1, 5), (8, 1, 7), (16, 1, 11)])
+def test_more_sequences_than_are_kept_in_lds(Hq, Hkv, most):
+    rng = np.random.default_rng(most)
+    windows = [(int(rng.integers(0, 60)), int(rng.integers(0, most))) for _ in range(1500)]
+    c, table, ctx, cu, pt, dctx, dcu = pool(windows, Hkv, 64, 16)
+    kv = fill(c, table, ctx, cu, pt, 5)
+    q = torch.randn(int(cu[-1]), Hq, 64, generator=torch.Generator().manual_seed(6)).to(BF16)
+    out = torch.full_like(q, float("nan"), device="cuda")
+    ops.verify_attn_q8(q.cuda(), c, pt, dctx, dcu, most, out=out)
+    want = [ref.attention(f64(q[a:b]), K, V, int(L), 0.125) for a, b, (K, V), L in zip(cu[:-1], cu[1:], kv, ctx) if b > a]
+    check_rows(out, np.concatenate(want), BF16)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bound", [1, 3, 40, 5000])
+def test_a_window_bound_above_the_need(bound):
+    windows = [(200, 1), (0, 1), (33, 0), (700, 1)]
+    c, table, ctx, cu, pt, dctx, dcu = pool(windows, 2, 128, 16)
+    kv = fill(c, table, ctx, cu, pt, 5)
+    q = torch.randn(3, 8, 128, generator=torch.Generator().manual_seed(6)).to(BF16)
+    out = ops.verify_attn_q8(q.cuda(), c, pt, dctx, dcu, bound)
+    for b, (K, V) in enumerate(kv):
+        if cu[b + 1] > cu[b]:
+            check_rows(out[cu[b]: cu[b + 1]], ref.attention(f64(q[cu[b]: cu[b + 1]]), K, V, int(ctx[b]), 128 ** -0.5), BF16)
+
+
+@pytest.mark.gpu
+def test_a_captured_call_follows_its_lengths():
+    """One captured call over windows that change between replays: prompts, a few
+    rows over long contexts, nothing at all, and prompts again."""
+    B, T, Hq, Hkv, D, ps = 40, 6000, 16, 4, 64, 16
+    rng = np.random.default_rng(0)
+    prompts = [(0, int(n)) for n in rng.integers(1, 240, B)]
+    few = [(int(rng.integers(100, 600)), int(rng.integers(0, 9))) for _ in range(B)]
+    roomy = [(max(a[0], b[0]), max(a[1], b[1])) for a, b in zip(prompts, few)]
+    c, table, _, _, pt, _, _ = pool(roomy, Hkv, D, ps)
+    c.k.view(torch.uint8).fill_(0x30)
+    g = torch.Generator().manual_seed(1)
+    c.v.copy_(torch.randn(c.v.shape, generator=g).to(torch.float8_e4m3fn))
+    c.k.copy_(torch.randn(c.k.shape, generator=g).to(torch.float8_e4m3fn))
+    c.scale.fill_(127)
+    ctx, cu = torch.zeros(B, dtype=torch.int32).cuda(), torch.zeros(B + 1, dtype=torch.int32).cuda()
+    q = torch.randn(T, Hq, D, generator=g).to(BF16).cuda()
+    out = torch.zeros_like(q)
+    ws = torch.full((ops.attn_q8_workspace_size(B, Hq, Hkv, D, 240),), 255, dtype=torch.uint8, device="cuda")
+    call = lambda o, w: ops.verify_attn_q8(q, c, pt, ctx, cu, 240, out=o, workspace=w)  # noqa: E731
+
+    def set_windows(w):
+        ctx.copy_(torch.tensor([x[0] for x in w], dtype=torch.int32))
+        cu.copy_(torch.from_numpy(np.concatenate([[0], np.cumsum([x[1] for x in w])]).astype(np.int32)))
+
+    set_windows(few)
+    call(out, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, ws)
+    for w in (prompts, few, [(5, 0)] * B, prompts, few):
+        set_windows(w)
+        out.fill_(7.0)
+        want = call(torch.full_like(out, 7.0), None)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        n = sum(x[1] for x in w)
+        assert torch.isfinite(out).all() and (out[n:] == 7).all() and not (out[:n] == 7).all(-1).any()
+
+
+@pytest.mark.gpu
+def test_two_calls_at_once():
+    """Calls on two streams over one cache, each with a workspace of its own."""
+    windows = [(900, 8), (0, 64), (300, 1), (40, 30)]
+    c, table, ctx, cu, pt, dctx, dcu = pool(windows, 2, 128, 16)
+    fill(c, table, ctx, cu, pt, 5)
+    qs = [torch.randn(int(cu[-1]), 16, 128, generator=torch.Generator().manual_seed(i)).to(BF16).cuda() for i in range(2)]
+    want = [ops.verify_attn_q8(q, c, pt, dctx, dcu, 64) for q in qs]
+    streams = [torch.cuda.Stream() for _ in qs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(ops.verify_attn_q8(qs[i], c, pt, dctx, dcu, 64))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, want[i]) for o in got[i])
+
+
+@pytest.mark.gpu
 def test_long_contexts_of_shared_pages():
     """512 sequences that share one long prefix's pages, of many lengths: items of more than 256 steps."""
     B, k, Hq, Hkv, D, ps = 512, 5, 32, 2, 64, 64

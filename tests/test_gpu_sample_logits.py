@@ -117,6 +117,23 @@ def test_cuts_in_crowded_bins(dt, many):
 
 
 @pytest.mark.gpu
+def test_many_rows():
+    """More rows than workgroups at once; rows of one logit set repeat as their uniforms do."""
+    few = gauss(5, 300, F32)
+    rows = np.random.default_rng(0).integers(0, 5, 20000)
+    u = np.random.default_rng(1).integers(0, 50, 20000).astype(np.float32) / 50
+    token, logp = call(few[rows], u, 0.9, 30, 0.8)
+    for r in range(5):
+        for x in range(50):
+            same = (rows == r) & (u == np.float32(x) / np.float32(50))
+            assert len(set(token[same])) <= 1
+    some = np.arange(0, 20000, 97)
+    for i in some:
+        assert ref.draw_is_right(few[rows[i]].double().numpy(), float(np.float32(0.9)), 30, float(np.float32(0.8)), 0.0, float(u[i]),
+                                 int(token[i]), float(logp[i]))
+
+
+@pytest.mark.gpu
 def test_odd_temperatures():
     l = gauss(6, 3001, F32)
     token, logp = call(l, 0.5, T=[-1.0, float("nan"), 0.0, INF, 1e-30, 1e30])
