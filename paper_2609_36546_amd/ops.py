@@ -628,47 +628,69 @@ ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_YARN = 0, 1, 2, 3
 
 
-def _need_rows(t: torch.Tensor, name: str, dtype, device, ndim: int) -> int:
-    """Like _need, but rows (dim 0) may lie further apart than they are long,
-    as in a slice of a wider projection.  Returns the row stride in elements."""
+# The calls from here on check a tensor and give its address in one go: two of
+# them make up a step of 8 us on the device, so each check that is made twice, or
+# through an object that is built for it, shows.
+def _at(t: torch.Tensor, name: str, dtype, dev, ndim: int) -> int:
+    """_need, and the address."""
     try:
-        if t.is_cuda and t.dtype is dtype and t.device == device and isinstance(t, torch.Tensor):
+        if (t.dtype is dtype and t.get_device() == dev.index and t.dim() == ndim
+                and t.is_contiguous()):
+            return t.data_ptr()
+    except AttributeError:
+        pass                          # not a tensor: named below
+    _need(t, name, dtype, dev, ndim)
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, name: str, dtype, dev, ndim: int):
+    """Like _at, but rows (dim 0) may lie further apart than they are long, as in
+    a slice of a wider projection.  Returns the address, the row stride in
+    elements and the shape."""
+    try:
+        if t.dtype is dtype and t.get_device() == dev.index:
             size, step = t.shape, t.stride()
             if len(size) == ndim and size[0] > 1 and step[-1] == 1 and (ndim == 2 or step[1] == size[2]):
-                return step[0]        # a stride shorter than the row is refused by the library
+                return t.data_ptr(), step[0], size    # a stride shorter than the row is refused by the library
     except AttributeError:
         pass                          # not a tensor: named below
     if isinstance(t, torch.Tensor) and t.dim() == ndim and t.shape[0] > 0 and not t.is_contiguous():
-        _need(t[0], name, dtype, device, ndim - 1)
+        _need(t[0], name, dtype, dev, ndim - 1)
         if t.shape[0] > 1:
-            return t.stride(0)
+            return t.data_ptr(), t.stride(0), t.shape
     else:
-        _need(t, name, dtype, device, ndim)
+        _need(t, name, dtype, dev, ndim)
     n = 1
     for s in t.shape[1:]:
         n *= s
-    return n
+    return t.data_ptr(), n, t.shape
 
 
-def _need_workspace(t, dev):
+def _given_workspace(t, dev):
     if not (isinstance(t, torch.Tensor) and t.device == dev and t.is_contiguous()):
         raise ValueError(f"workspace must be a contiguous tensor on {dev}")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev):
-    _need(ctx_lens, "ctx_lens", torch.int32, dev, 1)
-    _need(cu_q, "cu_q", torch.int32, dev, 1)
-    B = ctx_lens.shape[0]
-    if cu_q.shape[0] != B + 1:
+    """Addresses of ctx_lens, cu_q and seq_ids, the sequences to handle, and the batch."""
+    ctx = _at(ctx_lens, "ctx_lens", torch.int32, dev, 1)
+    cu = _at(cu_q, "cu_q", torch.int32, dev, 1)
+    B = ctx_lens.size(0)
+    if cu_q.size(0) != B + 1:
         raise ValueError("cu_q must be [B+1]")
-    if seq_ids is not None:
-        _need(seq_ids, "seq_ids", torch.int32, dev, 1)
-        if n_seq is not None and n_seq > seq_ids.shape[0]:
-            raise ValueError("n_seq exceeds seq_ids")
-        return seq_ids.shape[0] if n_seq is None else n_seq
-    if n_seq is not None and n_seq > B:
-        raise ValueError("n_seq exceeds the batch")
-    return B if n_seq is None else n_seq
+    if seq_ids is None:
+        if n_seq is None:
+            n_seq = B
+        elif n_seq > B:
+            raise ValueError("n_seq exceeds the batch")
+        return ctx, cu, None, n_seq, B
+    ids = _at(seq_ids, "seq_ids", torch.int32, dev, 1)
+    if n_seq is None:
+        n_seq = seq_ids.size(0)
+    elif n_seq > seq_ids.size(0):
+        raise ValueError("n_seq exceeds seq_ids")
+    return ctx, cu, ids, n_seq, B
 
 
 def rope_inv_freq(rot: int, base: float = 10000.0, kind: int = ROPE_PLAIN, factor: float = 1.0,
@@ -694,33 +716,34 @@ def rope_window(q, k, inv_freq, ctx_lens, cu_q, max_q: int, seq_ids=None,
     k (in place).  Returns (q_out, k_out)."""
     dev, dt = q.device, q.dtype
     code = _dtype_code(dt)
-    qs = _need_rows(q, "q", dt, dev, 3)
-    ks = _need_rows(k, "k", dt, dev, 3)
-    T, Hq, D = q.shape
-    Hkv = k.shape[1]
-    if k.shape != (T, Hkv, D):
+    qp, qs, q_shape = _rows(q, "q", dt, dev, 3)
+    kp, ks, k_shape = _rows(k, "k", dt, dev, 3)
+    T, Hq, D = q_shape
+    Hkv = k_shape[1]
+    if k_shape[0] != T or k_shape[2] != D:
         raise ValueError("k must be [T,Hkv,D]")
-    _need(inv_freq, "inv_freq", torch.float32, dev, 1)
-    n_seq = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
+    freq = _at(inv_freq, "inv_freq", torch.float32, dev, 1)
+    ctx, cu, ids, n_seq, _ = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
     qos, kos = Hq * D, Hkv * D
     if q_out is None:
-        q_out = torch.empty(T, Hq, D, dtype=dt, device=dev)
+        q_out = torch.empty_like(q)       # dense rows; torch.empty of a torch.Size takes 0.8 us more
+        qop = q_out.data_ptr()
     else:
-        if q_out.shape != q.shape:
+        qop, qos, shape = _rows(q_out, "q_out", dt, dev, 3)
+        if shape != q_shape:
             raise ValueError("q_out must have q's shape")
-        qos = _need_rows(q_out, "q_out", dt, dev, 3)
     if k_out is None:
-        k_out = torch.empty(T, Hkv, D, dtype=dt, device=dev)
+        k_out = torch.empty_like(k)
+        kop = k_out.data_ptr()
     else:
-        if k_out.shape != k.shape:
+        kop, kos, shape = _rows(k_out, "k_out", dt, dev, 3)
+        if shape != k_shape:
             raise ValueError("k_out must have k's shape")
-        kos = _need_rows(k_out, "k_out", dt, dev, 3)
     if T == 0:
         n_seq = 0
-    st = lib().rope_window(_ptr(q), qs, _ptr(k), ks, _ptr(q_out), qos, _ptr(k_out), kos,
-                           _ptr(inv_freq), _ptr(ctx_lens), _ptr(cu_q), _ptr(seq_ids), n_seq, max_q,
-                           Hq, Hkv, D, 2 * inv_freq.shape[0], int(layout), float(factor),
-                           int(bool(inverse)), code, _stream(dev))
+    st = lib().rope_window(qp, qs, kp, ks, qop, qos, kop, kos, freq, ctx, cu, ids, n_seq, max_q,
+                           Hq, Hkv, D, 2 * inv_freq.size(0), int(layout), float(factor),
+                           1 if inverse else 0, code, _stream(dev))
     _check("rope_window", st)
     return q_out, k_out
 
@@ -754,14 +777,17 @@ class Q8Cache:
         return self.k.device
 
 
-def _q8_table(cache: Q8Cache, page_table, ctx_lens, dev):
+def _q8_table(cache: Q8Cache, page_table, B, dev):
+    """Address and width of the page table, once the cache is known to be on dev."""
     if not isinstance(cache, Q8Cache):
         raise TypeError("cache must be a Q8Cache")
-    if cache.device != dev:
+    if cache.k.get_device() != dev.index:
         raise ValueError(f"cache must be on {dev} (is on {cache.device})")
-    _need(page_table, "page_table", torch.int32, dev, 2)
-    if page_table.shape[0] != ctx_lens.shape[0]:
+    at = _at(page_table, "page_table", torch.int32, dev, 2)
+    n, max_pages = page_table.shape
+    if n != B:
         raise ValueError("page_table must be [B, maxp]")
+    return at, max_pages
 
 
 def kv_append_q8(k_new, v_new, cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int,
@@ -771,22 +797,21 @@ def kv_append_q8(k_new, v_new, cache: Q8Cache, page_table, ctx_lens, cu_q, max_q
     include/ipdv.h).  validate=True first runs check_page_table on host copies."""
     dev, dt = k_new.device, k_new.dtype
     code = _dtype_code(dt)
-    ks = _need_rows(k_new, "k_new", dt, dev, 3)
-    vs = _need_rows(v_new, "v_new", dt, dev, 3)
-    n_seq = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
-    _q8_table(cache, page_table, ctx_lens, dev)
-    T = k_new.shape[0]
-    if k_new.shape != (T, cache.Hkv, cache.D) or v_new.shape != k_new.shape:
+    kp, ks, shape = _rows(k_new, "k_new", dt, dev, 3)
+    vp, vs, v_shape = _rows(v_new, "v_new", dt, dev, 3)
+    ctx, cu, ids, n_seq, B = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
+    table, max_pages = _q8_table(cache, page_table, B, dev)
+    T, Hkv, D = shape
+    if Hkv != cache.Hkv or D != cache.D or v_shape != shape:
         raise ValueError("k_new and v_new must be [T,Hkv,D] of the cache's heads")
     if validate:
         check_page_table(page_table, ctx_lens, cu_q, max_q, cache.page_size, cache.num_pages,
                          seq_ids=seq_ids, n_seq=n_seq)
     if T == 0:
         n_seq = 0
-    st = lib().kv_append_q8(_ptr(k_new), ks, _ptr(v_new), vs, _ptr(cache.k), _ptr(cache.v),
-                            _ptr(cache.scale), _ptr(page_table), page_table.shape[1], _ptr(ctx_lens),
-                            _ptr(cu_q), _ptr(seq_ids), n_seq, max_q, cache.Hkv, cache.D,
-                            cache.page_size, cache.num_pages, code, _stream(dev))
+    st = lib().kv_append_q8(kp, ks, vp, vs, cache.k.data_ptr(), cache.v.data_ptr(),
+                            cache.scale.data_ptr(), table, max_pages, ctx, cu, ids, n_seq, max_q,
+                            Hkv, D, cache.page_size, cache.num_pages, code, _stream(dev))
     _check("kv_append_q8", st)
 
 
@@ -797,22 +822,24 @@ def kv_read_q8(cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int, rows: int
     the cached lengths in cu_q, whole sequences.  Returns (k, v)."""
     dev = cache.device
     code = _dtype_code(dtype)
-    n_seq = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
-    _q8_table(cache, page_table, ctx_lens, dev)
-    shape = (int(rows), cache.Hkv, cache.D)
+    ctx, cu, ids, n_seq, B = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
+    table, max_pages = _q8_table(cache, page_table, B, dev)
+    Hkv, D = cache.Hkv, cache.D
+    shape = (int(rows), Hkv, D)
     for t, name in ((k_out, "k_out"), (v_out, "v_out")):
         if t is not None:
             _need(t, name, dtype, dev, 3)
             if t.shape != shape:
                 raise ValueError(f"{name} must be [rows,Hkv,D]")
-    k_out = torch.empty(shape, dtype=dtype, device=dev) if k_out is None else k_out
-    v_out = torch.empty(shape, dtype=dtype, device=dev) if v_out is None else v_out
+    if k_out is None:
+        k_out = torch.empty(*shape, dtype=dtype, device=dev)
+    if v_out is None:
+        v_out = torch.empty_like(k_out)
     if shape[0] == 0:
         n_seq = 0
-    st = lib().kv_read_q8(_ptr(cache.k), _ptr(cache.v), _ptr(cache.scale), _ptr(page_table),
-                          page_table.shape[1], _ptr(ctx_lens), _ptr(cu_q), _ptr(seq_ids), n_seq,
-                          max_q, _ptr(k_out), _ptr(v_out), cache.Hkv, cache.D, cache.page_size,
-                          cache.num_pages, code, _stream(dev))
+    st = lib().kv_read_q8(cache.k.data_ptr(), cache.v.data_ptr(), cache.scale.data_ptr(), table,
+                          max_pages, ctx, cu, ids, n_seq, max_q, k_out.data_ptr(), v_out.data_ptr(),
+                          Hkv, D, cache.page_size, cache.num_pages, code, _stream(dev))
     _check("kv_read_q8", st)
     return k_out, v_out
 
@@ -829,32 +856,33 @@ def verify_attn_q8(q, cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int, se
     include/ipdv.h).  Returns out [T,Hq,D]."""
     dev, dt = q.device, q.dtype
     code = _dtype_code(dt)
-    qs = _need_rows(q, "q", dt, dev, 3)
-    n_seq = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
-    _q8_table(cache, page_table, ctx_lens, dev)
-    T, Hq, D = q.shape
+    qp, qs, shape = _rows(q, "q", dt, dev, 3)
+    ctx, cu, ids, n_seq, B = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
+    table, max_pages = _q8_table(cache, page_table, B, dev)
+    T, Hq, D = shape
+    Hkv = cache.Hkv
     if D != cache.D:
         raise ValueError("q and the cache have different head dims")
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     if out is None:
-        out = torch.empty(T, Hq, D, dtype=dt, device=dev)
+        out = torch.empty_like(q)
     else:
         _need(out, "out", dt, dev, 3)
-        if out.shape != q.shape:
+        if out.shape != shape:
             raise ValueError("out must have q's shape")
     if T == 0:
         n_seq = 0
     if workspace is None:
-        need = attn_q8_workspace_size(n_seq, Hq, cache.Hkv, D, max_q)
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+        size = max(attn_q8_workspace_size(n_seq, Hq, Hkv, D, max_q), 1)
+        workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        ws = workspace.data_ptr()
     else:
-        _need_workspace(workspace, dev)
-    st = lib().verify_attn_q8(_ptr(q), qs, _ptr(cache.k), _ptr(cache.v), _ptr(cache.scale),
-                              _ptr(page_table), page_table.shape[1], _ptr(ctx_lens), _ptr(cu_q),
-                              _ptr(seq_ids), n_seq, max_q, _ptr(out), Hq, cache.Hkv, D,
-                              cache.page_size, cache.num_pages, float(scale), code, _ptr(workspace),
-                              workspace.numel() * workspace.element_size(), _stream(dev))
+        ws, size = _given_workspace(workspace, dev)
+    st = lib().verify_attn_q8(qp, qs, cache.k.data_ptr(), cache.v.data_ptr(), cache.scale.data_ptr(),
+                              table, max_pages, ctx, cu, ids, n_seq, max_q, out.data_ptr(), Hq, Hkv,
+                              D, cache.page_size, cache.num_pages, float(scale), code, ws, size,
+                              _stream(dev))
     _check("verify_attn_q8", st)
     return out
 
@@ -872,30 +900,35 @@ def sample_logits(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
     their log-probs among what the filters kept."""
     dev, dt = logits.device, logits.dtype
     code = _dtype_code(dt)
-    ls = _need_rows(logits, "logits", dt, dev, 2)
-    M, V = logits.shape
-    for t, name, d in ((u, "u", torch.float32), (temperature, "temperature", torch.float32),
-                       (top_k, "top_k", torch.int32), (top_p, "top_p", torch.float32),
-                       (min_p, "min_p", torch.float32)):
-        if t is not None or name == "u":
-            _need(t, name, d, dev, 1)
-            if t.shape[0] != M:
-                raise ValueError(f"{name} must be [M]")
-    for t, name, d in ((token, "token", torch.int32), (logp, "logp", torch.float32)):
-        if t is not None:
-            _need(t, name, d, dev, 1)
-            if t.shape[0] != M:
-                raise ValueError(f"{name} must be [M]")
-    token = torch.empty(M, dtype=torch.int32, device=dev) if token is None else token
-    logp = torch.empty(M, dtype=torch.float32, device=dev) if logp is None else logp
+    lp, ls, (M, V) = _rows(logits, "logits", dt, dev, 2)
+
+    def of_rows(t, name, dtype):
+        if t is None:
+            return None
+        at = _at(t, name, dtype, dev, 1)
+        if t.size(0) != M:
+            raise ValueError(f"{name} must be [M]")
+        return at
+
+    f32, i32 = torch.float32, torch.int32
+    up = _at(u, "u", f32, dev, 1)
+    if u.size(0) != M:
+        raise ValueError("u must be [M]")
+    tp = of_rows(temperature, "temperature", f32)
+    kp = of_rows(top_k, "top_k", i32)
+    pp = of_rows(top_p, "top_p", f32)
+    mp = of_rows(min_p, "min_p", f32)
+    of_rows(token, "token", i32)
+    of_rows(logp, "logp", f32)
+    token = torch.empty(M, dtype=i32, device=dev) if token is None else token
+    logp = torch.empty(M, dtype=f32, device=dev) if logp is None else logp
     if workspace is None:
-        workspace = torch.empty(max(sample_logits_workspace_size(M, V), 1), dtype=torch.uint8,
-                                device=dev)
+        size = max(sample_logits_workspace_size(M, V), 1)
+        workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        ws = workspace.data_ptr()
     else:
-        _need_workspace(workspace, dev)
-    st = lib().sample_logits(_ptr(logits), ls, M, V, _ptr(u), _ptr(temperature), _ptr(top_k),
-                             _ptr(top_p), _ptr(min_p), _ptr(token), _ptr(logp), code,
-                             _ptr(workspace), workspace.numel() * workspace.element_size(),
-                             _stream(dev))
+        ws, size = _given_workspace(workspace, dev)
+    st = lib().sample_logits(lp, ls, M, V, up, tp, kp, pp, mp, token.data_ptr(), logp.data_ptr(),
+                             code, ws, size, _stream(dev))
     _check("sample_logits", st)
     return token, logp
