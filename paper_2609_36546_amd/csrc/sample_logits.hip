@@ -35,11 +35,11 @@
 //                 and stay in registers, and its loops stay rolled where they
 //                 can (63 KB of code took 17 us even unfiltered).
 //
-// At V = 151936: one fp32 row takes 6 us and 13 unfiltered, 8 and 17 with top-p
-// 0.9; 64 bf16 rows 11 and 13, and 18 and 17.  The chunk kernel is bound by its
+// At V = 151936: one fp32 row takes 5 us and 11 unfiltered, 8.5 and 17 with top-p
+// 0.9; 64 bf16 rows 11 and 11, and 18 and 17.  The chunk kernel is bound by its
 // vector instructions (about 25 an entry) and LDS atomics, the row kernel by the
 // latency of some ten dependent steps.  Lists that were not in bin order had to be
-// searched, and ended higher: a mixed batch of 64 took 58 us where this takes 38.
+// searched, and ended higher: a mixed batch of 64 took 58 us where this takes 37.
 //
 // A bin of many entries (equal logits by the thousand) is narrowed by digits of
 // the entries' order numbers until 256 are left, in LDS or, where they do not
