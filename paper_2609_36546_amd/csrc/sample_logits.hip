@@ -352,6 +352,34 @@ __device__ __forceinline__ T block_scan(T v, T* s_part) {
   return before + incl - v;
 }
 
+// Two at once.
+__device__ __forceinline__ int block_scan(int a, double b, int* part_a, double* part_b, double* before_b) {
+  const int lane = lane_id(), w = threadIdx.x >> 6;
+  const int incl_a = wave_incl_scan_i(a);
+  double incl_b = b;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const double up = __shfl_up(incl_b, o, kWave);
+    if (lane >= o) incl_b += up;
+  }
+  __syncthreads();
+  if (lane == kWave - 1) {
+    part_a[w] = incl_a;
+    part_b[w] = incl_b;
+  }
+  __syncthreads();
+  int before_a = 0;
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i)
+    if (i < w) {
+      before_a += part_a[i];
+      sum += part_b[i];
+    }
+  *before_b = sum + incl_b - b;
+  return before_a + incl_a - a;
+}
+
 struct Shared {
   double edge[kBins];               // e^(-t/8): mass of bin t's upper edge
   float edge_f[kBins];
@@ -530,6 +558,31 @@ struct RowWork {
     const int first = S.count_before[bin];
     // what is kept: entries with less than the need before them
     auto before = [&](int c, u64 mass) { return need.by_count ? first + c < need.count : base + e * (double)mass < need.mass; };
+    if (held && S.count[bin] <= kWave) {       // a wave's: the usual top-k, without the workgroup's barriers
+      if (tid < kWave) {
+        const int n = S.count[bin];
+        const u64 mine = tid < n ? S.hold[tid] : 0;
+        int rank = 0;
+#pragma unroll 8
+        for (int c = 0; c < n; ++c) rank += S.hold[c] > mine;
+        if (tid < n) S.sorted[rank] = mine;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");       // LDS keeps a wave's order: this binds the compiler only
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        const u64 o = tid < n ? S.sorted[tid] : 0, w = tid < n ? mass_of(o) : 0;
+        u64 upto = w;
+#pragma unroll
+        for (int i = 1; i < kWave; i <<= 1) {
+          const u64 up = __shfl_up(upto, i, kWave);
+          if (tid >= i) upto += up;
+        }
+        const bool here = tid < n && (tid == 0 || before(tid, upto - w));
+        const bool next = tid + 1 < n && before(tid + 1, upto);
+        if (here && !next) S.cut = o;
+      }
+      __syncthreads();
+      return;
+    }
     if (tid == 0) {
       S.lo = 0;
       S.hi = ~0ull;
@@ -612,10 +665,8 @@ struct RowWork {
     __syncthreads();
   }
 
-  // What the chunks keep of the gathered bin, given the cut: S.in_bin.
+  // What the chunks keep of the gathered bin, given the cut: into S.in_bin.
   __device__ void record(bool held, u64 cut) {
-    if (tid < kMaxChunks) S.in_bin[tid] = 0;
-    __syncthreads();
     each(held, [&](u64 o) {
       if (o >= cut)
         __hip_atomic_fetch_add(&S.in_bin[index_of(o) / kChunk], mass_of(o), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
@@ -706,8 +757,8 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
     __syncthreads();
     const int count = tid < kBins ? S.count[t] : 0;
     const double mass = tid < kBins ? (double)S.mass[t] * S.edge[t] * kUnitMass : 0.0;
-    const double mass_before = block_scan<double>(mass, S.part_d);
-    const int count_before = block_scan<int>(count, S.part_i);
+    double mass_before;
+    const int count_before = block_scan(count, mass, S.part_i, S.part_d, &mass_before);
     if (tid < kBins) {
       S.before[t] = mass_before;
       S.count_before[t] = count_before;
@@ -747,7 +798,9 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
       const int bin = S.bin;
       if (bin < 0 || bin == kBins - 1) continue;       // nothing that counts is cut
       if (pass < 2 && bin > bin_min && (pass == 1 || r.top_p == 1.f)) continue;      // min-p cuts above it
+      if (tid < kMaxChunks) S.in_bin[tid] = 0;         // record's, from here on the last cut's
       if (bin != bin_cut) held = work.gather(bin);
+      else if (pass == 2) __syncthreads();
       if (pass < 2) work.select(bin, held, need);
       cut = pass < 2 ? S.cut : bound;                  // at or above the last one
       work.record(held, cut);
