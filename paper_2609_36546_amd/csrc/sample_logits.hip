@@ -129,7 +129,10 @@ __device__ __forceinline__ float floor_near(const Row& r, float l, float* rest) 
 __device__ __forceinline__ double floor_y(const Row& r, float l, float* rest) {
 #pragma clang fp contract(off)
   if (fabsf(l * r.hi) < kFar) return (double)floor_near(r, l, rest);
-  const double z = (double)l * r.width, f = floor(z);
+  // A greater logit must not have a lesser floor (bins are differences from the
+  // maximum's, and index arrays): fp32 floors reach kFar - 1, and where fp32 has
+  // rounded its way up to kFar, z may still lie up to 1.5 below.
+  const double z = (double)l * r.width, f = z > 0.0 ? fmax(floor(z), (double)kFar - 1.0) : floor(z);
   *rest = (float)(z - f);
   return f;
 }

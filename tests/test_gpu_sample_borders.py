@@ -1,0 +1,27 @@
+"""sample_logits where its arithmetic changes hands or rounds: far bins, the
+least temperatures, needs and uniforms that fall between two prefix sums."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_36546_amd import ops
+from tests.test_gpu_sample_logits import BF16, F32, INF, call, check, gauss  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("T,l", [(float.fromhex(a), float.fromhex(b)) for a, b in (
+    # 8 l / T just below 2^24, and fp32 rounds 8 / T up: the next logit's floor in 64 bits is one less than l's in 32
+    ("0x1.eb94a4p-17", "0x1.eb94a0p+4"), ("0x1.dbdb7ep-15", "0x1.dbdb7ap+6"), ("0x1.f44f66p-11", "0x1.f44f62p+10"),
+    ("0x1.deb6fap-19", "0x1.deb6f6p+2"), ("0x1.e1f30ap-23", "0x1.e1f306p-2"))])
+@pytest.mark.parametrize("f", [dict(), dict(k=2), dict(k=9), dict(p=0.6), dict(m=0.3), dict(k=8, p=0.8, m=0.05)])
+def test_bins_next_to_the_end_of_fp32_fractions(T, l, f):
+    """Neighbouring logits on both sides of 8 l / T = 2^24, in one part of the vocabulary and in several."""
+    near = (np.array(l, np.float32).view(np.uint32) + np.arange(-6, 7, dtype=np.int64)).astype(np.uint32).view(np.float32)
+    rows = torch.full((4, 40000), float(l) - 1.0)
+    rng = np.random.default_rng(1)
+    for row, (lo, hi) in zip(rows, ((0, 16000), (16384, 32000), (0, 40000), (0, 40000))):
+        at = rng.choice(np.arange(lo, hi), 13, replace=False)
+        row[torch.from_numpy(at)] = torch.from_numpy(near)
+    rows[3][rows[3] == float(near.max())] = float(l) - 1.0      # a maximum of its own
+    check(rows, np.array([0.1, 0.5, 0.77, 0.999], np.float32), T=T, **f)
