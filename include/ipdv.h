@@ -682,9 +682,9 @@ size_t ipdv_sample_logits_workspace_size(int M, int V);
  * probability zero.  Masses are fp32 exponentials (relative error about 1e-7
  * each) summed exactly; a cut or a draw closer than that to a border may fall
  * on the border's other side.  The same call repeats bit for bit.
- * T = 0 draws the first entry of the order.  Entries of -inf are never drawn.  A
- * row that holds NaN or +inf, or nothing above -inf, and a row whose T is
- * negative or NaN, gets token -1 and logp NaN.
+ * T = 0 draws the first entry of the order; 0 < T < 2^-124 is taken as 2^-124.
+ * Entries of -inf are never drawn.  A row that holds NaN or +inf, or nothing
+ * above -inf, and a row whose T is negative or NaN, gets token -1 and logp NaN.
  *
  * logits [M, V] (dtype), row_stride elements from one row to the next (>= V);
  * u [M] float in [0, 1); temperature, top_p, min_p [M] float and top_k [M]

@@ -85,6 +85,10 @@ __device__ __forceinline__ ChunkRec chunk_rec(const SampleLogitsLaunch& p, int n
   return {hist, hist + kBins, start, reinterpret_cast<ChunkHead*>(start + kBins)};
 }
 
+// Temperatures below act as this: bins and slopes per unit of logit, 8 / T and
+// log2(e) / T, stay finite in fp32.
+constexpr float kLeastTemp = 0x1p-124f;
+
 // A row's parameters; greedy (T = 0) is the top entry at temperature 1.
 struct Row {
   double width;   // y = l * width
@@ -99,7 +103,7 @@ __device__ __forceinline__ Row row_of(const SampleLogitsLaunch& p, int m) {
   Row r;
   const float t = p.temperature ? p.temperature[m] : 1.f;
   r.bad = !(t >= 0.f);
-  r.temp = t > 0.f ? (double)t : 1.0;
+  r.temp = t > 0.f ? (double)fmaxf(t, kLeastTemp) : 1.0;
   r.width = kWidth / r.temp;
   r.hi = (float)r.width;
   r.lo = (float)(r.width - (double)r.hi);
@@ -881,7 +885,7 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
   float from_edge;
   floor_y(r, mx, &from_edge);
   constexpr float kPerBin = (float)(1.4426950408889634 / kWidth);
-  const float slope = fminf((float)(1.4426950408889634 / r.temp), __FLT_MAX__), offset = (from_edge - 1.f) * kPerBin;
+  const float slope = (float)(1.4426950408889634 / r.temp), offset = (from_edge - 1.f) * kPerBin;
   auto weight = [&](float l, int v) -> float {
     const float x = fmaf(fmaxf(l - mx, -__FLT_MAX__), slope, offset);
     const bool kept = l > l_cut || (l == l_cut && v <= v_cut);

@@ -25,3 +25,17 @@ def test_bins_next_to_the_end_of_fp32_fractions(T, l, f):
         row[torch.from_numpy(at)] = torch.from_numpy(near)
     rows[3][rows[3] == float(near.max())] = float(l) - 1.0      # a maximum of its own
     check(rows, np.array([0.1, 0.5, 0.77, 0.999], np.float32), T=T, **f)
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("T", [1e-45, 1e-39, 2.3e-38, 2.0 ** -124, 1e-37])
+@pytest.mark.parametrize("f", [dict(), dict(k=5), dict(p=0.9), dict(m=0.2), dict(k=3, p=0.7, m=0.5)])
+def test_least_temperatures_with_a_maximum_of_zero(dt, T, f):
+    """Log-probs of a certain token, maxima subtracted, and rows of zeros: 8 / T passes the largest fp32 number below 2.35e-38."""
+    l = -gauss(4, 40000, dt).abs() - 0.5
+    l[0] = -INF
+    l[0, 39000] = 0.0
+    l[1, 20001] = -0.0
+    l[2, [17000, 33000, 39999]] = 0.0
+    l[3] = 0.0
+    check(l, np.array([0.5, 0.0, 0.4, 0.7], np.float32), T=T, **f)
