@@ -359,8 +359,9 @@ __device__ __forceinline__ T block_scan(T v, T* s_part) {
   return before + incl - v;
 }
 
-// Two at once.
-__device__ __forceinline__ int block_scan(int a, double b, int* part_a, double* part_b, double* before_b) {
+// Two at once; the doubles also with this thread's, which is the next thread's
+// sum before it to the last bit.
+__device__ __forceinline__ int block_scan(int a, double b, int* part_a, double* part_b, double* before_b, double* end_b) {
   const int lane = lane_id(), w = threadIdx.x >> 6;
   const int incl_a = wave_incl_scan_i(a);
   double incl_b = b;
@@ -383,7 +384,9 @@ __device__ __forceinline__ int block_scan(int a, double b, int* part_a, double* 
       before_a += part_a[i];
       sum += part_b[i];
     }
-  *before_b = sum + incl_b - b;
+  const double left = __shfl_up(incl_b, 1, kWave);
+  *before_b = lane > 0 ? sum + left : sum;
+  *end_b = sum + incl_b;
   return before_a + incl_a - a;
 }
 
@@ -408,7 +411,8 @@ struct Shared {
   u64 part_u[kWaves];
   double part_d[kWaves];
   int part_i[kWaves];
-  int n, bin, found, chunk, token, bad;
+  int n, found, chunk, token, bad;
+  int bin[2];                       // where top-k's and top-p's cuts lie
   unsigned from_logits;             // chunks whose list stops above the bin looked for
   float low, high;                  // a bin's logits: [low, high)
   u64 cut, lo, hi, above_mass;
@@ -764,13 +768,14 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
     __syncthreads();
     const int count = tid < kBins ? S.count[t] : 0;
     const double mass = tid < kBins ? (double)S.mass[t] * S.edge[t] * kUnitMass : 0.0;
-    double mass_before;
-    const int count_before = block_scan(count, mass, S.part_i, S.part_d, &mass_before);
+    double mass_before, mass_end;
+    const int count_before = block_scan(count, mass, S.part_i, S.part_d, &mass_before, &mass_end);
     if (tid < kBins) {
       S.before[t] = mass_before;
       S.count_before[t] = count_before;
     }
     if (tid == kBins - 1) S.all = mass_before;         // the last bin has none
+    if (tid < 2) S.bin[tid] = kBins - 1;
     __syncthreads();
     RowWork<DT, VEC> work{p, S, r, m, n_chunks, tid, top};
     double kept = S.all;            // mass of what the filters so far leave
@@ -792,18 +797,12 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
       if (pass == 0 ? r.k == 0 : pass == 1 ? r.top_p == 1.f : r.min_p == 0.f) continue;
       const Need need{pass == 0, r.k, (double)r.top_p * kept};
       if (pass == 2 && bound <= cut) continue;
-      if (tid == 0) S.bin = -1;
+      // the first bin whose end meets the need, of those that hold entries
+      const u64 meets = __ballot(pass < 2 && count > 0 && (pass == 0 ? count_before + count >= r.k : mass_end >= need.mass));
+      if (lane == 0 && meets) atomicMin(&S.bin[pass], w * kWave + __ffsll((long long)meets) - 1);
       __syncthreads();
-      if (pass == 2) {
-        if (tid == 0) S.bin = bin_min;
-      } else if (count > 0 && (pass == 0 ? count_before < r.k && count_before + count >= r.k
-                                         : mass_before + mass >= need.mass &&
-                                               (mass_before < need.mass || count_before == 0))) {
-        S.bin = tid;                // where the need is met; a need of nothing, in the first
-      }
-      __syncthreads();
-      const int bin = S.bin;
-      if (bin < 0 || bin == kBins - 1) continue;       // nothing that counts is cut
+      const int bin = pass < 2 ? S.bin[pass] : bin_min;
+      if (bin == kBins - 1) continue;                  // nothing that counts is cut
       if (pass < 2 && bin > bin_min && (pass == 1 || r.top_p == 1.f)) continue;      // min-p cuts above it
       if (tid < kMaxChunks) S.in_bin[tid] = 0;         // record's, from here on the last cut's
       if (bin != bin_cut) held = work.gather(bin);

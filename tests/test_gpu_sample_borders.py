@@ -39,3 +39,27 @@ def test_least_temperatures_with_a_maximum_of_zero(dt, T, f):
     l[2, [17000, 33000, 39999]] = 0.0
     l[3] = 0.0
     check(l, np.array([0.5, 0.0, 0.4, 0.7], np.float32), T=T, **f)
+
+
+def test_a_need_between_two_sums():
+    """One entry of logit 0, k of -0.1 and n of another, top-p a hair (2e-12) above
+    the mass of the first k + 1: the next entry is kept too, and no more.  The mass
+    before the last bin, got by taking that bin off the sum up to it, is as much
+    above the sum up to the bin before."""
+    cases = [(-0.24, 2, 257117, "0x1.d21f4cp-17"), (-0.13, 2, 226936, "0x1.d91a0cp-17"), (-0.2, 1, 171842, "0x1.c649e0p-17"),
+             (-0.2, 1, 221202, "0x1.60eaecp-17"), (-0.2, 1, 117596, "0x1.4bec00p-16"), (-0.2, 1, 241385, "0x1.4368cap-17"),
+             (-0.13, 2, 242759, "0x1.ba43f4p-17"), (-0.2, 1, 102910, "0x1.7b49d8p-16")]
+    u = np.array([0.0, 0.3, 0.6, 0.95], np.float32)
+    l = torch.full((len(cases), 262144), -INF)
+    for row, (x, k, n, _) in zip(l, cases):
+        row[200: 200 + n] = x
+        row[50: 50 + k] = -0.1
+        row[20] = 0.0
+    p = np.array([float.fromhex(c[3]) for c in cases], np.float32)
+    token, logp = call(l.repeat_interleave(4, 0), np.tile(u, len(cases)), p=p.repeat(4))
+    for i, (x, k, _, _) in enumerate(cases):
+        v = np.array([20, *range(50, 50 + k), 200])
+        w = np.exp([0.0] + [-0.1] * k + [x])
+        at = np.searchsorted(np.cumsum(w) / w.sum(), u, side="right")
+        assert (token[4 * i: 4 * i + 4] == v[at]).all(), (i, token[4 * i: 4 * i + 4])
+        assert np.abs(logp[4 * i: 4 * i + 4] - np.log(w / w.sum())[at]).max() < 1e-5
