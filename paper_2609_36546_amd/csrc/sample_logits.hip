@@ -849,7 +849,7 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
       S.chunk = pick;
       S.rest = goal - (incl - mine);
       S.all = all;
-      S.token = -1;
+      S.token = kThreads;
       S.found = 0;
     }
   }
@@ -895,18 +895,18 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
   for (int i = 0; i < PER; ++i) part += weight(x[i], v0 + i);
   const double mine = (double)part;
   const double pre = block_scan<double>(mine, S.part_d);
-  if (mine > 0.0) {
-    atomicMax(&S.found, tid + 1);
-    if (pre <= goal && pre + mine > goal) S.token = tid;
-  }
+  const u64 some = __ballot(mine > 0.0), past = __ballot(mine > 0.0 && pre + mine > goal);
+  if (lane == 0 && some) atomicMax(&S.found, w * kWave + 63 - __clzll((long long)some));
+  if (lane == 0 && past) atomicMin(&S.token, w * kWave + __ffsll((long long)past) - 1);
   __syncthreads();
-  // One thread has it; rounding, or u at or above 1, leave it to the last that
-  // holds some.  A lane per entry finds which.
-  if (tid == (S.token >= 0 ? S.token : S.found - 1)) S.rest = goal - pre;
+  // The first thread whose end passes the goal has it; rounding, or u at or above
+  // 1, leave it to the last that holds some.  A lane per entry finds which.
+  const int who = S.token < kThreads ? S.token : S.found;
+  if (tid == who) S.rest = goal - pre;
   __syncthreads();
   if (w == 0) {
     static_assert(PER <= kWave, "a lane per entry");
-    const int v = S.chunk * kChunk + max(S.token >= 0 ? S.token : S.found - 1, 0) * PER + lane;
+    const int v = S.chunk * kChunk + who * PER + lane;
     const float l = lane < PER && v < p.V ? logit<DT>(p, m, v) : -INFINITY;
     const double one = (double)weight(l, v);
     double incl = one;

@@ -63,3 +63,17 @@ def test_a_need_between_two_sums():
         at = np.searchsorted(np.cumsum(w) / w.sum(), u, side="right")
         assert (token[4 * i: 4 * i + 4] == v[at]).all(), (i, token[4 * i: 4 * i + 4])
         assert np.abs(logp[4 * i: 4 * i + 4] - np.log(w / w.sum())[at]).max() < 1e-5
+
+
+def test_a_uniform_between_two_sums():
+    """A first entry of e^-27.7, nothing beside it, and zeros behind: uniforms next to
+    its share fall on it or on the first zero, which is the next that holds mass."""
+    V, M = 16384, 512
+    l = torch.zeros(1, V)
+    l[0, :32] = -INF
+    l[0, 0] = -27.7
+    share = np.exp(-27.7) / (V - 32 + np.exp(-27.7))
+    u = (share * (1 + np.linspace(-0.02, 0.02, M))).astype(np.float32)
+    token, _ = call(l.expand(M, V).contiguous(), u)
+    assert set(token) == {0, 32}
+    assert (np.diff(token) >= 0).all() and abs(u[np.argmax(token)] / share - 1) < 1e-4
