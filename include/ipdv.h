@@ -543,7 +543,8 @@ int source_split_kl(int M, int K,
 #define IPDV_ROPE_LINEAR 1   /* f_p / factor: positions interpolated */
 #define IPDV_ROPE_NTK 2      /* base * factor^(rot/(rot-2)): the lowest frequency is divided by factor */
 #define IPDV_ROPE_YARN 3     /* f_p / factor where a pair turns less than beta_slow times over
-                                original_len, f_p where more than beta_fast times, a ramp over p between */
+                                original_len, f_p where more than beta_fast times, a ramp over p between (its
+                                ends, rounded outwards to whole p, lie within 0 .. rot - 1) */
 
 /*
  * ipdv_rope_inv_freq -- the inverse frequencies of rope_window for a head of

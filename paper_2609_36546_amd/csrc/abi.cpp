@@ -487,17 +487,19 @@ int ipdv_rope_inv_freq(int rot, double base, int kind, double factor, int origin
   auto pair_of = [&](double turns) {
     return rot * std::log(original_len / (2.0 * M_PI * turns)) / (2.0 * std::log(base));
   };
+  // The ramp's ends.  The upper one may lie behind the last pair, which then turns
+  // more than beta_slow times and is not divided by the whole factor.
   double lo = 0.0, hi = 0.0;
   if (kind == IPDV_ROPE_YARN) {
     lo = std::max(0.0, std::floor(pair_of(beta_fast)));
-    hi = std::min(n - 1.0, std::ceil(pair_of(beta_slow)));
+    hi = std::min(rot - 1.0, std::ceil(pair_of(beta_slow)));
   }
   for (int p = 0; p < n; ++p) {
     double f = std::pow(base, -2.0 * p / rot);
     if (kind == IPDV_ROPE_LINEAR) {
       f /= factor;
     } else if (kind == IPDV_ROPE_YARN) {
-      const double ramp = std::min(1.0, std::max(0.0, (p - lo) / std::max(hi - lo, 1e-3)));
+      const double ramp = p >= hi ? 1.0 : p <= lo ? 0.0 : (p - lo) / (hi - lo);
       f = f / factor * ramp + f * (1.0 - ramp);
     }
     inv_freq[p] = (float)f;
