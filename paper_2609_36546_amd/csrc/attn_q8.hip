@@ -611,7 +611,7 @@ __device__ __forceinline__ bool deal(const Q8Params& a, Line& line, Deal& d, con
   if (tid == 0) d.above[Deal::kClasses] = items;
   __syncthreads();
   // A lane looks up one place: of this workgroup, of the round's first and of its last.
-  const int xcd = grid & 7 ? blockIdx.x : (blockIdx.x & 7) * (grid >> 3) + (blockIdx.x >> 3);
+  const int xcd = (blockIdx.x & 7) * (grid >> 3) + (blockIdx.x >> 3);
   const int round = lane / 3, who = lane % 3, p = who == 0 ? xcd : who == 1 ? 0 : grid - 1;
   const int k = round * grid + (round & 1 ? grid - 1 - p : p);
   int cls = 0, hi = Deal::kClasses;                 // above[cls] <= k < above[hi]
@@ -661,7 +661,8 @@ __device__ __forceinline__ bool begin_walk(const Q8Params& a, Line& line, const 
                                            Walk<false>& c) {
   const long n = spans(total, parts, gridDim.x);
   // Neighbouring spans to one XCD (workgroups go to the 8 XCDs in turn): a
-  // prompt's items of one head then find its keys in one L2.
+  // prompt's items of one head then find its keys in one L2.  The grid is a
+  // multiple of 8, so each of the 8 has workgroups for its `each` spans.
   const int each = (int)((n + 7) / 8), w = (int)(blockIdx.x & 7) * each + (int)(blockIdx.x >> 3);
   if ((int)(blockIdx.x >> 3) >= each || w >= n || total == 0) return false;
   const long p0 = span_start(total, n, w), p1 = span_start(total, n, w + 1);
@@ -1165,11 +1166,14 @@ Q8Plan plan_of(int n_seq, int Hq, int Hkv, int max_q, bool bf16) {
   p.rg = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   p.item_rows = 16 * p.qt * p.rg;
   p.parts = p.rg == 1 ? 4 : 2;
-  p.grid = 2 * device_cus();                        // as many as are resident
+  p.grid = attn_q8_grid(device_cus());
   return p;
 }
 
 }  // namespace
+
+// As many workgroups as are resident, alike on every XCD: the same number each.
+int attn_q8_grid(int cus) { return std::max(8, 2 * cus / 8 * 8); }
 
 size_t attn_q8_workspace(int n_seq, int Hq, int Hkv, int D, int max_q) {
   size_t most = 0;              // either type

@@ -234,6 +234,7 @@ struct AttnQ8Launch {
   void* workspace;
 };
 
+int attn_q8_grid(int cus);     // workgroups on so many compute units: a multiple of 8
 size_t attn_q8_workspace(int n_seq, int Hq, int Hkv, int D, int max_q);
 hipError_t launch_attn_q8(const AttnQ8Launch& L, hipStream_t st);
 
