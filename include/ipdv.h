@@ -623,8 +623,8 @@ int kv_append_q8(const void* k_new, int64_t k_row_stride, const void* v_new, int
 /*
  * kv_read_q8 -- rows of the 8-bit cache as values: positions L_b + i, i < k_b,
  * of every handled sequence to rows cu_q[b] + i of k_out and v_out [T, Hkv, D]
- * (dense, dtype).  With ctx_lens = 0 and the cached lengths in cu_q, whole
- * sequences.  An e4m3 value times its scale is exact in fp32, and in bf16 down
+ * (dense, dtype; T at least where the last handled window ends).  With ctx_lens
+ * = 0 and the cached lengths in cu_q, whole sequences.  An e4m3 value times its scale is exact in fp32, and in bf16 down
  * to 2^-133 (below, it is rounded); rows of scale byte 255 are NaN.  The other
  * arguments, requirements and errors are those of kv_append_q8.
  */

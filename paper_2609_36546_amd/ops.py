@@ -199,10 +199,13 @@ def attn_workspace_size(n_seq, Hq, Hkv, D, max_q, max_pages, page_size) -> int:
 
 
 def check_page_table(page_table, ctx_lens, cu_q, max_q: int, page_size: int, num_pages: int,
-                     seq_ids=None, n_seq: Optional[int] = None):
+                     seq_ids=None, n_seq: Optional[int] = None, rows: Optional[int] = None,
+                     writes: bool = True):
     """ipdv_check_page_table on host copies of the arrays (tensors on any
     device, or numpy arrays).  Raises IpdvError naming the first contract
-    violation; returns None when the table is valid."""
+    violation; returns None when the table is valid.  rows: the rows that the
+    window tensors hold, which the handled windows must not pass.  writes=False
+    is for calls that only read the pages: windows may share them."""
     import numpy as np
 
     def host(x):
@@ -217,11 +220,25 @@ def check_page_table(page_table, ctx_lens, cu_q, max_q: int, page_size: int, num
         raise ValueError("page_table must be [B, maxp] and cu_q [B+1]")
     if n_seq is None:
         n_seq = B if sid is None else sid.shape[0]
+    ids = np.arange(n_seq) if sid is None else sid[:n_seq]
+    ids = ids[(ids >= 0) & (ids < B)]               # others are named by the library
+    k = np.diff(cu.astype(np.int64))
+    if not writes and B > 0 and cu[0] == 0 and (k >= 0).all() and (ctx[ids] >= 0).all() and (k[ids] <= max_q).all():
+        # the same positions with no window among them
+        end = ctx.astype(np.int64) + k
+        ctx = np.ascontiguousarray(np.minimum(end, 2 ** 31 - 1).astype(np.int32))
+        cu_read = np.zeros(B + 1, np.int32)
+    else:
+        cu_read = cu
     p = lambda a: None if a is None else a.ctypes.data_as(ctypes.c_void_p)
     bad = ctypes.c_int32(-1)
-    st = lib().ipdv_check_page_table(p(pt), B, pt.shape[1], p(ctx), p(cu), p(sid), n_seq, max_q,
+    st = lib().ipdv_check_page_table(p(pt), B, pt.shape[1], p(ctx), p(cu_read), p(sid), n_seq, max_q,
                                      page_size, num_pages, ctypes.byref(bad))
     _check("ipdv_check_page_table", st)
+    if rows is not None:
+        for b in ids:
+            if k[b] > 0 and cu[b + 1] > rows:
+                raise IpdvError("check_page_table", -1, f"sequence {b}: rows {cu[b]} .. {cu[b + 1] - 1} of {rows}")
 
 
 def verify_attn_paged(q, k_new, v_new, k_cache, v_cache, page_table, ctx_lens, cu_q,
@@ -806,7 +823,7 @@ def kv_append_q8(k_new, v_new, cache: Q8Cache, page_table, ctx_lens, cu_q, max_q
         raise ValueError("k_new and v_new must be [T,Hkv,D] of the cache's heads")
     if validate:
         check_page_table(page_table, ctx_lens, cu_q, max_q, cache.page_size, cache.num_pages,
-                         seq_ids=seq_ids, n_seq=n_seq)
+                         seq_ids=seq_ids, n_seq=n_seq, rows=T)
     if T == 0:
         n_seq = 0
     st = lib().kv_append_q8(kp, ks, vp, vs, cache.k.data_ptr(), cache.v.data_ptr(),
@@ -816,10 +833,14 @@ def kv_append_q8(k_new, v_new, cache: Q8Cache, page_table, ctx_lens, cu_q, max_q
 
 
 def kv_read_q8(cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int, rows: int, seq_ids=None,
-               n_seq: Optional[int] = None, dtype=torch.bfloat16, k_out=None, v_out=None):
+               n_seq: Optional[int] = None, dtype=torch.bfloat16, k_out=None, v_out=None,
+               validate: bool = False):
     """The values that positions ctx_lens[b] + i stand for, as rows cu_q[b] + i
     of two [rows,Hkv,D] tensors (see include/ipdv.h); with ctx_lens zero and
-    the cached lengths in cu_q, whole sequences.  Returns (k, v)."""
+    the cached lengths in cu_q, whole sequences.  rows is cu_q's last entry, or
+    at least where the last handled window ends: the call does not look at cu_q
+    and would write behind the outputs.  validate=True checks that and the page
+    table on host copies first.  Returns (k, v)."""
     dev = cache.device
     code = _dtype_code(dtype)
     ctx, cu, ids, n_seq, B = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
@@ -835,6 +856,9 @@ def kv_read_q8(cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int, rows: int
         k_out = torch.empty(*shape, dtype=dtype, device=dev)
     if v_out is None:
         v_out = torch.empty_like(k_out)
+    if validate:
+        check_page_table(page_table, ctx_lens, cu_q, max_q, cache.page_size, cache.num_pages,
+                         seq_ids=seq_ids, n_seq=n_seq, rows=shape[0], writes=False)
     if shape[0] == 0:
         n_seq = 0
     st = lib().kv_read_q8(cache.k.data_ptr(), cache.v.data_ptr(), cache.scale.data_ptr(), table,
@@ -850,10 +874,11 @@ def attn_q8_workspace_size(n_seq, Hq, Hkv, D, max_q) -> int:
 
 def verify_attn_q8(q, cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int, seq_ids=None,
                    n_seq: Optional[int] = None, scale: Optional[float] = None, out=None,
-                   workspace=None):
+                   workspace=None, validate: bool = False):
     """Causal GQA attention of the window rows q [T,Hq,D] (bf16 or fp32; rows
     may be strided) over the 8-bit cache, which already holds the window (see
-    include/ipdv.h).  Returns out [T,Hq,D]."""
+    include/ipdv.h).  validate=True first runs check_page_table on host copies.
+    Returns out [T,Hq,D]."""
     dev, dt = q.device, q.dtype
     code = _dtype_code(dt)
     qp, qs, shape = _rows(q, "q", dt, dev, 3)
@@ -871,6 +896,9 @@ def verify_attn_q8(q, cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int, se
         _need(out, "out", dt, dev, 3)
         if out.shape != shape:
             raise ValueError("out must have q's shape")
+    if validate:
+        check_page_table(page_table, ctx_lens, cu_q, max_q, cache.page_size, cache.num_pages,
+                         seq_ids=seq_ids, n_seq=n_seq, rows=T, writes=False)
     if T == 0:
         n_seq = 0
     if workspace is None:
