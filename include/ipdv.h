@@ -645,6 +645,10 @@ size_t ipdv_attn_q8_workspace_size(int n_seq, int Hq, int Hkv, int D, int max_q)
  * (kv_append_q8 on the same stream).  A NaN row of the cache makes the rows
  * that see it NaN, and no others; slots behind a sequence's last position may
  * hold anything.
+ * Sums, maxima and the normalisation are fp32.  A bf16 call rounds each
+ * probability to bf16 once, before its product with V, and holds a query's
+ * channels to 8 bits down to 2^-14 of its largest, below that to 2^-21 of the
+ * largest; an fp32 call keeps 24 bits of both.
  *
  * q [T, Hq, D] (dtype), q_row_stride elements from one row to the next (>= Hq *
  * D); out [T, Hq, D] dense (dtype).  bf16 and fp32, D in {64, 128}.  The pages
@@ -681,8 +685,11 @@ size_t ipdv_sample_logits_workspace_size(int M, int V);
  *   logp[m]  = ln of token[m]'s share of the kept mass (optional; NULL)
  * Entries with less than e^-31.9 of the largest probability count as of
  * probability zero.  Masses are fp32 exponentials (relative error about 1e-7
- * each) summed exactly; a cut or a draw closer than that to a border may fall
- * on the border's other side.  The same call repeats bit for bit.
+ * each), summed exactly for the cuts and for the part of 16384 entries that the
+ * draw falls in; inside it 32 neighbours at a time are summed in fp32, and an entry
+ * of a small mass m (the largest 1) is off by 2^-24 |ln m| of it, so by less than
+ * 1e-7 of the row's.  A cut or a draw closer than that to a border may fall on the
+ * border's other side.  The same call repeats bit for bit.
  * T = 0 draws the first entry of the order; 0 < T < 2^-124 is taken as 2^-124.
  * Entries of -inf are never drawn.  A row that holds NaN or +inf, or nothing
  * above -inf, and a row whose T is negative or NaN, gets token -1 and logp NaN.

@@ -10,8 +10,9 @@
 // packed position-major into tiles of 16.  A wave holds QT tiles and walks
 // blocks of 64 keys, four 16-slot units:
 //
-//   S^T[64 keys x 16 rows] = K . Q^T   v_mfma_f32_16x16x32_bf16, A = key rows
-//   O^T[D x 16 rows] += V^T . P^T      A = value channels, B = P^T in place
+//   S^T[64 keys x 16 rows] = K . Q^T   A = key rows: v_mfma_scale_f32_16x16x128_f8f6f4 in
+//                                      bf16 calls, v_mfma_f32_16x16x32_bf16 in fp32 ones
+//   O^T[D x 16 rows] += V^T . P^T      v_mfma_f32_16x16x32_bf16, A = value channels, B = P^T in place
 //
 // The keys' tile t has MFMA row 4 u + e at unit u, slot 4 t + e.  A lane (row
 // c16, group j) then ends up with the scores of exactly the 16 slots of unit j,
@@ -21,12 +22,13 @@
 //
 // Precision.  The bf16 call's scores: a query's channels become two e4m3
 // numbers each, the first with the scale of the largest, the second what that
-// leaves (8 bits in all, as bf16 has, down to 2^-22 of the largest), and
-// the keys go into the scaled fp8 products as they lie in the cache, with their
+// leaves: 8 bits in all, as bf16 has, down to 2^-14 of the largest, where the first
+// goes subnormal; below, 2^-21 of the largest.  (Beside a channel of 10^5 one of 1
+// is off by up to 3%, beside one of 10^4 by nothing.)  The keys go into the scaled fp8 products as they lie in the cache, with their
 // own scale: nothing is rounded or converted on the way.  Values times
 // probabilities: an e4m3 value is exact in bf16, its scale goes into the
 // probability, which is rounded to bf16 once, as the bf16 cache's attention
-// does.  The fp32 call: keys and values exact in bf16 (the key's scale in the
+// does (a second bf16 term would double the value products).  The fp32 call: keys and values exact in bf16 (the key's scale in the
 // conversion), queries and probabilities split into three bf16 terms (24 bits).
 // Sums and the running maximum are fp32.
 //

@@ -8,10 +8,10 @@
 // Pairs are channels (p, p + R/2) or (2p, 2p + 1) of the first R channels; the
 // others pass through.
 //
-// Angles: position * f is exact in double (31 + 24 bits), and so is its
-// reduction to a fraction of a turn to about 1e-16 of the turns; only the
-// fraction goes to fp32.  In fp32 the angle of position 10^5 would be off by
-// 0.004.
+// Angles: position * f is exact in double below position 2^29 (29 + 24 bits) and
+// rounded to 2^-53 of itself from there on; its reduction to a fraction of a turn
+// adds 2^-52 of the turns, and only the fraction goes to fp32.  In fp32 the angle of
+// position 10^5 would be off by 0.004.
 //
 // Bound by one read and one write of the data, moved in 16-byte pieces where
 // the pairs allow it (two pieces R/2 apart, or one piece of whole pairs).  A

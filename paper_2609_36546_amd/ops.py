@@ -5,7 +5,9 @@ shape, passes raw pointers and the current HIP stream to the C ABI of the
 same name, and raises RuntimeError with the library's message on a non-OK
 status.  All arithmetic runs in the library's gfx950 kernels; there is no
 other path.  Outputs and workspaces can be passed in (to keep a call free of
-allocations) or are allocated here with torch.
+allocations) or are allocated here with torch.  No call is recorded by
+autograd, whether its inputs require gradients or not: a gradient is a call of
+its own (rope_window's with inverse=True).
 """
 from __future__ import annotations
 
@@ -729,8 +731,9 @@ def rope_window(q, k, inv_freq, ctx_lens, cu_q, max_q: int, seq_ids=None,
 
     q [T,Hq,D], k [T,Hkv,D] (bf16 or fp32; rows may be strided), inv_freq
     [rot/2] float32, ctx_lens [B], cu_q [B+1], seq_ids [n] int32 or None.
-    inverse=True turns back: the gradient of q and k.  q_out / k_out may be q /
-    k (in place).  Returns (q_out, k_out)."""
+    inverse=True turns back: the gradient of q and k from that of the outputs
+    (autograd does not record the call).  q_out / k_out may be q / k (in place).
+    Returns (q_out, k_out)."""
     dev, dt = q.device, q.dtype
     code = _dtype_code(dt)
     qp, qs, q_shape = _rows(q, "q", dt, dev, 3)

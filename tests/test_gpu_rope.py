@@ -148,3 +148,21 @@ def c_rope(**kw):
 def test_rope_refusals(kw, status):
     assert c_rope(**kw) == status
     assert (ops.lib().ipdv_last_error() != b"") == (status != 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", [ops.ROPE_HALF, ops.ROPE_INTERLEAVED])
+def test_rope_of_the_farthest_positions(layout):
+    """Odd positions whose product with a 24-bit frequency has more than 53 bits: the
+    plain form rounds it the same; the library's step to turns adds a constant's and
+    a product's rounding, 2^-53 of the angle each."""
+    windows = [(2 ** 29 + 12345, 3), (2 ** 30 + 1, 2), (2 ** 31 - 17, 9), (2 ** 24 + 3, 1)]
+    q, k, ctx, cu, pos = batch(windows, F32, 3, 2, 64)
+    f, _ = ops.rope_inv_freq(64, 1e4)
+    f[3] = 0.70710677
+    a, b = ops.rope_window(q, k, f.cuda(), ctx, cu, 9, layout=layout)
+    angle = 2.0 ** -52 * pos[:, None, None] * float(f.max())
+    for x, y in ((q, a), (k, b)):
+        want = ref.rope(f64(x), pos, f.numpy(), layout)
+        size = 2 * np.abs(f64(x)).max(-1, keepdims=True)
+        assert (np.abs(f64(y) - want) <= bound(want, f64(x), F32, 1.0) + angle * size).all()
