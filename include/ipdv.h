@@ -645,10 +645,10 @@ size_t ipdv_attn_q8_workspace_size(int n_seq, int Hq, int Hkv, int D, int max_q)
  * (kv_append_q8 on the same stream).  A NaN row of the cache makes the rows
  * that see it NaN, and no others; slots behind a sequence's last position may
  * hold anything.
- * Sums, maxima and the normalisation are fp32.  A bf16 call rounds each
- * probability to bf16 once, before its product with V, and holds a query's
- * channels to 8 bits down to 2^-14 of its largest, below that to 2^-21 of the
- * largest; an fp32 call keeps 24 bits of both.
+ * Sums, maxima and the normalisation are fp32.  A bf16 call holds a probability
+ * to 16 bits before its product with V where max_q * Hq / Hkv is at most 16, else
+ * rounds it to bf16 once; and a query's channels to 8 bits down to 2^-14 of its
+ * largest, below that to 2^-21 of the largest.  An fp32 call keeps 24 bits of both.
  *
  * q [T, Hq, D] (dtype), q_row_stride elements from one row to the next (>= Hq *
  * D); out [T, Hq, D] dense (dtype).  bf16 and fp32, D in {64, 128}.  The pages

@@ -24,13 +24,17 @@
 // numbers each, the first with the scale of the largest, the second what that
 // leaves: 8 bits in all, as bf16 has, down to 2^-14 of the largest, where the first
 // goes subnormal; below, 2^-21 of the largest.  (Beside a channel of 10^5 one of 1
-// is off by up to 3%, beside one of 10^4 by nothing.)  The keys go into the scaled fp8 products as they lie in the cache, with their
-// own scale: nothing is rounded or converted on the way.  Values times
-// probabilities: an e4m3 value is exact in bf16, its scale goes into the
-// probability, which is rounded to bf16 once, as the bf16 cache's attention
-// does (a second bf16 term would double the value products).  The fp32 call: keys and values exact in bf16 (the key's scale in the
-// conversion), queries and probabilities split into three bf16 terms (24 bits).
-// Sums and the running maximum are fp32.
+// is off by up to 3%, beside one of 10^4 by nothing.)  The keys go into the scaled
+// fp8 products as they lie in the cache, with their own scale: nothing is rounded or
+// converted on the way.  Values times probabilities: an e4m3 value is exact in bf16,
+// its scale goes into the probability.  With one row group a probability is two bf16
+// terms (16 bits; the second costs 1%, the call being bound by its bytes), else it
+// is rounded to bf16 once, as the bf16 cache's attention does (a second term: windows
+// of eight 89 to 100 us, prompts 94 to 112; without it the outputs' error, the half
+// step of bf16 included, is 0.0021 to 0.0023 instead of 0.0017).  The fp32 call: keys
+// and values exact in bf16 (the key's scale in the conversion), queries and
+// probabilities split into three bf16 terms (24 bits).  Sums and the running maximum
+// are fp32.
 //
 // Work split.  All steps (a step: the keys that a workgroup takes at once) of
 // all items (an item: one row group of one (sequence, KV head)) form one line,
@@ -296,9 +300,9 @@ __device__ __forceinline__ void scores(const B& f, const Queries<D, QT, NS>& Q, 
   }
 }
 
-// The block's probabilities and values.  `tail`: some row of the wave does not
-// see every key of the block.
-template <int D, int QT, int NS>
+// The block's probabilities, in PT bf16 terms, and values.  `tail`: some row of the
+// wave does not see every key of the block.
+template <int D, int QT, int PT>
 __device__ __forceinline__ void attend(uint4 (&v)[D / 16], uint4 vscale, floatx4 (&s)[QT][4], float c, bool tail, int t0, int n_keys,
                                        const int (&qlimit)[QT], floatx4 (&acc)[QT][D / 16], float (&m_run)[QT],
                                        float (&l_run)[QT]) {
@@ -355,7 +359,7 @@ __device__ __forceinline__ void attend(uint4 (&v)[D / 16], uint4 vscale, floatx4
       for (int dt = 0; dt < D / 16; ++dt) acc[q][dt] *= alpha;
     }
   }
-  bf16x8 pf[NS][QT][2];
+  bf16x8 pf[PT][QT][2];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {           // slot i of unit j
     const float vsc = __uint_as_float(((word(vscale, i >> 2) >> (8 * (i & 3))) & 255u) << 23);
@@ -363,24 +367,31 @@ __device__ __forceinline__ void attend(uint4 (&v)[D / 16], uint4 vscale, floatx4
     for (int q = 0; q < QT; ++q) {
       const float p = fast_exp2(fmaf(s[q][i >> 2][i & 3], c, -m_use[q]));
       l_run[q] += p;
-      __bf16 t[NS];
-      split<NS>(p * vsc, t);
+      __bf16 t[PT];
+      split<PT>(p * vsc, t);
 #pragma unroll
-      for (int n = 0; n < NS; ++n) pf[n][q][i >> 3][i & 7] = t[n];
+      for (int n = 0; n < PT; ++n) pf[n][q][i >> 3][i & 7] = t[n];
     }
   }
   __builtin_amdgcn_s_setprio(1);           // matrix work before the other wave's softmax: eight prompts 105 to 98 us
+  constexpr int AT = PT == 2 ? 2 : 1;      // channel tiles at once: of one, four products would wait for one another
 #pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt) {
-    const uint4 w = v[dt];
+  for (int dt = 0; dt < D / 16; dt += AT) {
 #pragma unroll
     for (int st = 0; st < 2; ++st) {       // slots 8 st .. 8 st + 7 of unit j
-      const bf16x8 vf = cvt8(st ? w.z : w.x, st ? w.w : w.y, 1.0f);
+      bf16x8 vf[AT];
 #pragma unroll
-      for (int n = 0; n < NS; ++n)
+      for (int x = 0; x < AT; ++x) {
+        const uint4 w = v[dt + x];
+        vf[x] = cvt8(st ? w.z : w.x, st ? w.w : w.y, 1.0f);
+      }
 #pragma unroll
-        for (int q = 0; q < QT; ++q)
-          acc[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][q][st], acc[q][dt], 0, 0, 0);
+      for (int n = 0; n < PT; ++n)
+#pragma unroll
+        for (int x = 0; x < AT; ++x)
+#pragma unroll
+          for (int q = 0; q < QT; ++q)
+            acc[q][dt + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[x], pf[n][q][st], acc[q][dt + x], 0, 0, 0);
     }
   }
   __builtin_amdgcn_s_setprio(0);
@@ -898,7 +909,7 @@ __global__ __launch_bounds__(256, 2) void attn_q8_keys_kernel(Q8Params a) {
         __builtin_amdgcn_sched_barrier(0);          // or the loads move up, into registers of their own
         if (more) load_keys<D>(a, f, (n + 1) * kBlk, units);
         __builtin_amdgcn_sched_barrier(0);
-        attend<D, QT, Rows<DT, D, QT>::NS>(f.v, f.vs, s, a.scale_log2, (n + 1) * kBlk > R.all_see, n * kBlk, R.n_keys, R.qlimit,
+        attend<D, QT, Rows<DT, D, QT>::NS == 1 ? 2 : 3>(f.v, f.vs, s, a.scale_log2, (n + 1) * kBlk > R.all_see, n * kBlk, R.n_keys, R.qlimit,
                                            R.acc, R.m_run, R.l_run);
         __builtin_amdgcn_sched_barrier(0);
         if (more) load_values<D>(a, f, (n + 1) * kBlk, units);

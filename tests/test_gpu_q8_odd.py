@@ -136,3 +136,22 @@ def test_queries_with_one_large_channel(Hq, D, k, size):
         a = slice(cu_all[b], cu_all[b + 1])
         want = ref.attention(held[cu[b]: cu[b + 1]], K[a], V[a], int(ctx[b]), D ** -0.5)
         check_rows(out[cu[b]: cu[b + 1]], want, BF16)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,ps,k", [(16, 8, 128, 16, 1), (8, 2, 64, 32, 4), (32, 2, 128, 16, 1), (3, 3, 64, 64, 5)])
+def test_probabilities_of_few_rows_keep_16_bits(Hq, Hkv, D, ps, k):
+    """bf16 calls of up to 16 rows per KV head: half a step of the result, half a step of 2^-16 of each probability (twice the
+    half step of two terms of 8 bits; an error of at most 2^-16 of sum p |V|, taken as three times the row's rms), and the
+    fp32 sums that check_rows has for fp32 calls."""
+    windows = [(1500, k), (0, k), (63, k), (64, 1)]
+    c, table, ctx, cu, pt, dctx, dcu = pool(windows, Hkv, D, ps)
+    kv = fill(c, table, ctx, cu, pt, 5)
+    q = torch.randn(int(cu[-1]), Hq, D, generator=torch.Generator().manual_seed(6)).to(BF16)
+    out = f64(ops.verify_attn_q8(q.cuda(), c, pt, dctx, dcu, k))
+    for b, (K, V) in enumerate(kv):
+        want = ref.attention(f64(q[cu[b]: cu[b + 1]]), K, V, int(ctx[b]), D ** -0.5)
+        rms = np.sqrt((want ** 2).mean(-1, keepdims=True))
+        off = np.abs(out[cu[b]: cu[b + 1]] - want)
+        tol = 2.0 ** -8 * np.abs(want) + (3 * 2.0 ** -16 + 2.0 ** -17) * rms
+        print("worst", (off / tol).max(), flush=True)
+        assert (off <= tol).all()
