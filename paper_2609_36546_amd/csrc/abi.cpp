@@ -609,6 +609,7 @@ static int kv_call(const char* what, bool append, const void* k_rows, int64_t k_
   L.page_size = page_size;
   L.log2ps = __builtin_ctz((unsigned)page_size);
   L.num_pages = num_pages;
+  L.slots = ipdv::table_slots(max_pages, page_size);
   L.dtype_bf16 = dtype == IPDV_BF16;
   hipError_t e = ipdv::launch_kv_q8(L, append, reinterpret_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return hip_fail(what, e);

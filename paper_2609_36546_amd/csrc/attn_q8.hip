@@ -92,7 +92,7 @@ struct Q8Params {
   struct SpanHead* span;   // [grid + 1]: what every span begins in; the last: the line's length
   float* part_o;       // [2 * grid][item rows][D]
   float* part_ml;      // [2 * grid][item rows][2]: maximum, sum
-  int max_pages, Hq, Hkv, G, log2g, log2ps, num_pages, n_seq, max_q;   // log2g: of G, or -1
+  int max_pages, Hq, Hkv, G, log2g, log2ps, num_pages, n_seq, max_q, slots;   // log2g: of G, or -1
   float scale_log2;
 };
 
@@ -405,7 +405,7 @@ struct Seq {
 __device__ __forceinline__ Seq seq_of(const Q8Params& a, int slot, int item_rows) {
   Seq s;
   s.b = a.seq_ids ? a.seq_ids[slot] : slot;
-  s.L = max(a.ctx_lens[s.b], 0);
+  s.L = min(max(a.ctx_lens[s.b], 0), a.slots);
   s.r0 = a.cu_q[s.b];
   s.kb = min(max(a.cu_q[s.b + 1] - s.r0, 0), a.max_q);
   s.rows = s.kb * a.G;
@@ -416,7 +416,7 @@ __device__ __forceinline__ Seq seq_of(const Q8Params& a, int slot, int item_rows
 __device__ __forceinline__ Seq same_seq_of(const Q8Params& a, int slot, int item_rows) {
   Seq s;
   s.b = a.seq_ids ? scalar(a.seq_ids)[slot] : slot;
-  s.L = max(scalar(a.ctx_lens)[s.b], 0);
+  s.L = min(max(scalar(a.ctx_lens)[s.b], 0), a.slots);
   s.r0 = scalar(a.cu_q)[s.b];
   s.kb = min(max(scalar(a.cu_q)[s.b + 1] - s.r0, 0), a.max_q);
   s.rows = s.kb * a.G;
@@ -1225,6 +1225,7 @@ hipError_t launch_attn_q8(const AttnQ8Launch& L, hipStream_t st) {
   p.num_pages = L.num_pages;
   p.n_seq = L.n_seq;
   p.max_q = L.max_q;
+  p.slots = table_slots(L.max_pages, L.page_size);
   p.scale_log2 = L.scale * 1.4426950408889634f;
   trace_begin(st);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(pl.grid), dim3(256), 0, st, p); };

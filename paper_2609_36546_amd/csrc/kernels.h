@@ -195,6 +195,13 @@ struct RopeLaunch {
 hipError_t launch_rope(const RopeLaunch& L, hipStream_t st);
 
 // ---- the 8-bit cache ----
+// Positions that a page table has slots for, which context lengths are cut at:
+// with windows below 2^27, positions stay below 2^31 whatever ctx_lens holds.
+inline int table_slots(int max_pages, int page_size) {
+  const int64_t n = (int64_t)max_pages * page_size, most = ((int64_t)1 << 31) - (1 << 28);
+  return (int)(n < most ? n : most);
+}
+
 struct KvLaunch {
   const void* k_in;            // append: rows [T, Hkv, D]
   const void* v_in;
@@ -209,7 +216,7 @@ struct KvLaunch {
   const int32_t* ctx_lens;
   const int32_t* cu_q;
   const int32_t* seq_ids;
-  int n_seq, max_q, Hkv, D, page_size, log2ps, num_pages;
+  int n_seq, max_q, Hkv, D, page_size, log2ps, num_pages, slots;
   bool dtype_bf16;
 };
 

@@ -131,7 +131,7 @@ __device__ __forceinline__ bool place(const KvLaunch& p, Place& w) {
   const int slot = sg / p.Hkv;
   w.g = sg - slot * p.Hkv;
   const int b = p.seq_ids ? p.seq_ids[slot] : slot;
-  w.L = max(p.ctx_lens[b], 0);
+  w.L = min(max(p.ctx_lens[b], 0), p.slots);
   w.r0 = p.cu_q[b];
   const int end = w.L + min(p.cu_q[b + 1] - w.r0, p.max_q);
   w.p0 = (w.L & ~(kUnit - 1)) + kUnit * (int)blockIdx.x;

@@ -155,3 +155,37 @@ def test_probabilities_of_few_rows_keep_16_bits(Hq, Hkv, D, ps, k):
         tol = 2.0 ** -8 * np.abs(want) + (3 * 2.0 ** -16 + 2.0 ** -17) * rms
         print("worst", (off / tol).max(), flush=True)
         assert (off <= tol).all()
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("Hq,k", [(4, 2), (8, 12), (32, 40)])
+def test_lengths_that_no_table_holds(dt, Hq, k):
+    """Context lengths up to the largest 32-bit number: what comes out is not specified, but every index stays in its
+    array, other sequences get what is theirs, and the walk ends with the table."""
+    windows = [(40, k), (0, k), (33, k)]
+    c, table, ctx, cu, pt, dctx, dcu = pool(windows, 2, 64, 16)
+    kv = fill(c, table, ctx, cu, pt, 5)
+    own = table[1][table[1] >= 0]
+    q = torch.randn(3 * k, Hq, 64, generator=torch.Generator().manual_seed(6)).to(dt)
+    kn = torch.randn(3 * k, 2, 64, generator=torch.Generator().manual_seed(7)).to(dt).cuda()
+    for L in (65, 4096, 2 ** 31 - 2 ** 28, 2 ** 31 - 200, 2 ** 31 - 100, 2 ** 31 - 65, 2 ** 31 - 11, 2 ** 31 - 1):
+        bad = dctx.clone()
+        bad[1] = L
+        out = torch.full_like(q, 7.0, device="cuda")
+        ops.verify_attn_q8(q.cuda(), c, pt, bad, dcu, k, out=out)
+        for b in (0, 2):
+            want = ref.attention(f64(q[cu[b]: cu[b + 1]]), *kv[b], int(ctx[b]), 0.125)
+            check_rows(out[cu[b]: cu[b + 1]], want, dt)
+        rk, _ = ops.kv_read_q8(c, pt, bad, dcu, k, 3 * k, dtype=F32)
+        for b in (0, 2):
+            assert np.array_equal(f64(rk[cu[b]: cu[b + 1]]), kv[b][0][ctx[b]:])
+        # what the append may have changed lies in the sequence's own pages
+        mine = torch.ones(c.num_pages, dtype=torch.bool)
+        mine[torch.from_numpy(own).long()] = False
+        mine[0] = False                                     # entries of -1 stand for it
+        before = [t.view(torch.uint8).clone() for t in (c.k, c.v, c.scale)]
+        only = torch.tensor([1], dtype=torch.int32).cuda()
+        ops.kv_append_q8(kn, kn, c, pt, bad, dcu, k, seq_ids=only)
+        for t, w in zip((c.k, c.v, c.scale), before):
+            assert torch.equal(t.view(torch.uint8)[mine.cuda()], w[mine.cuda()])
+            t.view(torch.uint8).copy_(w)
