@@ -698,6 +698,7 @@ size_t ipdv_sample_logits_workspace_size(int M, int V);
  * u [M] float in [0, 1); temperature, top_p, min_p [M] float and top_k [M]
  * int32, each NULL for off (temperature: 1).  Requirements: 0 <= M < 2^22, 1 <=
  * V <= 262144, M * V < 2^35; workspace on a 16-byte boundary.
+ * The workspace is written by the call; two calls that may overlap need one each.
  *
  * Errors: IPDV_EINVAL, IPDV_EUNSUPPORTED (dtype, V, M), IPDV_EWORKSPACE, IPDV_EHIP.
  */

@@ -54,11 +54,12 @@
 // request for a line that is still on its way holds the cache up.)
 //
 // What bounds it, in bf16 at D = 128: one token each of 64 sequences of 1024 to
-// 8192 tokens, 16 heads on 8, the bytes (609 MB in 120 us, the rate of a copy);
-// windows of eight, 32 heads on 4, the vector instructions beside the loads (313
-// MB in 94 us, of which the loads alone take 62 and the merge 10); prompts, the
-// vector instructions of softmax and conversion, about 430 per 64 keys and 32 rows
-// beside 48 matrix ones (eight of 512 to 1024 tokens in 94 us, 430 TFLOP/s).
+// 8192 tokens, 16 heads on 8, the bytes (609 MB in 121 us, the rate of a copy);
+// windows of eight, 32 heads on 4, the vector instructions beside the loads, 275 per
+// wave and 64 keys (313 MB, at a copy's rate 61 us, in 93, of which the merge takes
+// 11); prompts, the vector instructions of softmax, masks and conversion, 560 per 64
+// keys and 32 rows beside 48 matrix ones (eight of 512 to 1024 tokens in 94 us, 430
+// TFLOP/s; vector pipes issuing 58% of the time, and shares that are not even).
 #include <algorithm>
 #include <type_traits>
 
@@ -1168,9 +1169,14 @@ struct Q8Plan {
 // Row groups share the keys that they load, and leave fewer parts of them to
 // merge; but where rows are few they are copies, and their work is wasted.  Two
 // tiles per wave share a key's conversion, and halve the waves that a row count
-// fills.  Measured (32 heads on 4, D = 128; 64 windows over 1024 to 8192 tokens;
-// us) at rg = 1 / 2 / 4 with one tile: 8 rows 66 / 66 / 76, 32 rows 102 / 76 / 86,
-// 64 rows 182 / 111 / 97; with two at rg = 2: 64 rows 106; at rg = 4, one tile / two:
+// fills.  Measured (32 heads on 4; 64 windows over 1024 to 8192 tokens; both kernels,
+// us) at rg = 1 / 2 / 4 with one tile, for 16, 32 and 64 rows:
+//   bf16, D = 128   82 / 78 / 84    109 / 85 / 93     187 / 118 / 99
+//   bf16, D = 64    47 / 48 / 63     67 / 54 / 71     112 / 80 / 76
+//   fp32, D = 128   83 / 85 / 106   118 / 101 / 135   200 / 162 / 149
+//   fp32, D = 64    50 / 54 / 77     75 / 68 / 100    124 / 109 / 105
+// (rg = 1 has two terms of each probability in bf16, the others one).  Two tiles, the
+// first kernel alone, D = 128: at rg = 2 64 rows take 106; at rg = 4, one tile / two,
 // 128 rows 101 / 92, eight prompts 124 / 100.
 Q8Plan plan_of(int n_seq, int Hq, int Hkv, int max_q, bool bf16) {
   Q8Plan p;

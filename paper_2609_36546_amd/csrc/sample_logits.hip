@@ -37,7 +37,9 @@
 //
 // At V = 151936: one fp32 row takes 5 us and 11 unfiltered, 8.5 and 17 with top-p
 // 0.9; 64 bf16 rows 11 and 11, and 18 and 17.  The chunk kernel is bound by its
-// vector instructions (about 25 an entry) and LDS atomics, the row kernel by the
+// vector instructions (31 to 35 an entry with the list's pass, which issue 81% of
+// the time) and LDS atomics, of which it gives rows that need none (an unfiltered
+// one: a mass per chunk would do) as many as the others; the row kernel by the
 // latency of some ten dependent steps.  Lists that were not in bin order had to be
 // searched, and ended higher: a mixed batch of 64 took 58 us where this takes 37.
 //
