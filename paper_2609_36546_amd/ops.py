@@ -841,9 +841,9 @@ def kv_read_q8(cache: Q8Cache, page_table, ctx_lens, cu_q, max_q: int, rows: int
     """The values that positions ctx_lens[b] + i stand for, as rows cu_q[b] + i
     of two [rows,Hkv,D] tensors (see include/ipdv.h); with ctx_lens zero and
     the cached lengths in cu_q, whole sequences.  rows is cu_q's last entry, or
-    at least where the last handled window ends: the call does not look at cu_q
-    and would write behind the outputs.  validate=True checks that and the page
-    table on host copies first.  Returns (k, v)."""
+    at least where the last handled window ends: cu_q is read on the device
+    alone, and rows beyond would be written behind the outputs.  validate=True
+    checks that and the page table on host copies first.  Returns (k, v)."""
     dev = cache.device
     code = _dtype_code(dtype)
     ctx, cu, ids, n_seq, B = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
