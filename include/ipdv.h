@@ -40,7 +40,14 @@
  *   verify_attn_q8           -- the verification stage's attention over the
  *                               8-bit cache;
  *   sample_logits            -- a draw per row from logits, filtered by
- *                               temperature, top-k, top-p and min-p.
+ *                               temperature, top-k, top-p and min-p;
+ *   verify_attn_masked       -- the verification stage's attention with capped
+ *                               scores, a distance bias, sliding windows and
+ *                               ranges of keys per row;
+ *   attn_mass, kv_evict      -- the attention weight that each cached key gathers,
+ *                               and the cache cut to the keys of the largest;
+ *   verify_drafts            -- the verdict on drafts by both models' probabilities,
+ *                               with the replacement drawn from what is left.
  *
  * Conventions common to every entry point:
  *   - All array arguments are DEVICE pointers owned by the caller (except the
@@ -708,6 +715,174 @@ int sample_logits(const void* logits, int64_t row_stride, int M, int V, const fl
                   void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * What a score is before the softmax (verify_attn_masked, attn_mass).  For row r
+ * = cu_q[b] + i at position p = L_b + i, head h and key j:
+ *   x = scale * q . K_j
+ *   x = softcap * tanh(x / softcap)              (softcap > 0; 0: off)
+ *   x = x - slopes[h] * |p - j|                  (slopes [Hq] float; NULL: off)
+ * over the keys  max(first_key[r], p - window + 1, 0) <= j < end_key[r]  and
+ * j < L_b + k_b:
+ *   window            keys that a row sees at most, its own the last of them (0: off)
+ *   first_key [T] int32   e.g. where the row's document begins (NULL: 0)
+ *   end_key [T] int32     e.g. the end of a prefix that sees itself whole (NULL: p + 1)
+ * A row may be left without keys.  The struct is read on the host; its arrays are
+ * device memory.  A NULL struct is one of zeros.
+ */
+typedef struct {
+  float softcap;
+  int32_t window;
+  const float* slopes;
+  const int32_t* first_key;
+  const int32_t* end_key;
+} ipdv_score_mod;
+
+/* Workspace bytes verify_attn_masked needs (0 if the arguments are invalid).
+ * `window` as in the call's ipdv_score_mod, has_end_key whether it has an end_key. */
+size_t ipdv_attn_masked_workspace_size(int n_seq, int Hq, int Hkv, int D, int max_q,
+                                       int max_pages_per_seq, int page_size,
+                                       int window, int has_end_key);
+
+/*
+ * verify_attn_masked -- verify_attn_paged with modified scores x (ipdv_score_mod):
+ * appends the window, then
+ *   out[r, h, :] = sum_j softmax_j(x) V_j,   lse[r, h] = ln sum_j e^x
+ * over the keys that the row sees; a row that sees none gets 0 and -inf.  Keys and
+ * values of slots that a row does not see may hold anything, NaN and infinities
+ * included; a value that is not finite makes the rows that see it not finite.
+ * Maxima, sums and lse are fp32; a bf16 call holds a probability to 16 bits before its
+ * product with V where max_q * Hq / Hkv is at most 16, else rounds it to bf16 once.
+ *
+ * q [T, Hq, D] (dtype), q_row_stride elements from one row to the next (>= Hq *
+ * D); k_new, v_new [T, Hkv, D] (dtype; both NULL: the window is in the cache
+ * already); lse [T, Hq] float or NULL; mod a HOST pointer or NULL.  bf16 and fp32, D
+ * in {64, 128}.  The cache and the other arguments as in verify_attn_paged.  q's rows,
+ * k_new, v_new, the caches, out and workspace start on 16-byte boundaries.
+ * The workspace is written by the call; two calls that may overlap need one each.
+ *
+ * Errors: IPDV_EINVAL (also: softcap negative or not finite, window < 0),
+ * IPDV_EUNSUPPORTED (D, page_size, dtype, alignment, sizes), IPDV_EWORKSPACE, IPDV_EHIP.
+ */
+int verify_attn_masked(const void* q, int64_t q_row_stride, const void* k_new, const void* v_new,
+                       void* k_cache, void* v_cache,
+                       const int32_t* page_table, int max_pages_per_seq,
+                       const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* seq_ids,
+                       int n_seq, int max_q, const ipdv_score_mod* mod, void* out, float* lse,
+                       int Hq, int Hkv, int D, int page_size, int num_pages, float scale,
+                       int dtype, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * attn_mass -- the attention weight that every cached key gathers from a window: for
+ * position j of handled sequence b and KV head g, at its place in the pages,
+ *   mass_out = decay * mass_in + sum over rows r and heads h of g of e^(x - lse[r, h])
+ * with x and the rows' keys as in verify_attn_masked, whose lse the call takes.  j runs
+ * over all positions below L_b + k_b, also those that no row sees; those of the window
+ * itself (j >= L_b) start at 0, and so do all where mass_in is NULL.  Slots of other
+ * positions are left as they are.  The window must be in the cache.
+ *
+ * q, k_cache, mod, scale and the batch's arguments as in verify_attn_masked; lse [T,
+ * Hq] float; mass_in, mass_out [num_pages, Hkv, page_size] float, the same array or
+ * two that do not overlap; 0 <= decay, finite.  Requirement:
+ * max_pages_per_seq * page_size + max_q <= 2^22.  A page that two handled sequences
+ * share gets the mass of one of them (with mass_in == mass_out, of both in either order
+ * or of one): let them have pages of their own, or take them in calls of their own.
+ *
+ * Errors: IPDV_EINVAL, IPDV_EUNSUPPORTED, IPDV_EHIP.
+ */
+int attn_mass(const void* q, int64_t q_row_stride, const void* k_cache, const float* lse,
+              const int32_t* page_table, int max_pages_per_seq,
+              const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* seq_ids,
+              int n_seq, int max_q, const ipdv_score_mod* mod,
+              const float* mass_in, float decay, float* mass_out,
+              int Hq, int Hkv, int D, int page_size, int num_pages, float scale,
+              int dtype, void* hip_stream);
+
+/*
+ * kv_evict -- sequences cut to their heaviest keys.  Of handled sequence b's L_b positions
+ * every KV head keeps
+ *   n = min(max(keep[b], 0), L_b, max_dst_pages * page_size):
+ * the first min(n_sink, n), the last n_recent (as far as n reaches), and of the others
+ * those of the largest mass; equal masses: the lower position; NaN below everything.
+ * In ascending order they become positions 0 .. n - 1 of dst_table's pages, keys, values
+ * and masses.  new_lens[b] = n; kept[b, g, i] = the position that i was, -1 for i >= n.
+ * The heads of a sequence keep positions of their own, so that a slot no longer stands
+ * for one position: distance biases and sliding windows then count slots.
+ *
+ * k_cache, v_cache as in verify_attn_paged (dtype, in/out), mass [num_pages, Hkv,
+ * page_size] float (in/out); page_table [B, max_pages_per_seq], dst_table [B,
+ * max_dst_pages] int32; ctx_lens, keep [B] int32; seq_ids [n_seq] int32 or NULL;
+ * new_lens [B], kept [B, Hkv, max_dst_pages * page_size] int32 (entries of other sequences
+ * are left).  The pages that dst_table names for positions 0 .. n - 1 must belong to no
+ * other sequence and hold nothing that the call reads: not the sequence's own, either.
+ * Slots behind position n - 1 are left as they are.
+ * Requirements: D in {64, 128}; both tables times page_size <= 2^22; num_pages *
+ * page_size and num_pages * Hkv below 2^31; the caches, mass on 16-byte boundaries.
+ *
+ * Errors: IPDV_EINVAL (also: n_sink or n_recent < 0), IPDV_EUNSUPPORTED, IPDV_EHIP.
+ */
+int kv_evict(void* k_cache, void* v_cache, float* mass,
+             const int32_t* page_table, int max_pages_per_seq,
+             const int32_t* dst_table, int max_dst_pages,
+             const int32_t* ctx_lens, const int32_t* keep, const int32_t* seq_ids, int n_seq,
+             int n_sink, int n_recent, int32_t* new_lens, int32_t* kept,
+             int Hkv, int D, int page_size, int num_pages, int dtype, void* hip_stream);
+
+/* A row's filters, arrays of one entry per row, each NULL for off (sample_logits). */
+typedef struct {
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+} ipdv_filters;
+
+/* Workspace bytes verify_drafts needs (0 if the arguments are invalid): whether the target's
+ * and the draft's filters have more than a temperature. */
+size_t ipdv_verify_drafts_workspace_size(int T, int V, int B, int target_filtered,
+                                         int draft_filtered);
+
+/*
+ * verify_drafts -- the verdict on drafted tokens by the two models' probabilities.  With p
+ * and q the target's and the draft's distributions at a row (softmax of the logits at the
+ * row's temperature over what its filters keep, as in sample_logits), x = prop_tok[r], for
+ * the rows r = cu_q[b] + i of sequence b in turn:
+ *   x >= 0: accepted if u_accept[r] * q(x) < p(x).  The first draft that is not ends the
+ *           window, and token[b] is drawn from max(0, p - q), normalised (from p, should
+ *           nothing be left of it);
+ *   x < 0:  no draft, e.g. the row behind the last: the window ends, token[b] is drawn from p;
+ *   an accepted x == eos_id ends the window, without a token.
+ * Tokens are drawn in index order by u_draw[b], as sample_logits does.  What a sequence
+ * emits, its n_acc[b] accepted drafts and the token, is distributed as the target's own draws
+ * are, if x was drawn from q.
+ *   n_acc[b]     accepted drafts
+ *   token[b]     the token behind them, -1 for none (all accepted, or the window ended by EOS
+ *                or by a row that cannot be drawn from)
+ *   finished[b]  1 if the last of these is eos_id
+ *   p_accept[r]  min(1, p(x) / q(x)), of every row; 0 where x < 0, and where p(x) = q(x) = 0
+ *   logp[b]      ln p(token[b]), NaN without one (optional; NULL)
+ * A row whose target logits (or, with a draft, its draft logits) hold NaN or +inf or nothing
+ * above -inf, or whose temperature is negative or NaN, ends its window without a token; its
+ * p_accept is NaN.  A draft at or beyond V has p(x) = 0 and is rejected.  draft_logits NULL:
+ * q(x) = 1, as of drafts looked up or taken greedily; draft_filters is then not read.
+ * Probabilities are 64-bit floats (relative error below 1e-9), except that top-p's cut is found
+ * as in sample_logits.  The same call repeats bit for bit.
+ *
+ * target_logits, draft_logits [T, V] (dtype), *_row_stride elements from one row to the next
+ * (>= V); prop_tok [T], cu_q [B+1] int32 (cu_q[B] <= T); u_accept [T], u_draw [B] float in [0,
+ * 1); filters HOST pointers to structs of device arrays of T entries, or NULL for off.
+ * Requirements: 0 <= T < 2^22, 0 <= B < 2^22, 1 <= V <= 262144, T * V < 2^35; workspace on a
+ * 16-byte boundary, written by the call: two calls that may overlap need one each.
+ *
+ * Errors: IPDV_EINVAL, IPDV_EUNSUPPORTED (dtype, V, T), IPDV_EWORKSPACE, IPDV_EHIP.
+ */
+int verify_drafts(const void* target_logits, int64_t target_row_stride,
+                  const void* draft_logits, int64_t draft_row_stride, int T, int V,
+                  const int32_t* prop_tok, const int32_t* cu_q, int B,
+                  const float* u_accept, const float* u_draw,
+                  const ipdv_filters* target_filters, const ipdv_filters* draft_filters,
+                  int32_t eos_id, int32_t* n_acc, int32_t* token, uint8_t* finished,
+                  float* p_accept, float* logp, int dtype,
+                  void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Optional timing hook for profilers and benchmarks (thread-local).  While
  * set, each kernel an entry point launches is bracketed by hipEventRecord of
  * the caller's events (hipEvent_t handles cast to void*), taken from
@@ -723,7 +898,9 @@ int sample_logits(const void* logits, int64_t row_stride, int M, int V, const fl
  * accept_scan_rule 1, sample_takeover 1, lmhead_sample 1, lmhead_pack_w 1,
  * lmhead_logp_gather 1, source_split_kl 1 (+1 with cu), rope_window 1,
  * kv_append_q8 1, kv_read_q8 1, verify_attn_q8 2 (attention, merge of cut
- * items), sample_logits 2 (chunks, rows).
+ * items), sample_logits 2 (chunks, rows), verify_attn_masked 3 (append, attention, merge;
+ * empty where there is none), attn_mass 1, kv_evict 2 (selection, move), verify_drafts 3
+ * (the rows' masses, with their cuts; what is left of rejected rows; draws).
  */
 int ipdv_trace_events(void* const* events, int capacity);
 int ipdv_trace_count(void);

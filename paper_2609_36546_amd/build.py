@@ -18,7 +18,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OUT = os.path.join(HERE, "libipdv.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 SOURCES = ["verify_attn.hip", "lmhead.hip", "accept_scan.hip", "kl.hip", "rope.hip", "kv_q8.hip",
-           "attn_q8.hip", "sample_logits.hip", "abi.cpp"]
+           "attn_q8.hip", "sample_logits.hip", "attn_masked.hip", "attn_mass.hip", "evict.hip", "drafts.hip",
+           "abi.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -29,7 +30,8 @@ FLAGS = [
 # Per-source code generation flags.  The attention kernels keep their MFMA
 # accumulators in arch VGPRs (they rescale them with VALU ops);
 # the LM-head GEMM needs AGPRs for its 256-register accumulator tile.
-EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for src in ("verify_attn.hip", "attn_q8.hip")}
+EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+         for src in ("verify_attn.hip", "attn_q8.hip", "attn_masked.hip", "attn_mass.hip")}
 
 
 def _run(cmd):

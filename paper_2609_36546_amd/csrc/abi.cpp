@@ -708,4 +708,164 @@ int sample_logits(const void* logits, int64_t stride, int M, int V, const float*
   return ok();
 }
 
+// The modifiers' checks, and the struct as the kernels take it.
+static int score_mod(const ipdv_score_mod* mod, ipdv::ScoreMod* out) {
+  *out = {};
+  if (!mod) return IPDV_OK;
+  if (!std::isfinite(mod->softcap) || mod->softcap < 0.f) return fail(IPDV_EINVAL, "softcap must be >= 0 and finite");
+  if (mod->window < 0) return fail(IPDV_EINVAL, "window must be >= 0 (got %d)", mod->window);
+  *out = {mod->softcap, mod->window, mod->slopes, mod->first_key, mod->end_key};
+  return IPDV_OK;
+}
+
+static int masked_shape_check(int n_seq, int Hq, int Hkv, int D, int max_q, int max_pages, int page_size, int window,
+                              bool ends) {
+  int st = attn_shape_check(n_seq, Hq, Hkv, D, max_q, max_pages, page_size);
+  if (st != IPDV_OK) return st;
+  if (max_q >= 1 << 27) return fail(IPDV_EUNSUPPORTED, "max_q too large");
+  if (ipdv::attn_masked_units(n_seq, Hq, Hkv, max_q, max_pages, page_size, window, ends) > 65535)
+    return fail(IPDV_EUNSUPPORTED, "max_q * Hq/Hkv too large");
+  return IPDV_OK;
+}
+
+size_t ipdv_attn_masked_workspace_size(int n_seq, int Hq, int Hkv, int D, int max_q, int max_pages, int page_size,
+                                       int window, int has_end_key) {
+  if (window < 0) return 0;
+  if (masked_shape_check(n_seq, Hq, Hkv, D, max_q, max_pages, page_size, window, has_end_key != 0) != IPDV_OK) return 0;
+  return ipdv::attn_masked_workspace(n_seq, Hq, Hkv, D, max_q, max_pages, page_size, window, has_end_key != 0);
+}
+
+// What verify_attn_masked and attn_mass check alike.
+static int masked_call_check(const void* q, int64_t q_stride, const void* k_cache, const int32_t* page_table,
+                             const int32_t* ctx_lens, const int32_t* cu_q, int n_seq, int Hq, int Hkv, int D,
+                             int num_pages, float scale, int dtype) {
+  if (dtype != IPDV_F32 && dtype != IPDV_BF16) return fail(IPDV_EUNSUPPORTED, "dtype %d", dtype);
+  if (num_pages < 1) return fail(IPDV_EINVAL, "num_pages must be >= 1 (got %d)", num_pages);
+  if ((int64_t)num_pages * Hkv >= (int64_t)1 << 31) return fail(IPDV_EUNSUPPORTED, "num_pages * Hkv exceeds 2^31 - 1");
+  if (!std::isfinite(scale) || !(scale > 0.f)) return fail(IPDV_EINVAL, "scale must be positive and finite");
+  if (q_stride < (int64_t)Hq * D) return fail(IPDV_EINVAL, "a row stride is shorter than the row");
+  if (n_seq > 0 && (!q || !k_cache || !page_table || !ctx_lens || !cu_q)) return fail(IPDV_EINVAL, "null required pointer");
+  const int size = dtype == IPDV_BF16 ? 2 : 4;
+  if (!on16(q) || !on16(k_cache) || q_stride * size % 16 != 0)
+    return fail(IPDV_EUNSUPPORTED, "q's rows and the caches must start on 16-byte boundaries");
+  return IPDV_OK;
+}
+
+int verify_attn_masked(const void* q, int64_t q_stride, const void* k_new, const void* v_new, void* k_cache, void* v_cache,
+                       const int32_t* page_table, int max_pages, const int32_t* ctx_lens, const int32_t* cu_q,
+                       const int32_t* seq_ids, int n_seq, int max_q, const ipdv_score_mod* mod, void* out, float* lse,
+                       int Hq, int Hkv, int D, int page_size, int num_pages, float scale, int dtype, void* workspace,
+                       size_t workspace_bytes, void* hip_stream) {
+  ipdv::ScoreMod m;
+  int st = score_mod(mod, &m);
+  if (st != IPDV_OK) return st;
+  st = masked_shape_check(n_seq, Hq, Hkv, D, max_q, max_pages, page_size, m.window, m.end_key != nullptr);
+  if (st != IPDV_OK) return st;
+  st = masked_call_check(q, q_stride, k_cache, page_table, ctx_lens, cu_q, n_seq, Hq, Hkv, D, num_pages, scale, dtype);
+  if (st != IPDV_OK) return st;
+  if (n_seq == 0) return ok();
+  if (!v_cache || !out) return fail(IPDV_EINVAL, "null required pointer");
+  if (!k_new != !v_new) return fail(IPDV_EINVAL, "k_new and v_new come together");
+  const size_t need =
+      ipdv::attn_masked_workspace(n_seq, Hq, Hkv, D, max_q, max_pages, page_size, m.window, m.end_key != nullptr);
+  if (!workspace || workspace_bytes < need)
+    return fail(IPDV_EWORKSPACE, "workspace of %zu bytes needed (got %zu)", need, workspace ? workspace_bytes : (size_t)0);
+  if (!on16(k_new) || !on16(v_new) || !on16(v_cache) || !on16(out) || !on16(workspace))
+    return fail(IPDV_EUNSUPPORTED, "the window, caches, out and workspace must start on 16-byte boundaries");
+  ipdv::AttnMaskedLaunch L{q, q_stride, k_new, v_new, k_cache, v_cache, page_table, max_pages, ctx_lens, cu_q, seq_ids,
+                           n_seq, max_q, m, out, lse, Hq, Hkv, D, page_size, num_pages, scale, dtype == IPDV_BF16,
+                           workspace};
+  hipError_t e = ipdv::launch_attn_masked(L, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return hip_fail("verify_attn_masked launch", e);
+  return ok();
+}
+
+int attn_mass(const void* q, int64_t q_stride, const void* k_cache, const float* lse, const int32_t* page_table,
+              int max_pages, const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* seq_ids, int n_seq, int max_q,
+              const ipdv_score_mod* mod, const float* mass_in, float decay, float* mass_out, int Hq, int Hkv, int D,
+              int page_size, int num_pages, float scale, int dtype, void* hip_stream) {
+  ipdv::ScoreMod m;
+  int st = score_mod(mod, &m);
+  if (st != IPDV_OK) return st;
+  st = attn_shape_check(n_seq, Hq, Hkv, D, max_q, max_pages, page_size);
+  if (st != IPDV_OK) return st;
+  if ((int64_t)max_pages * page_size + max_q > 1 << 22)
+    return fail(IPDV_EUNSUPPORTED, "max_pages_per_seq * page_size + max_q exceeds 2^22");
+  st = masked_call_check(q, q_stride, k_cache, page_table, ctx_lens, cu_q, n_seq, Hq, Hkv, D, num_pages, scale, dtype);
+  if (st != IPDV_OK) return st;
+  if (!std::isfinite(decay) || decay < 0.f) return fail(IPDV_EINVAL, "decay must be >= 0 and finite");
+  if (n_seq == 0) return ok();
+  if (!lse || !mass_out) return fail(IPDV_EINVAL, "null required pointer");
+  ipdv::AttnMaskedLaunch L{q, q_stride, nullptr, nullptr, const_cast<void*>(k_cache), nullptr, page_table, max_pages,
+                           ctx_lens, cu_q, seq_ids, n_seq, max_q, m, nullptr, const_cast<float*>(lse), Hq, Hkv, D,
+                           page_size, num_pages, scale, dtype == IPDV_BF16, nullptr, mass_in, mass_out, decay};
+  hipError_t e = ipdv::launch_attn_mass(L, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return hip_fail("attn_mass launch", e);
+  return ok();
+}
+
+int kv_evict(void* k_cache, void* v_cache, float* mass, const int32_t* page_table, int max_pages, const int32_t* dst_table,
+             int dst_pages, const int32_t* ctx_lens, const int32_t* keep, const int32_t* seq_ids, int n_seq, int n_sink,
+             int n_recent, int32_t* new_lens, int32_t* kept, int Hkv, int D, int page_size, int num_pages, int dtype,
+             void* hip_stream) {
+  int st = q8_check(n_seq, 1, Hkv, D, page_size, num_pages, max_pages, dtype);
+  if (st != IPDV_OK) return st;
+  if (dst_pages < 1) return fail(IPDV_EINVAL, "max_dst_pages must be >= 1 (got %d)", dst_pages);
+  if (n_sink < 0 || n_recent < 0) return fail(IPDV_EINVAL, "n_sink and n_recent must be >= 0");
+  if ((int64_t)max_pages * page_size > 1 << 22 || (int64_t)dst_pages * page_size > 1 << 22)
+    return fail(IPDV_EUNSUPPORTED, "a table holds more than 2^22 positions");
+  if ((int64_t)num_pages * page_size >= (int64_t)1 << 31)
+    return fail(IPDV_EUNSUPPORTED, "num_pages * page_size exceeds 2^31 - 1");
+  if (n_seq == 0) return ok();
+  if (!k_cache || !v_cache || !mass || !page_table || !dst_table || !ctx_lens || !keep || !new_lens || !kept)
+    return fail(IPDV_EINVAL, "null required pointer");
+  if (!on16(k_cache) || !on16(v_cache) || !on16(mass))
+    return fail(IPDV_EUNSUPPORTED, "the caches and mass must start on 16-byte boundaries");
+  ipdv::EvictLaunch L{k_cache, v_cache, mass, page_table, max_pages, dst_table, dst_pages, ctx_lens, keep, seq_ids,
+                      n_seq, n_sink, n_recent, new_lens, kept, Hkv, D, page_size, num_pages, dtype == IPDV_BF16};
+  hipError_t e = ipdv::launch_kv_evict(L, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return hip_fail("kv_evict launch", e);
+  return ok();
+}
+
+static int drafts_shape_check(int T, int V, int B) {
+  if (T < 0) return fail(IPDV_EINVAL, "T must be >= 0 (got %d)", T);
+  if (B < 0) return fail(IPDV_EINVAL, "B must be >= 0 (got %d)", B);
+  if (B >= 1 << 22) return fail(IPDV_EUNSUPPORTED, "B too large");
+  return sample_shape_check(T, V);
+}
+
+size_t ipdv_verify_drafts_workspace_size(int T, int V, int B, int target_filtered, int draft_filtered) {
+  if (drafts_shape_check(T, V, B) != IPDV_OK) return 0;
+  return ipdv::verify_drafts_workspace(T, V, B, target_filtered != 0, draft_filtered != 0);
+}
+
+int verify_drafts(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int T, int V,
+                  const int32_t* prop_tok, const int32_t* cu_q, int B, const float* u_accept, const float* u_draw,
+                  const ipdv_filters* target_filters, const ipdv_filters* draft_filters, int32_t eos_id, int32_t* n_acc,
+                  int32_t* token, uint8_t* finished, float* p_accept, float* logp, int dtype, void* workspace,
+                  size_t workspace_bytes, void* hip_stream) {
+  int st = drafts_shape_check(T, V, B);
+  if (st != IPDV_OK) return st;
+  if (dtype != IPDV_F32 && dtype != IPDV_BF16) return fail(IPDV_EUNSUPPORTED, "dtype %d", dtype);
+  if (target_stride < V || (draft && draft_stride < V)) return fail(IPDV_EINVAL, "a row stride is shorter than the row");
+  if (B == 0) return ok();
+  if (!cu_q || !u_draw || !n_acc || !token || !finished) return fail(IPDV_EINVAL, "null required pointer");
+  if (T > 0 && (!target || !prop_tok || !u_accept || !p_accept)) return fail(IPDV_EINVAL, "null required pointer");
+  auto filters = [](const ipdv_filters* f) {
+    return f ? ipdv::Filters{f->temperature, f->top_k, f->top_p, f->min_p} : ipdv::Filters{};
+  };
+  auto filtered = [](const ipdv::Filters& f) { return f.top_k || f.top_p || f.min_p; };
+  const ipdv::Filters tf = filters(target_filters), df = filters(draft ? draft_filters : nullptr);
+  const size_t need = ipdv::verify_drafts_workspace(T, V, B, filtered(tf), filtered(df));
+  if (!workspace || workspace_bytes < need)
+    return fail(IPDV_EWORKSPACE, "workspace of %zu bytes needed (got %zu)", need, workspace ? workspace_bytes : (size_t)0);
+  if (!on16(workspace)) return fail(IPDV_EUNSUPPORTED, "workspace must start on a 16-byte boundary");
+  ipdv::DraftLaunch L{target, target_stride, draft, draft_stride, T, V, B, prop_tok, cu_q, u_accept, u_draw, tf, df,
+                      eos_id, n_acc, token, finished, p_accept, logp, dtype == IPDV_BF16, workspace};
+  hipError_t e = ipdv::launch_verify_drafts(L, reinterpret_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return hip_fail("verify_drafts launch", e);
+  return ok();
+}
+
 }  // extern "C"

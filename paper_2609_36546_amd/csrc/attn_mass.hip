@@ -1,0 +1,240 @@
+// The attention weight that every cached key gathers from a window, for gfx950:
+//
+//   mass[j] = decay mass[j] + sum over rows i and heads h of the KV head of e^(x_ihj - lse_ih)
+//
+// with x the modified scores and lse their log-sum-exp, as attn_masked.hip has them;
+// keys of the window itself start at 0.  With lse in hand a weight needs nothing
+// of the row's other keys, so every key's sum belongs to one workgroup: no atomics,
+// no partial results, the same bits every time.
+//
+// Scores are taken as there, S^T[32 keys x 16 rows] = K . Q^T, a lane holding 8 keys of
+// one row.  Up to 64 rows (attn_mass_few_kernel) a wave keeps all of them in registers and
+// streams keys; with more (attn_mass_many_kernel) it keeps 128 keys and streams rows, the
+// four waves of a workgroup every fourth tile of them.  Weights are added per lane, over the rows
+// of a lane's column, and joined over the 16 columns at the end.
+#include <algorithm>
+#include <type_traits>
+
+#include "common.h"
+#include "kernels.h"
+#include "masked.h"
+
+namespace ipdv {
+namespace {
+
+constexpr int kWaves = 4;
+
+struct MassParams : WindowParams {
+  const float* lse;
+  const float* mass_in;
+  float* mass_out;
+  float decay;
+  int per;             // blocks of a workgroup
+};
+
+// Sum over the 16 lanes of a group that share a key.
+__device__ __forceinline__ float sum16(float v) {
+  v += dpp_move<0x140>(v);
+  v += dpp_move<0x141>(v);
+  v += dpp_move<0x4E>(v);
+  return v + dpp_move<0xB1>(v);
+}
+
+// Lane 8 j + i (i < 8, of the groups j of 16: lane 16 j + i) writes key t0 + 8 j + i.
+__device__ __forceinline__ void put(const MassParams& a, const Seq& s, const Parts& parts, int t0, float sum) {
+  const int lane = lane_id(), c16 = lane & 15, j = lane >> 4, key = t0 + 8 * j + c16;
+  if (c16 >= 8 || key >= s.L + s.kb) return;
+  const int ps = 1 << a.log2ps;
+  const size_t at = (size_t)parts.of(j >> 1) * (unsigned)ps + (unsigned)(key & (ps - 1));
+  if (a.mass_in && key < s.L) sum = fmaf(a.decay, a.mass_in[at], sum);
+  a.mass_out[at] = sum;
+}
+
+// Queries and what else belongs to the lane's row of a tile.
+template <typename DT, int D, int QT> struct RowTile {
+  Queries<DT, D, QT> Q;
+  RowInfo row[QT];
+  float lse2[QT];      // lse log2(e)
+  __device__ __forceinline__ void load(const MassParams& a, const Seq& s, int g, int t, int pr0) {
+    const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
+    const int pr = min(pr0 + c16, s.rows - 1), i = pr / a.G, h = g * a.G + pr - i * a.G;
+    row[t] = row_info(a, s, i, h);
+    // behind the last row its copies, of weight 0
+    lse2[t] = pr0 + c16 < s.rows ? a.lse[(size_t)(s.r0 + i) * a.Hq + h] * 1.4426950408889634f : INFINITY;
+    const DT* qr = reinterpret_cast<const DT*>(a.q) + (size_t)(s.r0 + i) * a.q_stride + (size_t)h * D;
+    if constexpr (sizeof(DT) == 2) {
+#pragma unroll
+      for (int ks = 0; ks < D / 32; ++ks) Q.q[t][ks] = ld16<bf16x8>(qr + 32 * ks + 8 * j);
+    } else {
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) Q.q[t][c] = ld16<floatx4>(qr + j * (D / 4) + 4 * c);
+    }
+  }
+  // Adds the tiles' weights of a block's keys.
+  __device__ __forceinline__ void add(const MassParams& a, floatx4 (&sc)[QT][2], int t0, bool masked, float (&sum)[8]) const {
+    const int k0 = t0 + 8 * (lane_id() >> 4);
+    modify<DT, QT>(a, row, k0, sc);
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float w = fast_exp2(sc[t][i >> 2][i & 3] - lse2[t]);
+        if (masked) w = k0 + i >= row[t].lo && k0 + i < row[t].hi ? w : 0.f;
+        sum[i] += w;
+      }
+  }
+};
+
+// One of the lane's eight sums, the one that it writes.
+__device__ __forceinline__ float pick(const float (&sum)[8]) {
+  const int c16 = lane_id() & 15;
+  float out = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float v = sum16(sum[i]);
+    out = c16 == i ? v : out;
+  }
+  return out;
+}
+
+template <typename DT, int D, int QT>
+__global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void attn_mass_few_kernel(MassParams a) {
+  if ((int)blockIdx.x >= a.n_seq * a.Hkv) return;
+  const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv;
+  const Seq s = seq_of(a, slot);
+  const int b0 = blockIdx.y * a.per, b1 = min(b0 + a.per, (s.L + s.kb + kBlk - 1) / kBlk);
+  const int first = b0 + uni(threadIdx.x / kWave);
+  if (first >= b1) return;
+  RowTile<DT, D, QT> R;
+  Span span{INT_MAX, 0, INT_MAX, 0};
+  if (s.rows > 0) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) R.load(a, s, g, t, 16 * t);
+    span = span_of<QT>(R.row);
+  }
+  const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
+  Parts parts, next;
+  parts.look_up(a, pt, first * kBlk, g);
+  Frags<DT, D> f;
+  if (span.sees(first * kBlk)) load_keys<DT, D>(a, f, first * kBlk, parts);
+  next.look_up(a, pt, (first + kWaves) * kBlk, g);
+  for (int n = first; n < b1; n += kWaves) {
+    const int t0 = n * kBlk;
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const bool seen = span.sees(t0);
+    floatx4 sc[QT][2];
+    if (seen) scores<DT, D, QT>(f, R.Q, sc);
+    __builtin_amdgcn_sched_barrier(0);
+    if (n + kWaves < b1 && span.sees(t0 + kWaves * kBlk)) load_keys<DT, D>(a, f, t0 + kWaves * kBlk, next);
+    __builtin_amdgcn_sched_barrier(0);
+    if (seen) R.add(a, sc, t0, !span.whole(t0), sum);
+    put(a, s, parts, t0, pick(sum));
+    parts = next;
+    next.look_up(a, pt, t0 + 2 * kWaves * kBlk, g);
+  }
+}
+
+template <typename DT, int D, int NB>
+__global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void attn_mass_many_kernel(MassParams a) {
+  __shared__ float s_sum[kWaves][NB][kBlk];
+  if ((int)blockIdx.x >= a.n_seq * a.Hkv) return;
+  const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv;
+  const Seq s = seq_of(a, slot);
+  // the first keys, which most rows see, first
+  const int t0 = blockIdx.y * NB * kBlk, end = s.L + s.kb;
+  if (t0 >= end) return;
+  const int wv = uni(threadIdx.x / kWave);
+  const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
+  Frags<DT, D> f[NB];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    Parts parts;
+    parts.look_up(a, pt, t0 + n * kBlk, g);
+    load_keys<DT, D>(a, f[n], t0 + n * kBlk, parts);
+  }
+  float sum[NB][8];
+#pragma unroll
+  for (int n = 0; n < NB; ++n)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[n][i] = 0.f;
+  // rows in front see none of these keys, unless their ranges' ends are given
+  const int row0 = a.end_key ? 0 : max(t0 - s.L, 0) * a.G;
+  // nor rows that these keys lie in front of the sliding window of
+  const long last = (long)t0 + NB * kBlk - 1 + a.window - 1 - s.L;      // the last position that may, counted from L
+  const int rows = (int)min((long)s.rows, (last + 1) * a.G);
+  const int tiles = (rows + 15) / 16;
+  RowTile<DT, D, 1> R, N;
+  int tile = row0 / 16 + wv;
+  if (tile < tiles) R.load(a, s, g, 0, 16 * tile);
+  for (; tile < tiles; tile += kWaves) {
+    if (tile + kWaves < tiles) N.load(a, s, g, 0, 16 * (tile + kWaves));
+    const Span span = span_of<1>(R.row);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const int tn = t0 + n * kBlk;
+      if (span.sees(tn)) {
+        floatx4 sc[1][2];
+        scores<DT, D, 1>(f[n], R.Q, sc);
+        R.add(a, sc, tn, !span.whole(tn), sum[n]);
+      }
+    }
+    R = N;
+  }
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    const float v = pick(sum[n]);
+    const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
+    if (c16 < 8) s_sum[wv][n][8 * j + c16] = v;
+  }
+  __syncthreads();
+  for (int n = wv; n < NB; n += kWaves) {
+    const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
+    float v = 0.f;
+    if (c16 < 8)
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) v += s_sum[i][n][8 * j + c16];
+    Parts parts;
+    parts.look_up(a, pt, t0 + n * kBlk, g);
+    put(a, s, parts, t0 + n * kBlk, v);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_attn_mass(const AttnMaskedLaunch& L, hipStream_t st) {
+  MassParams p{};
+  static_cast<WindowParams&>(p) = window_params(L);
+  p.lse = L.lse;
+  p.mass_in = L.mass_in;
+  p.mass_out = L.mass_out;
+  p.decay = L.decay;
+  const long rows = (long)L.max_q * p.G, sg = (long)L.n_seq * L.Hkv;
+  const long blocks = ((long)p.slots + L.max_q + kBlk - 1) / kBlk;
+  const unsigned gx = (unsigned)((sg + 7) / 8 * 8);
+  p.per = (int)std::max(std::clamp(sg * blocks / 2048, 4L, 32L), (blocks + 65534) / 65535);
+  trace_begin(st);
+  auto pick = [&](auto dt, auto dim) {
+    using DT = decltype(dt);
+    constexpr int D = decltype(dim)::value, NB = sizeof(DT) == 4 ? 2 : 4;
+    auto few = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(gx, (unsigned)((blocks + p.per - 1) / p.per)), dim3(256), 0, st, p);
+    };
+    if (rows <= 16) few(attn_mass_few_kernel<DT, D, 1>);
+    else if (rows <= 32) few(attn_mass_few_kernel<DT, D, 2>);
+    else if (rows <= 64 && sizeof(DT) == 2) few(attn_mass_few_kernel<DT, D, 4>);
+    else hipLaunchKernelGGL((attn_mass_many_kernel<DT, D, NB>), dim3(gx, (unsigned)((blocks + NB - 1) / NB)), dim3(256), 0, st, p);
+  };
+  typedef std::integral_constant<int, 64> D64;
+  typedef std::integral_constant<int, 128> D128;
+  if (L.dtype_bf16) {
+    if (L.D == 128) pick(bf16(), D128()); else pick(bf16(), D64());
+  } else {
+    if (L.D == 128) pick(float(), D128()); else pick(float(), D64());
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  trace_mark(st);
+  return hipSuccess;
+}
+
+}  // namespace ipdv

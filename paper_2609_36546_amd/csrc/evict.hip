@@ -1,0 +1,287 @@
+// Eviction from the paged cache by gathered attention weight, for gfx950: of a
+// sequence's L positions each KV head keeps n, the first n_sink, the last n_recent and
+// of the others those of the largest mass (equal masses: the lower position), and they
+// move, in order, to positions 0 .. n - 1 of other pages.
+//
+//   select kernel  one workgroup per (sequence, KV head): the mass of the last position
+//                  kept, found by its order number's four bytes from the top, each a
+//                  histogram in LDS of what the bytes before it leave; then the kept
+//                  positions by a scan in order, equal masses counted as they come.
+//   move kernel    64 kept positions of one (sequence, KV head) per workgroup: keys are
+//                  runs of 32 channels per slot, values and masses gathered slot by slot
+//                  and stored 16 bytes at a time.
+//
+// Whole numbers decide, in an order that does not depend on the atomics', so the same call
+// repeats bit for bit.
+#include <type_traits>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace ipdv {
+namespace {
+
+constexpr int kThreads = 1024;     // of the select kernel
+constexpr int kWaves = kThreads / kWave;
+constexpr int kRun = 16;           // neighbouring positions of a thread: in one page
+constexpr int kMove = 64;          // positions of a workgroup of the move kernel
+
+struct EvictParams : EvictLaunch {
+  int log2ps, slots, dst_slots;
+};
+
+// Masses as unsigned numbers of the same order; NaN below everything, -0 as 0.
+__device__ __forceinline__ unsigned order_of(float x) {
+  if (x != x) return 0u;
+  const unsigned u = __float_as_uint(x == 0.f ? 0.f : x);
+  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+
+struct Seq {
+  int b, L, n, lo, hi;     // kept without asking: positions below lo, and from hi on
+};
+__device__ __forceinline__ Seq seq_of(const EvictParams& a, int slot) {
+  Seq s;
+  s.b = a.seq_ids ? a.seq_ids[slot] : slot;
+  s.L = min(max(a.ctx_lens[s.b], 0), a.slots);
+  s.n = min(max(a.keep[s.b], 0), min(s.L, a.dst_slots));
+  s.lo = min(a.n_sink, s.n);
+  s.hi = s.L - min(a.n_recent, s.n - s.lo);
+  return s;
+}
+__device__ __forceinline__ int page_at(const EvictParams& a, const int32_t* table, int width, int pos) {
+  return min(max(table[min(pos >> a.log2ps, width - 1)], 0), a.num_pages - 1);
+}
+
+// Sums over the threads before this one of two counts; every thread calls.
+__device__ __forceinline__ int2 scan2(int2 v, int2* part, int2* all) {
+  const int lane = lane_id(), w = threadIdx.x / kWave;
+  const int x = wave_incl_scan_i(v.x), y = wave_incl_scan_i(v.y);
+  __syncthreads();                  // the previous call's readers are done
+  if (lane == kWave - 1) part[w] = make_int2(x, y);
+  __syncthreads();
+  int2 before = make_int2(x - v.x, y - v.y), sum = make_int2(0, 0);
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    const int2 p = part[i];
+    if (i < w) {
+      before.x += p.x;
+      before.y += p.y;
+    }
+    sum.x += p.x;
+    sum.y += p.y;
+  }
+  *all = sum;
+  return before;
+}
+
+// ONE: a round of threads holds all positions, so their masses are read once.
+template <bool ONE>
+__global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictParams a) {
+  __shared__ int s_hist[256];
+  __shared__ int2 s_part[kWaves];
+  __shared__ int s_digit, s_left;
+  const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv, tid = threadIdx.x;
+  const Seq s = seq_of(a, slot);
+  if (g == 0 && tid == 0) a.new_lens[s.b] = s.n;
+  int32_t* kept = a.kept + ((size_t)s.b * a.Hkv + g) * (unsigned)a.dst_slots;
+  const int32_t* table = a.page_table + (size_t)s.b * a.max_pages;
+  for (int i = s.n + tid; i < a.dst_slots; i += kThreads) kept[i] = -1;
+  if (s.n == 0) return;
+  if (s.n == s.L) {
+    for (int i = tid; i < s.n; i += kThreads) kept[i] = i;
+    return;
+  }
+  const int rounds = ONE ? 1 : (int)(((long)s.L + kThreads * kRun - 1) / (kThreads * kRun));
+  unsigned key[kRun];
+  auto load = [&](int round) {
+    const int p0 = (round * kThreads + tid) * kRun;
+    if (p0 >= s.L) return;
+    const float* m = a.mass + ((size_t)page_at(a, table, a.max_pages, p0) * a.Hkv + g) * (unsigned)a.page_size +
+                     (p0 & (a.page_size - 1));
+#pragma unroll
+    for (int i = 0; i < kRun; i += 4) {
+      const floatx4 v = ld16<floatx4>(m + i);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) key[i + c] = order_of(v[c]);
+    }
+  };
+  if (ONE) load(0);
+  auto candidate = [&](int p) { return p >= s.lo && p < s.hi; };
+  // The order number of the last position kept, from its top byte down: `least` so far,
+  // its bytes below `shift` open; `left` to be kept among those that agree with it.
+  int left = s.n - s.lo - (s.L - s.hi);
+  unsigned least = 0;
+  const bool ask = left > 0;        // else nothing beside what is kept unasked
+  for (int shift = 24; ask && shift >= 0; shift -= 8) {
+    if (tid < 256) s_hist[tid] = 0;
+    __syncthreads();
+    for (int r = 0; r < rounds; ++r) {
+      if (!ONE) load(r);
+      const int p0 = (r * kThreads + tid) * kRun;
+#pragma unroll
+      for (int i = 0; i < kRun; ++i)
+        if (candidate(p0 + i) && (shift == 24 || (key[i] ^ least) >> (shift + 8) == 0)) atomicAdd(&s_hist[(key[i] >> shift) & 255], 1);
+    }
+    __syncthreads();
+    if (tid < kWave) {              // a lane: four digits, from the top
+      int c[4], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        c[i] = s_hist[255 - 4 * tid - i];
+        sum += c[i];
+      }
+      int before = wave_incl_scan_i(sum) - sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (before < left && before + c[i] >= left) {
+          s_digit = 255 - 4 * tid - i;
+          s_left = left - before;
+        }
+        before += c[i];
+      }
+    }
+    __syncthreads();
+    least |= (unsigned)s_digit << shift;
+    left = s_left;
+    __syncthreads();
+  }
+  // All above `least` are kept, and the first `left` that equal it.
+  int2 base = make_int2(0, 0);
+  for (int r = 0; r < rounds; ++r) {
+    if (!ONE) load(r);
+    const int p0 = (r * kThreads + tid) * kRun;
+    int2 mine = make_int2(0, 0);
+    unsigned sure = 0, equal = 0;
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+      const int p = p0 + i;
+      const bool in = candidate(p);
+      sure |= (p < s.L && (!in || (ask && key[i] > least)) ? 1u : 0u) << i;
+      equal |= (in && ask && key[i] == least ? 1u : 0u) << i;
+    }
+    mine.x = __popc(sure);
+    mine.y = __popc(equal);
+    int2 all;
+    const int2 before = scan2(mine, s_part, &all);
+    int x = base.x + before.x, y = base.y + before.y;
+    for (unsigned on = sure | equal; on; on &= on - 1) {
+      const int i = __ffs(on) - 1;
+      const bool eq = (equal >> i) & 1;
+      if (!eq || y < left) kept[x + min(y, left)] = p0 + i;
+      x += eq ? 0 : 1;
+      y += eq ? 1 : 0;
+    }
+    base.x += all.x;
+    base.y += all.y;
+  }
+}
+
+template <typename DT, int D>
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictParams a) {
+  constexpr int EPL = 16 / (int)sizeof(DT);
+  typedef __attribute__((__vector_size__(16))) int i32x4;
+  __shared__ int s_src[kMove], s_dst[kMove / 16];      // page * page_size + slot; of a 16-slot run
+  const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv, tid = threadIdx.x;
+  const Seq s = seq_of(a, slot);
+  const int i0 = blockIdx.y * kMove, n = min(s.n - i0, kMove);
+  if (n <= 0) return;
+  const int ps = a.page_size;
+  if (tid < kMove) {
+    int at = 0;
+    if (tid < n) {
+      const int p = a.kept[((size_t)s.b * a.Hkv + g) * (unsigned)a.dst_slots + i0 + tid];
+      at = page_at(a, a.page_table + (size_t)s.b * a.max_pages, a.max_pages, p) * ps + (p & (ps - 1));
+    }
+    s_src[tid] = at;
+  } else if (tid < kMove + kMove / 16) {
+    const int p = i0 + 16 * (tid - kMove);
+    s_dst[tid - kMove] = page_at(a, a.dst_table + (size_t)s.b * a.dst_pages, a.dst_pages, p) * ps + (p & (ps - 1));
+  }
+  __syncthreads();
+  auto page = [&](int at) { return (size_t)(at >> a.log2ps) * a.Hkv + g; };
+  if (tid < n) {
+    const int from = s_src[tid], to = s_dst[tid >> 4] + (tid & 15);
+    a.mass[page(to) * ps + (to & (ps - 1))] = a.mass[page(from) * ps + (from & (ps - 1))];
+  }
+  // keys: 16 bytes of a slot's run of 32 channels
+  constexpr int KPS = 32 / EPL;                        // of a run
+  constexpr int KN = kMove * D / EPL / 256;
+  const DT* kc = reinterpret_cast<const DT*>(a.k_cache);
+  const DT* vc = reinterpret_cast<const DT*>(a.v_cache);
+  i32x4 k[KN];
+#pragma unroll
+  for (int x = 0; x < KN; ++x) {
+    const int e = tid + 256 * x, c = e % KPS, i = e / KPS % kMove, sl = e / KPS / kMove;
+    if (i < n) {
+      const int at = s_src[i];
+      k[x] = ld16<i32x4>(kc + (page(at) * (D / 32) + sl) * ps * 32 + (at & (ps - 1)) * 32 + EPL * c);
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < KN; ++x) {
+    const int e = tid + 256 * x, c = e % KPS, i = e / KPS % kMove, sl = e / KPS / kMove;
+    if (i < n) {
+      const int at = s_dst[i >> 4] + (i & 15);
+      *reinterpret_cast<i32x4*>(reinterpret_cast<DT*>(a.k_cache) + (page(at) * (D / 32) + sl) * ps * 32 +
+                                (at & (ps - 1)) * 32 + EPL * c) = k[x];
+    }
+  }
+  // values: a channel's run of EPL slots
+  constexpr int RUNS = kMove / EPL;
+  for (int e = tid; e < RUNS * D; e += 256) {
+    const int r = e % RUNS, ch = e / RUNS, i = r * EPL;
+    if (i >= n) continue;
+    DT v[EPL];
+#pragma unroll
+    for (int c = 0; c < EPL; ++c) {
+      const int at = s_src[i + c];                     // behind n: page 0, not used
+      v[c] = vc[(page(at) * D + ch) * ps + (at & (ps - 1))];
+    }
+    const int to = s_dst[i >> 4] + (i & 15);
+    DT* dst = reinterpret_cast<DT*>(a.v_cache) + (page(to) * D + ch) * ps + (to & (ps - 1));
+    if (i + EPL <= n) {
+      struct Run { DT e[EPL]; } run;
+#pragma unroll
+      for (int c = 0; c < EPL; ++c) run.e[c] = v[c];
+      *reinterpret_cast<i32x4*>(dst) = __builtin_bit_cast(i32x4, run);
+    } else {
+#pragma unroll
+      for (int c = 0; c < EPL; ++c)
+        if (i + c < n) dst[c] = v[c];
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_kv_evict(const EvictLaunch& L, hipStream_t st) {
+  EvictParams p{};
+  static_cast<EvictLaunch&>(p) = L;
+  p.log2ps = __builtin_ctz(L.page_size);
+  p.slots = table_slots(L.max_pages, L.page_size);
+  p.dst_slots = table_slots(L.dst_pages, L.page_size);
+  const int sg = L.n_seq * L.Hkv;
+  trace_begin(st);
+  if (p.slots <= kThreads * kRun)
+    hipLaunchKernelGGL(evict_select_kernel<true>, dim3(sg), dim3(kThreads), 0, st, p);
+  else
+    hipLaunchKernelGGL(evict_select_kernel<false>, dim3(sg), dim3(kThreads), 0, st, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  trace_mark(st);
+  auto move = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(sg, (p.dst_slots + kMove - 1) / kMove), dim3(256), 0, st, p);
+  };
+  if (L.dtype_bf16) {
+    if (L.D == 128) move(evict_move_kernel<bf16, 128>); else move(evict_move_kernel<bf16, 64>);
+  } else {
+    if (L.D == 128) move(evict_move_kernel<float, 128>); else move(evict_move_kernel<float, 64>);
+  }
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  trace_mark(st);
+  return hipSuccess;
+}
+
+}  // namespace ipdv

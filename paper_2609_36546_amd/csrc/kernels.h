@@ -245,6 +245,103 @@ int attn_q8_grid(int cus);     // workgroups on so many compute units: a multipl
 size_t attn_q8_workspace(int n_seq, int Hq, int Hkv, int D, int max_q);
 hipError_t launch_attn_q8(const AttnQ8Launch& L, hipStream_t st);
 
+// ---- attention with modified scores, and the weights that it gives ----
+struct ScoreMod {
+  float softcap;               // 0: off
+  int window;                  // 0: off
+  const float* slopes;         // [Hq] or null
+  const int32_t* first_key;    // [T] or null
+  const int32_t* end_key;      // [T] or null
+};
+
+struct AttnMaskedLaunch {
+  const void* q;
+  int64_t q_stride;
+  const void* k_new;           // null: the window is in the cache
+  const void* v_new;
+  void* k_cache;
+  void* v_cache;
+  const int32_t* page_table;
+  int max_pages;
+  const int32_t* ctx_lens;
+  const int32_t* cu_q;
+  const int32_t* seq_ids;
+  int n_seq, max_q;
+  ScoreMod mod;
+  void* out;
+  float* lse;
+  int Hq, Hkv, D, page_size, num_pages;
+  float scale;
+  bool dtype_bf16;
+  void* workspace;
+  // attn_mass: lse is read, weights are summed per key
+  const float* mass_in = nullptr;
+  float* mass_out = nullptr;
+  float decay = 0.f;
+};
+
+// The window's keys and values into the pages.
+hipError_t launch_append_window(const AttnMaskedLaunch& L, hipStream_t st);
+// Row tiles and their pieces that a call's grid has at most.
+int attn_masked_units(int n_seq, int Hq, int Hkv, int max_q, int max_pages, int page_size, int window, bool ends);
+size_t attn_masked_workspace(int n_seq, int Hq, int Hkv, int D, int max_q, int max_pages, int page_size, int window,
+                             bool ends);
+hipError_t launch_attn_masked(const AttnMaskedLaunch& L, hipStream_t st);
+hipError_t launch_attn_mass(const AttnMaskedLaunch& L, hipStream_t st);
+
+// ---- eviction ----
+struct EvictLaunch {
+  void* k_cache;
+  void* v_cache;
+  float* mass;
+  const int32_t* page_table;
+  int max_pages;
+  const int32_t* dst_table;
+  int dst_pages;
+  const int32_t* ctx_lens;
+  const int32_t* keep;
+  const int32_t* seq_ids;
+  int n_seq, n_sink, n_recent;
+  int32_t* new_lens;
+  int32_t* kept;
+  int Hkv, D, page_size, num_pages;
+  bool dtype_bf16;
+};
+
+hipError_t launch_kv_evict(const EvictLaunch& L, hipStream_t st);
+
+// ---- the verdict on drafts by probabilities ----
+struct Filters {
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+};
+
+struct DraftLaunch {
+  const void* target;          // [T, V]
+  int64_t target_stride;
+  const void* draft;           // [T, V] or null
+  int64_t draft_stride;
+  int T, V, B;
+  const int32_t* prop_tok;
+  const int32_t* cu_q;
+  const float* u_accept;
+  const float* u_draw;
+  Filters tf, df;
+  int32_t eos_id;
+  int32_t* n_acc;
+  int32_t* token;
+  uint8_t* finished;
+  float* p_accept;
+  float* logp;
+  bool dtype_bf16;
+  void* workspace;
+};
+
+size_t verify_drafts_workspace(int T, int V, int B, bool target_filters, bool draft_filters);
+hipError_t launch_verify_drafts(const DraftLaunch& L, hipStream_t st);
+
 // ---- filtered draws from logits ----
 struct SampleLogitsLaunch {
   const void* logits;          // [M, V]
@@ -259,10 +356,13 @@ struct SampleLogitsLaunch {
   float* logp;
   bool dtype_bf16;
   void* workspace;
+  unsigned long long* cuts = nullptr;      // launch_logit_cuts: [M] order numbers of the last entry kept
 };
 
 size_t sample_logits_workspace(int M, int V);
 hipError_t launch_sample_logits(const SampleLogitsLaunch& L, hipStream_t st);
+// The rows' cuts alone: u, token and logp are not used.
+hipError_t launch_logit_cuts(const SampleLogitsLaunch& L, hipStream_t st);
 
 // ---- verdict scan ----
 struct ScanLaunch {

@@ -1,0 +1,252 @@
+// What attn_masked.hip and attn_mass.hip share: a window's rows, what each sees, the
+// key operands of a block of 32 keys, and the modified scores.
+#pragma once
+
+#include <climits>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace ipdv {
+namespace {
+
+constexpr int kBlk = 32;                // keys per block
+
+struct WindowParams {
+  const void* q;
+  long q_stride;
+  const void* k_cache;
+  const int32_t* page_table;
+  const int32_t* ctx_lens;
+  const int32_t* cu_q;
+  const int32_t* seq_ids;
+  const int32_t* first_key;
+  const int32_t* end_key;
+  const float* slopes;
+  int max_pages, Hq, Hkv, G, log2ps, num_pages, n_seq, max_q, slots;
+  int window;          // keys that a row sees at most (INT_MAX: all)
+  float scale2;        // scale log2(e); with a cap 2 log2(e) scale / cap
+  float cap2;          // cap log2(e), 0: no cap
+  float cap_scale;     // scale / cap
+};
+inline WindowParams window_params(const AttnMaskedLaunch& L) {
+  WindowParams p{};
+  p.q = L.q;
+  p.q_stride = L.q_stride;
+  p.k_cache = L.k_cache;
+  p.page_table = L.page_table;
+  p.ctx_lens = L.ctx_lens;
+  p.cu_q = L.cu_q;
+  p.seq_ids = L.seq_ids;
+  p.first_key = L.mod.first_key;
+  p.end_key = L.mod.end_key;
+  p.slopes = L.mod.slopes;
+  p.max_pages = L.max_pages;
+  p.Hq = L.Hq;
+  p.Hkv = L.Hkv;
+  p.G = L.Hq / L.Hkv;
+  p.log2ps = __builtin_ctz(L.page_size);
+  p.num_pages = L.num_pages;
+  p.n_seq = L.n_seq;
+  p.max_q = L.max_q;
+  p.slots = table_slots(L.max_pages, L.page_size);
+  p.window = L.mod.window > 0 ? L.mod.window : INT_MAX;
+  const float log2e = 1.4426950408889634f, cap = L.mod.softcap;
+  p.cap2 = cap * log2e;
+  p.cap_scale = cap > 0.f ? L.scale / cap : 0.f;
+  p.scale2 = cap > 0.f ? 2.f * log2e * (L.scale / cap) : L.scale * log2e;
+  return p;
+}
+
+// Values that all lanes share and no kernel writes: scalar loads.
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+__device__ __forceinline__ ScalarInts scalar(const int32_t* p) { return (ScalarInts)(uintptr_t)p; }
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+struct Seq {
+  int b, L, r0, kb, rows;
+};
+__device__ __forceinline__ Seq seq_of(const WindowParams& a, int slot) {
+  Seq s;
+  s.b = a.seq_ids ? scalar(a.seq_ids)[slot] : slot;
+  s.L = min(max(scalar(a.ctx_lens)[s.b], 0), a.slots);
+  s.r0 = scalar(a.cu_q)[s.b];
+  s.kb = min(max(scalar(a.cu_q)[s.b + 1] - s.r0, 0), a.max_q);
+  s.rows = s.kb * a.G;
+  return s;
+}
+
+// What a row sees, and what biases its scores.
+struct RowInfo {
+  int lo, hi;          // keys lo .. hi - 1; none: INT_MAX, 0
+  int pos;
+  float slope2;        // slope log2(e)
+};
+__device__ __forceinline__ RowInfo row_info(const WindowParams& a, const Seq& s, int i, int head) {
+  RowInfo r;
+  r.pos = s.L + i;
+  r.lo = a.first_key ? max(a.first_key[s.r0 + i], 0) : 0;
+  r.hi = min(a.end_key ? a.end_key[s.r0 + i] : r.pos + 1, s.L + s.kb);
+  r.lo = max(r.lo, r.pos - a.window + 1);
+  if (r.lo >= r.hi) {
+    r.lo = INT_MAX;
+    r.hi = 0;
+  }
+  r.slope2 = a.slopes ? a.slopes[head] * 1.44269504f : 0.f;
+  return r;
+}
+// Over the wave's rows: what some row sees, and what every row sees.
+struct Span {
+  int lo, hi, all_lo, all_hi;
+  __device__ __forceinline__ bool sees(int t0) const { return t0 + kBlk > lo && t0 < hi; }
+  __device__ __forceinline__ bool whole(int t0) const { return t0 >= all_lo && t0 + kBlk <= all_hi; }
+};
+template <int QT> __device__ __forceinline__ Span span_of(const RowInfo (&row)[QT]) {
+  Span s{row[0].lo, row[0].hi, row[0].lo, row[0].hi};
+#pragma unroll
+  for (int t = 1; t < QT; ++t) {
+    s.lo = min(s.lo, row[t].lo);
+    s.hi = max(s.hi, row[t].hi);
+    s.all_lo = max(s.all_lo, row[t].lo);
+    s.all_hi = min(s.all_hi, row[t].hi);
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) {       // the lanes of a group of 16 hold the rows
+    s.lo = min(s.lo, __shfl_xor(s.lo, o, kWave));
+    s.hi = max(s.hi, __shfl_xor(s.hi, o, kWave));
+    s.all_lo = max(s.all_lo, __shfl_xor(s.all_lo, o, kWave));
+    s.all_hi = min(s.all_hi, __shfl_xor(s.all_hi, o, kWave));
+  }
+  return {uni(s.lo), uni(s.hi), uni(s.all_lo), uni(s.all_hi)};
+}
+
+// (page, head) of the two 16-slot parts of a block, and where in the page they
+// begin; entries are clamped into the pool.
+struct Parts {
+  int p0, p1;
+  __device__ __forceinline__ void look_up(const WindowParams& a, ScalarInts pt, int t0, int g) {
+    auto at = [&](int i) {
+      return min(max(pt[min((t0 + 16 * i) >> a.log2ps, a.max_pages - 1)], 0), a.num_pages - 1) * a.Hkv + g;
+    };
+    p0 = at(0);
+    p1 = at(1);
+  }
+  __device__ __forceinline__ unsigned of(int u) const {
+    const int q0 = p0, q1 = p1;
+    return (unsigned)(u ? q1 : q0);
+  }
+};
+
+// ---- operands in registers ----
+template <typename DT, int D> struct Frags;
+template <int D> struct Frags<bf16, D> {
+  bf16x8 k[2][D / 32];
+  bf16x8 v[D / 16];
+  __device__ __forceinline__ bf16x8 kf(int st, int ks) const { return k[st][ks]; }
+  __device__ __forceinline__ bf16x8 vf(int dt) const { return v[dt]; }
+};
+template <int D> struct Frags<float, D> {
+  floatx4 k[2][D / 16];       // lane group j: channels j D / 4 .. of a key
+  floatx4 v[D / 16][2];
+};
+
+template <typename DT, int D>
+__device__ __forceinline__ void load_keys(const WindowParams& a, Frags<DT, D>& f, int t0, const Parts& parts) {
+  const int lane = lane_id(), c16 = lane & 15, j = lane >> 4, ps = 1 << a.log2ps;
+  const int kgrp = 8 * (c16 >> 2);               // both sub-tiles' keys lie in one 16-slot part
+  const int slot = ((t0 + (kgrp & 16)) & (ps - 1)) + (kgrp & 15) + (c16 & 3);
+  const DT* base = reinterpret_cast<const DT*>(a.k_cache) + (size_t)parts.of(kgrp >> 4) * (unsigned)(ps * D);
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    if constexpr (sizeof(DT) == 2) {
+#pragma unroll
+      for (int ks = 0; ks < D / 32; ++ks) f.k[s][ks] = ld16<bf16x8>(base + (unsigned)((ks * ps + slot + 4 * s) * 32 + 8 * j));
+    } else {
+      const int d0 = j * (D / 4);
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c)
+        f.k[s][c] = ld16<floatx4>(base + (unsigned)((d0 / 32 * ps + slot + 4 * s) * 32 + (d0 & 31) + 4 * c));
+    }
+  }
+}
+template <typename DT, int D>
+__device__ __forceinline__ void load_values(const WindowParams& a, const void* v_cache, Frags<DT, D>& f, int t0, const Parts& parts) {
+  const int lane = lane_id(), c16 = lane & 15, j = lane >> 4, ps = 1 << a.log2ps;
+  const int slot = ((t0 + 16 * (j >> 1)) & (ps - 1)) + 8 * (j & 1);
+  const DT* base = reinterpret_cast<const DT*>(v_cache) + (size_t)parts.of(j >> 1) * (unsigned)(ps * D);
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) {
+    const DT* p = base + (unsigned)((16 * dt + c16) * ps + slot);
+    if constexpr (sizeof(DT) == 2) {
+      f.v[dt] = ld16<bf16x8>(p);
+    } else {
+      f.v[dt][0] = ld16<floatx4>(p);
+      f.v[dt][1] = ld16<floatx4>(p + 4);
+    }
+  }
+}
+
+// ---- one block ----
+template <typename DT, int D, int QT> struct Queries;
+template <int D, int QT> struct Queries<bf16, D, QT> { bf16x8 q[QT][D / 32]; };
+template <int D, int QT> struct Queries<float, D, QT> { floatx4 q[QT][D / 16]; };
+
+template <typename DT, int D, int QT, class F>
+__device__ __forceinline__ void scores(const F& f, const Queries<DT, D, QT>& Q, floatx4 (&s)[QT][2]) {
+#pragma unroll
+  for (int t = 0; t < QT; ++t) s[t][0] = s[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+  if constexpr (sizeof(DT) == 2) {
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks)
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const bf16x8 k = f.kf(st, ks);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) s[t][st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, Q.q[t][ks], s[t][st], 0, 0, 0);
+      }
+  } else {
+#pragma unroll
+    for (int ks = 0; ks < D / 4; ++ks)
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+          s[t][st] = __builtin_amdgcn_mfma_f32_16x16x4f32(f.k[st][ks >> 2][ks & 3], Q.q[t][ks >> 2][ks & 3], s[t][st], 0, 0, 0);
+  }
+}
+
+// Raw products to modified scores in log2 units.
+template <typename DT, int QT>
+__device__ __forceinline__ void modify(const WindowParams& a, const RowInfo (&row)[QT], int k0, floatx4 (&s)[QT][2]) {
+  if (a.cap2 != 0.f) {
+    // tanh x = 1 - 2 / (e^2x + 1): infinities give +-1.  Off by 2^-23 of the cap near 0, which
+    // fp32 calls do not have.
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = s[t][i >> 2][i & 3];
+        if constexpr (sizeof(DT) == 2)
+          s[t][i >> 2][i & 3] = fmaf(__builtin_amdgcn_rcpf(fast_exp2(x * a.scale2) + 1.f), -2.f * a.cap2, a.cap2);
+        else
+          s[t][i >> 2][i & 3] = a.cap2 * tanhf(x * a.cap_scale);
+      }
+  } else {
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[t][i >> 2][i & 3] *= a.scale2;
+  }
+  if (a.slopes) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const float d = (float)(row[t].pos - k0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        s[t][i >> 2][i & 3] = fmaf(-row[t].slope2, fabsf(d - (float)i), s[t][i >> 2][i & 3]);
+    }
+  }
+}
+
+}  // namespace
+}  // namespace ipdv

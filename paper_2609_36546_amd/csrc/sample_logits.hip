@@ -50,6 +50,7 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "logit_order.h"
 
 namespace ipdv {
 namespace {
@@ -64,6 +65,7 @@ constexpr double kWidth = 8.0;    // bins per unit of l / T
 constexpr int kCountShift = 45;   // 16384 masses of about 2^30 at most stay below
 constexpr unsigned long long kMassMask = (1ull << kCountShift) - 1;
 typedef unsigned long long u64;
+static_assert(kMaxChunks * kChunk <= 1 << kIndexBits, "an index has 18 bits");
 
 struct ChunkHead {
   double floor_max;   // floor(y) of the chunk's maximum, -inf without a finite logit
@@ -86,10 +88,6 @@ __device__ __forceinline__ ChunkRec chunk_rec(const SampleLogitsLaunch& p, int n
   int* start = reinterpret_cast<int*>(hist + kBins + kList);
   return {hist, hist + kBins, start, reinterpret_cast<ChunkHead*>(start + kBins)};
 }
-
-// Temperatures below act as this: bins and slopes per unit of logit, 8 / T and
-// log2(e) / T, stay finite in fp32.
-constexpr float kLeastTemp = 0x1p-124f;
 
 // A row's parameters; greedy (T = 0) is the top entry at temperature 1.
 struct Row {
@@ -159,25 +157,6 @@ __device__ __forceinline__ int classify(const Row& r, float l, double top, unsig
   }
   *mass = mass_above(x);
   return (int)d;
-}
-
-// Logits as unsigned numbers of the same order, and back to one of equal order.
-__device__ __forceinline__ unsigned key_of(float l) {
-  const unsigned u = __float_as_uint(l == 0.f ? 0.f : l);   // -0 is +0
-  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
-}
-__device__ __forceinline__ float logit_of_key(unsigned key) {
-  return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
-}
-// Order of entries: logit, then the lower index.
-constexpr int kIndexBits = 18;
-static_assert(kMaxChunks * kChunk <= 1 << kIndexBits, "an index has 18 bits");
-__device__ __forceinline__ u64 order_of(float l, int v) {
-  return ((u64)key_of(l) << kIndexBits) | (unsigned)(((1 << kIndexBits) - 1) ^ v);
-}
-__device__ __forceinline__ float logit_of(u64 order) { return logit_of_key((unsigned)(order >> kIndexBits)); }
-__device__ __forceinline__ int index_of(u64 order) {
-  return (int)(((1 << kIndexBits) - 1) ^ (unsigned)(order & ((1 << kIndexBits) - 1)));
 }
 
 template <typename DT>
@@ -688,7 +667,9 @@ struct RowWork {
   }
 };
 
-template <typename DT, bool VEC>
+// CUTS: the row's cut is all that is asked for (0: everything is kept; of a row that
+// nothing can be drawn from, anything).
+template <typename DT, bool VEC, bool CUTS>
 __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int n_chunks) {
   __shared__ Shared S;
   const int m = blockIdx.x, tid = threadIdx.x, lane = lane_id(), w = tid >> 6;
@@ -702,7 +683,7 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
     if (2 * i + side < n_chunks) hist[i] = chunk_rec(p, n_chunks, m, 2 * i + side).hist[t];
   }
   const Row r = row_of(p, m);
-  const double u = (double)p.u[m];
+  const double u = CUTS ? 0.0 : (double)p.u[m];
   const bool filtered = r.k > 0 || r.top_p < 1.f || r.min_p > 0.f;
   if (filtered) {
 #pragma unroll
@@ -741,7 +722,8 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
   }
   __syncthreads();
   if (S.bad) {
-    if (tid == 0) {
+    if (tid == 0 && CUTS) p.cuts[m] = 0;
+    if (tid == 0 && !CUTS) {
       p.token[m] = -1;
       if (p.logp) p.logp[m] = __uint_as_float(0x7fc00000u);
     }
@@ -817,6 +799,10 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
       for (int s = 0; s < n_chunks; ++s) in += S.in_bin[s];
       kept = S.before[bin] + S.edge[bin] * kUnitMass * (double)in;
     }
+  }
+  if constexpr (CUTS) {
+    if (tid == 0) p.cuts[m] = cut;
+    return;
   }
   __syncthreads();
   {
@@ -938,11 +924,13 @@ int chunks_of(int V) { return (V + kChunk - 1) / kChunk; }
 
 size_t sample_logits_workspace(int M, int V) { return (size_t)M * chunks_of(V) * kChunkBytes; }
 
-hipError_t launch_sample_logits(const SampleLogitsLaunch& L, hipStream_t st) {
+namespace {
+
+template <bool CUTS> hipError_t launch(const SampleLogitsLaunch& L, hipStream_t st) {
   const int nc = chunks_of(L.V);
   const int size = L.dtype_bf16 ? 2 : 4;
   const bool vec = ((uintptr_t)L.logits & 15) == 0 && L.stride * size % 16 == 0 && (size_t)L.V * size % 16 == 0;
-  trace_begin(st);
+  if (!CUTS) trace_begin(st);
   auto go = [&](auto kernel, int n) { hipLaunchKernelGGL(kernel, dim3(n), dim3(kThreads), 0, st, L, nc); };
   if (L.dtype_bf16) {
     if (vec) go(chunk_kernel<bf16, true>, L.M * nc); else go(chunk_kernel<bf16, false>, L.M * nc);
@@ -951,16 +939,21 @@ hipError_t launch_sample_logits(const SampleLogitsLaunch& L, hipStream_t st) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  trace_mark(st);
+  if (!CUTS) trace_mark(st);
   if (L.dtype_bf16) {
-    if (vec) go(row_kernel<bf16, true>, L.M); else go(row_kernel<bf16, false>, L.M);
+    if (vec) go(row_kernel<bf16, true, CUTS>, L.M); else go(row_kernel<bf16, false, CUTS>, L.M);
   } else {
-    if (vec) go(row_kernel<float, true>, L.M); else go(row_kernel<float, false>, L.M);
+    if (vec) go(row_kernel<float, true, CUTS>, L.M); else go(row_kernel<float, false, CUTS>, L.M);
   }
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  trace_mark(st);
+  if (!CUTS) trace_mark(st);
   return hipSuccess;
 }
+
+}  // namespace
+
+hipError_t launch_sample_logits(const SampleLogitsLaunch& L, hipStream_t st) { return launch<false>(L, st); }
+hipError_t launch_logit_cuts(const SampleLogitsLaunch& L, hipStream_t st) { return launch<true>(L, st); }
 
 }  // namespace ipdv

@@ -1880,6 +1880,27 @@ hipError_t launch_verify_attn_noalloc(const AttnLaunch& L, const AttnPlan& pl, h
   return launch_verify_attn(l2, pl, st);
 }
 
+hipError_t launch_append_window(const AttnMaskedLaunch& L, hipStream_t st) {
+  AttnParams p{};
+  p.k_new = L.k_new;
+  p.v_new = L.v_new;
+  p.k_cache = L.k_cache;
+  p.v_cache = L.v_cache;
+  p.page_table = L.page_table;
+  p.ctx_lens = L.ctx_lens;
+  p.cu_q = L.cu_q;
+  p.seq_ids = L.seq_ids;
+  p.max_pages = L.max_pages;
+  p.Hkv = L.Hkv;
+  p.page_size = L.page_size;
+  p.log2ps = __builtin_ctz(L.page_size);
+  p.num_pages = L.num_pages;
+  p.n_seq = L.n_seq;
+  p.al16 = 1;
+  if (L.dtype_bf16) return L.D == 64 ? launch_append<bf16, 64>(p, L.max_q, st) : launch_append<bf16, 128>(p, L.max_q, st);
+  return L.D == 64 ? launch_append<float, 64>(p, L.max_q, st) : launch_append<float, 128>(p, L.max_q, st);
+}
+
 hipError_t launch_verify_attn(const AttnLaunch& L, const AttnPlan& pl, hipStream_t st) {
   AttnParams p{};
   p.q = L.q;

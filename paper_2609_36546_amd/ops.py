@@ -105,6 +105,22 @@ def lib() -> ctypes.CDLL:
         L.sample_logits.argtypes = [vp, i64, ci, ci, f32p, f32p, i32p, f32p, f32p, i32p, f32p, ci,
                                     vp, cs, vp]
         L.sample_logits.restype = ci
+        L.ipdv_attn_masked_workspace_size.argtypes = [ci] * 9
+        L.ipdv_attn_masked_workspace_size.restype = cs
+        L.verify_attn_masked.argtypes = [vp, i64, vp, vp, vp, vp, i32p, ci, i32p, i32p, i32p, ci, ci,
+                                         vp, vp, f32p, ci, ci, ci, ci, ci, cf, ci, vp, cs, vp]
+        L.verify_attn_masked.restype = ci
+        L.attn_mass.argtypes = [vp, i64, vp, f32p, i32p, ci, i32p, i32p, i32p, ci, ci, vp, f32p, cf,
+                                f32p, ci, ci, ci, ci, ci, cf, ci, vp]
+        L.attn_mass.restype = ci
+        L.kv_evict.argtypes = [vp, vp, f32p, i32p, ci, i32p, ci, i32p, i32p, i32p, ci, ci, ci, i32p,
+                               i32p, ci, ci, ci, ci, ci, vp]
+        L.kv_evict.restype = ci
+        L.ipdv_verify_drafts_workspace_size.argtypes = [ci] * 5
+        L.ipdv_verify_drafts_workspace_size.restype = cs
+        L.verify_drafts.argtypes = [vp, i64, vp, i64, ci, ci, i32p, i32p, ci, f32p, f32p, vp, vp,
+                                    ctypes.c_int32, i32p, i32p, u8p, f32p, f32p, ci, vp, cs, vp]
+        L.verify_drafts.restype = ci
         L.ipdv_trace_events.argtypes = [ctypes.c_void_p, ci]
         L.ipdv_trace_events.restype = ci
         L.ipdv_trace_count.restype = ci
@@ -963,3 +979,308 @@ def sample_logits(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
                              code, ws, size, _stream(dev))
     _check("sample_logits", st)
     return token, logp
+
+
+# ---------------------------------------------------------------------------
+# Attention with modified scores, the weights it gives and eviction by them, and
+# the verdict on drafts by probabilities.
+
+class _ScoreMod(ctypes.Structure):
+    _fields_ = [("softcap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p),
+                ("first_key", ctypes.c_void_p), ("end_key", ctypes.c_void_p)]
+
+
+class _Filters(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
+                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
+
+
+def _sized(t, name: str, dtype, dev, n: int):
+    """Address of an optional [n] tensor."""
+    if t is None:
+        return None
+    at = _at(t, name, dtype, dev, 1)
+    if t.size(0) != n:
+        raise ValueError(f"{name} must be [{n}]")
+    return at
+
+
+def _score_mod(softcap, window, slopes, first_key, end_key, T, Hq, dev):
+    return _ScoreMod(float(softcap), int(window), _sized(slopes, "slopes", torch.float32, dev, Hq),
+                     _sized(first_key, "first_key", torch.int32, dev, T),
+                     _sized(end_key, "end_key", torch.int32, dev, T))
+
+
+def _paged(k_cache, page_table, dt, dev, D: int, B: int):
+    """Addresses of the key pages and the page table, Hkv, page size, pages and table width."""
+    kc = _at(k_cache, "k_cache", dt, dev, 5)
+    P, Hkv, slices, ps, run = k_cache.shape
+    if run != 32 or slices * 32 != D:
+        raise ValueError("k_cache must be [P,Hkv,D/32,ps,32]")
+    table = _at(page_table, "page_table", torch.int32, dev, 2)
+    n, max_pages = page_table.shape
+    if n != B:
+        raise ValueError("page_table must be [B, maxp]")
+    return kc, table, Hkv, ps, P, max_pages
+
+
+def attn_masked_workspace_size(n_seq, Hq, Hkv, D, max_q, max_pages, page_size, window=0,
+                               has_end_key=False) -> int:
+    return int(lib().ipdv_attn_masked_workspace_size(n_seq, Hq, Hkv, D, max_q, max_pages, page_size,
+                                                     window, 1 if has_end_key else 0))
+
+
+def verify_attn_masked(q, k_new, v_new, k_cache, v_cache, page_table, ctx_lens, cu_q, max_q: int,
+                       softcap: float = 0.0, window: int = 0, slopes=None, first_key=None,
+                       end_key=None, seq_ids=None, n_seq: Optional[int] = None,
+                       scale: Optional[float] = None, out=None, lse=None, workspace=None,
+                       validate: bool = False):
+    """verify_attn_paged with modified scores (see include/ipdv.h): a tanh cap, a
+    sliding window, distance slopes [Hq] float32, and each row's first and end
+    key [T] int32.
+
+    q [T,Hq,D] (bf16 or fp32; rows may be strided), k_new/v_new [T,Hkv,D] or both
+    None (the window is in the cache), k_cache [P,Hkv,D/32,ps,32], v_cache
+    [P,Hkv,D,ps].  lse: a [T,Hq] float32 tensor to write, or True for a new one.
+    validate=True first runs check_page_table on host copies.  Returns out
+    [T,Hq,D], or (out, lse)."""
+    dev, dt = q.device, q.dtype
+    code = _dtype_code(dt)
+    qp, qs, shape = _rows(q, "q", dt, dev, 3)
+    T, Hq, D = shape
+    ctx, cu, ids, n_seq, B = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
+    kc, table, Hkv, ps, P, max_pages = _paged(k_cache, page_table, dt, dev, D, B)
+    vc = _at(v_cache, "v_cache", dt, dev, 4)
+    if v_cache.shape != (P, Hkv, D, ps):
+        raise ValueError("v_cache must be [P,Hkv,D,ps]")
+    kn = vn = None
+    if k_new is not None or v_new is not None:
+        kn, vn = _at(k_new, "k_new", dt, dev, 3), _at(v_new, "v_new", dt, dev, 3)
+        if k_new.shape != (T, Hkv, D) or v_new.shape != (T, Hkv, D):
+            raise ValueError("k_new / v_new must be [T,Hkv,D]")
+    mod = _score_mod(softcap, window, slopes, first_key, end_key, T, Hq, dev)
+    if scale is None:
+        scale = 1.0 / math.sqrt(D)
+    if out is None:
+        out = torch.empty(T, Hq, D, dtype=dt, device=dev)
+    else:
+        _need(out, "out", dt, dev, 3)
+        if out.shape != shape:
+            raise ValueError("out must have q's shape")
+    if lse is True:
+        lse = torch.empty(T, Hq, dtype=torch.float32, device=dev)
+    elif lse is False:
+        lse = None
+    lp = None
+    if lse is not None:
+        lp = _at(lse, "lse", torch.float32, dev, 2)
+        if lse.shape != (T, Hq):
+            raise ValueError("lse must be [T,Hq]")
+    if validate:
+        check_page_table(page_table, ctx_lens, cu_q, max_q, ps, P, seq_ids=seq_ids, n_seq=n_seq,
+                         rows=T, writes=k_new is not None)
+    if T == 0:
+        n_seq = 0
+    if workspace is None:
+        size = max(attn_masked_workspace_size(n_seq, Hq, Hkv, D, max_q, max_pages, ps, int(window),
+                                              end_key is not None), 1)
+        workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        ws = workspace.data_ptr()
+    else:
+        ws, size = _given_workspace(workspace, dev)
+    st = lib().verify_attn_masked(qp, qs, kn, vn, kc, vc, table, max_pages, ctx, cu, ids, n_seq,
+                                  max_q, ctypes.addressof(mod), out.data_ptr(), lp, Hq, Hkv, D, ps,
+                                  P, float(scale), code, ws, size, _stream(dev))
+    _check("verify_attn_masked", st)
+    return out if lse is None else (out, lse)
+
+
+def attn_mass(q, k_cache, lse, page_table, ctx_lens, cu_q, max_q: int, mass=None,
+              decay: float = 1.0, out=None, softcap: float = 0.0, window: int = 0, slopes=None,
+              first_key=None, end_key=None, seq_ids=None, n_seq: Optional[int] = None,
+              scale: Optional[float] = None, validate: bool = False):
+    """The attention weight that every cached key gathers from a window (see
+    include/ipdv.h), added to decay * mass.
+
+    q, k_cache, the batch and the modifiers as in the verify_attn_masked call that
+    gave lse [T,Hq]; mass [P,Hkv,ps] float32 is updated in place, or written to
+    `out` (mass None: there is none yet).  Returns the updated tensor."""
+    dev, dt = q.device, q.dtype
+    code = _dtype_code(dt)
+    qp, qs, (T, Hq, D) = _rows(q, "q", dt, dev, 3)
+    ctx, cu, ids, n_seq, B = _window_args(ctx_lens, cu_q, seq_ids, n_seq, dev)
+    kc, table, Hkv, ps, P, max_pages = _paged(k_cache, page_table, dt, dev, D, B)
+    lp = _at(lse, "lse", torch.float32, dev, 2)
+    if lse.shape != (T, Hq):
+        raise ValueError("lse must be [T,Hq]")
+    mod = _score_mod(softcap, window, slopes, first_key, end_key, T, Hq, dev)
+    if out is None:
+        if mass is None:
+            raise ValueError("mass or out must be given")
+        out = mass
+    mp = None
+    for t, name in ((mass, "mass"), (out, "out")):
+        if t is not None:
+            mp = _at(t, name, torch.float32, dev, 3)
+            if t.shape != (P, Hkv, ps):
+                raise ValueError(f"{name} must be [P,Hkv,ps]")
+    if scale is None:
+        scale = 1.0 / math.sqrt(D)
+    if validate:
+        check_page_table(page_table, ctx_lens, cu_q, max_q, ps, P, seq_ids=seq_ids, n_seq=n_seq,
+                         rows=T)
+    st = lib().attn_mass(qp, qs, kc, lp, table, max_pages, ctx, cu, ids, n_seq, max_q,
+                         ctypes.addressof(mod), None if mass is None else mass.data_ptr(),
+                         float(decay), mp, Hq, Hkv, D, ps, P, float(scale), code, _stream(dev))
+    _check("attn_mass", st)
+    return out
+
+
+def kv_evict(k_cache, v_cache, mass, page_table, dst_table, ctx_lens, keep, n_sink: int = 0,
+             n_recent: int = 0, seq_ids=None, n_seq: Optional[int] = None, new_lens=None, kept=None,
+             validate: bool = False):
+    """Sequences cut to their heaviest keys, moved to dst_table's pages (see
+    include/ipdv.h).
+
+    k_cache [P,Hkv,D/32,ps,32], v_cache [P,Hkv,D,ps] (bf16 or fp32), mass
+    [P,Hkv,ps] float32, page_table [B,maxp], dst_table [B,maxd], ctx_lens and keep
+    [B] int32.  validate=True first checks both tables on host copies.  Returns
+    (new_lens [B], kept [B,Hkv,maxd*ps]) int32."""
+    dev, dt = k_cache.device, k_cache.dtype
+    code = _dtype_code(dt)
+    ctx = _at(ctx_lens, "ctx_lens", torch.int32, dev, 1)
+    B = ctx_lens.size(0)
+    if k_cache.dim() != 5:
+        raise ValueError("k_cache must be [P,Hkv,D/32,ps,32]")
+    D = 32 * k_cache.shape[2]
+    kc, table, Hkv, ps, P, max_pages = _paged(k_cache, page_table, dt, dev, D, B)
+    vc = _at(v_cache, "v_cache", dt, dev, 4)
+    mp = _at(mass, "mass", torch.float32, dev, 3)
+    if v_cache.shape != (P, Hkv, D, ps) or mass.shape != (P, Hkv, ps):
+        raise ValueError("v_cache must be [P,Hkv,D,ps] and mass [P,Hkv,ps]")
+    dst = _at(dst_table, "dst_table", torch.int32, dev, 2)
+    if dst_table.shape[0] != B:
+        raise ValueError("dst_table must be [B, maxd]")
+    max_dst = dst_table.shape[1]
+    kp = _at(keep, "keep", torch.int32, dev, 1)
+    if keep.size(0) != B:
+        raise ValueError("keep must be [B]")
+    ids = None
+    if seq_ids is not None:
+        ids = _at(seq_ids, "seq_ids", torch.int32, dev, 1)
+    most = B if seq_ids is None else seq_ids.size(0)
+    if n_seq is None:
+        n_seq = most
+    elif n_seq > most:
+        raise ValueError("n_seq exceeds the batch")
+    slots = (B, Hkv, max_dst * ps)
+    if new_lens is None:
+        new_lens = torch.empty(B, dtype=torch.int32, device=dev)
+    elif _sized(new_lens, "new_lens", torch.int32, dev, B) is None:
+        raise ValueError("new_lens must be [B]")
+    if kept is None:
+        kept = torch.empty(*slots, dtype=torch.int32, device=dev)
+    else:
+        _need(kept, "kept", torch.int32, dev, 3)
+        if kept.shape != slots:
+            raise ValueError("kept must be [B,Hkv,maxd*ps]")
+    if validate:
+        _check_evict(page_table, dst_table, ctx_lens, keep, ps, P, seq_ids, n_seq)
+    st = lib().kv_evict(kc, vc, mp, table, max_pages, dst, max_dst, ctx, kp, ids, n_seq, int(n_sink),
+                        int(n_recent), new_lens.data_ptr(), kept.data_ptr(), Hkv, D, ps, P, code,
+                        _stream(dev))
+    _check("kv_evict", st)
+    return new_lens, kept
+
+
+def _check_evict(page_table, dst_table, ctx_lens, keep, ps, P, seq_ids, n_seq):
+    """check_page_table of both tables, and that no page is both read and written."""
+    import numpy as np
+
+    host = lambda t: t.detach().cpu().numpy().astype(np.int64)  # noqa: E731
+    ctx, want = host(ctx_lens), host(keep)
+    B = ctx.shape[0]
+    zero = np.zeros(B + 1, np.int32)
+    check_page_table(page_table, ctx.astype(np.int32), zero, 1, ps, P, seq_ids=seq_ids, n_seq=n_seq)
+    n = np.clip(want, 0, np.minimum(ctx, dst_table.shape[1] * ps))
+    # the kept rows as windows of empty sequences: pages that they write are their own
+    cu = np.concatenate([[0], np.cumsum(n)]).astype(np.int32)
+    check_page_table(dst_table, zero[:B], cu, max(1, int(n.max(initial=0))), ps, P, seq_ids=seq_ids,
+                     n_seq=n_seq)
+    ids = np.arange(n_seq) if seq_ids is None else host(seq_ids)[:n_seq]
+    src, dst = host(page_table), host(dst_table)
+    read = {int(p) for b in ids for p in src[b, : -(-int(ctx[b]) // ps)]}
+    for b in ids:
+        for p in dst[b, : -(-int(n[b]) // ps)]:
+            if int(p) in read:
+                raise IpdvError("kv_evict", -1, f"sequence {b}: page {int(p)} is read and written")
+
+
+def verify_drafts_workspace_size(T, V, B, target_filtered=False, draft_filtered=False) -> int:
+    return int(lib().ipdv_verify_drafts_workspace_size(T, V, B, 1 if target_filtered else 0,
+                                                       1 if draft_filtered else 0))
+
+
+def verify_drafts(target_logits, draft_logits, prop_tok, cu_q, u_accept, u_draw, temperature=None,
+                  top_k=None, top_p=None, min_p=None, draft_temperature=None, draft_top_k=None,
+                  draft_top_p=None, draft_min_p=None, eos_id: int = -1, outs=None, workspace=None):
+    """The verdict on drafted tokens by the two models' probabilities (see
+    include/ipdv.h).
+
+    target_logits, draft_logits [T,V] (bf16 or fp32; rows may be strided;
+    draft_logits None: the drafts are certain), prop_tok [T] int32 (-1: no draft),
+    cu_q [B+1] int32, u_accept [T] and u_draw [B] float32 in [0, 1); the target's
+    and the draft's filters per row, as in sample_logits.  Returns dict n_acc,
+    token [B] int32, finished [B] uint8, p_accept [T] float32, logp [B] float32
+    (`outs` may hold these to be written)."""
+    dev, dt = target_logits.device, target_logits.dtype
+    code = _dtype_code(dt)
+    tp, ts, (T, V) = _rows(target_logits, "target_logits", dt, dev, 2)
+    dp, ds = None, V
+    if draft_logits is not None:
+        dp, ds, shape = _rows(draft_logits, "draft_logits", dt, dev, 2)
+        if shape != (T, V):
+            raise ValueError("draft_logits must have target_logits' shape")
+    elif any(t is not None for t in (draft_temperature, draft_top_k, draft_top_p, draft_min_p)):
+        raise ValueError("the draft's filters need draft_logits")
+    f32, i32 = torch.float32, torch.int32
+    cu = _at(cu_q, "cu_q", i32, dev, 1)
+    B = cu_q.size(0) - 1
+    if B < 0:
+        raise ValueError("cu_q must be [B+1]")
+    need = lambda t, name, dtype, n: _sized(t, name, dtype, dev, n)  # noqa: E731
+    for t, name in ((prop_tok, "prop_tok"), (u_accept, "u_accept"), (u_draw, "u_draw")):
+        if t is None:
+            raise TypeError(f"{name} must be a torch.Tensor")
+    xp, ua, ud = need(prop_tok, "prop_tok", i32, T), need(u_accept, "u_accept", f32, T), need(u_draw, "u_draw", f32, B)
+    tf = _Filters(need(temperature, "temperature", f32, T), need(top_k, "top_k", i32, T),
+                  need(top_p, "top_p", f32, T), need(min_p, "min_p", f32, T))
+    df = _Filters(need(draft_temperature, "draft_temperature", f32, T),
+                  need(draft_top_k, "draft_top_k", i32, T), need(draft_top_p, "draft_top_p", f32, T),
+                  need(draft_min_p, "draft_min_p", f32, T))
+    if outs is None:
+        outs = {}
+    made = {}
+    for name, dtype, n in (("n_acc", i32, B), ("token", i32, B), ("finished", torch.uint8, B),
+                           ("p_accept", f32, T), ("logp", f32, B)):
+        t = outs.get(name)
+        if t is None:
+            t = torch.empty(n, dtype=dtype, device=dev)
+        else:
+            need(t, name, dtype, n)
+        made[name] = t
+    if workspace is None:
+        size = max(verify_drafts_workspace_size(
+            T, V, B, any(t is not None for t in (top_k, top_p, min_p)),
+            any(t is not None for t in (draft_top_k, draft_top_p, draft_min_p))), 1)
+        workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        ws = workspace.data_ptr()
+    else:
+        ws, size = _given_workspace(workspace, dev)
+    st = lib().verify_drafts(tp, ts, dp, ds, T, V, xp, cu, B, ua, ud, ctypes.addressof(tf),
+                             ctypes.addressof(df), int(eos_id), made["n_acc"].data_ptr(),
+                             made["token"].data_ptr(), made["finished"].data_ptr(),
+                             made["p_accept"].data_ptr(), made["logp"].data_ptr(), code, ws, size,
+                             _stream(dev))
+    _check("verify_drafts", st)
+    return made

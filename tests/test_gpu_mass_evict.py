@@ -1,0 +1,258 @@
+"""Attention weights summed per cached key, and eviction by them, against 64-bit plain
+forms; their refusals."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_36546_amd import ops
+from tests import masked_reference as ref
+from tests.masked_reference import BF16, F32, Batch, f64, limits
+
+RAGGED = [(0, 1), (5, 0), (15, 2), (16, 16), (700, 3), (100, 13), (31, 33)]
+
+
+def dev(x, t=np.int32):
+    return None if x is None else torch.from_numpy(np.ascontiguousarray(x, t)).cuda()
+
+
+def masses(b, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    return torch.rand(b.kc.shape[0], b.Hkv, b.ps, generator=g)
+
+
+def check_mass(b, got, lse, before, decay, mod, seqs=None, first=None, end=None):
+    """Every slot of the pool: what the sequences' positions gather, and the others as they were."""
+    got, want = f64(got), f64(before if before is not None else got)
+    err = np.zeros_like(want)
+    old = None if before is None else f64(before)
+    for i in range(len(b.ctx)) if seqs is None else seqs:
+        L, k, r = int(b.ctx[i]), int(b.k[i]), b.rows(i)
+        lo, hi = limits(L, k, mod.get("window", 0), None if first is None else first[r], None if end is None else end[r])
+        slopes = None if mod.get("slopes") is None else f64(mod["slopes"])
+        w, e = ref.weights(f64(b.q[r]), b.K[i], f64(lse[r]), L, b.scale, lo, hi, mod.get("softcap", 0.0), slopes)
+        for p in range(L + k):
+            page, slot = int(b.table[i, p // b.ps]), p % b.ps
+            was = decay * old[page, :, slot] if old is not None and p < L else 0.0
+            want[page, :, slot] = was + w[p]
+            err[page, :, slot] = e[p] + 2.0 ** -23 * (was + w[p])
+    assert (np.abs(got - want) <= err).all(), np.nanmax(np.abs(got - want) / np.maximum(err, 1e-30))
+
+
+def appended(b, **mod):
+    """The window into the cache, and its lse."""
+    return ops.verify_attn_masked(b.q.cuda(), b.k_new.cuda(), b.v_new.cuda(), b.kc, b.vc, *b.args, lse=True, **mod)[1]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("Hq,Hkv,D,ps", [(4, 2, 64, 16), (3, 1, 128, 32), (32, 4, 128, 16), (5, 5, 64, 64)])
+@pytest.mark.parametrize("mod", [{}, dict(softcap=8.0), dict(window=40), dict(softcap=30.0, slopes=True)])
+def test_mass(dt, Hq, Hkv, D, ps, mod):
+    b = Batch(RAGGED, Hq, Hkv, D, ps, dt, seed=Hq)
+    mod = dict(mod)
+    if "slopes" in mod:
+        mod["slopes"] = dev(2.0 ** -np.arange(1.0, Hq + 1), np.float32)
+    lse = appended(b, **mod)
+    m = masses(b)
+    got = ops.attn_mass(b.q.cuda(), b.kc, lse, *b.args, mass=m.cuda(), decay=0.5, **mod)
+    check_mass(b, got, lse, m, 0.5, mod)
+    # the same out of place, and without earlier masses
+    out = m.cuda()
+    same = ops.attn_mass(b.q.cuda(), b.kc, lse, *b.args, mass=m.cuda(), decay=0.5, out=out, **mod)
+    assert same is out and torch.equal(same, got)
+    out = torch.full_like(out, 3.0)
+    ops.attn_mass(b.q.cuda(), b.kc, lse, *b.args, out=out, **mod)
+    check_mass(b, out, lse, torch.full_like(m, 3.0), 0.0, mod)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("windows", [[(0, 1)], [(1500, 1), (3, 1)], [(0, 300), (77, 20)], [(640, 9)]])
+@pytest.mark.parametrize("ranged", [False, True])
+def test_mass_of_lengths_and_ranges(dt, windows, ranged):
+    b = Batch(windows, 16, 2, 64, 16, dt, seed=3)
+    rng = np.random.default_rng(1)
+    n = np.repeat(b.ctx + b.k, b.k)
+    first, end = (rng.integers(-3, n + 2), rng.integers(0, n + 9)) if ranged else (None, None)
+    mod = dict(first_key=dev(first), end_key=dev(end))
+    lse = appended(b, **mod)
+    got = ops.attn_mass(b.q.cuda(), b.kc, lse, *b.args, out=torch.zeros(b.kc.shape[0], 2, 16, device="cuda"), **mod)
+    check_mass(b, got, lse, torch.zeros(got.shape), 0.0, {}, first=first, end=end)
+    # a row's weights are one: the masses of a sequence are its rows that see a key, times the heads
+    rows = np.isfinite(f64(lse)).sum()
+    assert abs(f64(got).sum() - rows) < 1e-4 * max(rows, 1)
+
+
+@pytest.mark.gpu
+def test_mass_of_some_sequences():
+    b = Batch(RAGGED, 4, 2, 64, 16, BF16, seed=5)
+    lse = appended(b)
+    m = masses(b)
+    some = torch.tensor([6, 1, 3], dtype=torch.int32).cuda()
+    got = ops.attn_mass(b.q.cuda(), b.kc, lse, *b.args, mass=m.cuda(), decay=0.9, seq_ids=some)
+    check_mass(b, got, lse, m, 0.9, {}, seqs=[6, 1, 3])
+
+
+# --- eviction ---
+
+def evicted(ctx, n_dst, Hkv, D, ps, dt, seed, keep):
+    """A filled cache with masses, and a destination table in pages of their own."""
+    b = Batch([(n, 0) for n in ctx], Hkv, Hkv, D, ps, dt, seed=seed, extra=sum(-(-n // ps) for n in n_dst) + 2)
+    table = np.full((len(ctx), max(1, max(-(-n // ps) for n in n_dst))), -1, np.int32)
+    at = 0
+    for i, n in enumerate(n_dst):
+        n = -(-n // ps)
+        table[i, :n] = b.free[at: at + n]
+        at += n
+    return b, table, dev(table), dev(np.array(keep))
+
+
+def kept_of(mass, L, n, sink, recent):
+    """The positions kept, ascending: mass [L] float64."""
+    sink = min(sink, n)
+    recent = min(recent, n - sink)
+    free = list(range(sink, L - recent))
+    key = [(-np.inf if np.isnan(mass[p]) else mass[p], -p) for p in free]
+    best = sorted(range(len(free)), key=lambda i: key[i], reverse=True)[: n - sink - recent]
+    return sorted(list(range(sink)) + [free[i] for i in best] + list(range(L - recent, L)))
+
+
+def check_evict(b, table, before, keep, sink, recent, new_lens, kept, mass, seqs=None):
+    k0, v0, m0 = before
+    kh, vh, mh = b.kc.cpu(), b.vc.cpu(), mass.cpu()
+    kx, vx, mx = k0.clone(), v0.clone(), m0.clone()
+    ps = b.ps
+    slots = table.shape[1] * ps
+    for i in range(len(b.ctx)) if seqs is None else seqs:
+        L = int(b.ctx[i])
+        n = max(0, min(int(keep[i]), L, slots))
+        assert int(new_lens[i]) == n
+        p = np.arange(L)
+        for h in range(b.Hkv):
+            want = kept_of(f64(m0)[b.table[i, p // ps], h, p % ps], L, n, sink, recent)
+            got = kept[i, h].cpu().numpy()
+            assert np.array_equal(got[:n], want) and (got[n:] == -1).all()
+            for j, s in enumerate(want):
+                to, tj, fr, fj = int(table[i, j // ps]), j % ps, int(b.table[i, s // ps]), s % ps
+                kx[to, h, :, tj, :], vx[to, h, :, tj], mx[to, h, tj] = k0[fr, h, :, fj, :], v0[fr, h, :, fj], m0[fr, h, fj]
+    bits = lambda t: t.view(torch.int16 if t.element_size() == 2 else torch.int32)  # noqa: E731
+    for got, want in ((kh, kx), (vh, vx), (mh, mx)):
+        assert torch.equal(bits(got), bits(want))          # slots behind the kept ones, too
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("Hkv,D,ps", [(2, 64, 16), (3, 128, 32), (1, 64, 64), (2, 128, 16)])
+@pytest.mark.parametrize("sink,recent", [(0, 0), (4, 32), (1, 1000)])
+def test_evict(dt, Hkv, D, ps, sink, recent):
+    ctx, keep = [0, 1, 17, 130, 333, 64, 200, 90], [3, 0, 16, 64, 200, 64, -2, 1]
+    n = [max(0, min(a, c)) for a, c in zip(keep, ctx)]
+    b, table, dst, dkeep = evicted(ctx, n, Hkv, D, ps, dt, 1, keep)
+    m = masses(b, 2)
+    g = np.random.default_rng(4)
+    m[torch.from_numpy(g.random(m.shape) < 0.2)] = 0.25                  # equal masses
+    m[torch.from_numpy(g.random(m.shape) < 0.05)] = float("nan")
+    m[torch.from_numpy(g.random(m.shape) < 0.05)] = -1.5
+    m[torch.from_numpy(g.random(m.shape) < 0.03)] = -0.0
+    m[torch.from_numpy(g.random(m.shape) < 0.03)] = 0.0
+    m[torch.from_numpy(g.random(m.shape) < 0.02)] = float("inf")
+    before = b.kc.cpu(), b.vc.cpu(), m.clone()
+    mass = m.cuda()
+    new_lens, kept = ops.kv_evict(b.kc, b.vc, mass, b.args[0], dst, b.args[1], dkeep, sink, recent, validate=True)
+    check_evict(b, table, before, keep, sink, recent, new_lens, kept, mass)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("L,n", [(16384, 9000), (16400, 5), (40000, 12345), (1023, 1022)])
+def test_evict_of_long_sequences(L, n):
+    """Lengths around what one round of threads holds; masses of few values."""
+    b, table, dst, dkeep = evicted([L], [n], 1, 64, 64, BF16, 3, [n])
+    m = torch.round(8 * masses(b, 5)) / 8
+    before = b.kc.cpu(), b.vc.cpu(), m.clone()
+    mass = m.cuda()
+    wide = torch.full((1, 700), -1, dtype=torch.int32, device="cuda")
+    wide[:, : b.table.shape[1]] = b.args[0]
+    new_lens, kept = ops.kv_evict(b.kc, b.vc, mass, wide, dst, b.args[1], dkeep, 4, 64)
+    check_evict(b, table, before, [n], 4, 64, new_lens, kept, mass)
+
+
+@pytest.mark.gpu
+def test_evict_some_sequences_into_tables_that_hold_less():
+    ctx, keep = [100, 60, 48, 77], [90, 60, 20, 70]
+    b, table, dst, dkeep = evicted(ctx, [32, 32, 20, 32], 2, 64, 16, BF16, 6, keep)
+    assert table.shape[1] == 2
+    m = masses(b, 1)
+    before = b.kc.cpu(), b.vc.cpu(), m.clone()
+    mass = m.cuda()
+    some = torch.tensor([3, 0, 2], dtype=torch.int32).cuda()
+    kept = torch.full((4, 2, 32), 9, dtype=torch.int32, device="cuda")
+    new_lens = torch.full((4,), 9, dtype=torch.int32, device="cuda")
+    ops.kv_evict(b.kc, b.vc, mass, b.args[0], dst, b.args[1], dkeep, 2, 5, seq_ids=some, new_lens=new_lens, kept=kept)
+    check_evict(b, table, before, keep, 2, 5, new_lens, kept, mass, seqs=[3, 0, 2])
+    assert (kept[1] == 9).all() and int(new_lens[1]) == 9
+
+
+@pytest.mark.gpu
+def test_validate_names_pages_that_are_read_and_written():
+    b, table, dst, dkeep = evicted([40, 40], [20, 20], 2, 64, 16, BF16, 6, [20, 20])
+    mass = masses(b).cuda()
+    bad = table.copy()
+    bad[1, 0] = b.table[0, 2]
+    with pytest.raises(ops.IpdvError, match="read and written"):
+        ops.kv_evict(b.kc, b.vc, mass, b.args[0], dev(bad), b.args[1], dkeep, validate=True)
+    bad = table.copy()
+    bad[1, 0] = bad[0, 0]
+    with pytest.raises(ops.IpdvError, match="written by"):
+        ops.kv_evict(b.kc, b.vc, mass, b.args[0], dev(bad), b.args[1], dkeep, validate=True)
+    for kw in (dict(mass=mass[:, :1]), dict(keep=dkeep[:1]), dict(dst_table=dst[:1]), dict(v_cache=b.vc.float()),
+               dict(new_lens=dkeep[:1]), dict(kept=torch.zeros(2, 2, 5, dtype=torch.int32, device="cuda"))):
+        good = dict(k_cache=b.kc, v_cache=b.vc, mass=mass, page_table=b.args[0], dst_table=dst, ctx_lens=b.args[1], keep=dkeep)
+        with pytest.raises(ValueError):
+            ops.kv_evict(**{**good, **kw})
+    q = torch.zeros(0, 2, 64, dtype=BF16, device="cuda")
+    lse = torch.zeros(0, 2, device="cuda")
+    for kw in (dict(mass=None), dict(mass=mass[:1]), dict(lse=lse[:, :1]), dict(out=mass.half())):
+        good = dict(q=q, k_cache=b.kc, lse=lse, page_table=b.args[0], ctx_lens=b.args[1], cu_q=b.args[2], max_q=1, mass=mass)
+        with pytest.raises(ValueError):
+            ops.attn_mass(**{**good, **kw})
+
+
+# --- refusals (no GPU) ---
+
+def c_mass(mod=None, **kw):
+    a = dict(q=16, qs=256, kc=16, lse=16, pt=16, mp=4, ctx=16, cu=16, n=2, mq=3, mi=16, decay=1.0, mo=16, Hq=4, Hkv=2, D=64,
+             ps=16, P=8, scale=0.125, dtype=1)
+    a.update(kw)
+    m = ops._ScoreMod(**mod) if mod else None
+    return ops.lib().attn_mass(a["q"], a["qs"], a["kc"], a["lse"], a["pt"], a["mp"], a["ctx"], a["cu"], None, a["n"], a["mq"],
+                               ops.ctypes.addressof(m) if m else None, a["mi"], a["decay"], a["mo"], a["Hq"], a["Hkv"],
+                               a["D"], a["ps"], a["P"], a["scale"], a["dtype"], None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(q=None), -1), (dict(kc=None), -1), (dict(lse=None), -1), (dict(mo=None), -1), (dict(ctx=None), -1), (dict(Hq=5), -1),
+    (dict(mq=0), -1), (dict(n=-1), -1), (dict(scale=-1.0), -1), (dict(qs=255), -1), (dict(decay=-0.1), -1),
+    (dict(decay=float("inf")), -1), (dict(mod=dict(window=-1)), -1), (dict(mod=dict(softcap=-1.0)), -1), (dict(D=96), -2),
+    (dict(ps=8), -2), (dict(dtype=2), -2), (dict(q=8), -2), (dict(kc=8), -2), (dict(mp=1 << 20), -2), (dict(n=0, q=None), 0)])
+def test_mass_refusals(kw, status):
+    assert c_mass(**kw) == status
+    assert (ops.lib().ipdv_last_error() != b"") == (status != 0)
+
+
+def c_evict(**kw):
+    a = dict(kc=16, vc=16, m=16, pt=16, mp=4, dt=16, md=4, ctx=16, keep=16, n=2, sink=0, recent=0, nl=16, kept=16, Hkv=2, D=64,
+             ps=16, P=8, dtype=1)
+    a.update(kw)
+    return ops.lib().kv_evict(a["kc"], a["vc"], a["m"], a["pt"], a["mp"], a["dt"], a["md"], a["ctx"], a["keep"], None, a["n"],
+                              a["sink"], a["recent"], a["nl"], a["kept"], a["Hkv"], a["D"], a["ps"], a["P"], a["dtype"], None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(kc=None), -1), (dict(vc=None), -1), (dict(m=None), -1), (dict(dt=None), -1), (dict(keep=None), -1),
+    (dict(nl=None), -1), (dict(kept=None), -1), (dict(n=-1), -1), (dict(sink=-1), -1), (dict(recent=-1), -1), (dict(md=0), -1),
+    (dict(mp=0), -1), (dict(Hkv=0), -1), (dict(P=0), -1), (dict(D=32), -2), (dict(ps=24), -2), (dict(dtype=7), -2),
+    (dict(kc=8), -2), (dict(m=8), -2), (dict(mp=1 << 20), -2), (dict(md=1 << 20), -2), (dict(P=1 << 28), -2),
+    (dict(n=0, kc=None), 0)])
+def test_evict_refusals(kw, status):
+    assert c_evict(**kw) == status
+    assert (ops.lib().ipdv_last_error() != b"") == (status != 0)
