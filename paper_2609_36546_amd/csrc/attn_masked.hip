@@ -19,9 +19,10 @@
 // Masks.  A row's range [first, end) is a pair of bounds in its lane.  A wave knows
 // the union of its rows' ranges, which it walks, and their intersection: blocks
 // inside it need no mask.  In the others a value that is not finite must not reach
-// rows that do not see it, and a probability of zero does not keep it out.  Eight
-// more products with zeros find out whether the block holds one (NaN then); if so,
-// its keys are added one at a time, to the rows that see them.
+// rows that do not see it, and a probability of zero does not keep it out.  So sums that have
+// become not finite are taken anew, from the first key, with such values taken out and NaN
+// for the rows that see them.  (A branch inside the walk would cost it a copy of the sums: 163
+// registers instead of 96 with one tile per wave.)
 //
 // Work split.  A workgroup takes a piece of the keys of one row tile; tiles of
 // a window that has few are cut into more pieces (split_of), joined by a second
@@ -64,7 +65,7 @@ __device__ __forceinline__ Split split_of(const MaskedParams& a, const Seq& s, i
   p.nt = (s.rows + tile_rows - 1) / tile_rows;
   // blocks of a tile at most: up to the window's end, or of the sliding window of
   // the tile's positions (which a range's end may lie behind, if it is given)
-  long nb = ((long)s.L + s.kb + kBlk - 1) / kBlk;
+  long nb = (s.end + kBlk - 1) / kBlk;
   if (!a.end_key) nb = min(nb, ((long)a.window + tile_rows / a.G + 1 + 2 * kBlk) / kBlk);
   p.per = max(a.per * p.nt, a.walk);
   p.np = (int)((nb + p.per - 1) / p.per);
@@ -83,10 +84,6 @@ struct Rows {
     const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      m[t] = -INFINITY;
-      l[t] = 0.f;
-#pragma unroll
-      for (int dt = 0; dt < D / 16; ++dt) acc[t][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
       const int pr = min(pr0 + 16 * t + c16, pr_last), i = pr / a.G, h = g * a.G + pr - i * a.G;   // behind the last: its copies
       row[t] = row_info(a, s, i, h);
       const DT* qr = reinterpret_cast<const DT*>(a.q) + (size_t)(s.r0 + i) * a.q_stride + (size_t)h * D;
@@ -105,13 +102,35 @@ struct Rows {
       for (int ks = 0; ks < (int)(sizeof(Q.q[0]) / 16); ++ks) asm volatile("" : "+v"(Q.q[t][ks]));
   }
 
-  // One block.  `masked`: some row does not see all of it.
-  template <class F> __device__ __forceinline__ void block(const MaskedParams& a, const F& f, int t0, bool masked) {
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      m[t] = -INFINITY;
+      l[t] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) acc[t][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  // Whether some sum of this lane is not finite.
+  __device__ __forceinline__ bool odd() const {
+    float x = 0.f;
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x = fmaf(acc[t][dt][e], 0.f, x);
+    return x != x;
+  }
+
+  // One block.  `masked`: some row does not see all of it.  CAREFUL: its values may be not finite.
+  template <bool CAREFUL, class F>
+  __device__ __forceinline__ void block(const MaskedParams& a, const F& f, int t0, bool masked) {
     floatx4 s[QT][2];
     scores<DT, D, QT>(f, Q, s);
-    weigh(a, f, s, t0, masked);
+    weigh<CAREFUL>(a, f, s, t0, masked);
   }
-  template <class F>
+  template <bool CAREFUL, class F>
   __device__ __forceinline__ void weigh(const MaskedParams& a, const F& f, floatx4 (&s)[QT][2], int t0, bool masked) {
     const int k0 = t0 + 8 * (lane_id() >> 4);         // the lane's first key
     modify<DT, QT>(a, row, k0, s);
@@ -164,15 +183,9 @@ struct Rows {
           p[0][t][i] = static_cast<bf16>(x);
           if constexpr (PT == 2) p[1][t][i] = static_cast<bf16>(x - static_cast<float>(p[0][t][i]));
         }
-      if (masked) {
-        floatx4 z = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.vf(dt), bf16x8{}, z, 0, 0, 0);
-        const float any = z[0] + z[1] + z[2] + z[3];
-        if (__any(any != any)) {
-          one_by_one(f, p, t0);
-          return;
-        }
+      if constexpr (CAREFUL) {
+        without_odd(f, p, t0);
+        return;
       }
 #pragma unroll
       for (int dt = 0; dt < D / 16; ++dt) {
@@ -191,16 +204,9 @@ struct Rows {
           s[t][i >> 2][i & 3] = x;
           l[t] += x;
         }
-      if (masked) {
-        float z = 0.f;
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) z = fmaf(f.v[dt][i >> 2][i & 3], 0.f, z);
-        if (__any(z != z)) {
-          one_by_one(f, &s, t0);
-          return;
-        }
+      if constexpr (CAREFUL) {
+        without_odd(f, s, t0);
+        return;
       }
 #pragma unroll
       for (int dt = 0; dt < D / 16; ++dt)
@@ -212,42 +218,52 @@ struct Rows {
     }
   }
 
-  // The block's values key by key, each to the rows that see it.
-  template <class F, class P> __device__ __forceinline__ void one_by_one(const F& f, const P* p, int t0) {
-    const int j = lane_id() >> 4;
-#pragma unroll 1
-    for (int kk = 0; kk < kBlk; ++kk) {
-      const int mine = kk - 8 * j;               // of the lane's eight, if it is one of them
-      asm volatile("" : : : "memory");           // operands read anew: kept over the loop, they would cost the walk its registers
+  // A block with values that are not finite: they are taken out, and what rows that see
+  // them have of their channels becomes NaN: those are found by a product of "is not finite" and
+  // "is seen", in zeros and ones.
+  template <class F, class P> __device__ __forceinline__ void without_odd(const F& f, const P& p, int t0) {
+    const int k0 = t0 + 8 * (lane_id() >> 4);
 #pragma unroll
-      for (int dt = 0; dt < D / 16; ++dt) {
-        __builtin_amdgcn_sched_barrier(0);
+    for (int dt = 0; dt < D / 16; ++dt) {
+      __builtin_amdgcn_sched_barrier(0);         // one channel tile after the other: registers
+      floatx4 odd[QT];
+#pragma unroll
+      for (int t = 0; t < QT; ++t) odd[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (sizeof(DT) == 2) {
+        bf16x8 v = f.vf(dt), o;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float x = static_cast<float>(v[i]);
+          const bool is = !(fabsf(x) < INFINITY);
+          o[i] = static_cast<bf16>(is ? 1.f : 0.f);
+          v[i] = static_cast<bf16>(is ? 0.f : x);
+        }
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-          floatx4 r = {0.f, 0.f, 0.f, 0.f};
-          if constexpr (sizeof(DT) == 2) {
-            bf16x8 v = f.vf(dt);
+          bf16x8 see;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i == mine ? v[i] : static_cast<bf16>(0.f);
+          for (int i = 0; i < 8; ++i) see[i] = static_cast<bf16>(k0 + i >= row[t].lo && k0 + i < row[t].hi ? 1.f : 0.f);
+          odd[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(o, see, odd[t], 0, 0, 0);
 #pragma unroll
-            for (int n = 0; n < PT; ++n) {
-              bf16x8 w;
+          for (int n = 0; n < PT; ++n) acc[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[n][t], acc[t][dt], 0, 0, 0);
+        }
+      } else {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) w[i] = i == mine ? p[n][t][i] : static_cast<bf16>(0.f);
-              r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w, r, 0, 0, 0);
-            }
-          } else {
-            float v = 0.f, w = 0.f;
+        for (int i = 0; i < 8; ++i) {
+          const float x = f.v[dt][i >> 2][i & 3];
+          const bool is = !(fabsf(x) < INFINITY);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              v = i == mine ? f.v[dt][i >> 2][i & 3] : v;
-              w = i == mine ? (*p)[t][i >> 2][i & 3] : w;
-            }
-            r = __builtin_amdgcn_mfma_f32_16x16x4f32(v, w, r, 0, 0, 0);
+          for (int t = 0; t < QT; ++t) {
+            const float see = k0 + i >= row[t].lo && k0 + i < row[t].hi ? 1.f : 0.f;
+            odd[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(is ? 1.f : 0.f, see, odd[t], 0, 0, 0);
+            acc[t][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(is ? 0.f : x, p[t][i >> 2][i & 3], acc[t][dt], 0, 0, 0);
           }
-          if (t0 + kk >= row[t].lo && t0 + kk < row[t].hi) acc[t][dt] += r;
         }
       }
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[t][dt][e] = odd[t][e] > 0.f ? __uint_as_float(0x7fc00000u) : acc[t][dt][e];
     }
   }
 
@@ -311,6 +327,22 @@ struct Rows {
   }
 };
 
+// What some row of the workgroup sees.
+__device__ __forceinline__ Span join_spans(const Span& mine, int (&s_span)[kWaves][2]) {
+  if (lane_id() == 0) {
+    s_span[threadIdx.x / kWave][0] = mine.lo;
+    s_span[threadIdx.x / kWave][1] = mine.hi;
+  }
+  __syncthreads();
+  Span all = mine;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    all.lo = min(all.lo, uni(s_span[i][0]));
+    all.hi = max(all.hi, uni(s_span[i][1]));
+  }
+  return all;
+}
+
 // A workgroup's piece: the blocks b0 .. b1 - 1 of a tile.
 struct Piece {
   int b0, b1;
@@ -331,12 +363,15 @@ __device__ __forceinline__ size_t part_row_of(const MaskedParams& a, const Split
   return ((size_t)blockIdx.x * a.units + (size_t)tile * sp.np + piece) * tile_rows;
 }
 
-// Few rows: the four waves take every fourth block of the piece.
-template <typename DT, int D, int QT>
-__global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void masked_keys_kernel(MaskedParams a) {
-  constexpr int kRows = 16 * QT, kTile = (D / 16) * kWave, PT = sizeof(DT) == 2 ? 2 : 1;
-  __shared__ floatx4 s_acc[2][kTile];
+// Operands straight into registers.  Few rows (OWN false): the four waves take every fourth
+// block of the piece.  More in fp32 (OWN): rows of their own, and the same blocks, which the
+// first to ask leaves in the vector cache.
+template <typename DT, int D, int QT, bool OWN>
+__global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys_kernel(MaskedParams a) {
+  constexpr int kRows = (OWN ? kWaves : 1) * 16 * QT, kStep = OWN ? 1 : kWaves, kTile = (D / 16) * kWave, PT = sizeof(DT) == 2 ? 2 : 1;
+  __shared__ floatx4 s_acc[2][OWN ? 1 : kTile];
   __shared__ float s_ml[2][32];
+  __shared__ int s_span[kWaves][2];
   if ((int)blockIdx.x >= a.n_seq * a.Hkv) return;
   const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv;
   const Seq s = seq_of(a, slot);
@@ -345,39 +380,52 @@ __global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void masked_keys_kern
   const int tile = blockIdx.y / sp.np, piece = blockIdx.y - tile * sp.np;
   if (tile >= sp.nt) return;
   const int pr0 = tile * kRows, pr_last = min(pr0 + kRows, s.rows) - 1;
+  const int wv = uni(threadIdx.x / kWave), wr0 = OWN ? pr0 + 16 * QT * wv : pr0;
   Rows<DT, D, QT, PT> R;
-  R.begin(a, s, g, pr0, pr_last);
-  const Span all = span_of<QT>(R.row);
+  R.begin(a, s, g, wr0, pr_last);
+  const Span mine = span_of<QT>(R.row);
   Piece p;
-  if (!piece_of(a, sp, all, tile, piece, p)) return;
-  const int wv = uni(threadIdx.x / kWave);
+  if (!piece_of(a, sp, OWN ? join_spans(mine, s_span) : mine, tile, piece, p)) return;
   const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
-  const int first = p.b0 + wv;
-  if (first < p.b1) {
+  int first = p.b0 + (OWN ? 0 : wv), last = p.b1;
+  if (OWN) {
+    first = max(first, mine.lo / kBlk);
+    last = wr0 > pr_last ? 0 : min(last, (mine.hi + kBlk - 1) / kBlk);
+  }
+  auto walk = [&](auto careful) __attribute__((always_inline)) {
+    constexpr bool CAREFUL = decltype(careful)::value;
+    R.reset();
+    if (first >= last) return;
     Parts parts;
     parts.look_up(a, pt, first * kBlk, g);
     Frags<DT, D> f;
     load_keys<DT, D>(a, f, first * kBlk, parts);
     load_values<DT, D>(a, a.v_cache, f, first * kBlk, parts);
-    parts.look_up(a, pt, (first + kWaves) * kBlk, g);
-    for (int n = first; n < p.b1; n += kWaves) {
+    parts.look_up(a, pt, (first + kStep) * kBlk, g);
+    for (int n = first; n < last; n += kStep) {
       const int t0 = n * kBlk;
       // the next keys are asked for once the scores have used theirs, the next
       // values once the products have
       floatx4 sc[QT][2];
       scores<DT, D, QT>(f, R.Q, sc);
-      const bool more = n + kWaves < p.b1;
+      const bool more = n + kStep < last;
       __builtin_amdgcn_sched_barrier(0);
-      if (more) load_keys<DT, D>(a, f, t0 + kWaves * kBlk, parts);
+      if (more) load_keys<DT, D>(a, f, t0 + kStep * kBlk, parts);
       __builtin_amdgcn_sched_barrier(0);
-      R.weigh(a, f, sc, t0, !all.whole(t0));
+      R.template weigh<CAREFUL>(a, f, sc, t0, CAREFUL || !mine.whole(t0));
       __builtin_amdgcn_sched_barrier(0);
-      if (more) load_values<DT, D>(a, a.v_cache, f, t0 + kWaves * kBlk, parts);
-      parts.look_up(a, pt, t0 + 2 * kWaves * kBlk, g);
+      if (more) load_values<DT, D>(a, a.v_cache, f, t0 + kStep * kBlk, parts);
+      parts.look_up(a, pt, t0 + 2 * kStep * kBlk, g);
       __builtin_amdgcn_sched_barrier(0);
     }
-  }
+  };
+  walk(std::false_type());
+  if (__any(R.odd())) walk(std::true_type());
   R.join_lanes();
+  if (OWN) {
+    R.finish(a, s, g, wr0, pr_last, p.whole, part_row_of(a, sp, tile, piece, kRows) + 16 * QT * wv);
+    return;
+  }
 #pragma unroll
   for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -469,7 +517,7 @@ template <int D, bool WIDE> struct Loader {
 };
 
 template <int D, bool WIDE, int QT>
-__global__ __launch_bounds__(256, QT == 2 ? 2 : 3) void masked_tile_kernel(MaskedParams a) {
+__global__ __launch_bounds__(256, 3) void masked_tile_kernel(MaskedParams a) {
   typedef Loader<D, WIDE> Load;
   constexpr int kRows = 64 * QT;
   __shared__ __attribute__((aligned(1024))) char s_ring[kRing * Load::kUnit];
@@ -487,24 +535,16 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : 3) void masked_tile_kernel(Maske
   Rows<bf16, D, QT, 1> R;
   R.begin(a, s, g, wr0, pr_last);
   const Span mine = span_of<QT>(R.row);
-  if (lane_id() == 0) {
-    s_span[t][0] = mine.lo;
-    s_span[t][1] = mine.hi;
-  }
-  __syncthreads();
-  Span all = mine;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    all.lo = min(all.lo, uni(s_span[i][0]));
-    all.hi = max(all.hi, uni(s_span[i][1]));
-  }
   Piece p;
-  if (!piece_of(a, sp, all, tile, piece, p)) return;
-  if (p.b0 < p.b1) {
-    const bool has_rows = wr0 <= pr_last;
-    const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
-    const Load load(t, 1 << a.log2ps);
-    const LdsFrags<D, WIDE> lane_at(nullptr);
+  if (!piece_of(a, sp, join_spans(mine, s_span), tile, piece, p)) return;
+  const bool has_rows = wr0 <= pr_last;
+  const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
+  const Load load(t, 1 << a.log2ps);
+  const LdsFrags<D, WIDE> lane_at(nullptr);
+  auto walk = [&](auto careful) __attribute__((always_inline)) {
+    constexpr bool CAREFUL = decltype(careful)::value;
+    R.reset();
+    if (p.b0 >= p.b1) return;
     Parts parts;
     // Behind the piece's end its last unit is loaded again, so that every wait has the same count.
     auto look_up = [&](int n) { parts.look_up(a, pt, min(n, p.b1 - 1) * kBlk, g); };
@@ -530,66 +570,71 @@ __global__ __launch_bounds__(256, QT == 2 ? 2 : 3) void masked_tile_kernel(Maske
       if (has_rows && mine.sees(t0)) {
         LdsFrags<D, WIDE> f = lane_at;
         f.at = s_ring + use * Load::kUnit;
-        R.block(a, f, t0, !mine.whole(t0));
+        R.template block<CAREFUL>(a, f, t0, CAREFUL || !mine.whole(t0));
       }
       use = use + 1 == kRing ? 0 : use + 1;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // none may land after the workgroup has gone
-  }
+  };
+  walk(std::false_type());
+  // all waves together, since they share the loads; also the barrier before the ring is filled again
+  if (__syncthreads_or(R.odd())) walk(std::true_type());
   R.join_lanes();
   R.finish(a, s, g, wr0, pr_last, p.whole, part_row_of(a, sp, tile, piece, kRows) + 16 * QT * t);
 }
 
-// Joins the pieces of every tile that was cut: 16 rows per workgroup, 16 lanes per row.
+// Joins the pieces of every tile that was cut: kMergeRows neighbouring rows per workgroup,
+// 16 lanes per row.
+constexpr int kMergeRows = 64;
 template <typename DT, int D>
 __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedParams a, int tile_rows) {
   const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv;
   const Seq s = seq_of(a, slot);
-  const int pr = blockIdx.y * 16 + (int)threadIdx.x / 16;
-  if ((int)blockIdx.y * 16 >= s.rows) return;
-  const Split sp = split_of(a, s, tile_rows);
-  const int tile = pr / tile_rows;
-  if (pr >= s.rows) return;
-  const int n = a.pieces[(size_t)blockIdx.x * a.tiles + tile];
-  if (n == 1) return;
   const int d = ((int)threadIdx.x & 15) * (D / 16);
   constexpr int V = D / 64;                     // of four channels
-  const size_t r0 = part_row_of(a, sp, tile, 0, tile_rows) + pr - tile * tile_rows;
-  float m = -INFINITY, l = 0.f;
-  floatx4 o[V];
+  const Split sp = split_of(a, s, tile_rows);
+  const int last = min((int)(blockIdx.y + 1) * kMergeRows, s.rows);
+  for (int pr = blockIdx.y * kMergeRows + (int)threadIdx.x / 16; pr < last; pr += 16) {
+    const int tile = pr / tile_rows;
+    const int n = a.pieces[(size_t)blockIdx.x * a.tiles + tile];
+    if (n == 1) continue;
+    const size_t r0 = part_row_of(a, sp, tile, 0, tile_rows) + pr - tile * tile_rows;
+    float m = -INFINITY, l = 0.f;
+    floatx4 o[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < V; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int c = 0; c < n; ++c) {
-    const size_t r = r0 + (size_t)c * tile_rows;
-    const float2 ml = a.part_ml[r];
-    floatx4 x[V];
+    for (int c = 0; c < n; ++c) {
+      const size_t r = r0 + (size_t)c * tile_rows;
+      const float2 ml = a.part_ml[r];
+      floatx4 x[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = ld16<floatx4>(a.part_o + r * D + d + 4 * i);
-    const float mx = fmaxf(m, ml.x), mu = mx == -INFINITY ? 0.f : mx;
-    const float u = fast_exp2(m - mu), w = fast_exp2(ml.x - mu);
-    m = mx;
-    l = l * u + ml.y * w;
+      for (int i = 0; i < V; ++i) x[i] = ld16<floatx4>(a.part_o + r * D + d + 4 * i);
+      const float mx = fmaxf(m, ml.x), mu = mx == -INFINITY ? 0.f : mx;
+      const float u = fast_exp2(m - mu), w = fast_exp2(ml.x - mu);
+      m = mx;
+      l = l * u + ml.y * w;
 #pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = o[i] * u + x[i] * w;
+      for (int i = 0; i < V; ++i) o[i] = o[i] * u + x[i] * w;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int i = pr / a.G, h = g * a.G + pr - i * a.G;
+    const size_t r = (size_t)(s.r0 + i) * a.Hq + h;
+    DT* out = reinterpret_cast<DT*>(a.out) + r * D + d;
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      typedef DT __attribute__((ext_vector_type(4))) Four;
+      Four w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = from_f32<DT>(o[c][e] * inv);
+      *reinterpret_cast<Four*>(out + 4 * c) = w;
+    }
+    if (a.lse && (threadIdx.x & 15) == 0) a.lse[r] = (m + fast_log2(l)) * kLn2;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int i = pr / a.G, h = g * a.G + pr - i * a.G;
-  const size_t r = (size_t)(s.r0 + i) * a.Hq + h;
-  DT* out = reinterpret_cast<DT*>(a.out) + r * D + d;
-#pragma unroll
-  for (int c = 0; c < V; ++c) {
-    typedef DT __attribute__((ext_vector_type(4))) Four;
-    Four w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = from_f32<DT>(o[c][e] * inv);
-    *reinterpret_cast<Four*>(out + 4 * c) = w;
-  }
-  if (a.lse && (threadIdx.x & 15) == 0) a.lse[r] = (m + fast_log2(l)) * kLn2;
 }
 
 struct Plan {
-  bool shared;                // masked_tile_kernel
+  bool shared;                // waves of rows of their own
   int qt, tile_rows, tiles, units, per, walk;
   bool cut;                   // some tile may be cut
   size_t part_rows;
@@ -597,14 +642,16 @@ struct Plan {
 Plan plan_of(int n_seq, int Hq, int Hkv, int max_q, long slots, int window, bool ends, bool bf16) {
   Plan p;
   const long rows = (long)max_q * (Hq / Hkv), sg = (long)n_seq * Hkv;
-  p.shared = bf16 && rows > 16;
-  p.qt = p.shared ? (rows > 64 ? 2 : 1) : rows > 16 ? 2 : 1;
+  p.shared = rows > 16;
+  p.qt = p.shared && bf16 && rows > 64 ? 2 : 1;
   p.tile_rows = (p.shared ? 64 : 16) * p.qt;
   p.tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
-  long nb = (slots + max_q + kBlk - 1) / kBlk;
+  long nb = (slots + kBlk - 1) / kBlk;
   if (!ends) nb = std::min(nb, ((long)(window > 0 ? window : INT_MAX) + p.tile_rows / (Hq / Hkv) + 1 + 2 * kBlk) / kBlk);
   p.per = p.shared ? 16 : 8;
-  p.walk = (int)std::clamp(sg * nb / 2048, (long)p.per, 64L);
+  // With rows enough to fill the chip by themselves, walks of up to 48 blocks stay whole: the
+  // merge costs more.
+  p.walk = sg * p.tiles >= 512 ? 48 : (int)std::clamp(sg * nb / 2048, (long)p.per, 64L);
   p.per = (int)std::max((long)p.per, nb / 16384);      // units stay few under a table for millions of tokens
   const int least = std::max(p.per, p.walk);
   p.cut = nb > least;
@@ -669,11 +716,11 @@ hipError_t launch_attn_masked(const AttnMaskedLaunch& L, hipStream_t st) {
     constexpr int D = decltype(dim)::value;
     if constexpr (sizeof(DT) == 2) {
       const bool wide = L.page_size > 16;
-      if (!pl.shared) go(masked_keys_kernel<DT, D, 1>);
+      if (!pl.shared) go(masked_keys_kernel<DT, D, 1, false>);
       else if (pl.qt == 1) { if (wide) go(masked_tile_kernel<D, true, 1>); else go(masked_tile_kernel<D, false, 1>); }
       else { if (wide) go(masked_tile_kernel<D, true, 2>); else go(masked_tile_kernel<D, false, 2>); }
     } else {
-      if (pl.qt == 1) go(masked_keys_kernel<DT, D, 1>); else go(masked_keys_kernel<DT, D, 2>);
+      if (pl.shared) go(masked_keys_kernel<DT, D, 1, true>); else go(masked_keys_kernel<DT, D, 1, false>);
     }
   };
   typedef std::integral_constant<int, 64> D64;
@@ -688,7 +735,7 @@ hipError_t launch_attn_masked(const AttnMaskedLaunch& L, hipStream_t st) {
   trace_mark(st);
   if (pl.cut) {
     auto merge = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3(sg, pl.tiles * pl.tile_rows / 16), dim3(256), 0, st, p, pl.tile_rows);
+      hipLaunchKernelGGL(kernel, dim3(sg, (unsigned)(((long)pl.tiles * pl.tile_rows + kMergeRows - 1) / kMergeRows)), dim3(256), 0, st, p, pl.tile_rows);
     };
     if (L.dtype_bf16) {
       if (L.D == 128) merge(masked_merge_kernel<bf16, 128>); else merge(masked_merge_kernel<bf16, 64>);

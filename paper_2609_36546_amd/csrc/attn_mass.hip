@@ -9,8 +9,8 @@
 //
 // Scores are taken as there, S^T[32 keys x 16 rows] = K . Q^T, a lane holding 8 keys of
 // one row.  Up to 64 rows (attn_mass_few_kernel) a wave keeps all of them in registers and
-// streams keys; with more (attn_mass_many_kernel) it keeps 128 keys and streams rows, the
-// four waves of a workgroup every fourth tile of them.  Weights are added per lane, over the rows
+// streams keys; with more (attn_mass_many_kernel) it keeps a block of keys and streams rows, with
+// many the eight waves of a workgroup every eighth tile of them.  Weights are added per lane, over the rows
 // of a lane's column, and joined over the 16 columns at the end.
 #include <algorithm>
 #include <type_traits>
@@ -43,7 +43,7 @@ __device__ __forceinline__ float sum16(float v) {
 // Lane 8 j + i (i < 8, of the groups j of 16: lane 16 j + i) writes key t0 + 8 j + i.
 __device__ __forceinline__ void put(const MassParams& a, const Seq& s, const Parts& parts, int t0, float sum) {
   const int lane = lane_id(), c16 = lane & 15, j = lane >> 4, key = t0 + 8 * j + c16;
-  if (c16 >= 8 || key >= s.L + s.kb) return;
+  if (c16 >= 8 || key >= s.end) return;
   const int ps = 1 << a.log2ps;
   const size_t at = (size_t)parts.of(j >> 1) * (unsigned)ps + (unsigned)(key & (ps - 1));
   if (a.mass_in && key < s.L) sum = fmaf(a.decay, a.mass_in[at], sum);
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void attn_mass_few_ke
   if ((int)blockIdx.x >= a.n_seq * a.Hkv) return;
   const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv;
   const Seq s = seq_of(a, slot);
-  const int b0 = blockIdx.y * a.per, b1 = min(b0 + a.per, (s.L + s.kb + kBlk - 1) / kBlk);
+  const int b0 = blockIdx.y * a.per, b1 = min(b0 + a.per, (s.end + kBlk - 1) / kBlk);
   const int first = b0 + uni(threadIdx.x / kWave);
   if (first >= b1) return;
   RowTile<DT, D, QT> R;
@@ -134,24 +134,21 @@ __global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void attn_mass_few_ke
   }
 }
 
-template <typename DT, int D, int NB>
-__global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void attn_mass_many_kernel(MassParams a) {
-  __shared__ float s_sum[kWaves][NB][kBlk];
+// RS waves share NB blocks of keys and take every RS-th tile of rows; the others have blocks
+// of their own.
+constexpr int kMany = 8;           // waves
+template <typename DT, int D, int NB, int RS>
+__global__ __launch_bounds__(64 * kMany) void attn_mass_many_kernel(MassParams a) {
+  constexpr int KS = kMany / RS;
+  __shared__ float s_sum[kMany][NB][kBlk];
   if ((int)blockIdx.x >= a.n_seq * a.Hkv) return;
   const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv;
   const Seq s = seq_of(a, slot);
+  const int wv = uni(threadIdx.x / kWave), rs = wv % RS;
   // the first keys, which most rows see, first
-  const int t0 = blockIdx.y * NB * kBlk, end = s.L + s.kb;
-  if (t0 >= end) return;
-  const int wv = uni(threadIdx.x / kWave);
+  const int t0 = (blockIdx.y * KS + wv / RS) * NB * kBlk;
+  if ((int)blockIdx.y * KS * NB * kBlk >= s.end) return;
   const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
-  Frags<DT, D> f[NB];
-#pragma unroll
-  for (int n = 0; n < NB; ++n) {
-    Parts parts;
-    parts.look_up(a, pt, t0 + n * kBlk, g);
-    load_keys<DT, D>(a, f[n], t0 + n * kBlk, parts);
-  }
   float sum[NB][8];
 #pragma unroll
   for (int n = 0; n < NB; ++n)
@@ -161,38 +158,46 @@ __global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void attn_mass_many_k
   const int row0 = a.end_key ? 0 : max(t0 - s.L, 0) * a.G;
   // nor rows that these keys lie in front of the sliding window of
   const long last = (long)t0 + NB * kBlk - 1 + a.window - 1 - s.L;      // the last position that may, counted from L
-  const int rows = (int)min((long)s.rows, (last + 1) * a.G);
+  const int rows = t0 < s.end ? (int)max(min((long)s.rows, (last + 1) * a.G), 0l) : 0;
   const int tiles = (rows + 15) / 16;
-  RowTile<DT, D, 1> R, N;
-  int tile = row0 / 16 + wv;
-  if (tile < tiles) R.load(a, s, g, 0, 16 * tile);
-  for (; tile < tiles; tile += kWaves) {
-    if (tile + kWaves < tiles) N.load(a, s, g, 0, 16 * (tile + kWaves));
-    const Span span = span_of<1>(R.row);
+  int tile = row0 / 16 + rs;
+  if (tile < tiles) {
+    Frags<DT, D> f[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-      const int tn = t0 + n * kBlk;
-      if (span.sees(tn)) {
-        floatx4 sc[1][2];
-        scores<DT, D, 1>(f[n], R.Q, sc);
-        R.add(a, sc, tn, !span.whole(tn), sum[n]);
-      }
+      Parts parts;
+      parts.look_up(a, pt, t0 + n * kBlk, g);
+      load_keys<DT, D>(a, f[n], t0 + n * kBlk, parts);
     }
-    R = N;
+    RowTile<DT, D, 1> R, N;
+    R.load(a, s, g, 0, 16 * tile);
+    for (; tile < tiles; tile += RS) {
+      if (tile + RS < tiles) N.load(a, s, g, 0, 16 * (tile + RS));
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        const int tn = t0 + n * kBlk;
+        if (__any(R.row[0].lo < tn + kBlk && R.row[0].hi > tn)) {
+          floatx4 sc[1][2];
+          scores<DT, D, 1>(f[n], R.Q, sc);
+          R.add(a, sc, tn, !__all(R.row[0].lo <= tn && R.row[0].hi >= tn + kBlk), sum[n]);
+        }
+      }
+      R = N;
+    }
   }
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    const float v = pick(sum[n]);
+    float v = pick(sum[n]);
     const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
-    if (c16 < 8) s_sum[wv][n][8 * j + c16] = v;
-  }
-  __syncthreads();
-  for (int n = wv; n < NB; n += kWaves) {
-    const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
-    float v = 0.f;
-    if (c16 < 8)
+    if constexpr (RS > 1) {
+      if (c16 < 8) s_sum[wv][n][8 * j + c16] = v;
+      __syncthreads();
+      if (rs != n % RS) continue;
+      v = 0.f;
+      if (c16 < 8)
 #pragma unroll
-      for (int i = 0; i < kWaves; ++i) v += s_sum[i][n][8 * j + c16];
+        for (int i = 0; i < RS; ++i) v += s_sum[wv - rs + i][n][8 * j + c16];
+    }
     Parts parts;
     parts.look_up(a, pt, t0 + n * kBlk, g);
     put(a, s, parts, t0 + n * kBlk, v);
@@ -209,20 +214,26 @@ hipError_t launch_attn_mass(const AttnMaskedLaunch& L, hipStream_t st) {
   p.mass_out = L.mass_out;
   p.decay = L.decay;
   const long rows = (long)L.max_q * p.G, sg = (long)L.n_seq * L.Hkv;
-  const long blocks = ((long)p.slots + L.max_q + kBlk - 1) / kBlk;
+  const long blocks = ((long)p.slots + kBlk - 1) / kBlk;
   const unsigned gx = (unsigned)((sg + 7) / 8 * 8);
   p.per = (int)std::max(std::clamp(sg * blocks / 2048, 4L, 32L), (blocks + 65534) / 65535);
   trace_begin(st);
   auto pick = [&](auto dt, auto dim) {
     using DT = decltype(dt);
-    constexpr int D = decltype(dim)::value, NB = sizeof(DT) == 4 ? 2 : 4;
+    constexpr int D = decltype(dim)::value, NB = 1;
     auto few = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, dim3(gx, (unsigned)((blocks + p.per - 1) / p.per)), dim3(256), 0, st, p);
     };
     if (rows <= 16) few(attn_mass_few_kernel<DT, D, 1>);
     else if (rows <= 32) few(attn_mass_few_kernel<DT, D, 2>);
     else if (rows <= 64 && sizeof(DT) == 2) few(attn_mass_few_kernel<DT, D, 4>);
-    else hipLaunchKernelGGL((attn_mass_many_kernel<DT, D, NB>), dim3(gx, (unsigned)((blocks + NB - 1) / NB)), dim3(256), 0, st, p);
+    else {
+      auto many = [&](auto kernel, int at_once) {
+        hipLaunchKernelGGL(kernel, dim3(gx, (unsigned)((blocks + at_once - 1) / at_once)), dim3(64 * kMany), 0, st, p);
+      };
+      if (rows > 512) many(attn_mass_many_kernel<DT, D, NB, kMany>, NB);
+      else many(attn_mass_many_kernel<DT, D, NB, 1>, NB * kMany);
+    }
   };
   typedef std::integral_constant<int, 64> D64;
   typedef std::integral_constant<int, 128> D128;

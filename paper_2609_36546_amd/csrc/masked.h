@@ -65,6 +65,7 @@ __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlan
 
 struct Seq {
   int b, L, r0, kb, rows;
+  int end;             // positions that the table has slots for (all, if the lengths fit it)
 };
 __device__ __forceinline__ Seq seq_of(const WindowParams& a, int slot) {
   Seq s;
@@ -73,6 +74,7 @@ __device__ __forceinline__ Seq seq_of(const WindowParams& a, int slot) {
   s.r0 = scalar(a.cu_q)[s.b];
   s.kb = min(max(scalar(a.cu_q)[s.b + 1] - s.r0, 0), a.max_q);
   s.rows = s.kb * a.G;
+  s.end = min(s.L + s.kb, a.slots);
   return s;
 }
 
@@ -86,7 +88,7 @@ __device__ __forceinline__ RowInfo row_info(const WindowParams& a, const Seq& s,
   RowInfo r;
   r.pos = s.L + i;
   r.lo = a.first_key ? max(a.first_key[s.r0 + i], 0) : 0;
-  r.hi = min(a.end_key ? a.end_key[s.r0 + i] : r.pos + 1, s.L + s.kb);
+  r.hi = min(a.end_key ? a.end_key[s.r0 + i] : r.pos + 1, s.end);
   r.lo = max(r.lo, r.pos - a.window + 1);
   if (r.lo >= r.hi) {
     r.lo = INT_MAX;
