@@ -84,7 +84,7 @@ struct Rows {
     const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      const int pr = min(pr0 + 16 * t + c16, pr_last), i = pr / a.G, h = g * a.G + pr - i * a.G;   // behind the last: its copies
+      const int pr = min(pr0 + 16 * t + c16, pr_last), i = row_of(a, pr), h = g * a.G + pr - i * a.G;   // behind the last: its copies
       row[t] = row_info(a, s, i, h);
       const DT* qr = reinterpret_cast<const DT*>(a.q) + (size_t)(s.r0 + i) * a.q_stride + (size_t)h * D;
       if constexpr (sizeof(DT) == 2) {
@@ -133,7 +133,8 @@ struct Rows {
   template <bool CAREFUL, class F>
   __device__ __forceinline__ void weigh(const MaskedParams& a, const F& f, floatx4 (&s)[QT][2], int t0, bool masked) {
     const int k0 = t0 + 8 * (lane_id() >> 4);         // the lane's first key
-    modify<DT, QT>(a, row, k0, s);
+    const float none[QT] = {};
+    modify<DT, QT>(a, row, none, k0, s);
     if (masked) {
       asm volatile("");                // a branch: else every block is masked
 #pragma unroll
@@ -304,7 +305,7 @@ struct Rows {
       const int pr = pr0 + 16 * t + c16;
       if (pr > pr_last) continue;
       if (whole) {
-        const int i = pr / a.G, h = g * a.G + pr - i * a.G;
+        const int i = row_of(a, pr), h = g * a.G + pr - i * a.G;
         const size_t r = (size_t)(s.r0 + i) * a.Hq + h;
         DT* o = reinterpret_cast<DT*>(a.out) + r * D + 4 * j;
         const float inv = l[t] == 0.f ? 0.f : 1.f / l[t];      // a row without keys: 0
@@ -349,18 +350,18 @@ struct Piece {
   bool whole;
 };
 // False if the tile has no such piece.
-__device__ __forceinline__ bool piece_of(const MaskedParams& a, const Split& sp, const Span& all, int tile, int piece, Piece& p) {
+__device__ __forceinline__ bool piece_of(const MaskedParams& a, const Split& sp, const Span& all, int sg, int tile, int piece, Piece& p) {
   const int blo = all.lo >= all.hi ? 0 : all.lo / kBlk, bhi = all.lo >= all.hi ? 0 : (all.hi + kBlk - 1) / kBlk;
   const int n = max((bhi - blo + sp.per - 1) / sp.per, 1);
   if (piece >= n) return false;
-  if (piece == 0 && threadIdx.x == 0) a.pieces[(size_t)blockIdx.x * a.tiles + tile] = n;
+  if (piece == 0 && threadIdx.x == 0) a.pieces[(size_t)sg * a.tiles + tile] = n;
   p.b0 = blo + piece * sp.per;
   p.b1 = min(p.b0 + sp.per, bhi);
   p.whole = n == 1;
   return true;
 }
-__device__ __forceinline__ size_t part_row_of(const MaskedParams& a, const Split& sp, int tile, int piece, int tile_rows) {
-  return ((size_t)blockIdx.x * a.units + (size_t)tile * sp.np + piece) * tile_rows;
+__device__ __forceinline__ size_t part_row_of(const MaskedParams& a, const Split& sp, int sg, int tile, int piece, int tile_rows) {
+  return ((size_t)sg * a.units + (size_t)tile * sp.np + piece) * tile_rows;
 }
 
 // Operands straight into registers.  Few rows (OWN false): the four waves take every fourth
@@ -372,8 +373,9 @@ __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys
   __shared__ floatx4 s_acc[2][OWN ? 1 : kTile];
   __shared__ float s_ml[2][32];
   __shared__ int s_span[kWaves][2];
-  if ((int)blockIdx.x >= a.n_seq * a.Hkv) return;
-  const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv;
+  const int sg = slot_head_of(a, blockIdx.x, blockIdx.y, gridDim.x);
+  if (sg < 0) return;
+  const int slot = sg / a.Hkv, g = sg - slot * a.Hkv;
   const Seq s = seq_of(a, slot);
   if (s.rows == 0) return;
   const Split sp = split_of(a, s, kRows);
@@ -385,7 +387,7 @@ __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys
   R.begin(a, s, g, wr0, pr_last);
   const Span mine = span_of<QT>(R.row);
   Piece p;
-  if (!piece_of(a, sp, OWN ? join_spans(mine, s_span) : mine, tile, piece, p)) return;
+  if (!piece_of(a, sp, OWN ? join_spans(mine, s_span) : mine, sg, tile, piece, p)) return;
   const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
   int first = p.b0 + (OWN ? 0 : wv), last = p.b1;
   if (OWN) {
@@ -423,7 +425,7 @@ __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys
   if (__any(R.odd())) walk(std::true_type());
   R.join_lanes();
   if (OWN) {
-    R.finish(a, s, g, wr0, pr_last, p.whole, part_row_of(a, sp, tile, piece, kRows) + 16 * QT * wv);
+    R.finish(a, s, g, wr0, pr_last, p.whole, part_row_of(a, sp, sg, tile, piece, kRows) + 16 * QT * wv);
     return;
   }
 #pragma unroll
@@ -435,7 +437,7 @@ __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys
       if (wv < half) R.take(t, s_acc[wv], s_ml[wv]);
       __syncthreads();
     }
-  if (wv == 0) R.finish(a, s, g, pr0, pr_last, p.whole, part_row_of(a, sp, tile, piece, kRows));
+  if (wv == 0) R.finish(a, s, g, pr0, pr_last, p.whole, part_row_of(a, sp, sg, tile, piece, kRows));
 }
 
 // ---- more rows: keys shared through LDS ----
@@ -522,8 +524,9 @@ __global__ __launch_bounds__(256, 3) void masked_tile_kernel(MaskedParams a) {
   constexpr int kRows = 64 * QT;
   __shared__ __attribute__((aligned(1024))) char s_ring[kRing * Load::kUnit];
   __shared__ int s_span[kWaves][2];
-  if ((int)blockIdx.x >= a.n_seq * a.Hkv) return;
-  const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv;
+  const int sg = slot_head_of(a, blockIdx.x, blockIdx.y, gridDim.x);
+  if (sg < 0) return;
+  const int slot = sg / a.Hkv, g = sg - slot * a.Hkv;
   const Seq s = seq_of(a, slot);
   if (s.rows == 0) return;
   const Split sp = split_of(a, s, kRows);
@@ -536,7 +539,7 @@ __global__ __launch_bounds__(256, 3) void masked_tile_kernel(MaskedParams a) {
   R.begin(a, s, g, wr0, pr_last);
   const Span mine = span_of<QT>(R.row);
   Piece p;
-  if (!piece_of(a, sp, join_spans(mine, s_span), tile, piece, p)) return;
+  if (!piece_of(a, sp, join_spans(mine, s_span), sg, tile, piece, p)) return;
   const bool has_rows = wr0 <= pr_last;
   const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
   const Load load(t, 1 << a.log2ps);
@@ -580,7 +583,7 @@ __global__ __launch_bounds__(256, 3) void masked_tile_kernel(MaskedParams a) {
   // all waves together, since they share the loads; also the barrier before the ring is filled again
   if (__syncthreads_or(R.odd())) walk(std::true_type());
   R.join_lanes();
-  R.finish(a, s, g, wr0, pr_last, p.whole, part_row_of(a, sp, tile, piece, kRows) + 16 * QT * t);
+  R.finish(a, s, g, wr0, pr_last, p.whole, part_row_of(a, sp, sg, tile, piece, kRows) + 16 * QT * t);
 }
 
 // Joins the pieces of every tile that was cut: kMergeRows neighbouring rows per workgroup,
@@ -598,7 +601,7 @@ __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedParams a, int t
     const int tile = pr / tile_rows;
     const int n = a.pieces[(size_t)blockIdx.x * a.tiles + tile];
     if (n == 1) continue;
-    const size_t r0 = part_row_of(a, sp, tile, 0, tile_rows) + pr - tile * tile_rows;
+    const size_t r0 = part_row_of(a, sp, blockIdx.x, tile, 0, tile_rows) + pr - tile * tile_rows;
     float m = -INFINITY, l = 0.f;
     floatx4 o[V];
 #pragma unroll
@@ -618,7 +621,7 @@ __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedParams a, int t
       for (int i = 0; i < V; ++i) o[i] = o[i] * u + x[i] * w;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int i = pr / a.G, h = g * a.G + pr - i * a.G;
+    const int i = row_of(a, pr), h = g * a.G + pr - i * a.G;
     const size_t r = (size_t)(s.r0 + i) * a.Hq + h;
     DT* out = reinterpret_cast<DT*>(a.out) + r * D + d;
 #pragma unroll

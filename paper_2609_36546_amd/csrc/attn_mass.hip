@@ -10,7 +10,7 @@
 // Scores are taken as there, S^T[32 keys x 16 rows] = K . Q^T, a lane holding 8 keys of
 // one row.  Up to 64 rows (attn_mass_few_kernel) a wave keeps all of them in registers and
 // streams keys; with more (attn_mass_many_kernel) it keeps a block of keys and streams rows, with
-// many the eight waves of a workgroup every eighth tile of them.  Weights are added per lane, over the rows
+// many the 16 waves of a workgroup every 16th tile of them.  Weights are added per lane, over the rows
 // of a lane's column, and joined over the 16 columns at the end.
 #include <algorithm>
 #include <type_traits>
@@ -53,15 +53,32 @@ __device__ __forceinline__ void put(const MassParams& a, const Seq& s, const Par
 // Queries and what else belongs to the lane's row of a tile.
 template <typename DT, int D, int QT> struct RowTile {
   Queries<DT, D, QT> Q;
+  RowLoads raw[QT];
+  float lse[QT];
   RowInfo row[QT];
-  float lse2[QT];      // lse log2(e)
-  __device__ __forceinline__ void load(const MassParams& a, const Seq& s, int g, int t, int pr0) {
+  float less_lse2[QT]; // -lse log2(e)
+  int at[QT];          // window row
+  // Asked for; `arrive` makes them what the rest works with.  Behind the last row its copies.
+  // Where G is a power of two a whole tile's addresses are a uniform base and an offset that
+  // the lane has in every tile (a product of 64 bits costs as much as a score).
+  __device__ __forceinline__ void ask(const MassParams& a, const Seq& s, int g, int t, int pr0) {
     const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
-    const int pr = min(pr0 + c16, s.rows - 1), i = pr / a.G, h = g * a.G + pr - i * a.G;
-    row[t] = row_info(a, s, i, h);
-    // behind the last row its copies, of weight 0
-    lse2[t] = pr0 + c16 < s.rows ? a.lse[(size_t)(s.r0 + i) * a.Hq + h] * 1.4426950408889634f : INFINITY;
-    const DT* qr = reinterpret_cast<const DT*>(a.q) + (size_t)(s.r0 + i) * a.q_stride + (size_t)h * D;
+    const DT* q = reinterpret_cast<const DT*>(a.q);
+    if (a.log2g >= 0 && pr0 + 16 <= s.rows) {
+      const int i = pr0 >> a.log2g, h = g * a.G + (pr0 & (a.G - 1)), li = c16 >> a.log2g, lh = c16 & (a.G - 1);
+      at[t] = i + li;
+      raw[t].ask(a, s, i, h, li, lh);
+      lse[t] = (a.lse + (size_t)(s.r0 + i) * a.Hq + h)[li * a.Hq + lh];
+      load_row(t, q + (size_t)(s.r0 + i) * a.q_stride + (size_t)h * D + ((size_t)li * a.q_stride + lh * D), j);
+    } else {
+      const int pr = min(pr0 + c16, s.rows - 1), i = row_of(a, pr), h = g * a.G + pr - i * a.G;
+      at[t] = i;
+      raw[t].ask(a, s, i, h);
+      lse[t] = a.lse[(size_t)(s.r0 + i) * a.Hq + h];
+      load_row(t, q + (size_t)(s.r0 + i) * a.q_stride + (size_t)h * D, j);
+    }
+  }
+  __device__ __forceinline__ void load_row(int t, const DT* qr, int j) {
     if constexpr (sizeof(DT) == 2) {
 #pragma unroll
       for (int ks = 0; ks < D / 32; ++ks) Q.q[t][ks] = ld16<bf16x8>(qr + 32 * ks + 8 * j);
@@ -70,15 +87,19 @@ template <typename DT, int D, int QT> struct RowTile {
       for (int c = 0; c < D / 16; ++c) Q.q[t][c] = ld16<floatx4>(qr + j * (D / 4) + 4 * c);
     }
   }
+  __device__ __forceinline__ void arrive(const MassParams& a, const Seq& s, int t, int pr0) {
+    row[t] = raw[t].info(a, s, at[t]);
+    less_lse2[t] = pr0 + (lane_id() & 15) < s.rows ? lse[t] * -1.4426950408889634f : -INFINITY;      // copies: of weight 0
+  }
   // Adds the tiles' weights of a block's keys.
   __device__ __forceinline__ void add(const MassParams& a, floatx4 (&sc)[QT][2], int t0, bool masked, float (&sum)[8]) const {
     const int k0 = t0 + 8 * (lane_id() >> 4);
-    modify<DT, QT>(a, row, k0, sc);
+    modify<DT, QT>(a, row, less_lse2, k0, sc);
 #pragma unroll
     for (int t = 0; t < QT; ++t)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        float w = fast_exp2(sc[t][i >> 2][i & 3] - lse2[t]);
+        float w = fast_exp2(sc[t][i >> 2][i & 3]);
         if (masked) w = k0 + i >= row[t].lo && k0 + i < row[t].hi ? w : 0.f;
         sum[i] += w;
       }
@@ -99,8 +120,9 @@ __device__ __forceinline__ float pick(const float (&sum)[8]) {
 
 template <typename DT, int D, int QT>
 __global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void attn_mass_few_kernel(MassParams a) {
-  if ((int)blockIdx.x >= a.n_seq * a.Hkv) return;
-  const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv;
+  const int sg = slot_head_of(a, blockIdx.x, blockIdx.y, gridDim.x);
+  if (sg < 0) return;
+  const int slot = sg / a.Hkv, g = sg - slot * a.Hkv;
   const Seq s = seq_of(a, slot);
   const int b0 = blockIdx.y * a.per, b1 = min(b0 + a.per, (s.end + kBlk - 1) / kBlk);
   const int first = b0 + uni(threadIdx.x / kWave);
@@ -109,7 +131,10 @@ __global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void attn_mass_few_ke
   Span span{INT_MAX, 0, INT_MAX, 0};
   if (s.rows > 0) {
 #pragma unroll
-    for (int t = 0; t < QT; ++t) R.load(a, s, g, t, 16 * t);
+    for (int t = 0; t < QT; ++t) {
+      R.ask(a, s, g, t, 16 * t);
+      R.arrive(a, s, t, 16 * t);
+    }
     span = span_of<QT>(R.row);
   }
   const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
@@ -134,15 +159,15 @@ __global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void attn_mass_few_ke
   }
 }
 
-// RS waves share NB blocks of keys and take every RS-th tile of rows; the others have blocks
-// of their own.
-constexpr int kMany = 8;           // waves
-template <typename DT, int D, int NB, int RS>
-__global__ __launch_bounds__(64 * kMany) void attn_mass_many_kernel(MassParams a) {
-  constexpr int KS = kMany / RS;
-  __shared__ float s_sum[kMany][NB][kBlk];
-  if ((int)blockIdx.x >= a.n_seq * a.Hkv) return;
-  const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv;
+// RS of W waves share NB blocks of keys and take every RS-th tile of rows; the others have
+// blocks of their own.
+template <typename DT, int D, int NB, int RS, int W>
+__global__ __launch_bounds__(64 * W) void attn_mass_many_kernel(MassParams a) {
+  constexpr int KS = W / RS;
+  __shared__ float s_sum[W][NB][kBlk];
+  const int sg = slot_head_of(a, blockIdx.x, blockIdx.y, gridDim.x);
+  if (sg < 0) return;
+  const int slot = sg / a.Hkv, g = sg - slot * a.Hkv;
   const Seq s = seq_of(a, slot);
   const int wv = uni(threadIdx.x / kWave), rs = wv % RS;
   // the first keys, which most rows see, first
@@ -169,20 +194,32 @@ __global__ __launch_bounds__(64 * kMany) void attn_mass_many_kernel(MassParams a
       parts.look_up(a, pt, t0 + n * kBlk, g);
       load_keys<DT, D>(a, f[n], t0 + n * kBlk, parts);
     }
-    RowTile<DT, D, 1> R, N;
-    R.load(a, s, g, 0, 16 * tile);
-    for (; tile < tiles; tile += RS) {
-      if (tile + RS < tiles) N.load(a, s, g, 0, 16 * (tile + RS));
+    // two tiles in turn: one is asked for while the other is worked on
+    RowTile<DT, D, 1> R[2];
+    auto work = [&](RowTile<DT, D, 1>& r, int at) __attribute__((always_inline)) {
+      r.arrive(a, s, 0, 16 * at);
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         const int tn = t0 + n * kBlk;
-        if (__any(R.row[0].lo < tn + kBlk && R.row[0].hi > tn)) {
+        if (__any(r.row[0].lo < tn + kBlk && r.row[0].hi > tn)) {
           floatx4 sc[1][2];
-          scores<DT, D, 1>(f[n], R.Q, sc);
-          R.add(a, sc, tn, !__all(R.row[0].lo <= tn && R.row[0].hi >= tn + kBlk), sum[n]);
+          scores<DT, D, 1>(f[n], r.Q, sc);
+          r.add(a, sc, tn, !__all(r.row[0].lo <= tn && r.row[0].hi >= tn + kBlk), sum[n]);
         }
       }
-      R = N;
+    };
+    R[0].ask(a, s, g, 0, 16 * tile);
+    for (;;) {
+      R[1].ask(a, s, g, 0, 16 * (tile + RS));     // behind the last tile: its last row, not used
+      __builtin_amdgcn_sched_barrier(0);
+      work(R[0], tile);
+      if ((tile += RS) >= tiles) break;
+      __builtin_amdgcn_sched_barrier(0);
+      R[0].ask(a, s, g, 0, 16 * (tile + RS));
+      __builtin_amdgcn_sched_barrier(0);
+      work(R[1], tile);
+      if ((tile += RS) >= tiles) break;
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 #pragma unroll
@@ -220,7 +257,7 @@ hipError_t launch_attn_mass(const AttnMaskedLaunch& L, hipStream_t st) {
   trace_begin(st);
   auto pick = [&](auto dt, auto dim) {
     using DT = decltype(dt);
-    constexpr int D = decltype(dim)::value, NB = 1;
+    constexpr int D = decltype(dim)::value;
     auto few = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, dim3(gx, (unsigned)((blocks + p.per - 1) / p.per)), dim3(256), 0, st, p);
     };
@@ -228,11 +265,12 @@ hipError_t launch_attn_mass(const AttnMaskedLaunch& L, hipStream_t st) {
     else if (rows <= 32) few(attn_mass_few_kernel<DT, D, 2>);
     else if (rows <= 64 && sizeof(DT) == 2) few(attn_mass_few_kernel<DT, D, 4>);
     else {
-      auto many = [&](auto kernel, int at_once) {
-        hipLaunchKernelGGL(kernel, dim3(gx, (unsigned)((blocks + at_once - 1) / at_once)), dim3(64 * kMany), 0, st, p);
+      auto many = [&](auto kernel, int at_once, int waves) {
+        hipLaunchKernelGGL(kernel, dim3(gx, (unsigned)((blocks + at_once - 1) / at_once)), dim3(64 * waves), 0, st, p);
       };
-      if (rows > 512) many(attn_mass_many_kernel<DT, D, NB, kMany>, NB);
-      else many(attn_mass_many_kernel<DT, D, NB, 1>, NB * kMany);
+      constexpr int RS = sizeof(DT) * D > 256 ? 8 : 16;       // 128 registers do not do for fp32 at D = 128
+      if (rows > 64 * RS) many(attn_mass_many_kernel<DT, D, 1, RS, RS>, 1, RS);
+      else many(attn_mass_many_kernel<DT, D, 1, 1, 4>, 4, 4);
     }
   };
   typedef std::integral_constant<int, 64> D64;

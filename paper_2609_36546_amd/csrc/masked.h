@@ -24,6 +24,7 @@ struct WindowParams {
   const int32_t* end_key;
   const float* slopes;
   int max_pages, Hq, Hkv, G, log2ps, num_pages, n_seq, max_q, slots;
+  int log2g;           // of G, or -1
   int window;          // keys that a row sees at most (INT_MAX: all)
   float scale2;        // scale log2(e); with a cap 2 log2(e) scale / cap
   float cap2;          // cap log2(e), 0: no cap
@@ -45,6 +46,7 @@ inline WindowParams window_params(const AttnMaskedLaunch& L) {
   p.Hq = L.Hq;
   p.Hkv = L.Hkv;
   p.G = L.Hq / L.Hkv;
+  p.log2g = (p.G & (p.G - 1)) ? -1 : __builtin_ctz(p.G);
   p.log2ps = __builtin_ctz(L.page_size);
   p.num_pages = L.num_pages;
   p.n_seq = L.n_seq;
@@ -78,25 +80,54 @@ __device__ __forceinline__ Seq seq_of(const WindowParams& a, int slot) {
   return s;
 }
 
+// The (sequence slot, head) of workgroup x in row y of a grid whose width is a multiple of 8:
+// rows are turned by the heads, since workgroups go to the 8 XCDs in turn.  So the work of one
+// sequence, long or short, is shared out over all of them, and what follows on in
+// y (tiles that read the same keys) stays on one XCD as far as that allows.  (By x alone, masses of
+// eight prompts of 512 to 1024 tokens, 4 heads, kept the CUs busy for 57% of the time.)  -1: none.
+__device__ __forceinline__ int slot_head_of(const WindowParams& a, int x, int y, int width) {
+  const int at = (int)(((unsigned)x + (unsigned)width - (unsigned)y % (unsigned)width * (unsigned)a.Hkv % (unsigned)width) %
+                       (unsigned)width);
+  return at < a.n_seq * a.Hkv ? at : -1;
+}
+
 // What a row sees, and what biases its scores.
 struct RowInfo {
   int lo, hi;          // keys lo .. hi - 1; none: INT_MAX, 0
   int pos;
   float slope2;        // slope log2(e)
 };
-__device__ __forceinline__ RowInfo row_info(const WindowParams& a, const Seq& s, int i, int head) {
-  RowInfo r;
-  r.pos = s.L + i;
-  r.lo = a.first_key ? max(a.first_key[s.r0 + i], 0) : 0;
-  r.hi = min(a.end_key ? a.end_key[s.r0 + i] : r.pos + 1, s.end);
-  r.lo = max(r.lo, r.pos - a.window + 1);
-  if (r.lo >= r.hi) {
-    r.lo = INT_MAX;
-    r.hi = 0;
+// What that takes from memory: loaded without branches (any address, where there is
+// no array), so that it can be under way while other rows are worked on.
+struct RowLoads {
+  int first, end;
+  float slope;
+  // (i and head in a uniform and a lane's part)
+  __device__ __forceinline__ void ask(const WindowParams& a, const Seq& s, int i, int head, int lane_i = 0, int lane_h = 0) {
+    first = (a.first_key ? a.first_key + s.r0 + i : a.cu_q)[a.first_key ? lane_i : 0];
+    end = (a.end_key ? a.end_key + s.r0 + i : a.cu_q)[a.end_key ? lane_i : 0];
+    slope = (a.slopes ? a.slopes + head : reinterpret_cast<const float*>(a.cu_q))[a.slopes ? lane_h : 0];
   }
-  r.slope2 = a.slopes ? a.slopes[head] * 1.44269504f : 0.f;
-  return r;
+  __device__ __forceinline__ RowInfo info(const WindowParams& a, const Seq& s, int i) const {
+    RowInfo r;
+    r.pos = s.L + i;
+    r.lo = max(a.first_key ? max(first, 0) : 0, r.pos - a.window + 1);
+    r.hi = min(a.end_key ? end : r.pos + 1, s.end);
+    if (r.lo >= r.hi) {
+      r.lo = INT_MAX;
+      r.hi = 0;
+    }
+    r.slope2 = a.slopes ? slope * 1.44269504f : 0.f;
+    return r;
+  }
+};
+__device__ __forceinline__ RowInfo row_info(const WindowParams& a, const Seq& s, int i, int head) {
+  RowLoads l;
+  l.ask(a, s, i, head);
+  return l.info(a, s, i);
 }
+// Window row of a packed row.
+__device__ __forceinline__ int row_of(const WindowParams& a, int pr) { return a.log2g >= 0 ? pr >> a.log2g : pr / a.G; }
 // Over the wave's rows: what some row sees, and what every row sees.
 struct Span {
   int lo, hi, all_lo, all_hi;
@@ -217,27 +248,29 @@ __device__ __forceinline__ void scores(const F& f, const Queries<DT, D, QT>& Q, 
   }
 }
 
-// Raw products to modified scores in log2 units.
+// Raw products to modified scores in log2 units, plus a number per row.
 template <typename DT, int QT>
-__device__ __forceinline__ void modify(const WindowParams& a, const RowInfo (&row)[QT], int k0, floatx4 (&s)[QT][2]) {
+__device__ __forceinline__ void modify(const WindowParams& a, const RowInfo (&row)[QT], const float (&plus)[QT], int k0, floatx4 (&s)[QT][2]) {
   if (a.cap2 != 0.f) {
     // tanh x = 1 - 2 / (e^2x + 1): infinities give +-1.  Off by 2^-23 of the cap near 0, which
     // fp32 calls do not have.
 #pragma unroll
-    for (int t = 0; t < QT; ++t)
+    for (int t = 0; t < QT; ++t) {
+      const float top = a.cap2 + plus[t];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float x = s[t][i >> 2][i & 3];
         if constexpr (sizeof(DT) == 2)
-          s[t][i >> 2][i & 3] = fmaf(__builtin_amdgcn_rcpf(fast_exp2(x * a.scale2) + 1.f), -2.f * a.cap2, a.cap2);
+          s[t][i >> 2][i & 3] = fmaf(__builtin_amdgcn_rcpf(fast_exp2(x * a.scale2) + 1.f), -2.f * a.cap2, top);
         else
-          s[t][i >> 2][i & 3] = a.cap2 * tanhf(x * a.cap_scale);
+          s[t][i >> 2][i & 3] = fmaf(a.cap2, tanhf(x * a.cap_scale), plus[t]);
       }
+    }
   } else {
 #pragma unroll
     for (int t = 0; t < QT; ++t)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[t][i >> 2][i & 3] *= a.scale2;
+      for (int i = 0; i < 8; ++i) s[t][i >> 2][i & 3] = fmaf(s[t][i >> 2][i & 3], a.scale2, plus[t]);
   }
   if (a.slopes) {
 #pragma unroll
