@@ -40,6 +40,7 @@ namespace ipdv {
 namespace {
 
 constexpr int kWaves = 4;
+constexpr int kStageValues = 128;       // QT x D up to which there are registers for a block's values
 constexpr float kRescaleSlack = 8.0f;   // log2 units a stale running max may lag
 constexpr float kLn2 = 0.69314718055994531f;
 
@@ -95,7 +96,10 @@ struct Rows {
         for (int c = 0; c < D / 16; ++c) Q.q[t][c] = ld16<floatx4>(qr + j * (D / 4) + 4 * c);
       }
     }
-    // here before loads that the compiler does not count are under way
+  }
+  // The queries are here from now on: the compiler counts its own loads only, and would wait for
+  // them inside the walk, with others under way.
+  __device__ __forceinline__ void queries_here() {
 #pragma unroll
     for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -128,7 +132,15 @@ struct Rows {
   __device__ __forceinline__ void block(const MaskedParams& a, const F& f, int t0, bool masked) {
     floatx4 s[QT][2];
     scores<DT, D, QT>(f, Q, s);
-    weigh<CAREFUL>(a, f, s, t0, masked);
+    if constexpr (QT * D <= kStageValues) {      // asked for before the softmax: LDS takes its time
+      Frags<DT, D> r;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) r.v[dt] = f.vf(dt);
+      __builtin_amdgcn_sched_barrier(0);
+      weigh<CAREFUL>(a, r, s, t0, masked);
+    } else {                           // no registers for them
+      weigh<CAREFUL>(a, f, s, t0, masked);
+    }
   }
   template <bool CAREFUL, class F>
   __device__ __forceinline__ void weigh(const MaskedParams& a, const F& f, floatx4 (&s)[QT][2], int t0, bool masked) {
@@ -346,19 +358,24 @@ __device__ __forceinline__ Span join_spans(const Span& mine, int (&s_span)[kWave
 
 // A workgroup's piece: the blocks b0 .. b1 - 1 of a tile.
 struct Piece {
-  int b0, b1;
+  int b0, b1, n;           // n: pieces of the tile
   bool whole;
 };
 // False if the tile has no such piece.
-__device__ __forceinline__ bool piece_of(const MaskedParams& a, const Split& sp, const Span& all, int sg, int tile, int piece, Piece& p) {
+__device__ __forceinline__ bool piece_of(const Split& sp, const Span& all, int piece, Piece& p) {
   const int blo = all.lo >= all.hi ? 0 : all.lo / kBlk, bhi = all.lo >= all.hi ? 0 : (all.hi + kBlk - 1) / kBlk;
-  const int n = max((bhi - blo + sp.per - 1) / sp.per, 1);
+  const int nb = bhi - blo, n = max((nb + sp.per - 1) / sp.per, 1);
   if (piece >= n) return false;
-  if (piece == 0 && threadIdx.x == 0) a.pieces[(size_t)sg * a.tiles + tile] = n;
-  p.b0 = blo + piece * sp.per;
-  p.b1 = min(p.b0 + sp.per, bhi);
+  p.n = n;
+  // even pieces: shares of the first nb % n one block more
+  const int each = nb / n, more = nb - each * n;
+  p.b0 = blo + piece * each + min(piece, more);
+  p.b1 = p.b0 + each + (piece < more ? 1 : 0);
   p.whole = n == 1;
   return true;
+}
+__device__ __forceinline__ void note_pieces(const MaskedParams& a, const Piece& p, int sg, int tile, int piece) {
+  if (piece == 0 && threadIdx.x == 0) a.pieces[(size_t)sg * a.tiles + tile] = p.n;
 }
 __device__ __forceinline__ size_t part_row_of(const MaskedParams& a, const Split& sp, int sg, int tile, int piece, int tile_rows) {
   return ((size_t)sg * a.units + (size_t)tile * sp.np + piece) * tile_rows;
@@ -387,7 +404,7 @@ __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys
   R.begin(a, s, g, wr0, pr_last);
   const Span mine = span_of<QT>(R.row);
   Piece p;
-  if (!piece_of(a, sp, OWN ? join_spans(mine, s_span) : mine, sg, tile, piece, p)) return;
+  if (!piece_of(sp, OWN ? join_spans(mine, s_span) : mine, piece, p)) return;
   const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
   int first = p.b0 + (OWN ? 0 : wv), last = p.b1;
   if (OWN) {
@@ -421,8 +438,10 @@ __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys
       __builtin_amdgcn_sched_barrier(0);
     }
   };
+  R.queries_here();
   walk(std::false_type());
   if (__any(R.odd())) walk(std::true_type());
+  note_pieces(a, p, sg, tile, piece);
   R.join_lanes();
   if (OWN) {
     R.finish(a, s, g, wr0, pr_last, p.whole, part_row_of(a, sp, sg, tile, piece, kRows) + 16 * QT * wv);
@@ -499,22 +518,30 @@ template <int D, bool WIDE> struct Loader {
       }
     }
   }
-  __device__ __forceinline__ void issue(const MaskedParams& a, const Parts& parts, int t0, int t, char* buf) const {
+  // `lds`: LDS address of the wave's first piece of the unit.
+  __device__ __forceinline__ void issue(const MaskedParams& a, const Parts& parts, int t0, int t, unsigned lds) const {
     const int ps = 1 << a.log2ps;
-    const size_t page = (size_t)(unsigned)(2 * D * ps);
     const int o0 = t0 & (ps - 1), o1 = (t0 + 16) & (ps - 1);
+    // byte offsets of both parts' (page, head), the same in either cache
+    const size_t size = (size_t)(unsigned)(2 * D * ps);
+    const size_t at0 = (size_t)(unsigned)uni((int)parts.of(0)) * size, at1 = (size_t)(unsigned)uni((int)parts.of(1)) * size;
+    const char* kc = reinterpret_cast<const char*>(a.k_cache);
+    const char* vc = reinterpret_cast<const char*>(a.v_cache);
+    // D = 128: a wave's pieces are of one part after the other; D = 64: of one part
+    constexpr int PER = D / 32;                // pieces of a part
 #pragma unroll
     for (int i = 0; i < kKeys; ++i) {
-      const int part = (t + 4 * i) / (D / 32);
-      dma16(reinterpret_cast<const char*>(a.k_cache) + (size_t)(unsigned)uni((int)parts.of(part)) * page +
-                (unsigned)(64 * (part ? o1 : o0)), k[i], buf + 1024 * (t + 4 * i));
+      const bool second = PER == 4 ? i : t >= PER;
+      load_to(lds + 4096 * i, kc + (second ? at1 + (unsigned)(64 * o1) : at0 + (unsigned)(64 * o0)), k[i]);
     }
 #pragma unroll
     for (int i = 0; i < kLoads - kKeys; ++i) {
-      const int part = WIDE ? 0 : (t + 4 * i) / (D / 32);
-      dma16(reinterpret_cast<const char*>(a.v_cache) + (size_t)(unsigned)uni((int)parts.of(part)) * page +
-                (unsigned)(WIDE ? 2 * o0 : 0), v[i], buf + 1024 * (t + 4 * (i + kKeys)));
+      const bool second = !WIDE && (PER == 4 ? i : t >= PER);
+      load_to(lds + 4096 * (i + kKeys), vc + (WIDE ? at0 + (unsigned)(2 * o0) : second ? at1 : at0), v[i]);
     }
+  }
+  static __device__ __forceinline__ void load_to(unsigned lds, const char* base, unsigned off) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "memory", "m0");
   }
 };
 
@@ -539,11 +566,12 @@ __global__ __launch_bounds__(256, 3) void masked_tile_kernel(MaskedParams a) {
   R.begin(a, s, g, wr0, pr_last);
   const Span mine = span_of<QT>(R.row);
   Piece p;
-  if (!piece_of(a, sp, join_spans(mine, s_span), sg, tile, piece, p)) return;
+  if (!piece_of(sp, join_spans(mine, s_span), piece, p)) return;
   const bool has_rows = wr0 <= pr_last;
   const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
   const Load load(t, 1 << a.log2ps);
   const LdsFrags<D, WIDE> lane_at(nullptr);
+  const unsigned ring = uni((int)(unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)s_ring + 1024 * t);
   auto walk = [&](auto careful) __attribute__((always_inline)) {
     constexpr bool CAREFUL = decltype(careful)::value;
     R.reset();
@@ -551,14 +579,14 @@ __global__ __launch_bounds__(256, 3) void masked_tile_kernel(MaskedParams a) {
     Parts parts;
     // Behind the piece's end its last unit is loaded again, so that every wait has the same count.
     auto look_up = [&](int n) { parts.look_up(a, pt, min(n, p.b1 - 1) * kBlk, g); };
-    auto issue = [&](int n, int buf) { load.issue(a, parts, min(n, p.b1 - 1) * kBlk, t, s_ring + buf * Load::kUnit); };
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // only the ring's loads from here on
+    auto issue = [&](int n, int buf) { load.issue(a, parts, min(n, p.b1 - 1) * kBlk, t, ring + buf * Load::kUnit); };
 #pragma unroll
     for (int i = 0; i < kRing - 1; ++i) {
       look_up(p.b0 + i);
       issue(p.b0 + i, i);
     }
     look_up(p.b0 + kRing - 1);
+    if (!CAREFUL) R.queries_here();                      // only the ring's loads from here on
     int use = 0, fill = kRing - 1;
     for (int n = p.b0; n < p.b1; ++n) {
       // Unit n is there (this wave's loads by the count, the others' by the barrier), and
@@ -582,22 +610,22 @@ __global__ __launch_bounds__(256, 3) void masked_tile_kernel(MaskedParams a) {
   walk(std::false_type());
   // all waves together, since they share the loads; also the barrier before the ring is filled again
   if (__syncthreads_or(R.odd())) walk(std::true_type());
+  note_pieces(a, p, sg, tile, piece);
   R.join_lanes();
   R.finish(a, s, g, wr0, pr_last, p.whole, part_row_of(a, sp, sg, tile, piece, kRows) + 16 * QT * t);
 }
 
-// Joins the pieces of every tile that was cut: kMergeRows neighbouring rows per workgroup,
-// 16 lanes per row.
-constexpr int kMergeRows = 64;
+// Joins the pieces of every tile that was cut: some neighbouring rows per workgroup, 16
+// lanes per row.
 template <typename DT, int D>
-__global__ __launch_bounds__(256) void masked_merge_kernel(MaskedParams a, int tile_rows) {
+__global__ __launch_bounds__(256) void masked_merge_kernel(MaskedParams a, int tile_rows, int merge_rows) {
   const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv;
   const Seq s = seq_of(a, slot);
   const int d = ((int)threadIdx.x & 15) * (D / 16);
   constexpr int V = D / 64;                     // of four channels
   const Split sp = split_of(a, s, tile_rows);
-  const int last = min((int)(blockIdx.y + 1) * kMergeRows, s.rows);
-  for (int pr = blockIdx.y * kMergeRows + (int)threadIdx.x / 16; pr < last; pr += 16) {
+  const int last = min((int)(blockIdx.y + 1) * merge_rows, s.rows);
+  for (int pr = blockIdx.y * merge_rows + (int)threadIdx.x / 16; pr < last; pr += 16) {
     const int tile = pr / tile_rows;
     const int n = a.pieces[(size_t)blockIdx.x * a.tiles + tile];
     if (n == 1) continue;
@@ -654,7 +682,7 @@ Plan plan_of(int n_seq, int Hq, int Hkv, int max_q, long slots, int window, bool
   p.per = p.shared ? 16 : 8;
   // With rows enough to fill the chip by themselves, walks of up to 48 blocks stay whole: the
   // merge costs more.
-  p.walk = sg * p.tiles >= 512 ? 48 : (int)std::clamp(sg * nb / 2048, (long)p.per, 64L);
+  p.walk = sg * p.tiles >= 512 ? 48 : (int)std::clamp(sg * nb / 1024, (long)p.per, 64L);
   p.per = (int)std::max((long)p.per, nb / 16384);      // units stay few under a table for millions of tokens
   const int least = std::max(p.per, p.walk);
   p.cut = nb > least;
@@ -738,7 +766,9 @@ hipError_t launch_attn_masked(const AttnMaskedLaunch& L, hipStream_t st) {
   trace_mark(st);
   if (pl.cut) {
     auto merge = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3(sg, (unsigned)(((long)pl.tiles * pl.tile_rows + kMergeRows - 1) / kMergeRows)), dim3(256), 0, st, p, pl.tile_rows);
+      const int rows = pl.tiles > 8 ? 64 : 16;         // of many tiles, most are whole
+      hipLaunchKernelGGL(kernel, dim3(sg, (unsigned)(((long)pl.tiles * pl.tile_rows + rows - 1) / rows)), dim3(256), 0, st, p,
+                         pl.tile_rows, rows);
     };
     if (L.dtype_bf16) {
       if (L.D == 128) merge(masked_merge_kernel<bf16, 128>); else merge(masked_merge_kernel<bf16, 64>);

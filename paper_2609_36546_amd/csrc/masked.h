@@ -143,14 +143,16 @@ template <int QT> __device__ __forceinline__ Span span_of(const RowInfo (&row)[Q
     s.all_lo = max(s.all_lo, row[t].lo);
     s.all_hi = min(s.all_hi, row[t].hi);
   }
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) {       // the lanes of a group of 16 hold the rows
-    s.lo = min(s.lo, __shfl_xor(s.lo, o, kWave));
-    s.hi = max(s.hi, __shfl_xor(s.hi, o, kWave));
-    s.all_lo = max(s.all_lo, __shfl_xor(s.all_lo, o, kWave));
-    s.all_hi = min(s.all_hi, __shfl_xor(s.all_hi, o, kWave));
-  }
-  return {uni(s.lo), uni(s.hi), uni(s.all_lo), uni(s.all_hi)};
+  // the lanes of a group of 16 hold the rows
+  auto join = [](int v, auto op) {
+    v = op(v, dpp_move_i<0x140>(v));
+    v = op(v, dpp_move_i<0x141>(v));
+    v = op(v, dpp_move_i<0x4E>(v));
+    return uni(op(v, dpp_move_i<0xB1>(v)));
+  };
+  auto least = [](int x, int y) { return min(x, y); };
+  auto most = [](int x, int y) { return max(x, y); };
+  return {join(s.lo, least), join(s.hi, most), join(s.all_lo, most), join(s.all_hi, least)};
 }
 
 // (page, head) of the two 16-slot parts of a block, and where in the page they
