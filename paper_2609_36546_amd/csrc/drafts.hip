@@ -7,12 +7,13 @@
 // so that whatever is emitted is distributed as p.
 //
 //   stats kernel    one workgroup per row, model and 8192 entries: maximum and mass against
-//                   it.  Reads every logit once; bound by their bytes as much as by its
-//                   vector instructions.
-//   rest kernel     one workgroup per sequence and 8192 entries: the sequence's first row that
-//                   ends it, from the rows' masses (every workgroup for itself), and the mass of
-//                   max(0, p - q) in the chunk where that row is a rejected draft.
-//   draw kernel     one workgroup per sequence: the chunk where the mass passes u, in it
+//                   it, by quarters too.  Reads every logit once; its vector instructions
+//                   (22 an entry, 15 of them in 64 bits) take longer than its bytes.
+//   verdict kernel  one workgroup per sequence: the rows' masses joined, p(x) and q(x), the first
+//                   row that ends the window.
+//   rest kernel     one workgroup per rejected row and 8192 entries: masses of max(0, p - q), by
+//                   quarters.
+//   draw kernel     one workgroup per sequence: the quarter where the mass passes u, in it
 //                   the entry.
 //
 // Precision.  A token is a whole number next to borders that lie as close as the
@@ -38,6 +39,7 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kChunk = 8192;
 constexpr int kPer = kChunk / kThreads;
 constexpr int kMaxChunks = 32;     // V <= 262144
+constexpr int kQuarter = kChunk / kWaves;
 typedef unsigned long long u64;
 
 // A chunk of one row: its kept mass against its maximum, which it may have none of.
@@ -56,6 +58,7 @@ struct Model {
   const float* temperature;
   const u64* cuts;   // [T] or null: everything is kept
   Rec* recs;         // [T][chunks]
+  double* quarters;  // [T][chunks][4]: the record's mass by quarters
 };
 struct DraftParams {
   Model target, draft;       // draft.logits null: the drafts are certain
@@ -70,24 +73,30 @@ struct DraftParams {
   uint8_t* finished;
   float* p_accept;
   float* logp;
-  double* rest;              // [B][chunks]: masses of max(0, p - q)
-  int* verdict;              // [B]: what find_end found
+  double* rest;              // [B][chunks][4]: masses of max(0, p - q)
+  int* verdict;              // [B]: 8 * the row that ends the window + how (kNone: none)
 };
+constexpr int kNone = 0x7fffffff;
 
-// 2^y for y <= 0 (and not below -1000).
+// a b + c with c in scalar registers: the compiler would take the form that adds to its operand and
+// copy every coefficient for it, two instructions each.
+__device__ __forceinline__ double fma_s(double a, double b, double c) {
+  double r;
+  asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
+  return r;
+}
+// 2^(d slope) for d slope <= 0 (and not below -1000).
 __device__ __forceinline__ double exp2_of(double d, double slope) {
   const double magic = 6755399441055744.0;         // 1.5 * 2^52: the sum's low bits are the nearest whole number
   const double t = fma(d, slope, magic), f = fma(d, slope, magic - t);
-  double p = 1.5201920948780836e-05;
-  p = fma(p, f, 0.00015469291124750825);
-  p = fma(p, f, 0.001333392256603758);
-  p = fma(p, f, 0.009618027253729474);
-  p = fma(p, f, 0.05550410353445379);
-  p = fma(p, f, 0.2402265119815696);
-  p = fma(p, f, 0.693147180728448);
-  p = fma(p, f, 0.999999999961681);
-  const u64 bits = __builtin_bit_cast(u64, p) + ((u64)__double2loint(t) << 52);
-  return __builtin_bit_cast(double, bits);
+  double p = fma_s(f, 1.5201920948780836e-05, 0.00015469291124750825);
+  p = fma_s(p, f, 0.001333392256603758);
+  p = fma_s(p, f, 0.009618027253729474);
+  p = fma_s(p, f, 0.05550410353445379);
+  p = fma_s(p, f, 0.2402265119815696);
+  p = fma_s(p, f, 0.693147180728448);
+  p = fma_s(p, f, 0.999999999961681);
+  return __hiloint2double((int)((unsigned)__double2hiint(p) + ((unsigned)__double2loint(t) << 20)), __double2loint(p));
 }
 
 // A row's temperature: log2(e) / T, and the distance from the maximum behind which nothing
@@ -118,39 +127,54 @@ struct RowMass {
   float max, l_cut;
   int v_cut;
   bool bad;
-  __device__ __forceinline__ bool keeps(float l, int v) const { return l > l_cut || (l == l_cut && v <= v_cut); }
+  __device__ __forceinline__ bool keeps(float l, int v) const { return (l > l_cut) | ((l == l_cut) & (v <= v_cut)); }
   __device__ __forceinline__ double mass(float l, int v) const {      // the probability
-    return keeps(l, v) && l > -INFINITY ? mass_of(l, max, far, slope) * inv : 0.0;
+    const double m = mass_of(l, max, far, slope) * inv;
+    return keeps(l, v) & (l > -INFINITY) ? m : 0.0;
   }
 };
+template <int CTRL> __device__ __forceinline__ double dpp_move_d(double v) {
+  return __hiloint2double(dpp_move_i<CTRL>(__double2hiint(v)), dpp_move_i<CTRL>(__double2loint(v)));
+}
+// Sum over 32 neighbouring lanes, in all of them.
+__device__ __forceinline__ double sum32(double v) {
+  v += dpp_move_d<0x140>(v);
+  v += dpp_move_d<0x141>(v);
+  v += dpp_move_d<0x4E>(v);
+  v += dpp_move_d<0xB1>(v);
+  return v + __hiloint2double(__float_as_int(lane_xor16(__int_as_float(__double2hiint(v)))),
+                              __float_as_int(lane_xor16(__int_as_float(__double2loint(v)))));
+}
 // Every lane of a group of 32 calls; all get the result.
 __device__ __forceinline__ RowMass join(const DraftParams& p, const Model& m, int r) {
   const int c = lane_id() & 31;
   const Scale sc = scale_of(m, r);
   Rec rec{0.0, 0, -INFINITY, 0};
   if (c < p.chunks) rec = m.recs[(size_t)r * p.chunks + c];
+  const u64 given = m.cuts ? m.cuts[r] : 0;
   float mx = rec.max;
+  mx = fmaxf(mx, dpp_move<0x140>(mx));
+  mx = fmaxf(mx, dpp_move<0x141>(mx));
+  mx = fmaxf(mx, dpp_move<0x4E>(mx));
+  mx = fmaxf(mx, dpp_move<0xB1>(mx));
+  mx = fmaxf(mx, lane_xor16(mx));
+  const bool bad = (unsigned)(__ballot(rec.bad) >> (lane_id() & 32)) != 0;
   u64 top = rec.top;
-  int bad = rec.bad;
+  if (__any(sc.first_only && !m.cuts)) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    mx = fmaxf(mx, __shfl_xor(mx, o, kWave));
-    bad |= __shfl_xor(bad, o, kWave);
-    const u64 other = __shfl_xor(top, o, kWave);
-    top = other > top ? other : top;
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 other = __shfl_xor(top, o, kWave);
+      top = other > top ? other : top;
+    }
   }
-  double mass = rec.max > -INFINITY && rec.mass > 0.0
-                    ? rec.mass * mass_of(rec.max, mx, sc.far, sc.slope) : 0.0;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) mass += __shfl_xor(mass, o, kWave);
+  const double mass = sum32(rec.max > -INFINITY && rec.mass > 0.0 ? rec.mass * mass_of(rec.max, mx, sc.far, sc.slope) : 0.0);
   RowMass out;
   out.bad = bad || sc.bad || !(mx > -INFINITY);
   out.slope = sc.slope;
   out.far = sc.far;
-  out.inv = 1.0 / mass;
+  out.inv = sc.first_only ? 1.0 : 1.0 / mass;      // the cut is the maximum's
   out.max = mx;
-  out.cut = m.cuts ? m.cuts[r] : sc.first_only ? top : 0;
-  if (sc.first_only) out.inv = 1.0;                // the cut is the maximum's
+  out.cut = m.cuts ? given : sc.first_only ? top : 0;
   out.l_cut = out.cut ? logit_of(out.cut) : -__FLT_MAX__;
   out.v_cut = out.cut ? index_of(out.cut) : p.V;
   return out;
@@ -163,30 +187,20 @@ template <typename DT> __device__ __forceinline__ double prob(const DraftParams&
 }
 
 __device__ __forceinline__ double wave_sum_d(double v) {
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) v += __shfl_xor(v, o, kWave);
-  return v;
-}
-__device__ __forceinline__ double block_sum(double v, double* part) {
-  v = wave_sum_d(v);
-  __syncthreads();
-  if (lane_id() == 0) part[threadIdx.x / kWave] = v;
-  __syncthreads();
-  v = 0.0;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) v += part[i];
-  return v;
+  v = sum32(v);
+  return v + __hiloint2double(lane_xor32(__double2hiint(v)), lane_xor32(__double2loint(v)));
 }
 
-// A chunk's entries in registers as they came: entry i of the thread is
-// (i / N) * kThreads N + tid N + i % N.
+// A chunk's entries in registers as they came, a quarter to each wave.
 typedef __attribute__((__vector_size__(16))) int i32x4;
 template <typename DT, bool VEC> struct Entries {
   static constexpr int N = VEC ? 16 / (int)sizeof(DT) : 1;
   typedef std::conditional_t<VEC, i32x4, DT> Raw;
   struct Lane { DT e[N]; };
   Raw raw[kPer / N];
-  __device__ __forceinline__ static int at(int i) { return (i / N * kThreads + (int)threadIdx.x) * N + i % N; }
+  __device__ __forceinline__ static int at(int i) {
+    return (int)threadIdx.x / kWave * kQuarter + (i / N * kWave + lane_id()) * N + i % N;
+  }
   __device__ __forceinline__ void load(const Model& m, int r, int v0, int V) {
     const DT* src = reinterpret_cast<const DT*>(m.logits) + (size_t)r * m.stride + v0;
     const int n = V - v0;
@@ -207,11 +221,12 @@ template <typename DT, bool VEC> struct Entries {
 };
 
 template <typename DT, bool VEC, bool CUT>
-__global__ __launch_bounds__(kThreads) void draft_stats_kernel(DraftParams p, Model m) {
+__global__ __launch_bounds__(kThreads) void draft_stats_kernel(DraftParams p) {
   __shared__ float s_max[kWaves];
   __shared__ double s_part[kWaves];
   __shared__ u64 s_top[kWaves];
   __shared__ int s_bad;
+  const Model& m = blockIdx.y ? p.draft : p.target;
   const int r = blockIdx.x / p.chunks, c = blockIdx.x - r * p.chunks, v0 = c * kChunk, tid = threadIdx.x;
   Entries<DT, VEC> x;
   x.load(m, r, v0, p.V);
@@ -233,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void draft_stats_kernel(DraftParams p, Mo
   if (mx == INFINITY) s_bad = 1;
   u64 top = 0;
   double sum = 0.0;
-  if (!CUT && sc.first_only) {
+  if (sc.first_only && !(CUT && m.cuts)) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const u64 o = x.get(i) == mx && mx > -INFINITY ? order_of(mx, v0 + Entries<DT, VEC>::at(i)) : 0;
@@ -249,63 +264,34 @@ __global__ __launch_bounds__(kThreads) void draft_stats_kernel(DraftParams p, Mo
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) top = s_top[i] > top ? s_top[i] : top;
   } else if (mx > -INFINITY && mx < INFINITY) {
-    const u64 cut = CUT ? m.cuts[r] : 0;
+    const u64 cut = CUT && m.cuts ? m.cuts[r] : 0;
     const float l_cut = cut ? logit_of(cut) : -__FLT_MAX__;
     const int v_cut = cut ? index_of(cut) : p.V;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const float l = x.get(i);
-      const double e = mass_of(l, mx, sc.far, sc.slope);
-      if (CUT) {
-        const int v = v0 + Entries<DT, VEC>::at(i);
-        sum += l > l_cut || (l == l_cut && v <= v_cut) ? e : 0.0;
-      } else {
-        sum += e;                                  // of -inf: 2^-1000
+      if (!CUT) {
+        sum += mass_of(l, mx, sc.far, sc.slope);   // of -inf: 2^-1000
+      } else if ((l > l_cut) | ((l == l_cut) & (v0 + Entries<DT, VEC>::at(i) <= v_cut))) {      // few: a branch
+        sum += mass_of(l, mx, sc.far, sc.slope);
       }
     }
   }
-  sum = block_sum(sum, s_part);
-  if (tid == 0) m.recs[(size_t)r * p.chunks + c] = {sum, top, mx, s_bad};
+  sum = wave_sum_d(sum);
+  const size_t at = (size_t)r * p.chunks + c;
+  if (lane_id() == 0) {
+    s_part[tid / kWave] = sum;
+    m.quarters[at * kWaves + tid / kWave] = sum;
+  }
+  __syncthreads();
+  if (tid == 0) m.recs[at] = {(s_part[0] + s_part[1]) + (s_part[2] + s_part[3]), top, mx, s_bad};
 }
+
+// Sums of less come from entries of -inf, which are never drawn.
+constexpr double kNothing = 0x1p-900;
 
 // How a window ends.
 enum { kGoesOn = 0, kRejected = 1, kNoDraft = 2, kBad = 3, kEos = 4 };
-
-// The first row of sequence b that ends it, by all threads of the workgroup: in s_end, row * 8 +
-// how (INT_MAX: none).  `write`: the rows' p_accept too.
-template <typename DT>
-__device__ __forceinline__ void find_end(const DraftParams& p, int b, int r0, int k, bool write, int* s_end) {
-  if (threadIdx.x == 0) *s_end = 0x7fffffff;
-  __syncthreads();
-  for (int i0 = 0; i0 < k; i0 += kThreads / 32) {
-    const int i = i0 + (int)threadIdx.x / 32, r = r0 + min(i, k - 1);
-    const int x = p.prop_tok[r];
-    const RowMass t = join(p, p.target, r);
-    RowMass d{};
-    if (p.draft.logits) d = join(p, p.draft, r);
-    if (i < k && (threadIdx.x & 31) == 0) {
-      int how = kGoesOn;
-      float ratio = 0.f;
-      if (t.bad || (x >= 0 && d.bad)) {
-        how = kBad;
-        ratio = __uint_as_float(0x7fc00000u);
-      } else if (x < 0) {
-        how = kNoDraft;
-      } else {
-        double pt = 0.0, pd = p.draft.logits ? 0.0 : 1.0;
-        if (x < p.V) {
-          pt = prob<DT>(p, p.target, t, r, x);
-          if (p.draft.logits) pd = prob<DT>(p, p.draft, d, r, x);
-        }
-        ratio = pt >= pd ? (pt > 0.0 ? 1.f : 0.f) : (float)(pt / pd);
-        how = !((double)p.u_accept[r] * pd < pt) ? kRejected : x == p.eos_id ? kEos : kGoesOn;
-      }
-      if (write) p.p_accept[r] = ratio;
-      if (how != kGoesOn) atomicMin(s_end, 8 * min(i, 0xfffffff) + how);
-    }
-  }
-  __syncthreads();
-}
 
 struct Window {
   int r0, k;
@@ -317,6 +303,52 @@ __device__ __forceinline__ Window window_of(const DraftParams& p, int b) {
   return w;
 }
 
+// The rows of a sequence, eight at a time, 32 lanes each.
+template <typename DT>
+__global__ __launch_bounds__(kThreads) void draft_verdict_kernel(DraftParams p) {
+  __shared__ int s_end;
+  const int b = blockIdx.x;
+  if (threadIdx.x == 0) s_end = kNone;
+  __syncthreads();
+  const Window w = window_of(p, b);
+  for (int i0 = 0; i0 < w.k; i0 += kThreads / 32) {
+    const int i = i0 + (int)threadIdx.x / 32, r = w.r0 + min(i, w.k - 1);
+    const int x = p.prop_tok[r];
+    const float u = p.u_accept[r];
+    const bool drafted = x >= 0 && x < p.V, given = p.draft.logits != nullptr;
+    // asked for before the records are joined
+    const float lt = drafted ? logit<DT>(p.target, r, x) : 0.f, ld = drafted && given ? logit<DT>(p.draft, r, x) : 0.f;
+    const RowMass t = join(p, p.target, r);
+    RowMass d{};
+    if (given) d = join(p, p.draft, r);
+    if (i < w.k && (threadIdx.x & 31) == 0) {
+      int how = kGoesOn;
+      float ratio = 0.f;
+      if (t.bad || (x >= 0 && d.bad)) {
+        how = kBad;
+        ratio = __uint_as_float(0x7fc00000u);
+      } else if (x < 0) {
+        how = kNoDraft;
+      } else {
+        const double pt = drafted ? t.mass(lt, x) : 0.0, pd = !given ? 1.0 : drafted ? d.mass(ld, x) : 0.0;
+        ratio = pt >= pd ? (pt > 0.0 ? 1.f : 0.f) : (float)(pt / pd);
+        how = !((double)u * pd < pt) ? kRejected : x == p.eos_id ? kEos : kGoesOn;
+      }
+      p.p_accept[r] = ratio;
+      if (how != kGoesOn) atomicMin(&s_end, 8 * i + how);
+    }
+  }
+  __syncthreads();
+  const int end = s_end, how = end == kNone ? kGoesOn : end & 7;
+  if (threadIdx.x != 0) return;
+  p.verdict[b] = end;
+  if (how == kRejected || how == kNoDraft) return;           // the draw kernel's
+  p.n_acc[b] = how == kGoesOn ? w.k : (end >> 3) + (how == kEos ? 1 : 0);
+  p.token[b] = -1;
+  p.finished[b] = how == kEos;
+  if (p.logp) p.logp[b] = __uint_as_float(0x7fc00000u);
+}
+
 // An entry's mass in what a rejected row is drawn from.
 __device__ __forceinline__ double rest_of(const RowMass& t, float lt, const RowMass& d, float ld, bool certain, int x, int v) {
   const double m = t.mass(lt, v);
@@ -326,157 +358,178 @@ __device__ __forceinline__ double rest_of(const RowMass& t, float lt, const RowM
 
 template <typename DT, bool VEC>
 __global__ __launch_bounds__(kThreads) void draft_rest_kernel(DraftParams p) {
-  __shared__ int s_end;
-  __shared__ double s_part[kWaves];
   const int b = blockIdx.x / p.chunks, c = blockIdx.x - b * p.chunks;
-  const Window w = window_of(p, b);
-  find_end<DT>(p, b, w.r0, w.k, c == 0, &s_end);
-  const int end = s_end;
-  if (c == 0 && threadIdx.x == 0) p.verdict[b] = end;
-  if (end == 0x7fffffff || (end & 7) != kRejected) return;
-  const int r = w.r0 + (end >> 3), x = p.prop_tok[r], v0 = c * kChunk;
+  const int end = p.verdict[b];
+  if (end == kNone || (end & 7) != kRejected) return;
+  const int r = window_of(p, b).r0 + (end >> 3), v0 = c * kChunk;
   const bool certain = !p.draft.logits;
-  const RowMass t = join(p, p.target, r);
-  RowMass d{};
-  if (!certain) d = join(p, p.draft, r);
   Entries<DT, VEC> lt, ld;
   lt.load(p.target, r, v0, p.V);
   if (!certain) ld.load(p.draft, r, v0, p.V);
+  const int x = p.prop_tok[r];
+  const RowMass t = join(p, p.target, r);
+  RowMass d{};
+  if (!certain) d = join(p, p.draft, r);
   double sum = 0.0;
+  if (t.cut | d.cut | (u64)certain) {
 #pragma unroll
-  for (int i = 0; i < kPer; ++i)
-    sum += rest_of(t, lt.get(i), d, certain ? 0.f : ld.get(i), certain, x, v0 + Entries<DT, VEC>::at(i));
-  sum = block_sum(sum, s_part);
-  if (threadIdx.x == 0) p.rest[(size_t)b * p.chunks + c] = sum;
+    for (int i = 0; i < kPer; ++i)
+      sum += rest_of(t, lt.get(i), d, certain ? 0.f : ld.get(i), certain, x, v0 + Entries<DT, VEC>::at(i));
+  } else {                                         // everything is kept, -inf of 2^-1000
+    // both probabilities rounded alike: of equal ones nothing is left
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const double m = mass_of(lt.get(i), t.max, t.far, t.slope) * t.inv, q = mass_of(ld.get(i), d.max, d.far, d.slope) * d.inv;
+      sum += fmax(m - q, 0.0);
+    }
+  }
+  sum = wave_sum_d(sum);
+  if (lane_id() == 0) p.rest[((size_t)b * p.chunks + c) * kWaves + threadIdx.x / kWave] = sum;
+}
+
+// Inclusive sums over the lanes of a wave, in lane order.
+__device__ __forceinline__ double wave_scan_d(double v) {
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const double up = __shfl_up(v, o, kWave);
+    if (lane_id() >= o) v += up;
+  }
+  return v;
 }
 
 template <typename DT, bool VEC>
 __global__ __launch_bounds__(kThreads) void draft_draw_kernel(DraftParams p) {
+  constexpr int PER = kQuarter / kThreads;         // neighbouring entries of a thread
+  constexpr int QN = kMaxChunks * kWaves / kWave;  // quarters of a lane
   __shared__ double s_part[kWaves], s_goal;
-  __shared__ int s_chunk, s_hit[2];
-  __shared__ double s_before;
+  __shared__ int s_quarter, s_hit[2];
   const int b = blockIdx.x, tid = threadIdx.x, lane = lane_id(), wv = tid / kWave;
-  const Window w = window_of(p, b);
-  const int end = p.verdict[b], how = end == 0x7fffffff ? kGoesOn : end & 7;
-  const int n = how == kGoesOn ? w.k : (end >> 3) + (how == kEos ? 1 : 0);
-  if (how != kRejected && how != kNoDraft) {
-    if (tid == 0) {
-      p.n_acc[b] = n;
-      p.token[b] = -1;
-      p.finished[b] = how == kEos;
-      if (p.logp) p.logp[b] = __uint_as_float(0x7fc00000u);
-    }
-    return;
-  }
-  const int r = w.r0 + n, x = p.prop_tok[r];
-  const RowMass t = join(p, p.target, r);
+  const int end = p.verdict[b], how = end == kNone ? kGoesOn : end & 7;
+  if (how != kRejected && how != kNoDraft) return;
+  const int n = end >> 3, r = window_of(p, b).r0 + n, quarters = p.chunks * kWaves;
+  const int x = p.prop_tok[r];
+  const float u = p.u_draw[b];
   const bool certain = !p.draft.logits;
+  // masses of the quarters, a lane QN neighbours: of the rest, or (a rest of nothing: rounding, a u
+  // of 1) of p itself
+  double mine[QN], whole[QN];
+#pragma unroll
+  for (int i = 0; i < QN; ++i) {
+    const int q = lane * QN + i;
+    mine[i] = how == kRejected && q < quarters ? p.rest[(size_t)b * quarters + q] : 0.0;
+    whole[i] = q < quarters ? p.target.quarters[(size_t)r * quarters + q] : 0.0;
+  }
+  const float chunk_max = lane * QN / kWaves < p.chunks ? p.target.recs[(size_t)r * p.chunks + lane * QN / kWaves].max : -INFINITY;
+  static_assert(kWaves % QN == 0, "a lane's quarters lie in one chunk");
+  const RowMass t = join(p, p.target, r);
   RowMass d{};
   if (!certain && how == kRejected) d = join(p, p.draft, r);
-  // masses of the chunks; a rest of nothing (rounding, a u of 1) leaves p itself
-  bool rest = how == kRejected;
-  const int c = lane & 31;
-  double mine = rest && c < p.chunks ? p.rest[(size_t)b * p.chunks + c] : 0.0;
-  double all = mine;
+  double all = 0.0;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) all += __shfl_xor(all, o, kWave);
-  if (!(all > 0.0)) {
-    rest = false;
-    mine = 0.0;
-    if (c < p.chunks) {
-      const Rec rec = p.target.recs[(size_t)r * p.chunks + c];
-      if (t.cut && !p.target.cuts)                 // temperature 0
-        mine = index_of(t.cut) / kChunk == c ? 1.0 : 0.0;
-      else if (rec.max > -INFINITY && rec.mass > 0.0)
-        mine = rec.mass * mass_of(rec.max, t.max, t.far, t.slope) * t.inv;
-    }
+  for (int i = 0; i < QN; ++i) all += mine[i];
+  const bool rest = how == kRejected && wave_sum_d(all) > kNothing;
+  if (!rest) {
+    const double f = chunk_max > -INFINITY ? mass_of(chunk_max, t.max, t.far, t.slope) * t.inv : 0.0;
+#pragma unroll
+    for (int i = 0; i < QN; ++i)
+      mine[i] = t.cut && !p.target.cuts ? (index_of(t.cut) / kQuarter == lane * QN + i ? 1.0 : 0.0)      // temperature 0
+                                        : whole[i] * f;
   }
   if (wv == 0) {
-    double incl = mine;
+    double part = 0.0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const double up = __shfl_up(incl, o, 32);
-      if (c >= o) incl += up;
-    }
-    const double goal = (double)p.u_draw[b] * __shfl(incl, 31, 32);
-    const unsigned some = (unsigned)__ballot(mine > 0.0);
-    unsigned hit = (unsigned)__ballot(mine > 0.0 && incl > goal);
-    if (hit == 0) hit = 1u << (31 - __clz((int)(some | 1u)));
-    const int pick = __ffs((int)hit) - 1;
-    if (lane == pick) {
-      s_chunk = pick;
-      s_goal = goal - (incl - mine);
+    for (int i = 0; i < QN; ++i) part += mine[i];
+    const double upto = wave_scan_d(part);
+    const double goal = (double)u * __shfl(upto, kWave - 1, kWave);
+    const u64 some = __ballot(part > kNothing);
+    u64 hit = __ballot(part > kNothing && upto > goal);
+    if (hit == 0) hit = 1ull << (63 - __clzll((long long)(some | 1)));
+    if (lane == __ffsll((long long)hit) - 1) {     // its first quarter whose end passes the goal, or its last that holds some
+      double before = upto - part;
+      int pick = 0;
+      bool found = false;
+      double at = before;
+#pragma unroll
+      for (int i = 0; i < QN; ++i) {
+        if (!found && mine[i] > kNothing) {
+          pick = i;
+          at = before;
+          found = before + mine[i] > goal;
+        }
+        before += mine[i];
+      }
+      s_quarter = lane * QN + pick;
+      s_goal = goal - at;
       s_hit[0] = kThreads;
       s_hit[1] = 0;
     }
   }
   __syncthreads();
-  // threads take neighbouring entries of the chunk
-  const int v0 = s_chunk * kChunk + tid * kPer;
+  const int v0 = s_quarter * kQuarter + tid * PER;
   const double goal = s_goal;
-  auto weigh = [&](float lt, float ld, int v) { return rest ? rest_of(t, lt, d, ld, certain, x, v) : t.mass(lt, v); };
-  auto at = [&](int v) {
-    const float lt = logit<DT>(p.target, r, v);
-    return weigh(lt, rest && !certain ? logit<DT>(p.draft, r, v) : 0.f, v);
-  };
-  double sum = 0.0;
-  if (VEC && v0 + kPer <= p.V) {
+  const bool both = rest && !certain;
+  float lt[PER], ld[PER];
+  if (VEC && v0 + PER <= p.V) {
     constexpr int N = 16 / (int)sizeof(DT);
     struct Lane { DT e[N]; };
     const DT* st = reinterpret_cast<const DT*>(p.target.logits) + (size_t)r * p.target.stride + v0;
-    const DT* sd = rest && !certain ? reinterpret_cast<const DT*>(p.draft.logits) + (size_t)r * p.draft.stride + v0 : st;
+    const DT* sd = both ? reinterpret_cast<const DT*>(p.draft.logits) + (size_t)r * p.draft.stride + v0 : st;
 #pragma unroll
-    for (int i = 0; i < kPer; i += N) {
+    for (int i = 0; i < PER; i += N) {
       const Lane et = __builtin_bit_cast(Lane, ld16<i32x4>(st + i)), ed = __builtin_bit_cast(Lane, ld16<i32x4>(sd + i));
 #pragma unroll
-      for (int k = 0; k < N; ++k) sum += weigh(to_f32(et.e[k]), to_f32(ed.e[k]), v0 + i + k);
+      for (int k = 0; k < N; ++k) {
+        lt[i + k] = to_f32(et.e[k]);
+        ld[i + k] = to_f32(ed.e[k]);
+      }
     }
   } else {
-    for (int i = 0; i < kPer && v0 + i < p.V; ++i) sum += at(v0 + i);
-  }
-  double incl = sum;
 #pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const double up = __shfl_up(incl, o, kWave);
-    if (lane >= o) incl += up;
+    for (int i = 0; i < PER; ++i) {
+      lt[i] = v0 + i < p.V ? logit<DT>(p.target, r, v0 + i) : -INFINITY;
+      ld[i] = both && v0 + i < p.V ? logit<DT>(p.draft, r, v0 + i) : -INFINITY;
+    }
   }
+  double m[PER], sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    m[i] = rest ? rest_of(t, lt[i], d, ld[i], certain, x, v0 + i) : t.mass(lt[i], v0 + i);
+    sum += m[i];
+  }
+  const double incl = wave_scan_d(sum);
   if (lane == kWave - 1) s_part[wv] = incl;
   __syncthreads();
   double before = 0.0;
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) before += i < wv ? s_part[i] : 0.0;
+  // a thread's end is the next one's beginning, to the last bit
   const double left = __shfl_up(incl, 1, kWave);
-  const double lo = lane > 0 ? before + left : before, hi = before + incl;
-  const u64 some = __ballot(sum > 0.0), past = __ballot(sum > 0.0 && hi > goal);
+  double at = lane > 0 ? before + left : before;
+  const double to = before + incl;
+  const u64 some = __ballot(sum > 0.0), past = __ballot(sum > 0.0 && to > goal);
   if (lane == 0 && some) atomicMax(&s_hit[1], wv * kWave + 63 - __clzll((long long)some));
   if (lane == 0 && past) atomicMin(&s_hit[0], wv * kWave + __ffsll((long long)past) - 1);
   __syncthreads();
-  // the first thread whose end passes the goal; rounding, or a u of 1, leave it to the last that holds some
-  const int who = s_hit[0] < kThreads ? s_hit[0] : s_hit[1];
-  if (tid == who) s_before = goal - lo;
-  __syncthreads();
-  if (wv != 0) return;
-  static_assert(kPer <= kWave, "a lane per entry");
-  const int v = s_chunk * kChunk + who * kPer + lane;
-  const double one = lane < kPer && v < p.V ? at(v) : 0.0;
-  double upto = one;
+  // the first thread whose end passes the goal; rounding, or a u of 1, leave it to the last that
+  // holds some; in it the first entry likewise
+  if (tid != (s_hit[0] < kThreads ? s_hit[0] : s_hit[1])) return;
+  int pick = 0;
+  float l = lt[0];
+  bool found = false;
 #pragma unroll
-  for (int o = 1; o < kPer; o <<= 1) {
-    const double up = __shfl_up(upto, o, kWave);
-    if (lane >= o) upto += up;
-  }
-  const u64 any = __ballot(one > 0.0);
-  u64 hit = __ballot(one > 0.0 && upto > s_before);
-  if (hit == 0) hit = 1ull << (63 - __clzll((long long)(any | 1)));
-  if (lane == __ffsll((long long)hit) - 1) {
-    p.n_acc[b] = n;
-    p.token[b] = v;
-    p.finished[b] = v == p.eos_id;
-    if (p.logp) {
-      const float l = logit<DT>(p.target, r, v);
-      p.logp[b] = (float)(((double)l - (double)t.max) * t.slope * 0.6931471805599453 + log(t.inv));
+  for (int i = 0; i < PER; ++i) {
+    if (!found && m[i] > 0.0) {
+      pick = i;
+      l = lt[i];
+      found = at + m[i] > goal;
     }
+    at += m[i];
   }
+  p.n_acc[b] = n;
+  p.token[b] = v0 + pick;
+  p.finished[b] = v0 + pick == p.eos_id;
+  if (p.logp) p.logp[b] = (float)(((double)l - (double)t.max) * t.slope * 0.6931471805599453 + log(t.inv));
 }
 
 int chunks_of(int V) { return (V + kChunk - 1) / kChunk; }
@@ -486,9 +539,9 @@ size_t align(size_t n) { return (n + 255) / 256 * 256; }
 
 size_t verify_drafts_workspace(int T, int V, int B, bool target_filters, bool draft_filters) {
   const size_t nc = chunks_of(V);
-  size_t n = 2 * align(T * nc * sizeof(Rec)) + align(B * nc * sizeof(double)) + align((size_t)B * sizeof(int));
+  size_t n = 2 * (align(T * nc * sizeof(Rec)) + align(T * nc * kWaves * 8)) + align(B * nc * kWaves * 8) + align((size_t)B * sizeof(int));
   n += (target_filters ? align((size_t)T * 8) : 0) + (draft_filters ? align((size_t)T * 8) : 0);
-  if (target_filters || draft_filters) n += align(sample_logits_workspace(T, V));
+  n += ((target_filters ? 1 : 0) + (draft_filters ? 1 : 0)) * align(sample_logits_workspace(T, V));
   return n;
 }
 
@@ -502,8 +555,13 @@ hipError_t launch_verify_drafts(const DraftLaunch& L, hipStream_t st) {
   };
   auto filtered = [](const Filters& f) { return f.top_k || f.top_p || f.min_p; };
   DraftParams p{};
-  p.target = {L.target, L.target_stride, L.tf.temperature, nullptr, (Rec*)take((size_t)L.T * nc * sizeof(Rec))};
-  p.draft = {L.draft, L.draft_stride, L.df.temperature, nullptr, (Rec*)take((size_t)L.T * nc * sizeof(Rec))};
+  auto model = [&](const void* logits, int64_t stride, const float* temperature) {
+    const size_t n = (size_t)L.T * nc;
+    Rec* recs = (Rec*)take(n * sizeof(Rec));
+    return Model{logits, stride, temperature, nullptr, recs, (double*)take(n * kWaves * 8)};
+  };
+  p.target = model(L.target, L.target_stride, L.tf.temperature);
+  p.draft = model(L.draft, L.draft_stride, L.df.temperature);
   p.T = L.T;
   p.V = L.V;
   p.B = L.B;
@@ -518,19 +576,23 @@ hipError_t launch_verify_drafts(const DraftLaunch& L, hipStream_t st) {
   p.finished = L.finished;
   p.p_accept = L.p_accept;
   p.logp = L.logp;
-  p.rest = (double*)take((size_t)L.B * nc * sizeof(double));
+  p.rest = (double*)take((size_t)L.B * nc * kWaves * 8);
   p.verdict = (int*)take((size_t)L.B * sizeof(int));
   trace_begin(st);
+  // the cuts of both models in one go
   u64* cuts[2] = {nullptr, nullptr};
-  const bool on[2] = {filtered(L.tf), L.draft && filtered(L.df)};
-  for (int i = 0; i < 2; ++i)
-    if (on[i]) cuts[i] = (u64*)take((size_t)L.T * 8);
-  for (int i = 0; i < 2; ++i) {
-    if (!on[i] || L.T == 0) continue;
+  SampleLogitsLaunch S[2];
+  int n = 0;
+  for (int i = 0; i < (L.draft ? 2 : 1); ++i) {
     const Filters& f = i ? L.df : L.tf;
-    SampleLogitsLaunch S{i ? L.draft : L.target, i ? L.draft_stride : L.target_stride, L.T, L.V, nullptr, f.temperature, f.top_k,
-                         f.top_p, f.min_p, nullptr, nullptr, L.dtype_bf16, ws, cuts[i]};
-    const hipError_t e = launch_logit_cuts(S, st);
+    if (!filtered(f)) continue;
+    cuts[i] = (u64*)take((size_t)L.T * 8);
+    S[n++] = SampleLogitsLaunch{i ? L.draft : L.target, i ? L.draft_stride : L.target_stride, L.T, L.V, nullptr, f.temperature,
+                                f.top_k, f.top_p, f.min_p, nullptr, nullptr, L.dtype_bf16,
+                                take(sample_logits_workspace(L.T, L.V)), cuts[i]};
+  }
+  if (n > 0 && L.T > 0) {
+    const hipError_t e = launch_logit_cuts(S, n, st);
     if (e != hipSuccess) return e;
   }
   p.target.cuts = cuts[0];
@@ -546,18 +608,21 @@ hipError_t launch_verify_drafts(const DraftLaunch& L, hipStream_t st) {
       if (vec) f(float(), std::true_type()); else f(float(), std::false_type());
     }
   };
+  const dim3 all(L.T * nc, L.draft ? 2 : 1);
   with([&](auto dt, auto v) {
     using DT = decltype(dt);
     constexpr bool VEC = decltype(v)::value;
-    for (int i = 0; i < (L.draft ? 2 : 1) && L.T > 0; ++i) {
-      const Model& m = i ? p.draft : p.target;
-      if (m.cuts)
-        hipLaunchKernelGGL((draft_stats_kernel<DT, VEC, true>), dim3(L.T * nc), dim3(kThreads), 0, st, p, m);
-      else
-        hipLaunchKernelGGL((draft_stats_kernel<DT, VEC, false>), dim3(L.T * nc), dim3(kThreads), 0, st, p, m);
-    }
+    if (L.T == 0) return;
+    if (n > 0)
+      hipLaunchKernelGGL((draft_stats_kernel<DT, VEC, true>), all, dim3(kThreads), 0, st, p);
+    else
+      hipLaunchKernelGGL((draft_stats_kernel<DT, VEC, false>), all, dim3(kThreads), 0, st, p);
   });
   hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  trace_mark(st);
+  with([&](auto dt, auto) { hipLaunchKernelGGL(draft_verdict_kernel<decltype(dt)>, dim3(L.B), dim3(kThreads), 0, st, p); });
+  e = hipGetLastError();
   if (e != hipSuccess) return e;
   trace_mark(st);
   with([&](auto dt, auto v) {

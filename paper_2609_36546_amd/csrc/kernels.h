@@ -361,8 +361,8 @@ struct SampleLogitsLaunch {
 
 size_t sample_logits_workspace(int M, int V);
 hipError_t launch_sample_logits(const SampleLogitsLaunch& L, hipStream_t st);
-// The rows' cuts alone: u, token and logp are not used.
-hipError_t launch_logit_cuts(const SampleLogitsLaunch& L, hipStream_t st);
+// The cuts alone of n = 1 or 2 sets of rows, of one type, M and V: u, token and logp are not used.
+hipError_t launch_logit_cuts(const SampleLogitsLaunch* L, int n, hipStream_t st);
 
 // ---- verdict scan ----
 struct ScanLaunch {

@@ -168,7 +168,7 @@ constexpr int kThreads = 512;     // of both kernels
 constexpr int kWaves = kThreads / kWave;
 
 template <typename DT, bool VEC>
-__global__ __launch_bounds__(kThreads, 6) void chunk_kernel(SampleLogitsLaunch p, int n_chunks) {
+__device__ __forceinline__ void chunk_work(const SampleLogitsLaunch& p, int n_chunks) {
   constexpr int N = VEC ? 16 / (int)sizeof(DT) : 1;   // entries per load
   constexpr int PER = kChunk / kThreads;
   __shared__ u64 s_hist[kBins];
@@ -313,6 +313,16 @@ __global__ __launch_bounds__(kThreads, 6) void chunk_kernel(SampleLogitsLaunch p
       rec.list[atomicAdd(&s_at[bin], 1)] = order_of(l[k], v0 + v[k]);
     }
   }
+}
+
+template <typename DT, bool VEC>
+__global__ __launch_bounds__(kThreads, 6) void chunk_kernel(SampleLogitsLaunch p, int n_chunks) {
+  chunk_work<DT, VEC>(p, n_chunks);
+}
+// Two sets of rows at once.
+template <typename DT, bool VEC>
+__global__ __launch_bounds__(kThreads, 6) void chunk_pair_kernel(SampleLogitsLaunch p, SampleLogitsLaunch q, int n_chunks) {
+  chunk_work<DT, VEC>(blockIdx.y ? q : p, n_chunks);
 }
 
 // ---- the row kernel ----
@@ -670,7 +680,7 @@ struct RowWork {
 // CUTS: the row's cut is all that is asked for (0: everything is kept; of a row that
 // nothing can be drawn from, anything).
 template <typename DT, bool VEC, bool CUTS>
-__global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int n_chunks) {
+__device__ __forceinline__ void row_work(const SampleLogitsLaunch& p, int n_chunks) {
   __shared__ Shared S;
   const int m = blockIdx.x, tid = threadIdx.x, lane = lane_id(), w = tid >> 6;
   const int t = tid & (kBins - 1), side = tid / kBins;
@@ -918,19 +928,30 @@ __global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int
   }
 }
 
+template <typename DT, bool VEC>
+__global__ __launch_bounds__(kThreads) void row_kernel(SampleLogitsLaunch p, int n_chunks) {
+  row_work<DT, VEC, false>(p, n_chunks);
+}
+template <typename DT, bool VEC>
+__global__ __launch_bounds__(kThreads) void cut_pair_kernel(SampleLogitsLaunch p, SampleLogitsLaunch q, int n_chunks) {
+  row_work<DT, VEC, true>(blockIdx.y ? q : p, n_chunks);
+}
+
 int chunks_of(int V) { return (V + kChunk - 1) / kChunk; }
 
 }  // namespace
 
 size_t sample_logits_workspace(int M, int V) { return (size_t)M * chunks_of(V) * kChunkBytes; }
 
-namespace {
-
-template <bool CUTS> hipError_t launch(const SampleLogitsLaunch& L, hipStream_t st) {
-  const int nc = chunks_of(L.V);
+static bool in_vectors(const SampleLogitsLaunch& L) {
   const int size = L.dtype_bf16 ? 2 : 4;
-  const bool vec = ((uintptr_t)L.logits & 15) == 0 && L.stride * size % 16 == 0 && (size_t)L.V * size % 16 == 0;
-  if (!CUTS) trace_begin(st);
+  return ((uintptr_t)L.logits & 15) == 0 && L.stride * size % 16 == 0 && (size_t)L.V * size % 16 == 0;
+}
+
+hipError_t launch_sample_logits(const SampleLogitsLaunch& L, hipStream_t st) {
+  const int nc = chunks_of(L.V);
+  const bool vec = in_vectors(L);
+  trace_begin(st);
   auto go = [&](auto kernel, int n) { hipLaunchKernelGGL(kernel, dim3(n), dim3(kThreads), 0, st, L, nc); };
   if (L.dtype_bf16) {
     if (vec) go(chunk_kernel<bf16, true>, L.M * nc); else go(chunk_kernel<bf16, false>, L.M * nc);
@@ -939,21 +960,36 @@ template <bool CUTS> hipError_t launch(const SampleLogitsLaunch& L, hipStream_t 
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (!CUTS) trace_mark(st);
+  trace_mark(st);
   if (L.dtype_bf16) {
-    if (vec) go(row_kernel<bf16, true, CUTS>, L.M); else go(row_kernel<bf16, false, CUTS>, L.M);
+    if (vec) go(row_kernel<bf16, true>, L.M); else go(row_kernel<bf16, false>, L.M);
   } else {
-    if (vec) go(row_kernel<float, true, CUTS>, L.M); else go(row_kernel<float, false, CUTS>, L.M);
+    if (vec) go(row_kernel<float, true>, L.M); else go(row_kernel<float, false>, L.M);
   }
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (!CUTS) trace_mark(st);
+  trace_mark(st);
   return hipSuccess;
 }
 
-}  // namespace
-
-hipError_t launch_sample_logits(const SampleLogitsLaunch& L, hipStream_t st) { return launch<false>(L, st); }
-hipError_t launch_logit_cuts(const SampleLogitsLaunch& L, hipStream_t st) { return launch<true>(L, st); }
+hipError_t launch_logit_cuts(const SampleLogitsLaunch* L, int n, hipStream_t st) {
+  const SampleLogitsLaunch &a = L[0], &b = L[n - 1];
+  const int nc = chunks_of(a.V);
+  const bool vec = in_vectors(a) && in_vectors(b);
+  auto go = [&](auto kernel, int m) { hipLaunchKernelGGL(kernel, dim3(m, n), dim3(kThreads), 0, st, a, b, nc); };
+  if (a.dtype_bf16) {
+    if (vec) go(chunk_pair_kernel<bf16, true>, a.M * nc); else go(chunk_pair_kernel<bf16, false>, a.M * nc);
+  } else {
+    if (vec) go(chunk_pair_kernel<float, true>, a.M * nc); else go(chunk_pair_kernel<float, false>, a.M * nc);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (a.dtype_bf16) {
+    if (vec) go(cut_pair_kernel<bf16, true>, a.M); else go(cut_pair_kernel<bf16, false>, a.M);
+  } else {
+    if (vec) go(cut_pair_kernel<float, true>, a.M); else go(cut_pair_kernel<float, false>, a.M);
+  }
+  return hipGetLastError();
+}
 
 }  // namespace ipdv

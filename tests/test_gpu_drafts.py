@@ -207,6 +207,20 @@ def test_entries_of_no_mass_and_far_temperatures():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("V,at", [(20000, 17000), (9000, 8999), (40000, 2100)])
+def test_whole_stretches_of_no_mass_are_not_drawn_from(V, at):
+    t = torch.full((3, V), -float("inf"))
+    t[:, at] = 2.0
+    t[:, at - 1] = 1.0
+    d = t.clone()
+    d[:, at - 1] = 3.0
+    for draft, df in ((None, {}), (d, {}), (d, {"top_k": torch.full((3,), 2, dtype=torch.int32)})):
+        got = call(t, draft, [at - 1, -1, 0], [0, 1, 2, 3], [0.999] * 3, [0.0] * 3, {}, df)
+        assert got["n_acc"].tolist() == [0, 0, 0]
+        assert got["token"].tolist() == [at, at - 1, at - 1 if draft is None else at]
+
+
+@pytest.mark.gpu
 def test_emitted_tokens_follow_the_target():
     """Many windows of one draft over a small vocabulary: the first token emitted is
     distributed as the target (each frequency within five standard deviations)."""
