@@ -725,25 +725,17 @@ int sample_logits(const void* logits, int64_t row_stride, int M, int V, const fl
  *   window            keys that a row sees at most, its own the last of them (0: off)
  *   first_key [T] int32   e.g. where the row's document begins (NULL: 0)
  *   end_key [T] int32     e.g. the end of a prefix that sees itself whole (NULL: p + 1)
- * A row may be left without keys.  The struct is read on the host; its arrays are
- * device memory.  A NULL struct is one of zeros.
+ * A row may be left without keys.
  */
-typedef struct {
-  float softcap;
-  int32_t window;
-  const float* slopes;
-  const int32_t* first_key;
-  const int32_t* end_key;
-} ipdv_score_mod;
 
 /* Workspace bytes verify_attn_masked needs (0 if the arguments are invalid).
- * `window` as in the call's ipdv_score_mod, has_end_key whether it has an end_key. */
+ * `window` as in the call, has_end_key whether it has an end_key. */
 size_t ipdv_attn_masked_workspace_size(int n_seq, int Hq, int Hkv, int D, int max_q,
                                        int max_pages_per_seq, int page_size,
                                        int window, int has_end_key);
 
 /*
- * verify_attn_masked -- verify_attn_paged with modified scores x (ipdv_score_mod):
+ * verify_attn_masked -- verify_attn_paged with modified scores x (see above):
  * appends the window, then
  *   out[r, h, :] = sum_j softmax_j(x) V_j,   lse[r, h] = ln sum_j e^x
  * over the keys that the row sees; a row that sees none gets 0 and -inf.  Keys and
@@ -754,8 +746,7 @@ size_t ipdv_attn_masked_workspace_size(int n_seq, int Hq, int Hkv, int D, int ma
  *
  * q [T, Hq, D] (dtype), q_row_stride elements from one row to the next (>= Hq *
  * D); k_new, v_new [T, Hkv, D] (dtype; both NULL: the window is in the cache
- * already); lse [T, Hq] float or NULL; mod a HOST pointer or NULL.  bf16 and fp32, D
- * in {64, 128}.  The cache and the other arguments as in verify_attn_paged.  q's rows,
+ * already); lse [T, Hq] float or NULL.  bf16 and fp32, D in {64, 128}.  The cache and the other arguments as in verify_attn_paged.  q's rows,
  * k_new, v_new, the caches, out and workspace start on 16-byte boundaries.
  * The workspace is written by the call; two calls that may overlap need one each.
  *
@@ -766,7 +757,8 @@ int verify_attn_masked(const void* q, int64_t q_row_stride, const void* k_new, c
                        void* k_cache, void* v_cache,
                        const int32_t* page_table, int max_pages_per_seq,
                        const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* seq_ids,
-                       int n_seq, int max_q, const ipdv_score_mod* mod, void* out, float* lse,
+                       int n_seq, int max_q, float softcap, int window, const float* slopes,
+                       const int32_t* first_key, const int32_t* end_key, void* out, float* lse,
                        int Hq, int Hkv, int D, int page_size, int num_pages, float scale,
                        int dtype, void* workspace, size_t workspace_bytes, void* hip_stream);
 
@@ -779,7 +771,7 @@ int verify_attn_masked(const void* q, int64_t q_row_stride, const void* k_new, c
  * itself (j >= L_b) start at 0, and so do all where mass_in is NULL.  Slots of other
  * positions are left as they are.  The window must be in the cache.
  *
- * q, k_cache, mod, scale and the batch's arguments as in verify_attn_masked; lse [T,
+ * q, k_cache, the scores' and the batch's arguments as in verify_attn_masked; lse [T,
  * Hq] float; mass_in, mass_out [num_pages, Hkv, page_size] float, the same array or
  * two that do not overlap; 0 <= decay, finite.  Requirement:
  * max_pages_per_seq * page_size + max_q <= 2^22.  A page that two handled sequences
@@ -791,7 +783,8 @@ int verify_attn_masked(const void* q, int64_t q_row_stride, const void* k_new, c
 int attn_mass(const void* q, int64_t q_row_stride, const void* k_cache, const float* lse,
               const int32_t* page_table, int max_pages_per_seq,
               const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* seq_ids,
-              int n_seq, int max_q, const ipdv_score_mod* mod,
+              int n_seq, int max_q, float softcap, int window, const float* slopes,
+              const int32_t* first_key, const int32_t* end_key,
               const float* mass_in, float decay, float* mass_out,
               int Hq, int Hkv, int D, int page_size, int num_pages, float scale,
               int dtype, void* hip_stream);
@@ -826,14 +819,6 @@ int kv_evict(void* k_cache, void* v_cache, float* mass,
              int n_sink, int n_recent, int32_t* new_lens, int32_t* kept,
              int Hkv, int D, int page_size, int num_pages, int dtype, void* hip_stream);
 
-/* A row's filters, arrays of one entry per row, each NULL for off (sample_logits). */
-typedef struct {
-  const float* temperature;
-  const int32_t* top_k;
-  const float* top_p;
-  const float* min_p;
-} ipdv_filters;
-
 /* Workspace bytes verify_drafts needs (0 if the arguments are invalid): whether the target's
  * and the draft's filters have more than a temperature. */
 size_t ipdv_verify_drafts_workspace_size(int T, int V, int B, int target_filtered,
@@ -861,13 +846,13 @@ size_t ipdv_verify_drafts_workspace_size(int T, int V, int B, int target_filtere
  * A row whose target logits (or, with a draft, its draft logits) hold NaN or +inf or nothing
  * above -inf, or whose temperature is negative or NaN, ends its window without a token; its
  * p_accept is NaN.  A draft at or beyond V has p(x) = 0 and is rejected.  draft_logits NULL:
- * q(x) = 1, as of drafts looked up or taken greedily; draft_filters is then not read.
+ * q(x) = 1, as of drafts looked up or taken greedily; the draft's filters are then not read.
  * Probabilities are 64-bit floats (relative error below 1e-9), except that top-p's cut is found
  * as in sample_logits.  The same call repeats bit for bit.
  *
  * target_logits, draft_logits [T, V] (dtype), *_row_stride elements from one row to the next
  * (>= V); prop_tok [T], cu_q [B+1] int32 (cu_q[B] <= T); u_accept [T], u_draw [B] float in [0,
- * 1); filters HOST pointers to structs of device arrays of T entries, or NULL for off.
+ * 1); temperature ... draft_min_p [T], each NULL for off (as in sample_logits).
  * Requirements: 0 <= T < 2^22, 0 <= B < 2^22, 1 <= V <= 262144, T * V < 2^35; workspace on a
  * 16-byte boundary, written by the call: two calls that may overlap need one each.
  *
@@ -877,7 +862,9 @@ int verify_drafts(const void* target_logits, int64_t target_row_stride,
                   const void* draft_logits, int64_t draft_row_stride, int T, int V,
                   const int32_t* prop_tok, const int32_t* cu_q, int B,
                   const float* u_accept, const float* u_draw,
-                  const ipdv_filters* target_filters, const ipdv_filters* draft_filters,
+                  const float* temperature, const int32_t* top_k, const float* top_p,
+                  const float* min_p, const float* draft_temperature,
+                  const int32_t* draft_top_k, const float* draft_top_p, const float* draft_min_p,
                   int32_t eos_id, int32_t* n_acc, int32_t* token, uint8_t* finished,
                   float* p_accept, float* logp, int dtype,
                   void* workspace, size_t workspace_bytes, void* hip_stream);

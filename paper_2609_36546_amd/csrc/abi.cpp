@@ -708,13 +708,9 @@ int sample_logits(const void* logits, int64_t stride, int M, int V, const float*
   return ok();
 }
 
-// The modifiers' checks, and the struct as the kernels take it.
-static int score_mod(const ipdv_score_mod* mod, ipdv::ScoreMod* out) {
-  *out = {};
-  if (!mod) return IPDV_OK;
-  if (!std::isfinite(mod->softcap) || mod->softcap < 0.f) return fail(IPDV_EINVAL, "softcap must be >= 0 and finite");
-  if (mod->window < 0) return fail(IPDV_EINVAL, "window must be >= 0 (got %d)", mod->window);
-  *out = {mod->softcap, mod->window, mod->slopes, mod->first_key, mod->end_key};
+static int score_mod_check(float softcap, int window) {
+  if (!std::isfinite(softcap) || softcap < 0.f) return fail(IPDV_EINVAL, "softcap must be >= 0 and finite");
+  if (window < 0) return fail(IPDV_EINVAL, "window must be >= 0 (got %d)", window);
   return IPDV_OK;
 }
 
@@ -753,11 +749,11 @@ static int masked_call_check(const void* q, int64_t q_stride, const void* k_cach
 
 int verify_attn_masked(const void* q, int64_t q_stride, const void* k_new, const void* v_new, void* k_cache, void* v_cache,
                        const int32_t* page_table, int max_pages, const int32_t* ctx_lens, const int32_t* cu_q,
-                       const int32_t* seq_ids, int n_seq, int max_q, const ipdv_score_mod* mod, void* out, float* lse,
-                       int Hq, int Hkv, int D, int page_size, int num_pages, float scale, int dtype, void* workspace,
+                       const int32_t* seq_ids, int n_seq, int max_q, float softcap, int window, const float* slopes,
+                       const int32_t* first_key, const int32_t* end_key, void* out, float* lse, int Hq, int Hkv, int D, int page_size, int num_pages, float scale, int dtype, void* workspace,
                        size_t workspace_bytes, void* hip_stream) {
-  ipdv::ScoreMod m;
-  int st = score_mod(mod, &m);
+  const ipdv::ScoreMod m{softcap, window, slopes, first_key, end_key};
+  int st = score_mod_check(softcap, window);
   if (st != IPDV_OK) return st;
   st = masked_shape_check(n_seq, Hq, Hkv, D, max_q, max_pages, page_size, m.window, m.end_key != nullptr);
   if (st != IPDV_OK) return st;
@@ -782,10 +778,11 @@ int verify_attn_masked(const void* q, int64_t q_stride, const void* k_new, const
 
 int attn_mass(const void* q, int64_t q_stride, const void* k_cache, const float* lse, const int32_t* page_table,
               int max_pages, const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* seq_ids, int n_seq, int max_q,
-              const ipdv_score_mod* mod, const float* mass_in, float decay, float* mass_out, int Hq, int Hkv, int D,
+              float softcap, int window, const float* slopes, const int32_t* first_key, const int32_t* end_key,
+              const float* mass_in, float decay, float* mass_out, int Hq, int Hkv, int D,
               int page_size, int num_pages, float scale, int dtype, void* hip_stream) {
-  ipdv::ScoreMod m;
-  int st = score_mod(mod, &m);
+  const ipdv::ScoreMod m{softcap, window, slopes, first_key, end_key};
+  int st = score_mod_check(softcap, window);
   if (st != IPDV_OK) return st;
   st = attn_shape_check(n_seq, Hq, Hkv, D, max_q, max_pages, page_size);
   if (st != IPDV_OK) return st;
@@ -842,7 +839,9 @@ size_t ipdv_verify_drafts_workspace_size(int T, int V, int B, int target_filtere
 
 int verify_drafts(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int T, int V,
                   const int32_t* prop_tok, const int32_t* cu_q, int B, const float* u_accept, const float* u_draw,
-                  const ipdv_filters* target_filters, const ipdv_filters* draft_filters, int32_t eos_id, int32_t* n_acc,
+                  const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                  const float* draft_temperature, const int32_t* draft_top_k, const float* draft_top_p,
+                  const float* draft_min_p, int32_t eos_id, int32_t* n_acc,
                   int32_t* token, uint8_t* finished, float* p_accept, float* logp, int dtype, void* workspace,
                   size_t workspace_bytes, void* hip_stream) {
   int st = drafts_shape_check(T, V, B);
@@ -852,11 +851,9 @@ int verify_drafts(const void* target, int64_t target_stride, const void* draft, 
   if (B == 0) return ok();
   if (!cu_q || !u_draw || !n_acc || !token || !finished) return fail(IPDV_EINVAL, "null required pointer");
   if (T > 0 && (!target || !prop_tok || !u_accept || !p_accept)) return fail(IPDV_EINVAL, "null required pointer");
-  auto filters = [](const ipdv_filters* f) {
-    return f ? ipdv::Filters{f->temperature, f->top_k, f->top_p, f->min_p} : ipdv::Filters{};
-  };
   auto filtered = [](const ipdv::Filters& f) { return f.top_k || f.top_p || f.min_p; };
-  const ipdv::Filters tf = filters(target_filters), df = filters(draft ? draft_filters : nullptr);
+  const ipdv::Filters tf{temperature, top_k, top_p, min_p};
+  const ipdv::Filters df = draft ? ipdv::Filters{draft_temperature, draft_top_k, draft_top_p, draft_min_p} : ipdv::Filters{};
   const size_t need = ipdv::verify_drafts_workspace(T, V, B, filtered(tf), filtered(df));
   if (!workspace || workspace_bytes < need)
     return fail(IPDV_EWORKSPACE, "workspace of %zu bytes needed (got %zu)", need, workspace ? workspace_bytes : (size_t)0);

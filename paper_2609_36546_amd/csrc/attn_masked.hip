@@ -45,7 +45,9 @@ constexpr float kRescaleSlack = 8.0f;   // log2 units a stale running max may la
 constexpr float kLn2 = 0.69314718055994531f;
 
 struct MaskedParams : WindowParams {
-  const void* v_cache;
+  const void* k_new;   // the window's rows, where the attention appends them itself (else null)
+  const void* v_new;
+  void* v_cache;
   void* out;
   float* lse;
   float* part_o;       // [n_seq * Hkv][units][tile rows][D]
@@ -381,6 +383,33 @@ __device__ __forceinline__ size_t part_row_of(const MaskedParams& a, const Split
   return ((size_t)sg * a.units + (size_t)tile * sp.np + piece) * tile_rows;
 }
 
+// The window's keys and values to their pages, by every workgroup those that it reads
+// (several may write the same), by the first of a (sequence, head) all; a kernel of its own for
+// it takes 2 to 6 us, and its launch 2.5 of the host's.
+constexpr int kAppendFew = 16;         // window rows up to which this is done
+template <typename DT, int D>
+__device__ __forceinline__ void append_own(const MaskedParams& a, const Seq& s, int g, const Piece& p, bool all) {
+  if (!a.k_new) return;
+  const int from = all ? s.L : max(s.L, p.b0 * kBlk), to = all ? s.L + s.kb : min(s.L + s.kb, p.b1 * kBlk);
+  if (from < to) {
+    const int32_t* table = a.page_table + (size_t)s.b * a.max_pages;
+    const int ps = 1 << a.log2ps;
+    const DT* kn = reinterpret_cast<const DT*>(a.k_new);
+    const DT* vn = reinterpret_cast<const DT*>(a.v_new);
+    DT* kc = reinterpret_cast<DT*>(const_cast<void*>(a.k_cache));
+    DT* vc = reinterpret_cast<DT*>(a.v_cache);
+    for (int e = threadIdx.x; e < (to - from) * D; e += 256) {
+      const int pos = from + e / D, d = e % D, sl = pos & (ps - 1);
+      const size_t page = (size_t)min(max(table[min(pos >> a.log2ps, a.max_pages - 1)], 0), a.num_pages - 1) * a.Hkv + g;
+      const size_t src = ((size_t)(s.r0 + pos - s.L) * a.Hkv + g) * D + d;
+      kc[((page * (D / 32) + d / 32) << a.log2ps) * 32 + sl * 32 + (d & 31)] = kn[src];
+      vc[((page * D + d) << a.log2ps) + sl] = vn[src];
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // written when the others pass the barrier
+  __syncthreads();
+}
+
 // Operands straight into registers.  Few rows (OWN false): the four waves take every fourth
 // block of the piece.  More in fp32 (OWN): rows of their own, and the same blocks, which the
 // first to ask leaves in the vector cache.
@@ -406,6 +435,7 @@ __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys
   Piece p;
   if (!piece_of(sp, OWN ? join_spans(mine, s_span) : mine, piece, p)) return;
   const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
+  append_own<DT, D>(a, s, g, p, tile == 0 && piece == 0);
   int first = p.b0 + (OWN ? 0 : wv), last = p.b1;
   if (OWN) {
     first = max(first, mine.lo / kBlk);
@@ -567,6 +597,7 @@ __global__ __launch_bounds__(256, 3) void masked_tile_kernel(MaskedParams a) {
   const Span mine = span_of<QT>(R.row);
   Piece p;
   if (!piece_of(sp, join_spans(mine, s_span), piece, p)) return;
+  append_own<bf16, D>(a, s, g, p, tile == 0 && piece == 0);
   const bool has_rows = wr0 <= pr_last;
   const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
   const Load load(t, 1 << a.log2ps);
@@ -686,15 +717,12 @@ Plan plan_of(int n_seq, int Hq, int Hkv, int max_q, long slots, int window, bool
   p.per = (int)std::max((long)p.per, nb / 16384);      // units stay few under a table for millions of tokens
   const int least = std::max(p.per, p.walk);
   p.cut = nb > least;
-  // the most units that a window of nt tiles has, over nt
+  // the most units that a window of nt tiles has: nt ceil(nb / max(per nt, walk)), over nt
   long units = p.tiles;
-  if (p.cut && p.tiles > 256) {
-    units = p.tiles + nb / p.per + 1;
-  } else if (p.cut) {
-    for (long nt = 1; nt <= p.tiles; ++nt) {
-      const long per = std::max(p.per * nt, (long)p.walk);
-      units = std::max(units, nt * ((nb + per - 1) / per));
-    }
+  if (p.cut) {
+    const long few = std::min((long)p.tiles, std::max(1L, (long)p.walk / p.per));
+    units = std::max(units, few * ((nb + p.walk - 1) / p.walk));
+    if (p.tiles > few) units = p.tiles + nb / p.per + 1;
   }
   p.units = (int)units;
   p.part_rows = p.cut ? (size_t)sg * p.units * p.tile_rows : 0;
@@ -735,7 +763,12 @@ hipError_t launch_attn_masked(const AttnMaskedLaunch& L, hipStream_t st) {
   p.walk = pl.walk;
   trace_begin(st);
   hipError_t e = hipSuccess;
-  if (L.k_new) e = launch_append_window(L, st);
+  if (L.k_new && L.max_q <= kAppendFew) {
+    p.k_new = L.k_new;
+    p.v_new = L.v_new;
+  } else if (L.k_new) {
+    e = launch_append_window(L, st);
+  }
   if (e != hipSuccess) return e;
   trace_mark(st);
   const int sg = L.n_seq * L.Hkv;

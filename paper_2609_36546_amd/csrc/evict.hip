@@ -4,9 +4,10 @@
 // move, in order, to positions 0 .. n - 1 of other pages.
 //
 //   select kernel  one workgroup per (sequence, KV head): the mass of the last position
-//                  kept, found by its order number's four bytes from the top, each a
-//                  histogram in LDS of what the bytes before it leave; then the kept
-//                  positions by a scan in order, equal masses counted as they come.
+//                  kept, found by its order number's three digits of 11 bits from the top,
+//                  each a histogram in LDS of what the digits before it leave (no more of them
+//                  than it takes); then the kept positions by a scan in order, equal masses
+//                  counted as they come.
 //   move kernel    64 kept positions of one (sequence, KV head) per workgroup: keys are
 //                  runs of 32 channels per slot, values and masses gathered slot by slot
 //                  and stored 16 bytes at a time.
@@ -23,6 +24,7 @@ namespace {
 
 constexpr int kThreads = 1024;     // of the select kernel
 constexpr int kWaves = kThreads / kWave;
+constexpr int kDigit = 11, kBins = 1 << kDigit;
 constexpr int kRun = 16;           // neighbouring positions of a thread: in one page
 constexpr int kMove = 64;          // positions of a workgroup of the move kernel
 
@@ -78,9 +80,9 @@ __device__ __forceinline__ int2 scan2(int2 v, int2* part, int2* all) {
 // ONE: a round of threads holds all positions, so their masses are read once.
 template <bool ONE>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictParams a) {
-  __shared__ int s_hist[256];
+  __shared__ int2 s_hist[kBins / 2];
   __shared__ int2 s_part[kWaves];
-  __shared__ int s_digit, s_left;
+  __shared__ int s_digit, s_left, s_count;
   const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv, tid = threadIdx.x;
   const Seq s = seq_of(a, slot);
   if (g == 0 && tid == 0) a.new_lens[s.b] = s.n;
@@ -108,42 +110,44 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictParams a) {
   };
   if (ONE) load(0);
   auto candidate = [&](int p) { return p >= s.lo && p < s.hi; };
-  // The order number of the last position kept, from its top byte down: `least` so far,
-  // its bytes below `shift` open; `left` to be kept among those that agree with it.
-  int left = s.n - s.lo - (s.L - s.hi);
+  // The order number of the last position kept, from its top digit down: `least` so far, its
+  // bits below `shift` open; `left` to be kept among those that agree with it above them.
+  int left = s.n - s.lo - (s.L - s.hi), shift = 32;
   unsigned least = 0;
   const bool ask = left > 0;        // else nothing beside what is kept unasked
-  for (int shift = 24; ask && shift >= 0; shift -= 8) {
-    if (tid < 256) s_hist[tid] = 0;
+  int* hist = reinterpret_cast<int*>(s_hist);
+  static_assert(kBins == 2 * kThreads, "two bins of a thread");
+  while (ask && shift > 0) {
+    const int above = shift;
+    shift = max(shift - kDigit, 0);
+    s_hist[tid] = make_int2(0, 0);
     __syncthreads();
     for (int r = 0; r < rounds; ++r) {
       if (!ONE) load(r);
       const int p0 = (r * kThreads + tid) * kRun;
 #pragma unroll
       for (int i = 0; i < kRun; ++i)
-        if (candidate(p0 + i) && (shift == 24 || (key[i] ^ least) >> (shift + 8) == 0)) atomicAdd(&s_hist[(key[i] >> shift) & 255], 1);
+        if (candidate(p0 + i) && (above == 32 || (key[i] ^ least) >> above == 0))
+          atomicAdd(&hist[(key[i] >> shift) & (kBins - 1)], 1);
     }
     __syncthreads();
-    if (tid < kWave) {              // a lane: four digits, from the top
-      int c[4], sum = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        c[i] = s_hist[255 - 4 * tid - i];
-        sum += c[i];
-      }
-      int before = wave_incl_scan_i(sum) - sum;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (before < left && before + c[i] >= left) {
-          s_digit = 255 - 4 * tid - i;
-          s_left = left - before;
-        }
-        before += c[i];
-      }
+    const int2 c = s_hist[kThreads - 1 - tid];     // from the top: .y, then .x
+    int2 all;
+    const int before = scan2(make_int2(c.x + c.y, 0), s_part, &all).x;
+    const bool hi = before < left && before + c.y >= left, lo = before + c.y < left && before + c.y + c.x >= left;
+    if (hi || lo) {
+      s_digit = 2 * (kThreads - 1 - tid) + (hi ? 1 : 0);
+      s_left = left - before - (hi ? 0 : c.y);
+      s_count = hi ? c.y : c.x;
     }
     __syncthreads();
     least |= (unsigned)s_digit << shift;
     left = s_left;
+    if (s_count == left) {          // all of the digit: none of them equals what is just below it
+      least -= 1;
+      shift = 0;
+      left = 0;
+    }
     __syncthreads();
   }
   // All above `least` are kept, and the first `left` that equal it.
@@ -178,7 +182,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictParams a) {
 }
 
 template <typename DT, int D>
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictParams a) {
+__global__ __launch_bounds__(256, 4) void evict_move_kernel(EvictParams a) {
   constexpr int EPL = 16 / (int)sizeof(DT);
   typedef __attribute__((__vector_size__(16))) int i32x4;
   __shared__ int s_src[kMove], s_dst[kMove / 16];      // page * page_size + slot; of a 16-slot run
@@ -228,27 +232,30 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictParams a) {
     }
   }
   // values: a channel's run of EPL slots
-  constexpr int RUNS = kMove / EPL;
-  for (int e = tid; e < RUNS * D; e += 256) {
-    const int r = e % RUNS, ch = e / RUNS, i = r * EPL;
-    if (i >= n) continue;
-    DT v[EPL];
+  constexpr int RUNS = kMove / EPL, VN = RUNS * D / 256;
+  static_assert(RUNS * D % 256 == 0, "whole rounds");
+  struct Run { DT e[EPL]; } run[VN];
+#pragma unroll
+  for (int x = 0; x < VN; ++x) {                       // all asked for before the first is stored
+    const int e = tid + 256 * x, i = e % RUNS * EPL, ch = e / RUNS;
 #pragma unroll
     for (int c = 0; c < EPL; ++c) {
-      const int at = s_src[i + c];                     // behind n: page 0, not used
-      v[c] = vc[(page(at) * D + ch) * ps + (at & (ps - 1))];
+      const int at = s_src[i + c];                     // behind n: a slot that is there, not used
+      run[x].e[c] = vc[(page(at) * D + ch) * ps + (at & (ps - 1))];
     }
+  }
+#pragma unroll
+  for (int x = 0; x < VN; ++x) {
+    const int e = tid + 256 * x, i = e % RUNS * EPL, ch = e / RUNS;
+    if (i >= n) continue;
     const int to = s_dst[i >> 4] + (i & 15);
     DT* dst = reinterpret_cast<DT*>(a.v_cache) + (page(to) * D + ch) * ps + (to & (ps - 1));
     if (i + EPL <= n) {
-      struct Run { DT e[EPL]; } run;
-#pragma unroll
-      for (int c = 0; c < EPL; ++c) run.e[c] = v[c];
-      *reinterpret_cast<i32x4*>(dst) = __builtin_bit_cast(i32x4, run);
+      *reinterpret_cast<i32x4*>(dst) = __builtin_bit_cast(i32x4, run[x]);
     } else {
 #pragma unroll
       for (int c = 0; c < EPL; ++c)
-        if (i + c < n) dst[c] = v[c];
+        if (i + c < n) dst[c] = run[x].e[c];
     }
   }
 }

@@ -12,6 +12,7 @@ its own (rope_window's with inverse=True).
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from typing import Optional
@@ -108,18 +109,20 @@ def lib() -> ctypes.CDLL:
         L.ipdv_attn_masked_workspace_size.argtypes = [ci] * 9
         L.ipdv_attn_masked_workspace_size.restype = cs
         L.verify_attn_masked.argtypes = [vp, i64, vp, vp, vp, vp, i32p, ci, i32p, i32p, i32p, ci, ci,
-                                         vp, vp, f32p, ci, ci, ci, ci, ci, cf, ci, vp, cs, vp]
+                                         cf, ci, f32p, i32p, i32p, vp, f32p, ci, ci, ci, ci, ci, cf,
+                                         ci, vp, cs, vp]
         L.verify_attn_masked.restype = ci
-        L.attn_mass.argtypes = [vp, i64, vp, f32p, i32p, ci, i32p, i32p, i32p, ci, ci, vp, f32p, cf,
-                                f32p, ci, ci, ci, ci, ci, cf, ci, vp]
+        L.attn_mass.argtypes = [vp, i64, vp, f32p, i32p, ci, i32p, i32p, i32p, ci, ci, cf, ci, f32p,
+                                i32p, i32p, f32p, cf, f32p, ci, ci, ci, ci, ci, cf, ci, vp]
         L.attn_mass.restype = ci
         L.kv_evict.argtypes = [vp, vp, f32p, i32p, ci, i32p, ci, i32p, i32p, i32p, ci, ci, ci, i32p,
                                i32p, ci, ci, ci, ci, ci, vp]
         L.kv_evict.restype = ci
         L.ipdv_verify_drafts_workspace_size.argtypes = [ci] * 5
         L.ipdv_verify_drafts_workspace_size.restype = cs
-        L.verify_drafts.argtypes = [vp, i64, vp, i64, ci, ci, i32p, i32p, ci, f32p, f32p, vp, vp,
-                                    ctypes.c_int32, i32p, i32p, u8p, f32p, f32p, ci, vp, cs, vp]
+        L.verify_drafts.argtypes = ([vp, i64, vp, i64, ci, ci, i32p, i32p, ci, f32p, f32p] +
+                                    [f32p, i32p, f32p, f32p] * 2 +
+                                    [ctypes.c_int32, i32p, i32p, u8p, f32p, f32p, ci, vp, cs, vp])
         L.verify_drafts.restype = ci
         L.ipdv_trace_events.argtypes = [ctypes.c_void_p, ci]
         L.ipdv_trace_events.restype = ci
@@ -985,16 +988,6 @@ def sample_logits(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
 # Attention with modified scores, the weights it gives and eviction by them, and
 # the verdict on drafts by probabilities.
 
-class _ScoreMod(ctypes.Structure):
-    _fields_ = [("softcap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p),
-                ("first_key", ctypes.c_void_p), ("end_key", ctypes.c_void_p)]
-
-
-class _Filters(ctypes.Structure):
-    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
-                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
-
-
 def _sized(t, name: str, dtype, dev, n: int):
     """Address of an optional [n] tensor."""
     if t is None:
@@ -1005,10 +998,11 @@ def _sized(t, name: str, dtype, dev, n: int):
     return at
 
 
-def _score_mod(softcap, window, slopes, first_key, end_key, T, Hq, dev):
-    return _ScoreMod(float(softcap), int(window), _sized(slopes, "slopes", torch.float32, dev, Hq),
-                     _sized(first_key, "first_key", torch.int32, dev, T),
-                     _sized(end_key, "end_key", torch.int32, dev, T))
+def _score_mod(slopes, first_key, end_key, T, Hq, dev):
+    """Addresses of the scores' arrays."""
+    return (_sized(slopes, "slopes", torch.float32, dev, Hq),
+            _sized(first_key, "first_key", torch.int32, dev, T),
+            _sized(end_key, "end_key", torch.int32, dev, T))
 
 
 def _paged(k_cache, page_table, dt, dev, D: int, B: int):
@@ -1024,6 +1018,7 @@ def _paged(k_cache, page_table, dt, dev, D: int, B: int):
     return kc, table, Hkv, ps, P, max_pages
 
 
+@functools.lru_cache(maxsize=1024)      # a step asks for the same ones: 1.5 us each
 def attn_masked_workspace_size(n_seq, Hq, Hkv, D, max_q, max_pages, page_size, window=0,
                                has_end_key=False) -> int:
     return int(lib().ipdv_attn_masked_workspace_size(n_seq, Hq, Hkv, D, max_q, max_pages, page_size,
@@ -1058,11 +1053,11 @@ def verify_attn_masked(q, k_new, v_new, k_cache, v_cache, page_table, ctx_lens, 
         kn, vn = _at(k_new, "k_new", dt, dev, 3), _at(v_new, "v_new", dt, dev, 3)
         if k_new.shape != (T, Hkv, D) or v_new.shape != (T, Hkv, D):
             raise ValueError("k_new / v_new must be [T,Hkv,D]")
-    mod = _score_mod(softcap, window, slopes, first_key, end_key, T, Hq, dev)
+    slopes_p, first_p, end_p = _score_mod(slopes, first_key, end_key, T, Hq, dev)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     if out is None:
-        out = torch.empty(T, Hq, D, dtype=dt, device=dev)
+        out = torch.empty_like(q)
     else:
         _need(out, "out", dt, dev, 3)
         if out.shape != shape:
@@ -1089,8 +1084,8 @@ def verify_attn_masked(q, k_new, v_new, k_cache, v_cache, page_table, ctx_lens, 
     else:
         ws, size = _given_workspace(workspace, dev)
     st = lib().verify_attn_masked(qp, qs, kn, vn, kc, vc, table, max_pages, ctx, cu, ids, n_seq,
-                                  max_q, ctypes.addressof(mod), out.data_ptr(), lp, Hq, Hkv, D, ps,
-                                  P, float(scale), code, ws, size, _stream(dev))
+                                  max_q, softcap, window, slopes_p, first_p, end_p, out.data_ptr(), lp,
+                                  Hq, Hkv, D, ps, P, scale, code, ws, size, _stream(dev))
     _check("verify_attn_masked", st)
     return out if lse is None else (out, lse)
 
@@ -1113,7 +1108,7 @@ def attn_mass(q, k_cache, lse, page_table, ctx_lens, cu_q, max_q: int, mass=None
     lp = _at(lse, "lse", torch.float32, dev, 2)
     if lse.shape != (T, Hq):
         raise ValueError("lse must be [T,Hq]")
-    mod = _score_mod(softcap, window, slopes, first_key, end_key, T, Hq, dev)
+    slopes_p, first_p, end_p = _score_mod(slopes, first_key, end_key, T, Hq, dev)
     if out is None:
         if mass is None:
             raise ValueError("mass or out must be given")
@@ -1130,8 +1125,9 @@ def attn_mass(q, k_cache, lse, page_table, ctx_lens, cu_q, max_q: int, mass=None
         check_page_table(page_table, ctx_lens, cu_q, max_q, ps, P, seq_ids=seq_ids, n_seq=n_seq,
                          rows=T)
     st = lib().attn_mass(qp, qs, kc, lp, table, max_pages, ctx, cu, ids, n_seq, max_q,
-                         ctypes.addressof(mod), None if mass is None else mass.data_ptr(),
-                         float(decay), mp, Hq, Hkv, D, ps, P, float(scale), code, _stream(dev))
+                         softcap, window, slopes_p, first_p, end_p,
+                         None if mass is None else mass.data_ptr(), decay, mp, Hq, Hkv, D, ps, P,
+                         scale, code, _stream(dev))
     _check("attn_mass", st)
     return out
 
@@ -1216,6 +1212,7 @@ def _check_evict(page_table, dst_table, ctx_lens, keep, ps, P, seq_ids, n_seq):
                 raise IpdvError("kv_evict", -1, f"sequence {b}: page {int(p)} is read and written")
 
 
+@functools.lru_cache(maxsize=1024)
 def verify_drafts_workspace_size(T, V, B, target_filtered=False, draft_filtered=False) -> int:
     return int(lib().ipdv_verify_drafts_workspace_size(T, V, B, 1 if target_filtered else 0,
                                                        1 if draft_filtered else 0))
@@ -1253,11 +1250,11 @@ def verify_drafts(target_logits, draft_logits, prop_tok, cu_q, u_accept, u_draw,
         if t is None:
             raise TypeError(f"{name} must be a torch.Tensor")
     xp, ua, ud = need(prop_tok, "prop_tok", i32, T), need(u_accept, "u_accept", f32, T), need(u_draw, "u_draw", f32, B)
-    tf = _Filters(need(temperature, "temperature", f32, T), need(top_k, "top_k", i32, T),
-                  need(top_p, "top_p", f32, T), need(min_p, "min_p", f32, T))
-    df = _Filters(need(draft_temperature, "draft_temperature", f32, T),
-                  need(draft_top_k, "draft_top_k", i32, T), need(draft_top_p, "draft_top_p", f32, T),
-                  need(draft_min_p, "draft_min_p", f32, T))
+    filters = (need(temperature, "temperature", f32, T), need(top_k, "top_k", i32, T),
+               need(top_p, "top_p", f32, T), need(min_p, "min_p", f32, T),
+               need(draft_temperature, "draft_temperature", f32, T),
+               need(draft_top_k, "draft_top_k", i32, T), need(draft_top_p, "draft_top_p", f32, T),
+               need(draft_min_p, "draft_min_p", f32, T))
     if outs is None:
         outs = {}
     made = {}
@@ -1271,14 +1268,13 @@ def verify_drafts(target_logits, draft_logits, prop_tok, cu_q, u_accept, u_draw,
         made[name] = t
     if workspace is None:
         size = max(verify_drafts_workspace_size(
-            T, V, B, any(t is not None for t in (top_k, top_p, min_p)),
-            any(t is not None for t in (draft_top_k, draft_top_p, draft_min_p))), 1)
+            T, V, B, not (top_k is None and top_p is None and min_p is None),
+            not (draft_top_k is None and draft_top_p is None and draft_min_p is None)), 1)
         workspace = torch.empty(size, dtype=torch.uint8, device=dev)
         ws = workspace.data_ptr()
     else:
         ws, size = _given_workspace(workspace, dev)
-    st = lib().verify_drafts(tp, ts, dp, ds, T, V, xp, cu, B, ua, ud, ctypes.addressof(tf),
-                             ctypes.addressof(df), int(eos_id), made["n_acc"].data_ptr(),
+    st = lib().verify_drafts(tp, ts, dp, ds, T, V, xp, cu, B, ua, ud, *filters, int(eos_id), made["n_acc"].data_ptr(),
                              made["token"].data_ptr(), made["finished"].data_ptr(),
                              made["p_accept"].data_ptr(), made["logp"].data_ptr(), code, ws, size,
                              _stream(dev))

@@ -321,7 +321,7 @@ def c_drafts(**kw):
              ws=256, wsb=1 << 30)
     a.update(kw)
     return ops.lib().verify_drafts(a["t"], a["ts"], a["d"], a["ds"], a["T"], a["V"], a["x"], a["cu"], a["B"], a["ua"], a["ud"],
-                                   None, None, -1, a["n"], a["tok"], a["fin"], a["pa"], a["lp"], a["dtype"], a["ws"], a["wsb"],
+                                   *[None] * 8, -1, a["n"], a["tok"], a["fin"], a["pa"], a["lp"], a["dtype"], a["ws"], a["wsb"],
                                    None)
 
 

@@ -247,14 +247,13 @@ def test_python_refusals():
 
 # --- refusals (no GPU) ---
 
-def c_attn(mod=None, **kw):
-    a = dict(q=16, qs=256, kn=16, vn=16, kc=16, vc=16, pt=16, mp=4, ctx=16, cu=16, n=2, mq=3, out=16, lse=16, Hq=4, Hkv=2,
+def c_attn(**kw):
+    a = dict(cap=0.0, window=0, q=16, qs=256, kn=16, vn=16, kc=16, vc=16, pt=16, mp=4, ctx=16, cu=16, n=2, mq=3, out=16, lse=16, Hq=4, Hkv=2,
              D=64, ps=16, P=8, scale=0.125, dtype=1, ws=256, wsb=1 << 30)
     a.update(kw)
-    m = ops._ScoreMod(**mod) if mod else None
     return ops.lib().verify_attn_masked(
         a["q"], a["qs"], a["kn"], a["vn"], a["kc"], a["vc"], a["pt"], a["mp"], a["ctx"], a["cu"], None, a["n"], a["mq"],
-        ops.ctypes.addressof(m) if m else None, a["out"], a["lse"], a["Hq"], a["Hkv"], a["D"], a["ps"], a["P"], a["scale"],
+        a["cap"], a["window"], None, None, None, a["out"], a["lse"], a["Hq"], a["Hkv"], a["D"], a["ps"], a["P"], a["scale"],
         a["dtype"], a["ws"], a["wsb"], None)
 
 
@@ -264,8 +263,8 @@ def c_attn(mod=None, **kw):
     (dict(qs=255), -1), (dict(P=0), -1), (dict(mp=0), -1), (dict(D=96), -2), (dict(ps=128), -2), (dict(dtype=2), -2),
     (dict(q=8), -2), (dict(out=24), -2), (dict(kn=8, vn=16), -2), (dict(qs=260), -2), (dict(mq=1 << 28, Hq=2), -2),
     (dict(P=1 << 30), -2), (dict(n=40000), -2), (dict(ws=None), -3), (dict(wsb=4), -3), (dict(ws=264), -2),
-    (dict(n=0, q=None), 0), (dict(mod=dict(softcap=-1.0)), -1), (dict(mod=dict(softcap=float("inf"))), -1),
-    (dict(mod=dict(softcap=float("nan"))), -1), (dict(mod=dict(window=-1)), -1)])
+    (dict(n=0, q=None), 0), (dict(cap=-1.0), -1), (dict(cap=float("inf")), -1),
+    (dict(cap=float("nan")), -1), (dict(window=-1), -1)])
 def test_attention_refusals(kw, status):
     assert c_attn(**kw) == status
     assert (ops.lib().ipdv_last_error() != b"") == (status != 0)

@@ -219,20 +219,19 @@ def test_validate_names_pages_that_are_read_and_written():
 
 # --- refusals (no GPU) ---
 
-def c_mass(mod=None, **kw):
-    a = dict(q=16, qs=256, kc=16, lse=16, pt=16, mp=4, ctx=16, cu=16, n=2, mq=3, mi=16, decay=1.0, mo=16, Hq=4, Hkv=2, D=64,
+def c_mass(**kw):
+    a = dict(cap=0.0, window=0, q=16, qs=256, kc=16, lse=16, pt=16, mp=4, ctx=16, cu=16, n=2, mq=3, mi=16, decay=1.0, mo=16, Hq=4, Hkv=2, D=64,
              ps=16, P=8, scale=0.125, dtype=1)
     a.update(kw)
-    m = ops._ScoreMod(**mod) if mod else None
     return ops.lib().attn_mass(a["q"], a["qs"], a["kc"], a["lse"], a["pt"], a["mp"], a["ctx"], a["cu"], None, a["n"], a["mq"],
-                               ops.ctypes.addressof(m) if m else None, a["mi"], a["decay"], a["mo"], a["Hq"], a["Hkv"],
+                               a["cap"], a["window"], None, None, None, a["mi"], a["decay"], a["mo"], a["Hq"], a["Hkv"],
                                a["D"], a["ps"], a["P"], a["scale"], a["dtype"], None)
 
 
 @pytest.mark.parametrize("kw,status", [
     (dict(q=None), -1), (dict(kc=None), -1), (dict(lse=None), -1), (dict(mo=None), -1), (dict(ctx=None), -1), (dict(Hq=5), -1),
     (dict(mq=0), -1), (dict(n=-1), -1), (dict(scale=-1.0), -1), (dict(qs=255), -1), (dict(decay=-0.1), -1),
-    (dict(decay=float("inf")), -1), (dict(mod=dict(window=-1)), -1), (dict(mod=dict(softcap=-1.0)), -1), (dict(D=96), -2),
+    (dict(decay=float("inf")), -1), (dict(window=-1), -1), (dict(cap=-1.0), -1), (dict(D=96), -2),
     (dict(ps=8), -2), (dict(dtype=2), -2), (dict(q=8), -2), (dict(kc=8), -2), (dict(mp=1 << 20), -2), (dict(n=0, q=None), 0)])
 def test_mass_refusals(kw, status):
     assert c_mass(**kw) == status
