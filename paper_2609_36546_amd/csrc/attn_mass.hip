@@ -9,8 +9,8 @@
 //
 // Scores are taken as there, S^T[32 keys x 16 rows] = K . Q^T, a lane holding 8 keys of
 // one row.  Up to 64 rows (attn_mass_few_kernel) a wave keeps all of them in registers and
-// streams keys; with more (attn_mass_many_kernel) it keeps a block of keys and streams rows, with
-// many the 16 waves of a workgroup every 16th tile of them.  Weights are added per lane, over the rows
+// streams keys; with more (attn_mass_many_kernel) it keeps one or two blocks of keys and streams
+// rows, with many the 8 waves of a workgroup every 8th tile of them.  Weights are added per lane, over the rows
 // of a lane's column, and joined over the 16 columns at the end.
 #include <algorithm>
 #include <type_traits>
@@ -98,11 +98,19 @@ template <typename DT, int D, int QT> struct RowTile {
 #pragma unroll
     for (int t = 0; t < QT; ++t)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float w = fast_exp2(sc[t][i >> 2][i & 3]);
-        if (masked) w = k0 + i >= row[t].lo && k0 + i < row[t].hi ? w : 0.f;
-        sum[i] += w;
-      }
+      for (int i = 0; i < 8; ++i) sc[t][i >> 2][i & 3] = fast_exp2(sc[t][i >> 2][i & 3]);
+    if (masked) {
+      asm volatile("");             // a branch: most blocks do without the comparisons
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          sc[t][i >> 2][i & 3] = k0 + i >= row[t].lo && k0 + i < row[t].hi ? sc[t][i >> 2][i & 3] : 0.f;
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[i] += sc[t][i >> 2][i & 3];
   }
 };
 
@@ -160,9 +168,13 @@ __global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void attn_mass_few_ke
 }
 
 // RS of W waves share NB blocks of keys and take every RS-th tile of rows; the others have
-// blocks of their own.
-template <typename DT, int D, int NB, int RS, int W>
-__global__ __launch_bounds__(64 * W) void attn_mass_many_kernel(MassParams a) {
+// blocks of their own.  PLAIN: without ranges and slopes, so nothing is loaded for them.
+template <typename DT, int D, int NB, int RS, int W, bool PLAIN>
+__global__ __launch_bounds__(64 * W, RS > 1 ? 1 : 2) void attn_mass_many_kernel(MassParams a) {
+  if constexpr (PLAIN) {
+    a.first_key = a.end_key = nullptr;
+    a.slopes = nullptr;
+  }
   constexpr int KS = W / RS;
   __shared__ float s_sum[W][NB][kBlk];
   const int sg = slot_head_of(a, blockIdx.x, blockIdx.y, gridDim.x);
@@ -253,7 +265,9 @@ hipError_t launch_attn_mass(const AttnMaskedLaunch& L, hipStream_t st) {
   const long rows = (long)L.max_q * p.G, sg = (long)L.n_seq * L.Hkv;
   const long blocks = ((long)p.slots + kBlk - 1) / kBlk;
   const unsigned gx = (unsigned)((sg + 7) / 8 * 8);
-  p.per = (int)std::max(std::clamp(sg * blocks / 2048, 4L, 32L), (blocks + 65534) / 65535);
+  // 64 windows by 1 to 8 Ki keys: of one row 130 us at 32 blocks, 123 at 8; of eight (64 packed rows)
+  // 90 and 113, as each workgroup first reads its rows
+  p.per = (int)std::max(std::clamp(sg * blocks / 2048, 4L, rows <= 16 ? 8L : rows <= 32 ? 16L : 32L), (blocks + 65534) / 65535);
   trace_begin(st);
   auto pick = [&](auto dt, auto dim) {
     using DT = decltype(dt);
@@ -268,9 +282,19 @@ hipError_t launch_attn_mass(const AttnMaskedLaunch& L, hipStream_t st) {
       auto many = [&](auto kernel, int at_once, int waves) {
         hipLaunchKernelGGL(kernel, dim3(gx, (unsigned)((blocks + at_once - 1) / at_once)), dim3(64 * waves), 0, st, p);
       };
-      constexpr int RS = sizeof(DT) * D > 256 ? 8 : 16;       // 128 registers do not do for fp32 at D = 128
-      if (rows > 64 * RS) many(attn_mass_many_kernel<DT, D, 1, RS, RS>, 1, RS);
-      else many(attn_mass_many_kernel<DT, D, 1, 1, 4>, 4, 4);
+      // two blocks per pass over a bf16 row: 24 windows of 64 rows 98 to 58 us; fp32, which the
+      // products bound, has more of waves of one
+      constexpr int NB = sizeof(DT) == 4 ? 1 : 2;
+      // Waves share blocks where there are too few for all, or the first keys' waves, which have
+      // every row, would end last (4 KV heads, G = 8: 8 prompts of 512 to 1024 tokens 358 to 75 us,
+      // 64 of them 535 to 442; 24 windows of 100 rows by 500 to 3000 keys take 136 us so, and 85
+      // by waves of their own; 16 by 256 to 512 keys 31 and 34).
+      const bool shared = rows > 512 && (rows > 4096 || sg * ((blocks + NB - 1) / NB) < 4096);
+      const bool plain = !p.first_key && !p.end_key && !p.slopes;
+      if (!shared && plain) many(attn_mass_many_kernel<DT, D, NB, 1, 4, true>, 4 * NB, 4);
+      else if (!shared) many(attn_mass_many_kernel<DT, D, NB, 1, 4, false>, 4 * NB, 4);
+      else if (plain) many(attn_mass_many_kernel<DT, D, NB, 8, 8, true>, NB, 8);
+      else many(attn_mass_many_kernel<DT, D, NB, 8, 8, false>, NB, 8);
     }
   };
   typedef std::integral_constant<int, 64> D64;
