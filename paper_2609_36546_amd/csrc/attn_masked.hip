@@ -26,7 +26,7 @@
 //
 // Work split.  A workgroup takes a piece of the keys of one row tile; tiles of
 // a window that has few are cut into more pieces (split_of), joined by a second
-// kernel.  Up to 16 rows (or in fp32) its four waves walk keys of their own, in registers
+// kernel.  Up to 16 rows, and in fp32, its four waves walk keys of their own, in registers
 // (masked_keys_kernel); with more rows they hold 16 or 32 rows each and share the
 // keys through a ring in LDS (masked_tile_kernel).
 #include <algorithm>
@@ -410,37 +410,34 @@ __device__ __forceinline__ void append_own(const MaskedParams& a, const Seq& s, 
   __syncthreads();
 }
 
-// Operands straight into registers.  Few rows (OWN false): the four waves take every fourth
-// block of the piece.  More in fp32 (OWN): rows of their own, and the same blocks, which the
-// first to ask leaves in the vector cache.
-template <typename DT, int D, int QT, bool OWN>
+// Operands straight into registers; the four waves take every fourth block of the piece, and
+// join their rows at the end.  (In fp32, where a block's products take 2 thousand clocks per 16
+// rows, waves with rows of their own left the longest tiles to run alone at the end: 6 prefixes
+// of 120 to 700 positions 80 us, 61 so; two windows of 300 rows by 1 to 4.5 Ki keys 995 and 513.)
+template <typename DT, int D, int QT>
 __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys_kernel(MaskedParams a) {
-  constexpr int kRows = (OWN ? kWaves : 1) * 16 * QT, kStep = OWN ? 1 : kWaves, kTile = (D / 16) * kWave, PT = sizeof(DT) == 2 ? 2 : 1;
-  __shared__ floatx4 s_acc[2][OWN ? 1 : kTile];
+  constexpr int kRows = 16 * QT, kTile = (D / 16) * kWave, PT = sizeof(DT) == 2 ? 2 : 1;
+  __shared__ floatx4 s_acc[2][kTile];
   __shared__ float s_ml[2][32];
-  __shared__ int s_span[kWaves][2];
   const int sg = slot_head_of(a, blockIdx.x, blockIdx.y, gridDim.x);
   if (sg < 0) return;
   const int slot = sg / a.Hkv, g = sg - slot * a.Hkv;
   const Seq s = seq_of(a, slot);
   if (s.rows == 0) return;
   const Split sp = split_of(a, s, kRows);
-  const int tile = blockIdx.y / sp.np, piece = blockIdx.y - tile * sp.np;
+  const int unit = gridDim.y - 1 - blockIdx.y;         // the last tiles, which see most, first
+  const int tile = unit / sp.np, piece = unit - tile * sp.np;
   if (tile >= sp.nt) return;
   const int pr0 = tile * kRows, pr_last = min(pr0 + kRows, s.rows) - 1;
-  const int wv = uni(threadIdx.x / kWave), wr0 = OWN ? pr0 + 16 * QT * wv : pr0;
+  const int wv = uni(threadIdx.x / kWave);
   Rows<DT, D, QT, PT> R;
-  R.begin(a, s, g, wr0, pr_last);
+  R.begin(a, s, g, pr0, pr_last);
   const Span mine = span_of<QT>(R.row);
   Piece p;
-  if (!piece_of(sp, OWN ? join_spans(mine, s_span) : mine, piece, p)) return;
+  if (!piece_of(sp, mine, piece, p)) return;
   const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
   append_own<DT, D>(a, s, g, p, tile == 0 && piece == 0);
-  int first = p.b0 + (OWN ? 0 : wv), last = p.b1;
-  if (OWN) {
-    first = max(first, mine.lo / kBlk);
-    last = wr0 > pr_last ? 0 : min(last, (mine.hi + kBlk - 1) / kBlk);
-  }
+  const int first = p.b0 + wv, last = p.b1;
   auto walk = [&](auto careful) __attribute__((always_inline)) {
     constexpr bool CAREFUL = decltype(careful)::value;
     R.reset();
@@ -450,21 +447,21 @@ __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys
     Frags<DT, D> f;
     load_keys<DT, D>(a, f, first * kBlk, parts);
     load_values<DT, D>(a, a.v_cache, f, first * kBlk, parts);
-    parts.look_up(a, pt, (first + kStep) * kBlk, g);
-    for (int n = first; n < last; n += kStep) {
+    parts.look_up(a, pt, (first + kWaves) * kBlk, g);
+    for (int n = first; n < last; n += kWaves) {
       const int t0 = n * kBlk;
       // the next keys are asked for once the scores have used theirs, the next
       // values once the products have
       floatx4 sc[QT][2];
       scores<DT, D, QT>(f, R.Q, sc);
-      const bool more = n + kStep < last;
+      const bool more = n + kWaves < last;
       __builtin_amdgcn_sched_barrier(0);
-      if (more) load_keys<DT, D>(a, f, t0 + kStep * kBlk, parts);
+      if (more) load_keys<DT, D>(a, f, t0 + kWaves * kBlk, parts);
       __builtin_amdgcn_sched_barrier(0);
       R.template weigh<CAREFUL>(a, f, sc, t0, CAREFUL || !mine.whole(t0));
       __builtin_amdgcn_sched_barrier(0);
-      if (more) load_values<DT, D>(a, a.v_cache, f, t0 + kStep * kBlk, parts);
-      parts.look_up(a, pt, t0 + 2 * kStep * kBlk, g);
+      if (more) load_values<DT, D>(a, a.v_cache, f, t0 + kWaves * kBlk, parts);
+      parts.look_up(a, pt, t0 + 2 * kWaves * kBlk, g);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -473,10 +470,6 @@ __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys
   if (__any(R.odd())) walk(std::true_type());
   note_pieces(a, p, sg, tile, piece);
   R.join_lanes();
-  if (OWN) {
-    R.finish(a, s, g, wr0, pr_last, p.whole, part_row_of(a, sp, sg, tile, piece, kRows) + 16 * QT * wv);
-    return;
-  }
 #pragma unroll
   for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -696,7 +689,7 @@ __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedParams a, int t
 }
 
 struct Plan {
-  bool shared;                // waves of rows of their own
+  bool shared;                // keys through LDS
   int qt, tile_rows, tiles, units, per, walk;
   bool cut;                   // some tile may be cut
   size_t part_rows;
@@ -704,8 +697,8 @@ struct Plan {
 Plan plan_of(int n_seq, int Hq, int Hkv, int max_q, long slots, int window, bool ends, bool bf16) {
   Plan p;
   const long rows = (long)max_q * (Hq / Hkv), sg = (long)n_seq * Hkv;
-  p.shared = rows > 16;
-  p.qt = p.shared && bf16 && rows > 64 ? 2 : 1;
+  p.shared = rows > 16 && bf16;
+  p.qt = rows > (bf16 ? 64 : 16) ? 2 : 1;
   p.tile_rows = (p.shared ? 64 : 16) * p.qt;
   p.tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
   long nb = (slots + kBlk - 1) / kBlk;
@@ -780,11 +773,11 @@ hipError_t launch_attn_masked(const AttnMaskedLaunch& L, hipStream_t st) {
     constexpr int D = decltype(dim)::value;
     if constexpr (sizeof(DT) == 2) {
       const bool wide = L.page_size > 16;
-      if (!pl.shared) go(masked_keys_kernel<DT, D, 1, false>);
+      if (!pl.shared) go(masked_keys_kernel<DT, D, 1>);
       else if (pl.qt == 1) { if (wide) go(masked_tile_kernel<D, true, 1>); else go(masked_tile_kernel<D, false, 1>); }
       else { if (wide) go(masked_tile_kernel<D, true, 2>); else go(masked_tile_kernel<D, false, 2>); }
     } else {
-      if (pl.shared) go(masked_keys_kernel<DT, D, 1, true>); else go(masked_keys_kernel<DT, D, 1, false>);
+      if (pl.qt == 2) go(masked_keys_kernel<DT, D, 2>); else go(masked_keys_kernel<DT, D, 1>);
     }
   };
   typedef std::integral_constant<int, 64> D64;
