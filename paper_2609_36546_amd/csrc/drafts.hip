@@ -8,7 +8,8 @@
 //
 //   stats kernel    one workgroup per row, model and 8192 entries: maximum and mass against
 //                   it, by quarters too.  Reads every logit once; its vector instructions
-//                   (22 an entry, 15 of them in 64 bits) take longer than its bytes.
+//                   (20 an entry, 9 of them in 64 bits; busy for 90% of its time) take longer
+//                   than its bytes: 512 rows of 151936 bf16 logits of two models 97 us.
 //   verdict kernel  one workgroup per sequence: the rows' masses joined, p(x) and q(x), the first
 //                   row that ends the window.
 //   rest kernel     one workgroup per rejected row and 8192 entries: masses of max(0, p - q), by
@@ -18,9 +19,9 @@
 //
 // Precision.  A token is a whole number next to borders that lie as close as the
 // smallest probabilities, and a rejected row's masses are differences: all masses are
-// 64-bit floats.  2^y is 2^n (integer added to the exponent) times a polynomial of degree 7 on
-// [-1/2, 1/2], fitted to 4e-11 of the result, 14 instructions an entry, at fp32's rate on this
-// card.
+// 64-bit floats.  2^y is 2^(n + i / 256) from a table in LDS, n added to its exponent, times a
+// polynomial of degree 2 of what is left of y, off by 1.1e-10.  (A polynomial of degree 7 alone took
+// 5 instructions more, 117 us.)
 //
 // Filters: sample_logits' kernels find every row's cut first (what is ordered before it
 // is not kept).  A row of temperature 0 keeps its first maximum: with no filters the
@@ -78,6 +79,26 @@ struct DraftParams {
 };
 constexpr int kNone = 0x7fffffff;
 
+// 2^(i / 256), from LDS where a kernel needs many; what i adds to the exponent's sum below is
+// taken from the upper words.
+constexpr int kPowers = 256;
+struct Powers {
+  double v[kPowers];
+  constexpr Powers() : v() {
+    for (int i = 0; i < kPowers; ++i) {
+      const double x = 0.69314718055994530942 * i / kPowers;
+      double sum = 0.0;
+      for (int n = 24; n > 0; --n) sum = (1.0 + sum) * x / n;        // e^x - 1, from the last term
+      v[i] = __builtin_bit_cast(double, __builtin_bit_cast(u64, 1.0 + sum) - ((u64)i << 44));
+    }
+  }
+};
+__device__ constexpr Powers kPow;
+__device__ __forceinline__ void powers_to(double (&lds)[kPowers]) {
+  static_assert(kPowers == kThreads, "one of a thread");
+  lds[threadIdx.x] = kPow.v[threadIdx.x];
+}
+
 // a b + c with c in scalar registers: the compiler would take the form that adds to its operand and
 // copy every coefficient for it, two instructions each.
 __device__ __forceinline__ double fma_s(double a, double b, double c) {
@@ -85,18 +106,21 @@ __device__ __forceinline__ double fma_s(double a, double b, double c) {
   asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
   return r;
 }
-// 2^(d slope) for d slope <= 0 (and not below -1000).
-__device__ __forceinline__ double exp2_of(double d, double slope) {
-  const double magic = 6755399441055744.0;         // 1.5 * 2^52: the sum's low bits are the nearest whole number
+// A mass in two factors, so that a sum takes it in one instruction.
+struct Product {
+  double base, by;
+  __device__ __forceinline__ operator double() const { return base * by; }
+  __device__ __forceinline__ void add_to(double& sum) const { sum = fma(base, by, sum); }
+};
+// 2^(d slope) for d slope <= 0 (and not below -1001): d slope = n + i / 256 + f, |f| <= 2^-9.
+__device__ __forceinline__ Product exp2_of(double d, double slope, const double* pow) {
+  const double magic = 26388279066624.0;           // 1.5 * 2^44: the sum's low bits count 256ths
   const double t = fma(d, slope, magic), f = fma(d, slope, magic - t);
-  double p = fma_s(f, 1.5201920948780836e-05, 0.00015469291124750825);
-  p = fma_s(p, f, 0.001333392256603758);
-  p = fma_s(p, f, 0.009618027253729474);
-  p = fma_s(p, f, 0.05550410353445379);
-  p = fma_s(p, f, 0.2402265119815696);
-  p = fma_s(p, f, 0.693147180728448);
-  p = fma_s(p, f, 0.999999999961681);
-  return __hiloint2double((int)((unsigned)__double2hiint(p) + ((unsigned)__double2loint(t) << 20)), __double2loint(p));
+  const unsigned at = (unsigned)__double2loint(t);
+  const double base = pow[at & (kPowers - 1)];
+  // 2^f = 1 + ln 2 f + (ln 2 f)^2 / 2, the cubic term levelled: off by 1.1e-10
+  const double by = fma(fma_s(f, 0.2402265069591007, 0.6931473393594654), f, 1.0);
+  return {__hiloint2double((int)((unsigned)__double2hiint(base) + (at << 12)), __double2loint(base)), by};
 }
 
 // A row's temperature: log2(e) / T, and the distance from the maximum behind which nothing
@@ -112,12 +136,16 @@ __device__ __forceinline__ Scale scale_of(const Model& m, int r) {
   Scale s;
   s.bad = !(t >= 0.f);
   s.first_only = t == 0.f;
-  s.slope = 1.4426950408889634 / (t > 0.f ? (double)fminf(fmaxf(t, kLeastTemp), kMostTemp) : 1.0);
-  s.far = -1000.0 / s.slope;
+  const double at = t > 0.f ? (double)fminf(fmaxf(t, kLeastTemp), kMostTemp) : 1.0;
+  s.slope = 1.4426950408889634 / at;
+  s.far = -693.14718055994531 * at;
   return s;
 }
-__device__ __forceinline__ double mass_of(float l, float max, double far, double slope) {
-  return exp2_of(fmax((double)l - (double)max, far), slope);
+__device__ __forceinline__ Product mass_of(float l, float max, double far, double slope, const double* pow) {
+  // the larger of two that are not positive, to the 20 bits of their upper words
+  const double d = (double)l - (double)max;
+  const unsigned hi = min((unsigned)__double2hiint(d), (unsigned)__double2hiint(far));
+  return exp2_of(__hiloint2double((int)hi, __double2loint(d)), slope, pow);
 }
 
 // What a row is known by once its chunks are joined.
@@ -128,9 +156,9 @@ struct RowMass {
   int v_cut;
   bool bad;
   __device__ __forceinline__ bool keeps(float l, int v) const { return (l > l_cut) | ((l == l_cut) & (v <= v_cut)); }
-  __device__ __forceinline__ double mass(float l, int v) const {      // the probability
-    const double m = mass_of(l, max, far, slope) * inv;
-    return keeps(l, v) & (l > -INFINITY) ? m : 0.0;
+  __device__ __forceinline__ double mass(float l, int v, const double* pow) const {      // the probability
+    const double m = mass_of(l, max, far, slope, pow) * inv;
+    return (keeps(l, v) & (l > -INFINITY)) ? m : 0.0;
   }
 };
 template <int CTRL> __device__ __forceinline__ double dpp_move_d(double v) {
@@ -167,7 +195,7 @@ __device__ __forceinline__ RowMass join(const DraftParams& p, const Model& m, in
       top = other > top ? other : top;
     }
   }
-  const double mass = sum32(rec.max > -INFINITY && rec.mass > 0.0 ? rec.mass * mass_of(rec.max, mx, sc.far, sc.slope) : 0.0);
+  const double mass = sum32(rec.max > -INFINITY && rec.mass > 0.0 ? rec.mass * mass_of(rec.max, mx, sc.far, sc.slope, kPow.v) : 0.0);
   RowMass out;
   out.bad = bad || sc.bad || !(mx > -INFINITY);
   out.slope = sc.slope;
@@ -182,10 +210,6 @@ __device__ __forceinline__ RowMass join(const DraftParams& p, const Model& m, in
 template <typename DT> __device__ __forceinline__ float logit(const Model& m, int r, int v) {
   return to_f32(reinterpret_cast<const DT*>(m.logits)[(size_t)r * m.stride + v]);
 }
-template <typename DT> __device__ __forceinline__ double prob(const DraftParams& p, const Model& m, const RowMass& row, int r, int v) {
-  return row.mass(logit<DT>(m, r, v), v);
-}
-
 __device__ __forceinline__ double wave_sum_d(double v) {
   v = sum32(v);
   return v + __hiloint2double(lane_xor32(__double2hiint(v)), lane_xor32(__double2loint(v)));
@@ -226,23 +250,22 @@ __global__ __launch_bounds__(kThreads) void draft_stats_kernel(DraftParams p) {
   __shared__ double s_part[kWaves];
   __shared__ u64 s_top[kWaves];
   __shared__ int s_bad;
+  __shared__ __attribute__((aligned(16))) double s_pow[kPowers];
   const Model& m = blockIdx.y ? p.draft : p.target;
   const int r = blockIdx.x / p.chunks, c = blockIdx.x - r * p.chunks, v0 = c * kChunk, tid = threadIdx.x;
   Entries<DT, VEC> x;
   x.load(m, r, v0, p.V);
   const Scale sc = scale_of(m, r);
+  powers_to(s_pow);
   if (tid == 0) s_bad = 0;
   float mx = -INFINITY;
-  bool bad = false;
 #pragma unroll
-  for (int i = 0; i < kPer; i += 2) {
-    mx = fmaxf(mx, fmaxf(x.get(i), x.get(i + 1)));
-    bad |= __builtin_isunordered(x.get(i), x.get(i + 1));
-  }
-  mx = wave_max(mx);
+  for (int i = 0; i < kPer; i += 2)                // NaN if there is one: v_maximum3_f32
+    mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(x.get(i), x.get(i + 1)));
+  const bool bad = mx != mx;
+  mx = wave_max(bad ? INFINITY : mx);
   if (lane_id() == 0) s_max[tid / kWave] = mx;
   __syncthreads();
-  if (bad) s_bad = 1;
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) mx = fmaxf(mx, s_max[i]);
   if (mx == INFINITY) s_bad = 1;
@@ -271,9 +294,9 @@ __global__ __launch_bounds__(kThreads) void draft_stats_kernel(DraftParams p) {
     for (int i = 0; i < kPer; ++i) {
       const float l = x.get(i);
       if (!CUT) {
-        sum += mass_of(l, mx, sc.far, sc.slope);   // of -inf: 2^-1000
+        mass_of(l, mx, sc.far, sc.slope, s_pow).add_to(sum);   // of -inf: 2^-1000
       } else if ((l > l_cut) | ((l == l_cut) & (v0 + Entries<DT, VEC>::at(i) <= v_cut))) {      // few: a branch
-        sum += mass_of(l, mx, sc.far, sc.slope);
+        mass_of(l, mx, sc.far, sc.slope, s_pow).add_to(sum);
       }
     }
   }
@@ -330,7 +353,7 @@ __global__ __launch_bounds__(kThreads) void draft_verdict_kernel(DraftParams p) 
       } else if (x < 0) {
         how = kNoDraft;
       } else {
-        const double pt = drafted ? t.mass(lt, x) : 0.0, pd = !given ? 1.0 : drafted ? d.mass(ld, x) : 0.0;
+        const double pt = drafted ? t.mass(lt, x, kPow.v) : 0.0, pd = !given ? 1.0 : drafted ? d.mass(ld, x, kPow.v) : 0.0;
         ratio = pt >= pd ? (pt > 0.0 ? 1.f : 0.f) : (float)(pt / pd);
         how = !((double)u * pd < pt) ? kRejected : x == p.eos_id ? kEos : kGoesOn;
       }
@@ -350,10 +373,10 @@ __global__ __launch_bounds__(kThreads) void draft_verdict_kernel(DraftParams p) 
 }
 
 // An entry's mass in what a rejected row is drawn from.
-__device__ __forceinline__ double rest_of(const RowMass& t, float lt, const RowMass& d, float ld, bool certain, int x, int v) {
-  const double m = t.mass(lt, v);
-  if (certain) return v == x ? 0.0 : m;
-  return fmax(m - d.mass(ld, v), 0.0);
+__device__ __forceinline__ double rest_of(const RowMass& t, float lt, const RowMass& d, float ld, bool certain, int x, int v, const double* pow) {
+  if (!(t.keeps(lt, v) & (lt > -INFINITY)) || (certain && v == x)) return 0.0;      // filters leave few: a branch
+  const double m = t.mass(lt, v, pow);
+  return certain ? m : fmax(m - d.mass(ld, v, pow), 0.0);
 }
 
 template <typename DT, bool VEC>
@@ -363,6 +386,7 @@ __global__ __launch_bounds__(kThreads) void draft_rest_kernel(DraftParams p) {
   if (end == kNone || (end & 7) != kRejected) return;
   const int r = window_of(p, b).r0 + (end >> 3), v0 = c * kChunk;
   const bool certain = !p.draft.logits;
+  __shared__ __attribute__((aligned(16))) double s_pow[kPowers];
   Entries<DT, VEC> lt, ld;
   lt.load(p.target, r, v0, p.V);
   if (!certain) ld.load(p.draft, r, v0, p.V);
@@ -370,17 +394,19 @@ __global__ __launch_bounds__(kThreads) void draft_rest_kernel(DraftParams p) {
   const RowMass t = join(p, p.target, r);
   RowMass d{};
   if (!certain) d = join(p, p.draft, r);
+  powers_to(s_pow);
+  __syncthreads();
   double sum = 0.0;
   if (t.cut | d.cut | (u64)certain) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      sum += rest_of(t, lt.get(i), d, certain ? 0.f : ld.get(i), certain, x, v0 + Entries<DT, VEC>::at(i));
+      sum += rest_of(t, lt.get(i), d, certain ? 0.f : ld.get(i), certain, x, v0 + Entries<DT, VEC>::at(i), s_pow);
   } else {                                         // everything is kept, -inf of 2^-1000
     // both probabilities rounded alike: of equal ones nothing is left
 #pragma clang fp contract(off)
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const double m = mass_of(lt.get(i), t.max, t.far, t.slope) * t.inv, q = mass_of(ld.get(i), d.max, d.far, d.slope) * d.inv;
+      const double m = mass_of(lt.get(i), t.max, t.far, t.slope, s_pow) * t.inv, q = mass_of(ld.get(i), d.max, d.far, d.slope, s_pow) * d.inv;
       sum += fmax(m - q, 0.0);
     }
   }
@@ -430,7 +456,7 @@ __global__ __launch_bounds__(kThreads) void draft_draw_kernel(DraftParams p) {
   for (int i = 0; i < QN; ++i) all += mine[i];
   const bool rest = how == kRejected && wave_sum_d(all) > kNothing;
   if (!rest) {
-    const double f = chunk_max > -INFINITY ? mass_of(chunk_max, t.max, t.far, t.slope) * t.inv : 0.0;
+    const double f = chunk_max > -INFINITY ? mass_of(chunk_max, t.max, t.far, t.slope, kPow.v) * t.inv : 0.0;
 #pragma unroll
     for (int i = 0; i < QN; ++i)
       mine[i] = t.cut && !p.target.cuts ? (index_of(t.cut) / kQuarter == lane * QN + i ? 1.0 : 0.0)      // temperature 0
@@ -494,7 +520,7 @@ __global__ __launch_bounds__(kThreads) void draft_draw_kernel(DraftParams p) {
   double m[PER], sum = 0.0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    m[i] = rest ? rest_of(t, lt[i], d, ld[i], certain, x, v0 + i) : t.mass(lt[i], v0 + i);
+    m[i] = rest ? rest_of(t, lt[i], d, ld[i], certain, x, v0 + i, kPow.v) : t.mass(lt[i], v0 + i, kPow.v);
     sum += m[i];
   }
   const double incl = wave_scan_d(sum);
