@@ -384,27 +384,28 @@ __device__ __forceinline__ size_t part_row_of(const MaskedParams& a, const Split
 }
 
 // The window's keys and values to their pages, by every workgroup those that it reads
-// (several may write the same), by the first of a (sequence, head) all; a kernel of its own for
-// it takes 2 to 6 us, and its launch 2.5 of the host's.
+// (several may write the same), by the first of a (sequence, head) all.  A kernel of its own for it
+// costs a launch, 2.5 us of the host's and 2 to 6 of the device's; this costs the workgroups at the
+// window a round trip (8 windows of eight by 1 to 8 Ki keys 37.0 to 36.1 us, one 23.7 to 22.1; 32
+// windows 83.5 and 86, 64 the same).
 constexpr int kAppendFew = 16;         // window rows up to which this is done
 template <typename DT, int D>
 __device__ __forceinline__ void append_own(const MaskedParams& a, const Seq& s, int g, const Piece& p, bool all) {
   if (!a.k_new) return;
   const int from = all ? s.L : max(s.L, p.b0 * kBlk), to = all ? s.L + s.kb : min(s.L + s.kb, p.b1 * kBlk);
-  if (from < to) {
-    const int32_t* table = a.page_table + (size_t)s.b * a.max_pages;
-    const int ps = 1 << a.log2ps;
-    const DT* kn = reinterpret_cast<const DT*>(a.k_new);
-    const DT* vn = reinterpret_cast<const DT*>(a.v_new);
-    DT* kc = reinterpret_cast<DT*>(const_cast<void*>(a.k_cache));
-    DT* vc = reinterpret_cast<DT*>(a.v_cache);
-    for (int e = threadIdx.x; e < (to - from) * D; e += 256) {
-      const int pos = from + e / D, d = e % D, sl = pos & (ps - 1);
-      const size_t page = (size_t)min(max(table[min(pos >> a.log2ps, a.max_pages - 1)], 0), a.num_pages - 1) * a.Hkv + g;
-      const size_t src = ((size_t)(s.r0 + pos - s.L) * a.Hkv + g) * D + d;
-      kc[((page * (D / 32) + d / 32) << a.log2ps) * 32 + sl * 32 + (d & 31)] = kn[src];
-      vc[((page * D + d) << a.log2ps) + sl] = vn[src];
-    }
+  if (from >= to) return;
+  const int32_t* table = a.page_table + (size_t)s.b * a.max_pages;
+  const int ps = 1 << a.log2ps;
+  const DT* kn = reinterpret_cast<const DT*>(a.k_new);
+  const DT* vn = reinterpret_cast<const DT*>(a.v_new);
+  DT* kc = reinterpret_cast<DT*>(const_cast<void*>(a.k_cache));
+  DT* vc = reinterpret_cast<DT*>(a.v_cache);
+  for (int e = threadIdx.x; e < (to - from) * D; e += 256) {
+    const int pos = from + e / D, d = e % D, sl = pos & (ps - 1);
+    const size_t page = (size_t)min(max(table[min(pos >> a.log2ps, a.max_pages - 1)], 0), a.num_pages - 1) * a.Hkv + g;
+    const size_t src = ((size_t)(s.r0 + pos - s.L) * a.Hkv + g) * D + d;
+    kc[((page * (D / 32) + d / 32) << a.log2ps) * 32 + sl * 32 + (d & 31)] = kn[src];
+    vc[((page * D + d) << a.log2ps) + sl] = vn[src];
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // written when the others pass the barrier
   __syncthreads();
@@ -703,10 +704,12 @@ Plan plan_of(int n_seq, int Hq, int Hkv, int max_q, long slots, int window, bool
   p.tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
   long nb = (slots + kBlk - 1) / kBlk;
   if (!ends) nb = std::min(nb, ((long)(window > 0 ? window : INT_MAX) + p.tile_rows / (Hq / Hkv) + 1 + 2 * kBlk) / kBlk);
-  p.per = p.shared ? 16 : 8;
+  // pieces of 8 blocks and 16: one window of eight 18 and 22 us, 24 of 13 by 200 to 3000 keys 43 and
+  // 49; fp32, of 4 and 8, 24 small ones 26 and 29
+  p.per = bf16 ? 8 : 4;
   // With rows enough to fill the chip by themselves, walks of up to 48 blocks stay whole: the
   // merge costs more.
-  p.walk = sg * p.tiles >= 512 ? 48 : (int)std::clamp(sg * nb / 1024, (long)p.per, 64L);
+  p.walk = sg * p.tiles >= 512 ? 48 : (int)std::clamp(sg * nb / (p.shared ? 1024 : 512), (long)p.per, 64L);
   p.per = (int)std::max((long)p.per, nb / 16384);      // units stay few under a table for millions of tokens
   const int least = std::max(p.per, p.walk);
   p.cut = nb > least;

@@ -8,10 +8,10 @@
 // no partial results, the same bits every time.
 //
 // Scores are taken as there, S^T[32 keys x 16 rows] = K . Q^T, a lane holding 8 keys of
-// one row.  Up to 64 rows (attn_mass_few_kernel) a wave keeps all of them in registers and
-// streams keys; with more (attn_mass_many_kernel) it keeps one or two blocks of keys and streams
-// rows, with many the 8 waves of a workgroup every 8th tile of them.  Weights are added per lane, over the rows
-// of a lane's column, and joined over the 16 columns at the end.
+// one row.  Up to 64 rows (attn_mass_few_kernel) a wave keeps all of them and streams keys; with
+// more (attn_mass_many_kernel) it keeps one or two blocks of keys and streams rows, with many
+// the 8 waves of a workgroup every 8th tile of them.  Weights are added per lane, over the rows of
+// a lane's column, and joined over the 16 columns at the end.
 #include <algorithm>
 #include <type_traits>
 
@@ -61,6 +61,7 @@ template <typename DT, int D, int QT> struct RowTile {
   // Asked for; `arrive` makes them what the rest works with.  Behind the last row its copies.
   // Where G is a power of two a whole tile's addresses are a uniform base and an offset that
   // the lane has in every tile (a product of 64 bits costs as much as a score).
+  template <bool QUERIES = true>
   __device__ __forceinline__ void ask(const MassParams& a, const Seq& s, int g, int t, int pr0) {
     const int lane = lane_id(), c16 = lane & 15, j = lane >> 4;
     const DT* q = reinterpret_cast<const DT*>(a.q);
@@ -69,13 +70,13 @@ template <typename DT, int D, int QT> struct RowTile {
       at[t] = i + li;
       raw[t].ask(a, s, i, h, li, lh);
       lse[t] = (a.lse + (size_t)(s.r0 + i) * a.Hq + h)[li * a.Hq + lh];
-      load_row(t, q + (size_t)(s.r0 + i) * a.q_stride + (size_t)h * D + ((size_t)li * a.q_stride + lh * D), j);
+      if (QUERIES) load_row(t, q + (size_t)(s.r0 + i) * a.q_stride + (size_t)h * D + ((size_t)li * a.q_stride + lh * D), j);
     } else {
       const int pr = min(pr0 + c16, s.rows - 1), i = row_of(a, pr), h = g * a.G + pr - i * a.G;
       at[t] = i;
       raw[t].ask(a, s, i, h);
       lse[t] = a.lse[(size_t)(s.r0 + i) * a.Hq + h];
-      load_row(t, q + (size_t)(s.r0 + i) * a.q_stride + (size_t)h * D, j);
+      if (QUERIES) load_row(t, q + (size_t)(s.r0 + i) * a.q_stride + (size_t)h * D, j);
     }
   }
   __device__ __forceinline__ void load_row(int t, const DT* qr, int j) {
@@ -126,25 +127,38 @@ __device__ __forceinline__ float pick(const float (&sum)[8]) {
   return out;
 }
 
+// The queries of four tiles lie in LDS: in registers they leave room for two waves per SIMD instead
+// of four, and each wave would load them all (64 windows of eight by 1 to 8 Ki keys, 64 packed rows:
+// 90 us so, 80 from LDS).
 template <typename DT, int D, int QT>
-__global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void attn_mass_few_kernel(MassParams a) {
+__global__ __launch_bounds__(256, QT == 4 ? 4 : sizeof(DT) == 4 ? 1 : 2) void attn_mass_few_kernel(MassParams a) {
+  constexpr bool LDS = QT == 4;
+  static_assert(!LDS || (sizeof(DT) == 2 && QT == kWaves), "a tile of a wave");
+  __shared__ bf16x8 s_q[LDS ? QT : 1][LDS ? D / 32 : 1][kWave];
   const int sg = slot_head_of(a, blockIdx.x, blockIdx.y, gridDim.x);
   if (sg < 0) return;
   const int slot = sg / a.Hkv, g = sg - slot * a.Hkv;
   const Seq s = seq_of(a, slot);
   const int b0 = blockIdx.y * a.per, b1 = min(b0 + a.per, (s.end + kBlk - 1) / kBlk);
-  const int first = b0 + uni(threadIdx.x / kWave);
-  if (first >= b1) return;
+  if (b0 >= b1) return;
+  const int wv = uni(threadIdx.x / kWave), first = b0 + wv;
   RowTile<DT, D, QT> R;
   Span span{INT_MAX, 0, INT_MAX, 0};
   if (s.rows > 0) {
+    if constexpr (LDS) {
+      RowTile<DT, D, 1> mine;
+      mine.ask(a, s, g, 0, 16 * wv);
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      R.ask(a, s, g, t, 16 * t);
-      R.arrive(a, s, t, 16 * t);
+      for (int ks = 0; ks < D / 32; ++ks) s_q[wv][ks][lane_id()] = mine.Q.q[0][ks];
     }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) R.template ask<!LDS>(a, s, g, t, 16 * t);
+#pragma unroll
+    for (int t = 0; t < QT; ++t) R.arrive(a, s, t, 16 * t);
     span = span_of<QT>(R.row);
   }
+  if (LDS) __syncthreads();
+  if (first >= b1) return;
   const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
   Parts parts, next;
   parts.look_up(a, pt, first * kBlk, g);
@@ -156,7 +170,23 @@ __global__ __launch_bounds__(256, sizeof(DT) == 4 ? 1 : 2) void attn_mass_few_ke
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const bool seen = span.sees(t0);
     floatx4 sc[QT][2];
-    if (seen) scores<DT, D, QT>(f, R.Q, sc);
+    if (seen) {
+      if constexpr (LDS) {
+        asm volatile("" ::: "memory");           // read anew: there are no registers to keep them
+#pragma unroll
+        for (int t = 0; t < QT; ++t) sc[t][0] = sc[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < D / 32; ++ks)
+#pragma unroll
+          for (int t = 0; t < QT; ++t) {
+            const bf16x8 q = s_q[t][ks][lane_id()];
+#pragma unroll
+            for (int st = 0; st < 2; ++st) sc[t][st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.kf(st, ks), q, sc[t][st], 0, 0, 0);
+          }
+      } else {
+        scores<DT, D, QT>(f, R.Q, sc);
+      }
+    }
     __builtin_amdgcn_sched_barrier(0);
     if (n + kWaves < b1 && span.sees(t0 + kWaves * kBlk)) load_keys<DT, D>(a, f, t0 + kWaves * kBlk, next);
     __builtin_amdgcn_sched_barrier(0);
@@ -265,9 +295,9 @@ hipError_t launch_attn_mass(const AttnMaskedLaunch& L, hipStream_t st) {
   const long rows = (long)L.max_q * p.G, sg = (long)L.n_seq * L.Hkv;
   const long blocks = ((long)p.slots + kBlk - 1) / kBlk;
   const unsigned gx = (unsigned)((sg + 7) / 8 * 8);
-  // 64 windows by 1 to 8 Ki keys: of one row 130 us at 32 blocks, 123 at 8; of eight (64 packed rows)
-  // 90 and 113, as each workgroup first reads its rows
-  p.per = (int)std::max(std::clamp(sg * blocks / 2048, 4L, rows <= 16 ? 8L : rows <= 32 ? 16L : 32L), (blocks + 65534) / 65535);
+  // 64 windows by 1 to 8 Ki keys: of one row 130 us at 32 blocks of a workgroup, 123 at 8; of eight (64
+  // packed rows) 83 at either, 80 at 16
+  p.per = (int)std::max(std::clamp(sg * blocks / 2048, 4L, rows <= 16 ? 8L : 16L), (blocks + 65534) / 65535);
   trace_begin(st);
   auto pick = [&](auto dt, auto dim) {
     using DT = decltype(dt);
@@ -277,8 +307,9 @@ hipError_t launch_attn_mass(const AttnMaskedLaunch& L, hipStream_t st) {
     };
     if (rows <= 16) few(attn_mass_few_kernel<DT, D, 1>);
     else if (rows <= 32) few(attn_mass_few_kernel<DT, D, 2>);
-    else if (rows <= 64 && sizeof(DT) == 2) few(attn_mass_few_kernel<DT, D, 4>);
-    else {
+    else if (rows <= 64 && sizeof(DT) == 2) {
+      if constexpr (sizeof(DT) == 2) few(attn_mass_few_kernel<DT, D, 4>);
+    } else {
       auto many = [&](auto kernel, int at_once, int waves) {
         hipLaunchKernelGGL(kernel, dim3(gx, (unsigned)((blocks + at_once - 1) / at_once)), dim3(64 * waves), 0, st, p);
       };
