@@ -491,7 +491,9 @@ __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys
 // slots].  Within a piece the 16-byte entries are permuted so that the lanes that a
 // 16-byte LDS read serves at once hit distinct banks; a load writes lane l's 16 bytes
 // to entry l, so the loading lane fetches what belongs there.
-constexpr int kRing = 3;
+// Two units with a tile per wave (64 windows of eight 155 to 145 us; a fourth workgroup per CU, for which
+// it leaves room, takes 160), three with two (packed prompts 57 us, with two units 59).
+constexpr int ring_of(int QT) { return QT == 1 ? 2 : 3; }
 __device__ __forceinline__ int key_entry(int slot, int q) { return 4 * slot + (q ^ (((slot >> 1) & 1) | ((slot >> 2) & 2))); }
 __device__ __forceinline__ int val_entry(int ch, int h) { return 2 * ch + (h ^ ((ch >> 2) & 1)); }
 __device__ __forceinline__ int wide_entry(int ch, int q) {
@@ -572,7 +574,7 @@ template <int D, bool WIDE> struct Loader {
 template <int D, bool WIDE, int QT>
 __global__ __launch_bounds__(256, 3) void masked_tile_kernel(MaskedParams a) {
   typedef Loader<D, WIDE> Load;
-  constexpr int kRows = 64 * QT;
+  constexpr int kRows = 64 * QT, kRing = ring_of(QT);
   __shared__ __attribute__((aligned(1024))) char s_ring[kRing * Load::kUnit];
   __shared__ int s_span[kWaves][2];
   const int sg = slot_head_of(a, blockIdx.x, blockIdx.y, gridDim.x);
