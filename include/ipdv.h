@@ -746,9 +746,11 @@ size_t ipdv_attn_masked_workspace_size(int n_seq, int Hq, int Hkv, int D, int ma
  *
  * q [T, Hq, D] (dtype), q_row_stride elements from one row to the next (>= Hq *
  * D); k_new, v_new [T, Hkv, D] (dtype; both NULL: the window is in the cache
- * already); lse [T, Hq] float or NULL.  bf16 and fp32, D in {64, 128}.  The cache and the other arguments as in verify_attn_paged.  q's rows,
- * k_new, v_new, the caches, out and workspace start on 16-byte boundaries.
+ * already); lse [T, Hq] float or NULL.  bf16 and fp32, D in {64, 128}.  The cache and the
+ * other arguments as in verify_attn_paged.  q's rows, k_new, v_new, the caches, out and
+ * workspace start on 16-byte boundaries.
  * The workspace is written by the call; two calls that may overlap need one each.
+ * max_q * Hq / Hkv may be 2^20 in any case, and more where the keys are few.
  *
  * Errors: IPDV_EINVAL (also: softcap negative or not finite, window < 0),
  * IPDV_EUNSUPPORTED (D, page_size, dtype, alignment, sizes), IPDV_EWORKSPACE, IPDV_EHIP.
@@ -853,8 +855,8 @@ size_t ipdv_verify_drafts_workspace_size(int T, int V, int B, int target_filtere
  * target_logits, draft_logits [T, V] (dtype), *_row_stride elements from one row to the next
  * (>= V); prop_tok [T], cu_q [B+1] int32 (cu_q[B] <= T); u_accept [T], u_draw [B] float in [0,
  * 1); temperature ... draft_min_p [T], each NULL for off (as in sample_logits).
- * Requirements: 0 <= T < 2^22, 0 <= B < 2^22, 1 <= V <= 262144, T * V < 2^35; workspace on a
- * 16-byte boundary, written by the call: two calls that may overlap need one each.
+ * Requirements: 0 <= T < 2^22, 0 <= B < 2^22, 1 <= V <= 262144, T * V and B * V < 2^35;
+ * workspace on a 16-byte boundary, written by the call: two calls that may overlap need one each.
  *
  * Errors: IPDV_EINVAL, IPDV_EUNSUPPORTED (dtype, V, T), IPDV_EWORKSPACE, IPDV_EHIP.
  */

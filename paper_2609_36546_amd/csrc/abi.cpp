@@ -750,8 +750,9 @@ static int masked_call_check(const void* q, int64_t q_stride, const void* k_cach
 int verify_attn_masked(const void* q, int64_t q_stride, const void* k_new, const void* v_new, void* k_cache, void* v_cache,
                        const int32_t* page_table, int max_pages, const int32_t* ctx_lens, const int32_t* cu_q,
                        const int32_t* seq_ids, int n_seq, int max_q, float softcap, int window, const float* slopes,
-                       const int32_t* first_key, const int32_t* end_key, void* out, float* lse, int Hq, int Hkv, int D, int page_size, int num_pages, float scale, int dtype, void* workspace,
-                       size_t workspace_bytes, void* hip_stream) {
+                       const int32_t* first_key, const int32_t* end_key, void* out, float* lse, int Hq, int Hkv, int D,
+                       int page_size, int num_pages, float scale, int dtype, void* workspace, size_t workspace_bytes,
+                       void* hip_stream) {
   const ipdv::ScoreMod m{softcap, window, slopes, first_key, end_key};
   int st = score_mod_check(softcap, window);
   if (st != IPDV_OK) return st;
@@ -828,7 +829,7 @@ int kv_evict(void* k_cache, void* v_cache, float* mass, const int32_t* page_tabl
 static int drafts_shape_check(int T, int V, int B) {
   if (T < 0) return fail(IPDV_EINVAL, "T must be >= 0 (got %d)", T);
   if (B < 0) return fail(IPDV_EINVAL, "B must be >= 0 (got %d)", B);
-  if (B >= 1 << 22) return fail(IPDV_EUNSUPPORTED, "B too large");
+  if (B >= 1 << 22 || (int64_t)B * V >= (int64_t)1 << 35) return fail(IPDV_EUNSUPPORTED, "B too large");
   return sample_shape_check(T, V);
 }
 

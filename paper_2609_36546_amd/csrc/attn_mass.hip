@@ -207,14 +207,15 @@ __global__ __launch_bounds__(64 * W, RS > 1 ? 1 : 2) void attn_mass_many_kernel(
   }
   constexpr int KS = W / RS;
   __shared__ float s_sum[W][NB][kBlk];
-  const int sg = slot_head_of(a, blockIdx.x, blockIdx.y, gridDim.x);
+  const int by = blockIdx.z * gridDim.y + blockIdx.y;
+  const int sg = slot_head_of(a, blockIdx.x, by, gridDim.x);
   if (sg < 0) return;
   const int slot = sg / a.Hkv, g = sg - slot * a.Hkv;
   const Seq s = seq_of(a, slot);
   const int wv = uni(threadIdx.x / kWave), rs = wv % RS;
   // the first keys, which most rows see, first
-  const int t0 = (blockIdx.y * KS + wv / RS) * NB * kBlk;
-  if ((int)blockIdx.y * KS * NB * kBlk >= s.end) return;
+  const int t0 = (by * KS + wv / RS) * NB * kBlk;
+  if (by * KS * NB * kBlk >= s.end) return;
   const ScalarInts pt = scalar(a.page_table + (size_t)s.b * a.max_pages);
   float sum[NB][8];
 #pragma unroll
@@ -311,7 +312,8 @@ hipError_t launch_attn_mass(const AttnMaskedLaunch& L, hipStream_t st) {
       if constexpr (sizeof(DT) == 2) few(attn_mass_few_kernel<DT, D, 4>);
     } else {
       auto many = [&](auto kernel, int at_once, int waves) {
-        hipLaunchKernelGGL(kernel, dim3(gx, (unsigned)((blocks + at_once - 1) / at_once)), dim3(64 * waves), 0, st, p);
+        const long ny = (blocks + at_once - 1) / at_once, nz = (ny + 65534) / 65535;
+        hipLaunchKernelGGL(kernel, dim3(gx, (unsigned)((ny + nz - 1) / nz), (unsigned)nz), dim3(64 * waves), 0, st, p);
       };
       // two blocks per pass over a bf16 row: 24 windows of 64 rows 98 to 58 us; fp32, which the
       // products bound, has more of waves of one

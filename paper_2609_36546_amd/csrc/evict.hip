@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256, 4) void evict_move_kernel(EvictParams a) {
   __shared__ int s_src[kMove], s_dst[kMove / 16];      // page * page_size + slot; of a 16-slot run
   const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv, tid = threadIdx.x;
   const Seq s = seq_of(a, slot);
-  const int i0 = blockIdx.y * kMove, n = min(s.n - i0, kMove);
+  const int i0 = (blockIdx.z * gridDim.y + blockIdx.y) * kMove, n = min(s.n - i0, kMove);
   if (n <= 0) return;
   const int ps = a.page_size;
   if (tid < kMove) {
@@ -278,7 +278,8 @@ hipError_t launch_kv_evict(const EvictLaunch& L, hipStream_t st) {
   if (e != hipSuccess) return e;
   trace_mark(st);
   auto move = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(sg, (p.dst_slots + kMove - 1) / kMove), dim3(256), 0, st, p);
+    const int ny = (p.dst_slots + kMove - 1) / kMove, nz = (ny + 65534) / 65535;
+    hipLaunchKernelGGL(kernel, dim3(sg, (ny + nz - 1) / nz, nz), dim3(256), 0, st, p);
   };
   if (L.dtype_bf16) {
     if (L.D == 128) move(evict_move_kernel<bf16, 128>); else move(evict_move_kernel<bf16, 64>);

@@ -11,7 +11,7 @@ from paper_2609_36546_amd import ops
 from tests import masked_reference as ref
 from tests.masked_reference import BF16, F32, Batch, check_attention, f64, limits
 from tests.test_gpu_drafts import call, check, rows
-from tests.test_gpu_mass_evict import appended, check_evict, check_mass, dev, masses
+from tests.test_gpu_mass_evict import appended, check_evict, check_mass, dev, evicted, masses
 
 
 def bits(t):
@@ -274,3 +274,55 @@ def test_a_shared_workspace_holds_nothing_between_calls():
         for s, state in ((a, want[0]), (c, want[1]), (a, want[0])):
             s.run()
             assert same(s.state(), state)
+
+
+# --- the largest tables and bounds ---
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("max_q", [9, 200])
+def test_masses_under_a_table_of_the_largest_width(dt, max_q):
+    """2^22 positions: more blocks of keys than a grid's second dimension holds."""
+    b = Batch([(900, 9), (5, 3)], 16, 2, 64, 64, dt, seed=6)
+    lse = appended(b)
+    m = masses(b)
+    pt, ctx, cu, _ = b.args
+    wide = torch.full((2, (1 << 22) // 64 - 4), -1, dtype=torch.int32).cuda()
+    wide[:, : pt.shape[1]] = pt
+    got = ops.attn_mass(b.q.cuda(), b.kc, lse, wide, ctx, cu, max_q, mass=m.cuda(), decay=0.5)
+    check_mass(b, got, lse, m, 0.5, {})
+
+
+@pytest.mark.gpu
+def test_attention_under_a_loose_bound_of_windows():
+    """A max_q of 2^17, 2^20 rows per KV head: half of what a call may have."""
+    b = Batch([(900, 2), (5, 9)], 8, 1, 64, 16, BF16, seed=3)
+    want, lse0 = ops.verify_attn_masked(b.q.cuda(), b.k_new.cuda(), b.v_new.cuda(), b.kc, b.vc, *b.args, lse=True, window=700)
+    pt, ctx, cu, _ = b.args
+    wide = torch.full((2, 5000), -1, dtype=torch.int32).cuda()
+    wide[:, : pt.shape[1]] = pt
+    out, lse = ops.verify_attn_masked(b.q.cuda(), None, None, b.kc, b.vc, wide, ctx, cu, 1 << 17, lse=True, window=700,
+                                      seq_ids=torch.tensor([1, 0], dtype=torch.int32).cuda())
+    for i, L in enumerate(b.ctx):
+        r, n = b.rows(i), int(b.k[i])
+        x = ref.attention(f64(b.q[r]), b.K[i], b.V[i], int(L), b.scale, *limits(int(L), n, 700))
+        check_attention(out[r], lse[r], x, BF16, int(L) + n, True)
+        check_attention(want[r], lse0[r], x, BF16, int(L) + n, b.max_q * 8 > 16)
+
+
+@pytest.mark.gpu
+def test_eviction_under_tables_of_the_largest_width():
+    b, table, dst, dkeep = evicted([300], [130], 2, 64, 64, BF16, 3, [130])
+    m = masses(b, 5)
+    before = b.kc.cpu(), b.vc.cpu(), m.clone()
+    mass = m.cuda()
+    wide = lambda t: torch.cat([t, torch.full((1, (1 << 22) // 64 - t.shape[1]), -1, dtype=torch.int32).cuda()], 1)  # noqa: E731
+    new, kept = ops.kv_evict(b.kc, b.vc, mass, wide(b.args[0]), wide(dst), b.args[1], dkeep, 4, 64)
+    assert (kept[0, :, 130:] == -1).all()
+    slots = table.shape[1] * 64
+    check_evict(b, table, before, [130], 4, 64, new, kept[:, :, :slots], mass)
+
+
+def test_batches_too_large_for_a_launch_are_refused():
+    size = ops.verify_drafts_workspace_size
+    assert size(0, 262144, 1 << 16) > 0 and size(0, 262144, 1 << 17) == 0
