@@ -888,8 +888,8 @@ int verify_drafts(const void* target_logits, int64_t target_row_stride,
  * lmhead_logp_gather 1, source_split_kl 1 (+1 with cu), rope_window 1,
  * kv_append_q8 1, kv_read_q8 1, verify_attn_q8 2 (attention, merge of cut
  * items), sample_logits 2 (chunks, rows), verify_attn_masked 3 (append, attention, merge;
- * empty where there is none), attn_mass 1, kv_evict 2 (selection, move), verify_drafts 4
- * (the rows' masses, with their cuts; verdicts; what is left of rejected rows; draws).
+ * empty where there is none), attn_mass 1, kv_evict 2 (selection, move), verify_drafts 3
+ * (the rows' masses, with their cuts; verdicts and what is left of rejected rows; draws).
  */
 int ipdv_trace_events(void* const* events, int capacity);
 int ipdv_trace_count(void);

@@ -392,7 +392,7 @@ constexpr int kAppendFew = 16;         // window rows up to which this is done
 template <typename DT, int D>
 __device__ __forceinline__ void append_own(const MaskedParams& a, const Seq& s, int g, const Piece& p, bool all) {
   if (!a.k_new) return;
-  const int from = all ? s.L : max(s.L, p.b0 * kBlk), to = all ? s.L + s.kb : min(s.L + s.kb, p.b1 * kBlk);
+  const int from = all ? s.L : max(s.L, p.b0 * kBlk), to = all ? s.end : min(s.end, p.b1 * kBlk);
   if (from >= to) return;
   const int32_t* table = a.page_table + (size_t)s.b * a.max_pages;
   const int ps = 1 << a.log2ps;

@@ -10,10 +10,10 @@
 //                   it, by quarters too.  Reads every logit once; its vector instructions
 //                   (20 an entry, 9 of them in 64 bits; busy for 90% of its time) take longer
 //                   than its bytes: 512 rows of 151936 bf16 logits of two models 97 us.
-//   verdict kernel  one workgroup per sequence: the rows' masses joined, p(x) and q(x), the first
-//                   row that ends the window.
-//   rest kernel     one workgroup per rejected row and 8192 entries: masses of max(0, p - q), by
-//                   quarters.
+//   rest kernel     one workgroup per sequence and 8192 entries: the rows' masses joined, p(x) and
+//                   q(x), the first row that ends the window, by each anew (a kernel of its own
+//                   took 6 us, and 2.5 of the host's); of a rejected row the masses of max(0, p - q),
+//                   by quarters.
 //   draw kernel     one workgroup per sequence: the quarter where the mass passes u, in it
 //                   the entry.
 //
@@ -326,11 +326,10 @@ __device__ __forceinline__ Window window_of(const DraftParams& p, int b) {
   return w;
 }
 
-// The rows of a sequence, eight at a time, 32 lanes each.
-template <typename DT>
-__global__ __launch_bounds__(kThreads) void draft_verdict_kernel(DraftParams p) {
+// How window b ends, for the whole workgroup: its rows, eight at a time, 32 lanes each.  `tell`:
+// what is known of it now goes to the outputs.
+template <typename DT> __device__ __forceinline__ int verdict_of(const DraftParams& p, int b, bool tell) {
   __shared__ int s_end;
-  const int b = blockIdx.x;
   if (threadIdx.x == 0) s_end = kNone;
   __syncthreads();
   const Window w = window_of(p, b);
@@ -357,19 +356,22 @@ __global__ __launch_bounds__(kThreads) void draft_verdict_kernel(DraftParams p) 
         ratio = pt >= pd ? (pt > 0.0 ? 1.f : 0.f) : (float)(pt / pd);
         how = !((double)u * pd < pt) ? kRejected : x == p.eos_id ? kEos : kGoesOn;
       }
-      p.p_accept[r] = ratio;
+      if (tell) p.p_accept[r] = ratio;
       if (how != kGoesOn) atomicMin(&s_end, 8 * i + how);
     }
   }
   __syncthreads();
   const int end = s_end, how = end == kNone ? kGoesOn : end & 7;
-  if (threadIdx.x != 0) return;
-  p.verdict[b] = end;
-  if (how == kRejected || how == kNoDraft) return;           // the draw kernel's
-  p.n_acc[b] = how == kGoesOn ? w.k : (end >> 3) + (how == kEos ? 1 : 0);
-  p.token[b] = -1;
-  p.finished[b] = how == kEos;
-  if (p.logp) p.logp[b] = __uint_as_float(0x7fc00000u);
+  if (tell && threadIdx.x == 0) {
+    p.verdict[b] = end;
+    if (how != kRejected && how != kNoDraft) {               // else the draw kernel's
+      p.n_acc[b] = how == kGoesOn ? w.k : (end >> 3) + (how == kEos ? 1 : 0);
+      p.token[b] = -1;
+      p.finished[b] = how == kEos;
+      if (p.logp) p.logp[b] = __uint_as_float(0x7fc00000u);
+    }
+  }
+  return end;
 }
 
 // An entry's mass in what a rejected row is drawn from.
@@ -382,7 +384,7 @@ __device__ __forceinline__ double rest_of(const RowMass& t, float lt, const RowM
 template <typename DT, bool VEC>
 __global__ __launch_bounds__(kThreads) void draft_rest_kernel(DraftParams p) {
   const int b = blockIdx.x / p.chunks, c = blockIdx.x - b * p.chunks;
-  const int end = p.verdict[b];
+  const int end = verdict_of<DT>(p, b, c == 0);
   if (end == kNone || (end & 7) != kRejected) return;
   const int r = window_of(p, b).r0 + (end >> 3), v0 = c * kChunk;
   const bool certain = !p.draft.logits;
@@ -645,10 +647,6 @@ hipError_t launch_verify_drafts(const DraftLaunch& L, hipStream_t st) {
       hipLaunchKernelGGL((draft_stats_kernel<DT, VEC, false>), all, dim3(kThreads), 0, st, p);
   });
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  trace_mark(st);
-  with([&](auto dt, auto) { hipLaunchKernelGGL(draft_verdict_kernel<decltype(dt)>, dim3(L.B), dim3(kThreads), 0, st, p); });
-  e = hipGetLastError();
   if (e != hipSuccess) return e;
   trace_mark(st);
   with([&](auto dt, auto v) {
