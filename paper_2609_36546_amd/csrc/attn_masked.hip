@@ -400,7 +400,7 @@ __device__ __forceinline__ void append_own(const MaskedParams& a, const Seq& s, 
   const DT* vn = reinterpret_cast<const DT*>(a.v_new);
   DT* kc = reinterpret_cast<DT*>(const_cast<void*>(a.k_cache));
   DT* vc = reinterpret_cast<DT*>(a.v_cache);
-  for (int e = threadIdx.x; e < (to - from) * D; e += 256) {
+  for (int e = threadIdx.x; e < (to - from) * D; e += blockDim.x) {
     const int pos = from + e / D, d = e % D, sl = pos & (ps - 1);
     const size_t page = (size_t)min(max(table[min(pos >> a.log2ps, a.max_pages - 1)], 0), a.num_pages - 1) * a.Hkv + g;
     const size_t src = ((size_t)(s.r0 + pos - s.L) * a.Hkv + g) * D + d;
@@ -411,15 +411,15 @@ __device__ __forceinline__ void append_own(const MaskedParams& a, const Seq& s, 
   __syncthreads();
 }
 
-// Operands straight into registers; the four waves take every fourth block of the piece, and
-// join their rows at the end.  (In fp32, where a block's products take 2 thousand clocks per 16
+// Operands straight into registers; the W waves take every W-th block of the piece, and join
+// their rows at the end.  (In fp32, where a block's products take 2 thousand clocks per 16
 // rows, waves with rows of their own left the longest tiles to run alone at the end: 6 prefixes
 // of 120 to 700 positions 80 us, 61 so; two windows of 300 rows by 1 to 4.5 Ki keys 995 and 513.)
-template <typename DT, int D, int QT>
-__global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys_kernel(MaskedParams a) {
+template <typename DT, int D, int QT, int W>
+__global__ __launch_bounds__(64 * W, W == 8 || sizeof(DT) * D > 256 ? 1 : 2) void masked_keys_kernel(MaskedParams a) {
   constexpr int kRows = 16 * QT, kTile = (D / 16) * kWave, PT = sizeof(DT) == 2 ? 2 : 1;
-  __shared__ floatx4 s_acc[2][kTile];
-  __shared__ float s_ml[2][32];
+  __shared__ floatx4 s_acc[W / 2][kTile];
+  __shared__ float s_ml[W / 2][32];
   const int sg = slot_head_of(a, blockIdx.x, blockIdx.y, gridDim.x);
   if (sg < 0) return;
   const int slot = sg / a.Hkv, g = sg - slot * a.Hkv;
@@ -448,21 +448,21 @@ __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys
     Frags<DT, D> f;
     load_keys<DT, D>(a, f, first * kBlk, parts);
     load_values<DT, D>(a, a.v_cache, f, first * kBlk, parts);
-    parts.look_up(a, pt, (first + kWaves) * kBlk, g);
-    for (int n = first; n < last; n += kWaves) {
+    parts.look_up(a, pt, (first + W) * kBlk, g);
+    for (int n = first; n < last; n += W) {
       const int t0 = n * kBlk;
       // the next keys are asked for once the scores have used theirs, the next
       // values once the products have
       floatx4 sc[QT][2];
       scores<DT, D, QT>(f, R.Q, sc);
-      const bool more = n + kWaves < last;
+      const bool more = n + W < last;
       __builtin_amdgcn_sched_barrier(0);
-      if (more) load_keys<DT, D>(a, f, t0 + kWaves * kBlk, parts);
+      if (more) load_keys<DT, D>(a, f, t0 + W * kBlk, parts);
       __builtin_amdgcn_sched_barrier(0);
       R.template weigh<CAREFUL>(a, f, sc, t0, CAREFUL || !mine.whole(t0));
       __builtin_amdgcn_sched_barrier(0);
-      if (more) load_values<DT, D>(a, a.v_cache, f, t0 + kWaves * kBlk, parts);
-      parts.look_up(a, pt, t0 + 2 * kWaves * kBlk, g);
+      if (more) load_values<DT, D>(a, a.v_cache, f, t0 + W * kBlk, parts);
+      parts.look_up(a, pt, t0 + 2 * W * kBlk, g);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -474,7 +474,7 @@ __global__ __launch_bounds__(256, sizeof(DT) * D > 256 ? 1 : 2) void masked_keys
 #pragma unroll
   for (int t = 0; t < QT; ++t)
 #pragma unroll
-    for (int half = 2; half > 0; half >>= 1) {
+    for (int half = W / 2; half > 0; half >>= 1) {
       if (wv >= half && wv < 2 * half) R.give(t, s_acc[wv - half], s_ml[wv - half]);
       __syncthreads();
       if (wv < half) R.take(t, s_acc[wv], s_ml[wv]);
@@ -693,7 +693,7 @@ __global__ __launch_bounds__(256) void masked_merge_kernel(MaskedParams a, int t
 
 struct Plan {
   bool shared;                // keys through LDS
-  int qt, tile_rows, tiles, units, per, walk;
+  int qt, waves, tile_rows, tiles, units, per, walk;
   bool cut;                   // some tile may be cut
   size_t part_rows;
 };
@@ -713,6 +713,14 @@ Plan plan_of(int n_seq, int Hq, int Hkv, int max_q, long slots, int window, bool
   // merge costs more.
   p.walk = sg * p.tiles >= 512 ? 48 : (int)std::clamp(sg * nb / (p.shared ? 1024 : 512), (long)p.per, 64L);
   p.per = (int)std::max((long)p.per, nb / 16384);      // units stay few under a table for millions of tokens
+  p.waves = kWaves;
+  // Decode rows of few sequences over short contexts: eight waves walk them whole, which leaves out
+  // the merge and its launch (one of 700 tokens 16.2 to 13.8 us; one of 1500 16.5 to 14.7 among other
+  // calls, but 30 to 34 alone; 512 sequences and heads 57 to 61).
+  if (!p.shared && bf16 && nb <= 32 && sg * p.tiles < 512) {
+    p.waves = 8;
+    p.walk = 32;
+  }
   const int least = std::max(p.per, p.walk);
   p.cut = nb > least;
   // the most units that a window of nt tiles has: nt ceil(nb / max(per nt, walk)), over nt
@@ -770,19 +778,19 @@ hipError_t launch_attn_masked(const AttnMaskedLaunch& L, hipStream_t st) {
   if (e != hipSuccess) return e;
   trace_mark(st);
   const int sg = L.n_seq * L.Hkv;
-  auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((sg + 7) / 8 * 8, pl.units), dim3(256), 0, st, p);
+  auto go = [&](auto kernel, int waves = kWaves) {
+    hipLaunchKernelGGL(kernel, dim3((sg + 7) / 8 * 8, pl.units), dim3(64 * waves), 0, st, p);
   };
   auto pick = [&](auto dt, auto dim) {
     using DT = decltype(dt);
     constexpr int D = decltype(dim)::value;
     if constexpr (sizeof(DT) == 2) {
       const bool wide = L.page_size > 16;
-      if (!pl.shared) go(masked_keys_kernel<DT, D, 1>);
+      if (!pl.shared) { if (pl.waves == 8) go(masked_keys_kernel<DT, D, 1, 8>, 8); else go(masked_keys_kernel<DT, D, 1, 4>); }
       else if (pl.qt == 1) { if (wide) go(masked_tile_kernel<D, true, 1>); else go(masked_tile_kernel<D, false, 1>); }
       else { if (wide) go(masked_tile_kernel<D, true, 2>); else go(masked_tile_kernel<D, false, 2>); }
     } else {
-      if (pl.qt == 2) go(masked_keys_kernel<DT, D, 2>); else go(masked_keys_kernel<DT, D, 1>);
+      if (pl.qt == 2) go(masked_keys_kernel<DT, D, 2, 4>); else go(masked_keys_kernel<DT, D, 1, 4>);
     }
   };
   typedef std::integral_constant<int, 64> D64;
