@@ -62,6 +62,45 @@ def test_masses_of_many_rows(dt, D, mod):
     check_mass(b, got, lse, m, 0.75, mod, first=first)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("D,ps,Hq,Hkv", [(64, 16, 8, 1), (128, 64, 8, 4), (128, 16, 3, 3)])
+@pytest.mark.parametrize("k", [1, 2])
+@pytest.mark.parametrize("mod", [dict(), dict(window=77), dict(softcap=6.0, first=True)])
+def test_few_rows_over_short_contexts(D, ps, Hq, Hkv, k, mod):
+    """Walks left whole by eight waves: lengths around their blocks, and a value that is not finite
+    among the keys, which the rows that see it get and no others."""
+    b = Batch([(n, k) for n in (0, 1, 31, 32, 33, 255, 257, 700, 1016)], Hq, Hkv, D, ps, BF16, seed=D + k)
+    p = np.concatenate([b.ctx[i] + np.arange(k) for i in range(len(b.ctx))])
+    mod, first = dict(mod), None
+    if mod.pop("first", False):
+        first = p // 300 * 300
+    lo = np.broadcast_to(limits(p, 1, mod.get("window", 0), first, p + 1)[0], p.shape)
+    out, lse = ops.verify_attn_masked(b.q.cuda(), b.k_new.cuda(), b.v_new.cuda(), b.kc, b.vc, *b.args, lse=True,
+                                      first_key=dev(first), **mod)
+    for bad in (False, True):
+        if bad:                                  # of the last two sequences
+            for i, at in ((7, 600), (8, 950)):
+                b.vc[int(b.table[i, at // ps]), 0, 5, at % ps] = float("nan")
+            out, lse = ops.verify_attn_masked(b.q.cuda(), None, None, b.kc, b.vc, *b.args, lse=True, first_key=dev(first), **mod)
+        for i, L in enumerate(b.ctx):
+            r, V = b.rows(i), b.V[i].copy()
+            if bad and i >= 7:
+                at = 600 if i == 7 else 950
+                V[at, 0, 5] = 0.0                # in place of it, in rows that do not see it
+                seen = lo[r] <= at
+                G = Hq // Hkv
+                got = f64(out[r])
+                assert np.isnan(got[seen][:, :G, 5]).all()
+                got[seen, :G, 5] = 0.0
+                assert np.isfinite(got).all()
+                if seen.any():
+                    continue
+            f = None if first is None else first[r]
+            want = ref.attention(f64(b.q[r]), b.K[i], V, int(L), b.scale, *limits(int(L), k, mod.get("window", 0), f),
+                                 mod.get("softcap", 0.0))
+            check_attention(out[r], lse[r], want, BF16, int(L) + k, k * Hq // Hkv > 16)
+
+
 class Loop:
     """Four sequences of a cache whose pages hold NaN until they are written."""
     CAP, SINK, RECENT = 15.0, 2, 6
