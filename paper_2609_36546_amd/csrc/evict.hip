@@ -8,9 +8,13 @@
 //                  each a histogram in LDS of what the digits before it leave (no more of them
 //                  than it takes); then the kept positions by a scan in order, equal masses
 //                  counted as they come.
+//                  11 us for a sequence of 8000, chains of dependent steps: loads, atomics,
+//                  scans, barriers.
 //   move kernel    64 kept positions of one (sequence, KV head) per workgroup: keys are
 //                  runs of 32 channels per slot, values and masses gathered slot by slot
-//                  and stored 16 bytes at a time.
+//                  and stored 16 bytes at a time.  Bound by bytes: kept values lie in every
+//                  line of the cache, so those are all read (32 sequences of 2 to 8 Ki positions
+//                  to 40%: 847 MB in 175 us).
 //
 // Whole numbers decide, in an order that does not depend on the atomics', so the same call
 // repeats bit for bit.
@@ -55,39 +59,49 @@ __device__ __forceinline__ int page_at(const EvictParams& a, const int32_t* tabl
   return min(max(table[min(pos >> a.log2ps, width - 1)], 0), a.num_pages - 1);
 }
 
-// Sums over the threads before this one of two counts; every thread calls.
-__device__ __forceinline__ int2 scan2(int2 v, int2* part, int2* all) {
-  const int lane = lane_id(), w = threadIdx.x / kWave;
-  const int x = wave_incl_scan_i(v.x), y = wave_incl_scan_i(v.y);
+// Sums over the threads before this one of two counts (PAIR; else of the first); every thread calls.
+// The waves' sums are scanned by the lanes of each wave (one after the other: 0.7 us a call).
+template <bool PAIR>
+__device__ __forceinline__ int2 scan(int2 v, int2* part, int2* all) {
+  static_assert(kWaves <= kWave, "a lane of a wave");
+  const int lane = lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int x = wave_incl_scan_i(v.x), y = PAIR ? wave_incl_scan_i(v.y) : 0;
   __syncthreads();                  // the previous call's readers are done
   if (lane == kWave - 1) part[w] = make_int2(x, y);
   __syncthreads();
-  int2 before = make_int2(x - v.x, y - v.y), sum = make_int2(0, 0);
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    const int2 p = part[i];
-    if (i < w) {
-      before.x += p.x;
-      before.y += p.y;
-    }
-    sum.x += p.x;
-    sum.y += p.y;
-  }
-  *all = sum;
-  return before;
+  const int2 p = part[lane % kWaves];
+  auto over = [&](int mine, int upto, int sum) {       // before this wave, and before the thread in it
+    const int s = wave_incl_scan_i(lane < kWaves ? sum : 0);
+    return make_int2(upto - mine + (w > 0 ? __builtin_amdgcn_readlane(s, max(w - 1, 0)) : 0),
+                     __builtin_amdgcn_readlane(s, kWaves - 1));
+  };
+  const int2 a = over(v.x, x, p.x), b = PAIR ? over(v.y, y, p.y) : make_int2(0, 0);
+  *all = make_int2(a.y, b.y);
+  return make_int2(a.x, b.x);
 }
 
 // ONE: a round of threads holds all positions, so their masses are read once.
 template <bool ONE>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictParams a) {
-  __shared__ int2 s_hist[kBins / 2];
+  // four copies of a bin for four lanes: most masses lie in few bins (0.7 us less)
+  __shared__ __attribute__((aligned(16))) int4 s_hist[kBins];
   __shared__ int2 s_part[kWaves];
   __shared__ int s_digit, s_left, s_count;
+  typedef __attribute__((__vector_size__(16))) float f32x4;
   const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv, tid = threadIdx.x;
+  const int32_t* table = a.page_table + (size_t)(a.seq_ids ? a.seq_ids[slot] : slot) * a.max_pages;
+  auto mass_at = [&](int p0) {
+    return a.mass + ((size_t)page_at(a, table, a.max_pages, p0) * a.Hkv + g) * (unsigned)a.page_size + (p0 & (a.page_size - 1));
+  };
+  f32x4 early[kRun / 4];               // asked for before the lengths are known
+  if (ONE && tid * kRun < a.slots) {
+    const float* m = mass_at(tid * kRun);
+#pragma unroll
+    for (int i = 0; i < kRun / 4; ++i) early[i] = ld16<f32x4>(m + 4 * i);
+  }
   const Seq s = seq_of(a, slot);
   if (g == 0 && tid == 0) a.new_lens[s.b] = s.n;
   int32_t* kept = a.kept + ((size_t)s.b * a.Hkv + g) * (unsigned)a.dst_slots;
-  const int32_t* table = a.page_table + (size_t)s.b * a.max_pages;
   for (int i = s.n + tid; i < a.dst_slots; i += kThreads) kept[i] = -1;
   if (s.n == 0) return;
   if (s.n == s.L) {
@@ -99,11 +113,10 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictParams a) {
   auto load = [&](int round) {
     const int p0 = (round * kThreads + tid) * kRun;
     if (p0 >= s.L) return;
-    const float* m = a.mass + ((size_t)page_at(a, table, a.max_pages, p0) * a.Hkv + g) * (unsigned)a.page_size +
-                     (p0 & (a.page_size - 1));
+    const float* m = mass_at(p0);
 #pragma unroll
     for (int i = 0; i < kRun; i += 4) {
-      const floatx4 v = ld16<floatx4>(m + i);
+      const f32x4 v = ONE ? early[i / 4] : ld16<f32x4>(m + i);
 #pragma unroll
       for (int c = 0; c < 4; ++c) key[i + c] = order_of(v[c]);
     }
@@ -115,12 +128,12 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictParams a) {
   int left = s.n - s.lo - (s.L - s.hi), shift = 32;
   unsigned least = 0;
   const bool ask = left > 0;        // else nothing beside what is kept unasked
-  int* hist = reinterpret_cast<int*>(s_hist);
+  int* hist = reinterpret_cast<int*>(s_hist) + (tid & 3);
   static_assert(kBins == 2 * kThreads, "two bins of a thread");
   while (ask && shift > 0) {
     const int above = shift;
     shift = max(shift - kDigit, 0);
-    s_hist[tid] = make_int2(0, 0);
+    s_hist[tid] = s_hist[kThreads + tid] = make_int4(0, 0, 0, 0);
     __syncthreads();
     for (int r = 0; r < rounds; ++r) {
       if (!ONE) load(r);
@@ -128,12 +141,13 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictParams a) {
 #pragma unroll
       for (int i = 0; i < kRun; ++i)
         if (candidate(p0 + i) && (above == 32 || (key[i] ^ least) >> above == 0))
-          atomicAdd(&hist[(key[i] >> shift) & (kBins - 1)], 1);
+          atomicAdd(&hist[4 * ((key[i] >> shift) & (kBins - 1))], 1);
     }
     __syncthreads();
-    const int2 c = s_hist[kThreads - 1 - tid];     // from the top: .y, then .x
+    const int4 h0 = s_hist[2 * (kThreads - 1 - tid)], h1 = s_hist[2 * (kThreads - 1 - tid) + 1];
+    const int2 c = make_int2(h0.x + h0.y + h0.z + h0.w, h1.x + h1.y + h1.z + h1.w);      // from the top: .y, then .x
     int2 all;
-    const int before = scan2(make_int2(c.x + c.y, 0), s_part, &all).x;
+    const int before = scan<false>(make_int2(c.x + c.y, 0), s_part, &all).x;
     const bool hi = before < left && before + c.y >= left, lo = before + c.y < left && before + c.y + c.x >= left;
     if (hi || lo) {
       s_digit = 2 * (kThreads - 1 - tid) + (hi ? 1 : 0);
@@ -167,7 +181,7 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictParams a) {
     mine.x = __popc(sure);
     mine.y = __popc(equal);
     int2 all;
-    const int2 before = scan2(mine, s_part, &all);
+    const int2 before = scan<true>(mine, s_part, &all);
     int x = base.x + before.x, y = base.y + before.y;
     for (unsigned on = sure | equal; on; on &= on - 1) {
       const int i = __ffs(on) - 1;
@@ -187,19 +201,22 @@ __global__ __launch_bounds__(256, 4) void evict_move_kernel(EvictParams a) {
   typedef __attribute__((__vector_size__(16))) int i32x4;
   __shared__ int s_src[kMove], s_dst[kMove / 16];      // page * page_size + slot; of a 16-slot run
   const int slot = blockIdx.x / a.Hkv, g = blockIdx.x - slot * a.Hkv, tid = threadIdx.x;
+  const int i0 = (blockIdx.z * gridDim.y + blockIdx.y) * kMove;
+  int p = 0;                                           // asked for before the lengths are known
+  if (tid < kMove && i0 + tid < a.dst_slots)
+    p = a.kept[((size_t)(a.seq_ids ? a.seq_ids[slot] : slot) * a.Hkv + g) * (unsigned)a.dst_slots + i0 + tid];
   const Seq s = seq_of(a, slot);
-  const int i0 = (blockIdx.z * gridDim.y + blockIdx.y) * kMove, n = min(s.n - i0, kMove);
+  const int n = min(s.n - i0, kMove);
   if (n <= 0) return;
   const int ps = a.page_size;
   if (tid < kMove) {
     int at = 0;
     if (tid < n) {
-      const int p = a.kept[((size_t)s.b * a.Hkv + g) * (unsigned)a.dst_slots + i0 + tid];
       at = page_at(a, a.page_table + (size_t)s.b * a.max_pages, a.max_pages, p) * ps + (p & (ps - 1));
     }
     s_src[tid] = at;
   } else if (tid < kMove + kMove / 16) {
-    const int p = i0 + 16 * (tid - kMove);
+    p = i0 + 16 * (tid - kMove);
     s_dst[tid - kMove] = page_at(a, a.dst_table + (size_t)s.b * a.dst_pages, a.dst_pages, p) * ps + (p & (ps - 1));
   }
   __syncthreads();
