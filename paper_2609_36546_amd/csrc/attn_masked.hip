@@ -26,8 +26,8 @@
 //
 // Work split.  A workgroup takes a piece of the keys of one row tile; tiles of
 // a window that has few are cut into more pieces (split_of), joined by a second
-// kernel.  Up to 16 rows, and in fp32, its four waves walk keys of their own, in registers
-// (masked_keys_kernel); with more rows they hold 16 or 32 rows each and share the
+// kernel.  Up to 16 rows, and in fp32, its waves walk keys of their own, in registers
+// (masked_keys_kernel); with more rows the four hold 16 or 32 rows each and share the
 // keys through a ring in LDS (masked_tile_kernel).
 #include <algorithm>
 #include <type_traits>
