@@ -1000,6 +1000,8 @@ def _sized(t, name: str, dtype, dev, n: int):
 
 def _score_mod(slopes, first_key, end_key, T, Hq, dev):
     """Addresses of the scores' arrays."""
+    if slopes is None and first_key is None and end_key is None:
+        return None, None, None
     return (_sized(slopes, "slopes", torch.float32, dev, Hq),
             _sized(first_key, "first_key", torch.int32, dev, T),
             _sized(end_key, "end_key", torch.int32, dev, T))
@@ -1218,6 +1220,9 @@ def verify_drafts_workspace_size(T, V, B, target_filtered=False, draft_filtered=
                                                        1 if draft_filtered else 0))
 
 
+_NO_FILTERS = (None,) * 8
+
+
 def verify_drafts(target_logits, draft_logits, prop_tok, cu_q, u_accept, u_draw, temperature=None,
                   top_k=None, top_p=None, min_p=None, draft_temperature=None, draft_top_k=None,
                   draft_top_p=None, draft_min_p=None, eos_id: int = -1, outs=None, workspace=None):
@@ -1245,38 +1250,37 @@ def verify_drafts(target_logits, draft_logits, prop_tok, cu_q, u_accept, u_draw,
     B = cu_q.size(0) - 1
     if B < 0:
         raise ValueError("cu_q must be [B+1]")
+    if prop_tok is None or u_accept is None or u_draw is None:
+        raise TypeError("prop_tok, u_accept and u_draw must be torch.Tensors")
     need = lambda t, name, dtype, n: _sized(t, name, dtype, dev, n)  # noqa: E731
-    for t, name in ((prop_tok, "prop_tok"), (u_accept, "u_accept"), (u_draw, "u_draw")):
-        if t is None:
-            raise TypeError(f"{name} must be a torch.Tensor")
     xp, ua, ud = need(prop_tok, "prop_tok", i32, T), need(u_accept, "u_accept", f32, T), need(u_draw, "u_draw", f32, B)
-    filters = (need(temperature, "temperature", f32, T), need(top_k, "top_k", i32, T),
-               need(top_p, "top_p", f32, T), need(min_p, "min_p", f32, T),
-               need(draft_temperature, "draft_temperature", f32, T),
-               need(draft_top_k, "draft_top_k", i32, T), need(draft_top_p, "draft_top_p", f32, T),
-               need(draft_min_p, "draft_min_p", f32, T))
-    if outs is None:
-        outs = {}
+    target_cut = not (top_k is None and top_p is None and min_p is None)
+    draft_cut = not (draft_top_k is None and draft_top_p is None and draft_min_p is None)
+    filters = _NO_FILTERS
+    if target_cut or draft_cut or temperature is not None or draft_temperature is not None:
+        filters = (need(temperature, "temperature", f32, T), need(top_k, "top_k", i32, T),
+                   need(top_p, "top_p", f32, T), need(min_p, "min_p", f32, T),
+                   need(draft_temperature, "draft_temperature", f32, T),
+                   need(draft_top_k, "draft_top_k", i32, T), need(draft_top_p, "draft_top_p", f32, T),
+                   need(draft_min_p, "draft_min_p", f32, T))
     made = {}
     for name, dtype, n in (("n_acc", i32, B), ("token", i32, B), ("finished", torch.uint8, B),
                            ("p_accept", f32, T), ("logp", f32, B)):
-        t = outs.get(name)
+        t = None if outs is None else outs.get(name)
         if t is None:
             t = torch.empty(n, dtype=dtype, device=dev)
         else:
             need(t, name, dtype, n)
         made[name] = t
+    n_acc, token, finished, p_accept, logp = made.values()
     if workspace is None:
-        size = max(verify_drafts_workspace_size(
-            T, V, B, not (top_k is None and top_p is None and min_p is None),
-            not (draft_top_k is None and draft_top_p is None and draft_min_p is None)), 1)
+        size = max(verify_drafts_workspace_size(T, V, B, target_cut, draft_cut), 1)
         workspace = torch.empty(size, dtype=torch.uint8, device=dev)
         ws = workspace.data_ptr()
     else:
         ws, size = _given_workspace(workspace, dev)
-    st = lib().verify_drafts(tp, ts, dp, ds, T, V, xp, cu, B, ua, ud, *filters, int(eos_id), made["n_acc"].data_ptr(),
-                             made["token"].data_ptr(), made["finished"].data_ptr(),
-                             made["p_accept"].data_ptr(), made["logp"].data_ptr(), code, ws, size,
-                             _stream(dev))
+    st = lib().verify_drafts(tp, ts, dp, ds, T, V, xp, cu, B, ua, ud, *filters, int(eos_id), n_acc.data_ptr(),
+                             token.data_ptr(), finished.data_ptr(), p_accept.data_ptr(),
+                             logp.data_ptr(), code, ws, size, _stream(dev))
     _check("verify_drafts", st)
     return made
