@@ -417,6 +417,7 @@ __device__ __forceinline__ void append_own(const MaskedParams& a, const Seq& s, 
 // of 120 to 700 positions 80 us, 61 so; two windows of 300 rows by 1 to 4.5 Ki keys 995 and 513.)
 template <typename DT, int D, int QT, int W>
 __global__ __launch_bounds__(64 * W, W == 8 || sizeof(DT) * D > 256 ? 1 : 2) void masked_keys_kernel(MaskedParams a) {
+  constexpr bool NT = sizeof(DT) == 2;                 // one tile per window; fp32 may have many (69 to 76 us)
   constexpr int kRows = 16 * QT, kTile = (D / 16) * kWave, PT = sizeof(DT) == 2 ? 2 : 1;
   __shared__ floatx4 s_acc[W / 2][kTile];
   __shared__ float s_ml[W / 2][32];
@@ -446,8 +447,8 @@ __global__ __launch_bounds__(64 * W, W == 8 || sizeof(DT) * D > 256 ? 1 : 2) voi
     Parts parts;
     parts.look_up(a, pt, first * kBlk, g);
     Frags<DT, D> f;
-    load_keys<DT, D>(a, f, first * kBlk, parts);
-    load_values<DT, D>(a, a.v_cache, f, first * kBlk, parts);
+    load_keys<DT, D, NT>(a, f, first * kBlk, parts);
+    load_values<DT, D, NT>(a, a.v_cache, f, first * kBlk, parts);
     parts.look_up(a, pt, (first + W) * kBlk, g);
     for (int n = first; n < last; n += W) {
       const int t0 = n * kBlk;
@@ -457,11 +458,11 @@ __global__ __launch_bounds__(64 * W, W == 8 || sizeof(DT) * D > 256 ? 1 : 2) voi
       scores<DT, D, QT>(f, R.Q, sc);
       const bool more = n + W < last;
       __builtin_amdgcn_sched_barrier(0);
-      if (more) load_keys<DT, D>(a, f, t0 + W * kBlk, parts);
+      if (more) load_keys<DT, D, NT>(a, f, t0 + W * kBlk, parts);
       __builtin_amdgcn_sched_barrier(0);
       R.template weigh<CAREFUL>(a, f, sc, t0, CAREFUL || !mine.whole(t0));
       __builtin_amdgcn_sched_barrier(0);
-      if (more) load_values<DT, D>(a, a.v_cache, f, t0 + W * kBlk, parts);
+      if (more) load_values<DT, D, NT>(a, a.v_cache, f, t0 + W * kBlk, parts);
       parts.look_up(a, pt, t0 + 2 * W * kBlk, g);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -491,9 +492,12 @@ __global__ __launch_bounds__(64 * W, W == 8 || sizeof(DT) * D > 256 ? 1 : 2) voi
 // slots].  Within a piece the 16-byte entries are permuted so that the lanes that a
 // 16-byte LDS read serves at once hit distinct banks; a load writes lane l's 16 bytes
 // to entry l, so the loading lane fetches what belongs there.
-// Two units with a tile per wave (64 windows of eight 155 to 145 us; a fourth workgroup per CU, for which
-// it leaves room, takes 160), three with two (packed prompts 57 us, with two units 59).
+// Two units with a tile per wave (64 windows of eight 155 to 145 us), three with two (packed prompts 57
+// us, with two units 59).
 constexpr int ring_of(int QT) { return QT == 1 ? 2 : 3; }
+// Of the CU's 160 KB more than a quarter: a fourth workgroup would take 64 windows of eight from 145 to
+// 160 us, 8 of them from 33 to 40.
+constexpr int kLeastLds = 41 * 1024;
 __device__ __forceinline__ int key_entry(int slot, int q) { return 4 * slot + (q ^ (((slot >> 1) & 1) | ((slot >> 2) & 2))); }
 __device__ __forceinline__ int val_entry(int ch, int h) { return 2 * ch + (h ^ ((ch >> 2) & 1)); }
 __device__ __forceinline__ int wide_entry(int ch, int q) {
@@ -545,6 +549,7 @@ template <int D, bool WIDE> struct Loader {
     }
   }
   // `lds`: LDS address of the wave's first piece of the unit.
+  template <bool NT>
   __device__ __forceinline__ void issue(const MaskedParams& a, const Parts& parts, int t0, int t, unsigned lds) const {
     const int ps = 1 << a.log2ps;
     const int o0 = t0 & (ps - 1), o1 = (t0 + 16) & (ps - 1);
@@ -558,24 +563,28 @@ template <int D, bool WIDE> struct Loader {
 #pragma unroll
     for (int i = 0; i < kKeys; ++i) {
       const bool second = PER == 4 ? i : t >= PER;
-      load_to(lds + 4096 * i, kc + (second ? at1 + (unsigned)(64 * o1) : at0 + (unsigned)(64 * o0)), k[i]);
+      load_to<NT>(lds + 4096 * i, kc + (second ? at1 + (unsigned)(64 * o1) : at0 + (unsigned)(64 * o0)), k[i]);
     }
 #pragma unroll
     for (int i = 0; i < kLoads - kKeys; ++i) {
       const bool second = !WIDE && (PER == 4 ? i : t >= PER);
-      load_to(lds + 4096 * (i + kKeys), vc + (WIDE ? at0 + (unsigned)(2 * o0) : second ? at1 : at0), v[i]);
+      load_to<NT>(lds + 4096 * (i + kKeys), vc + (WIDE ? at0 + (unsigned)(2 * o0) : second ? at1 : at0), v[i]);
     }
   }
-  static __device__ __forceinline__ void load_to(unsigned lds, const char* base, unsigned off) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "memory", "m0");
+  template <bool NT> static __device__ __forceinline__ void load_to(unsigned lds, const char* base, unsigned off) {
+    if constexpr (NT)
+      asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(lds), "v"(off), "s"(base) : "memory", "m0");
+    else
+      asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "memory", "m0");
   }
 };
 
-template <int D, bool WIDE, int QT>
+// NT: the ring's loads go past the caches' order of use.
+template <int D, bool WIDE, int QT, bool NT>
 __global__ __launch_bounds__(256, 3) void masked_tile_kernel(MaskedParams a) {
   typedef Loader<D, WIDE> Load;
   constexpr int kRows = 64 * QT, kRing = ring_of(QT);
-  __shared__ __attribute__((aligned(1024))) char s_ring[kRing * Load::kUnit];
+  __shared__ __attribute__((aligned(1024))) char s_ring[D == 128 && kRing * Load::kUnit < kLeastLds ? kLeastLds : kRing * Load::kUnit];
   __shared__ int s_span[kWaves][2];
   const int sg = slot_head_of(a, blockIdx.x, blockIdx.y, gridDim.x);
   if (sg < 0) return;
@@ -606,7 +615,7 @@ __global__ __launch_bounds__(256, 3) void masked_tile_kernel(MaskedParams a) {
     Parts parts;
     // Behind the piece's end its last unit is loaded again, so that every wait has the same count.
     auto look_up = [&](int n) { parts.look_up(a, pt, min(n, p.b1 - 1) * kBlk, g); };
-    auto issue = [&](int n, int buf) { load.issue(a, parts, min(n, p.b1 - 1) * kBlk, t, ring + buf * Load::kUnit); };
+    auto issue = [&](int n, int buf) { load.template issue<NT>(a, parts, min(n, p.b1 - 1) * kBlk, t, ring + buf * Load::kUnit); };
 #pragma unroll
     for (int i = 0; i < kRing - 1; ++i) {
       look_up(p.b0 + i);
@@ -787,8 +796,21 @@ hipError_t launch_attn_masked(const AttnMaskedLaunch& L, hipStream_t st) {
     if constexpr (sizeof(DT) == 2) {
       const bool wide = L.page_size > 16;
       if (!pl.shared) { if (pl.waves == 8) go(masked_keys_kernel<DT, D, 1, 8>, 8); else go(masked_keys_kernel<DT, D, 1, 4>); }
-      else if (pl.qt == 1) { if (wide) go(masked_tile_kernel<D, true, 1>); else go(masked_tile_kernel<D, false, 1>); }
-      else { if (wide) go(masked_tile_kernel<D, true, 2>); else go(masked_tile_kernel<D, false, 2>); }
+      else {
+        // One tile of a window reads its keys once.  Less than the 256 MB of the memory-side cache is
+        // left to it (4 KV heads, windows of eight by up to 8 Ki keys: 8 of them 33.6 us, 36.1 as a
+        // stream; 16 48.4 and 46.4, 64 142 and 132; packed prompts, of many tiles, 86 and 97).
+        const bool nt = pl.tiles == 1 && (long)sg * p.slots * D * 4 > 256L << 20;
+        auto tile = [&](auto w, auto q) {
+          constexpr bool WIDE = decltype(w)::value;
+          constexpr int QT = decltype(q)::value;
+          if (nt) go(masked_tile_kernel<D, WIDE, QT, true>); else go(masked_tile_kernel<D, WIDE, QT, false>);
+        };
+        typedef std::integral_constant<int, 1> One;
+        typedef std::integral_constant<int, 2> Two;
+        if (pl.qt == 1) { if (wide) tile(std::true_type(), One()); else tile(std::false_type(), One()); }
+        else { if (wide) tile(std::true_type(), Two()); else tile(std::false_type(), Two()); }
+      }
     } else {
       if (pl.qt == 2) go(masked_keys_kernel<DT, D, 2, 4>); else go(masked_keys_kernel<DT, D, 1, 4>);
     }

@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256, QT == 4 ? 4 : sizeof(DT) == 4 ? 1 : 2) void at
   Parts parts, next;
   parts.look_up(a, pt, first * kBlk, g);
   Frags<DT, D> f;
-  if (span.sees(first * kBlk)) load_keys<DT, D>(a, f, first * kBlk, parts);
+  if (span.sees(first * kBlk)) load_keys<DT, D, true>(a, f, first * kBlk, parts);
   next.look_up(a, pt, (first + kWaves) * kBlk, g);
   for (int n = first; n < b1; n += kWaves) {
     const int t0 = n * kBlk;
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256, QT == 4 ? 4 : sizeof(DT) == 4 ? 1 : 2) void at
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (n + kWaves < b1 && span.sees(t0 + kWaves * kBlk)) load_keys<DT, D>(a, f, t0 + kWaves * kBlk, next);
+    if (n + kWaves < b1 && span.sees(t0 + kWaves * kBlk)) load_keys<DT, D, true>(a, f, t0 + kWaves * kBlk, next);
     __builtin_amdgcn_sched_barrier(0);
     if (seen) R.add(a, sc, t0, !span.whole(t0), sum);
     put(a, s, parts, t0, pick(sum));
