@@ -225,7 +225,8 @@ __global__ __launch_bounds__(256, 4) void evict_move_kernel(EvictParams a) {
     const int from = s_src[tid], to = s_dst[tid >> 4] + (tid & 15);
     a.mass[page(to) * ps + (to & (ps - 1))] = a.mass[page(from) * ps + (from & (ps - 1))];
   }
-  // keys: 16 bytes of a slot's run of 32 channels
+  // keys: 16 bytes of a slot's run of 32 channels.  They, and what is stored, go past the caches'
+  // order of use (32 sequences 190 to 185 us); values do not: a line's neighbours come from it.
   constexpr int KPS = 32 / EPL;                        // of a run
   constexpr int KN = kMove * D / EPL / 256;
   const DT* kc = reinterpret_cast<const DT*>(a.k_cache);
@@ -236,7 +237,7 @@ __global__ __launch_bounds__(256, 4) void evict_move_kernel(EvictParams a) {
     const int e = tid + 256 * x, c = e % KPS, i = e / KPS % kMove, sl = e / KPS / kMove;
     if (i < n) {
       const int at = s_src[i];
-      k[x] = ld16<i32x4>(kc + (page(at) * (D / 32) + sl) * ps * 32 + (at & (ps - 1)) * 32 + EPL * c);
+      k[x] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(kc + (page(at) * (D / 32) + sl) * ps * 32 + (at & (ps - 1)) * 32 + EPL * c));
     }
   }
 #pragma unroll
@@ -244,8 +245,8 @@ __global__ __launch_bounds__(256, 4) void evict_move_kernel(EvictParams a) {
     const int e = tid + 256 * x, c = e % KPS, i = e / KPS % kMove, sl = e / KPS / kMove;
     if (i < n) {
       const int at = s_dst[i >> 4] + (i & 15);
-      *reinterpret_cast<i32x4*>(reinterpret_cast<DT*>(a.k_cache) + (page(at) * (D / 32) + sl) * ps * 32 +
-                                (at & (ps - 1)) * 32 + EPL * c) = k[x];
+      DT* dst = reinterpret_cast<DT*>(a.k_cache) + (page(at) * (D / 32) + sl) * ps * 32 + (at & (ps - 1)) * 32 + EPL * c;
+      __builtin_nontemporal_store(k[x], reinterpret_cast<i32x4*>(dst));
     }
   }
   // values: a channel's run of EPL slots
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256, 4) void evict_move_kernel(EvictParams a) {
     const int to = s_dst[i >> 4] + (i & 15);
     DT* dst = reinterpret_cast<DT*>(a.v_cache) + (page(to) * D + ch) * ps + (to & (ps - 1));
     if (i + EPL <= n) {
-      *reinterpret_cast<i32x4*>(dst) = __builtin_bit_cast(i32x4, run[x]);
+      __builtin_nontemporal_store(__builtin_bit_cast(i32x4, run[x]), reinterpret_cast<i32x4*>(dst));
     } else {
 #pragma unroll
       for (int c = 0; c < EPL; ++c)
