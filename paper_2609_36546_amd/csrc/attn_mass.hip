@@ -129,7 +129,7 @@ __device__ __forceinline__ float pick(const float (&sum)[8]) {
 
 // The queries of four tiles lie in LDS: in registers they leave room for two waves per SIMD instead
 // of four, and each wave would load them all (64 windows of eight by 1 to 8 Ki keys, 64 packed rows:
-// 90 us so, 80 from LDS).
+// 90 us so, 80 from LDS).  Keys, read once, are a stream.
 template <typename DT, int D, int QT>
 __global__ __launch_bounds__(256, QT == 4 ? 4 : sizeof(DT) == 4 ? 1 : 2) void attn_mass_few_kernel(MassParams a) {
   constexpr bool LDS = QT == 4;
@@ -296,8 +296,8 @@ hipError_t launch_attn_mass(const AttnMaskedLaunch& L, hipStream_t st) {
   const long rows = (long)L.max_q * p.G, sg = (long)L.n_seq * L.Hkv;
   const long blocks = ((long)p.slots + kBlk - 1) / kBlk;
   const unsigned gx = (unsigned)((sg + 7) / 8 * 8);
-  // 64 windows by 1 to 8 Ki keys: of one row 130 us at 32 blocks of a workgroup, 123 at 8; of eight (64
-  // packed rows) 83 at either, 80 at 16
+  // 64 windows by 1 to 8 Ki keys: of one row 130 us at 32 blocks of a workgroup, 123 at 8 (112 since
+  // keys are a stream); of eight (64 packed rows) 83 at either, 80 at 16
   p.per = (int)std::max(std::clamp(sg * blocks / 2048, 4L, rows <= 16 ? 8L : 16L), (blocks + 65534) / 65535);
   trace_begin(st);
   auto pick = [&](auto dt, auto dim) {
