@@ -350,6 +350,33 @@ def test_attention_under_a_loose_bound_of_windows():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("Hq,ps", [(8, 16), (8, 32), (16, 16), (16, 64)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("bad", [False, True])
+def test_windows_under_tables_of_more_than_the_caches_hold(Hq, ps, D, bad):
+    """Windows of one tile, whose keys are loaded as a stream, the window's own among them; a value that
+    is not finite stays with the rows that see it."""
+    b = Batch([(900, 2), (5, 9), (3000, 8), (31, 1)], Hq, 2, D, ps, BF16, seed=Hq + D)
+    if bad:
+        b.v_new[3, 0, 7] = float("nan")          # of the second window, seen from its second row on
+        b.V[1][5 + 1, 0, 7] = 0.0
+    pt, ctx, cu, _ = b.args
+    wide = torch.full((4, 1200000 // ps), -1, dtype=torch.int32).cuda()
+    wide[:, : pt.shape[1]] = pt
+    out, lse = ops.verify_attn_masked(b.q.cuda(), b.k_new.cuda(), b.v_new.cuda(), b.kc, b.vc, wide, ctx, cu, 9, lse=True, softcap=20.0)
+    for i, L in enumerate(b.ctx):
+        r, n = b.rows(i), int(b.k[i])
+        if bad and i == 1:
+            got = f64(out[r])
+            assert np.isnan(got[1:, : Hq // 2, 7]).all() and np.isfinite(got[0]).all()
+            got[1:, : Hq // 2, 7] = 0.0
+            assert np.isfinite(got).all()
+            continue
+        want = ref.attention(f64(b.q[r]), b.K[i], b.V[i], int(L), b.scale, *limits(int(L), n), 20.0)
+        check_attention(out[r], lse[r], want, BF16, int(L) + n, True)
+
+
+@pytest.mark.gpu
 def test_eviction_under_tables_of_the_largest_width():
     b, table, dst, dkeep = evicted([300], [130], 2, 64, 64, BF16, 3, [130])
     m = masses(b, 5)
