@@ -850,7 +850,9 @@ size_t ipdv_verify_drafts_workspace_size(int T, int V, int B, int target_filtere
  * p_accept is NaN.  A draft at or beyond V has p(x) = 0 and is rejected.  draft_logits NULL:
  * q(x) = 1, as of drafts looked up or taken greedily; the draft's filters are then not read.
  * Probabilities are 64-bit floats (relative error below 1e-9), except that top-p's cut is found
- * as in sample_logits.  The same call repeats bit for bit.
+ * as in sample_logits.  An entry 694 T or more below its row's maximum, less than 2^-1000 of the
+ * maximum's probability (a fill of -1e4, say), has none; T from 2^100 on is taken as 2^100.  (A u_draw
+ * of 0 may pass over entries of less than 2^-900, too.)  The same call repeats bit for bit.
  *
  * target_logits, draft_logits [T, V] (dtype), *_row_stride elements from one row to the next
  * (>= V); prop_tok [T], cu_q [B+1] int32 (cu_q[B] <= T); u_accept [T], u_draw [B] float in [0,

@@ -123,9 +123,9 @@ __device__ __forceinline__ Product exp2_of(double d, double slope, const double*
   return {__hiloint2double((int)((unsigned)__double2hiint(base) + (at << 12)), __double2loint(base)), by};
 }
 
-// A row's temperature: log2(e) / T, and the distance from the maximum behind which nothing
-// counts (2^-1000 of its mass).  T from 2^100 on acts as that, where an entry of -inf
-// still counts for nothing.
+// A row's temperature: log2(e) / T, and the distance from the maximum behind which an entry has no
+// probability (2^-1000 of the maximum's; sums take it for that, since they cannot tell).  T from 2^100
+// on acts as that, where an entry of -inf still counts for nothing.
 constexpr float kMostTemp = 0x1p100f;
 struct Scale {
   double slope, far;
@@ -152,13 +152,13 @@ __device__ __forceinline__ Product mass_of(float l, float max, double far, doubl
 struct RowMass {
   double slope, far, inv;    // 1 / mass against the maximum
   u64 cut;
-  float max, l_cut;
+  float max, l_cut;          // what the filters keep, and what has a probability at all
   int v_cut;
   bool bad;
   __device__ __forceinline__ bool keeps(float l, int v) const { return (l > l_cut) | ((l == l_cut) & (v <= v_cut)); }
   __device__ __forceinline__ double mass(float l, int v, const double* pow) const {      // the probability
     const double m = mass_of(l, max, far, slope, pow) * inv;
-    return (keeps(l, v) & (l > -INFINITY)) ? m : 0.0;
+    return keeps(l, v) ? m : 0.0;
   }
 };
 template <int CTRL> __device__ __forceinline__ double dpp_move_d(double v) {
@@ -205,6 +205,12 @@ __device__ __forceinline__ RowMass join(const DraftParams& p, const Model& m, in
   out.cut = m.cuts ? given : sc.first_only ? top : 0;
   out.l_cut = out.cut ? logit_of(out.cut) : -__FLT_MAX__;
   out.v_cut = out.cut ? index_of(out.cut) : p.V;
+  // a vocabulary masked by a finite fill: a u of 0 must not draw from it
+  const float l_far = (float)((double)mx + sc.far);
+  if (l_far > out.l_cut) {
+    out.l_cut = l_far;
+    out.v_cut = p.V;
+  }
   return out;
 }
 template <typename DT> __device__ __forceinline__ float logit(const Model& m, int r, int v) {
@@ -310,7 +316,7 @@ __global__ __launch_bounds__(kThreads) void draft_stats_kernel(DraftParams p) {
   if (tid == 0) m.recs[at] = {(s_part[0] + s_part[1]) + (s_part[2] + s_part[3]), top, mx, s_bad};
 }
 
-// Sums of less come from entries of -inf, which are never drawn.
+// Sums of less come from entries of no probability, which are never drawn.
 constexpr double kNothing = 0x1p-900;
 
 // How a window ends.
@@ -376,7 +382,7 @@ template <typename DT> __device__ __forceinline__ int verdict_of(const DraftPara
 
 // An entry's mass in what a rejected row is drawn from.
 __device__ __forceinline__ double rest_of(const RowMass& t, float lt, const RowMass& d, float ld, bool certain, int x, int v, const double* pow) {
-  if (!(t.keeps(lt, v) & (lt > -INFINITY)) || (certain && v == x)) return 0.0;      // filters leave few: a branch
+  if (!t.keeps(lt, v) || (certain && v == x)) return 0.0;      // filters leave few: a branch
   const double m = t.mass(lt, v, pow);
   return certain ? m : fmax(m - d.mass(ld, v, pow), 0.0);
 }
