@@ -382,6 +382,8 @@ template <typename DT> __device__ __forceinline__ int verdict_of(const DraftPara
 
 // An entry's mass in what a rejected row is drawn from.
 __device__ __forceinline__ double rest_of(const RowMass& t, float lt, const RowMass& d, float ld, bool certain, int x, int v, const double* pow) {
+  // both probabilities rounded alike: of equal ones nothing is left
+#pragma clang fp contract(off)
   if (!t.keeps(lt, v) || (certain && v == x)) return 0.0;      // filters leave few: a branch
   const double m = t.mass(lt, v, pow);
   return certain ? m : fmax(m - d.mass(ld, v, pow), 0.0);

@@ -7,7 +7,7 @@ import torch
 from tests import masked_reference as ref
 from tests import q8_reference as filters
 from tests.masked_reference import BF16, F32, f64
-from tests.test_gpu_drafts import call
+from tests.test_gpu_drafts import call, check, rows
 
 
 def at(f, name, m):
@@ -68,3 +68,95 @@ def test_a_vocabulary_masked_by_a_fill(dt, fill, V, allowed, temp):
         check_exactly(t, draft, f, df, x, cu, zero, zero, got)
         assert got["n_acc"].tolist() == [0, 0, 0, 1, 0]
         assert set(got["token"].tolist()) <= set(allowed)
+
+
+def every(T, **f):
+    return {n: torch.full((T,), v, dtype=torch.int32 if n == "top_k" else F32) for n, v in f.items()}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("V", [5003, 40000])
+@pytest.mark.parametrize("temp,k", [(0.05, 20), (0.1, 50), (0.2, 200), (0.2, 3000)])
+@pytest.mark.parametrize("certain", [False, True])
+def test_top_k_far_below_the_maximum(dt, V, temp, k, certain):
+    """The k-th entry lies more than 32 nats below the first.  Drafts inside, outside the
+    target's and outside both top-ks, at u of 0."""
+    T = 24
+    t, d, g = rows(V + k, T, V, dt)
+    f = every(T, temperature=temp, top_k=k)
+    df = {} if certain else f
+    d = None if certain else d
+    # one row of each sequence is drafted from inside, so that the second decides
+    x = np.zeros(T, np.int64)
+    last = []
+    for m in range(T):
+        inside, _ = kept(t, f, m)
+        other = kept(d, f, m)[0] if d is not None else np.zeros(0, np.int64)
+        last.append((f64(t)[m].max() - f64(t)[m][inside[-1]]) / temp)
+        only_draft = np.setdiff1d(other, inside)
+        out = np.setdiff1d(np.arange(V), np.union1d(inside, other))
+        x[m] = (inside[0], inside[-1], only_draft[0] if len(only_draft) else out[0], out[0], out[-1], -1)[m % 6]
+    assert np.mean(np.array(last) > 32) > 0.5
+    cu, u = [0, 2, 3, 4, 5, 6, 12, 13, 14, 15, 16, 17, 18, 24], np.zeros(T)
+    for ud in (np.zeros(13), torch.rand(13, generator=g).numpy()):
+        got = call(t, d, x, cu, u, ud, f, df)
+        if not ud.any():
+            check_exactly(t, d, f, df, x, cu, u, ud, got)
+        else:
+            check(t, d, f, df, x, cu, u, ud, got)
+    cut = np.isin(np.arange(T) % 6, (3, 4))
+    assert (f64(got["p_accept"])[cut] == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_drafts_outside_both_top_ks(dt):
+    t = torch.tensor([[0.0, -40.0, -41.0, -42.0]] * 4).to(dt)
+    f = every(4, top_k=2)
+    x, cu = np.array([3, 2, 1, 0]), [0, 1, 2, 4]
+    got = call(t, t, x, cu, [0.0] * 4, [0.0] * 3, f, f)
+    # nothing is left of max(0, p - q): drawn from p
+    assert got["p_accept"].tolist() == [0, 0, 1, 1]
+    assert got["n_acc"].tolist() == [0, 0, 2] and got["token"].tolist() == [0, 0, -1]
+    got = call(t, None, x, cu, [0.0] * 4, [0.0] * 3, f)
+    assert got["n_acc"].tolist() == [0, 0, 2] and got["token"].tolist() == [0, 0, -1]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("V", [300, 30000])
+@pytest.mark.parametrize("k", [2, 70, 1000, 29000, 40000])
+@pytest.mark.parametrize("ties", [False, True])
+def test_a_row_whose_entries_all_lie_far_below_its_first(dt, V, k, ties):
+    """One entry at 0, all others 40 to 100 nats below, in any order; with ties, of few values."""
+    T = 6
+    rng = np.random.default_rng(V + k)
+    l = -40.0 - (rng.integers(0, 7, (T, V)) * 8.0 if ties else 60.0 * rng.random((T, V)))
+    l[np.arange(T), rng.integers(0, V, T)] = 0.0
+    t = torch.from_numpy(l).to(F32).to(dt)
+    f = every(T, top_k=k)
+    x = np.zeros(T, np.int64)
+    for m in range(T):
+        order, n, _ = filters.kept_prefix(f64(t)[m], 1.0, 0, None, None)
+        x[m] = (order[min(k, V) - 1], order[k] if k < V else V, order[0], order[-1], -1, order[k // 2 % V])[m]
+    cu, u, ud = list(range(T + 1)), np.zeros(T), np.zeros(T)
+    check_exactly(t, None, f, {}, x, cu, u, ud, call(t, None, x, cu, u, ud, f))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("more", [{}, dict(top_k=3), dict(top_k=100), dict(temperature=0.5)])
+def test_a_min_p_far_below_the_maximum(dt, more):
+    """min-p of 1e-20: entries down to 46 nats are kept, others not."""
+    V, T = 9000, 4
+    t = torch.full((T, V), -60.0)
+    t[:, 77], t[:, 8191], t[:, 3], t[:, 500] = 0.0, -20.0, -22.0, -45.0
+    t[:, 40], t[:, 8999] = -47.0, -23.5
+    t = t.to(dt)
+    f = every(T, min_p=1e-20, **more)
+    x = np.array([40, 500, 8999, 12])
+    cu, u, ud = list(range(T + 1)), np.zeros(T), np.zeros(T)
+    got = call(t, None, x, cu, u, ud, f)
+    check_exactly(t, None, f, {}, x, cu, u, ud, got)
+    assert got["n_acc"].tolist()[0] == 0 and got["n_acc"].tolist()[3] == 0
