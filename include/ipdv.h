@@ -718,14 +718,16 @@ int sample_logits(const void* logits, int64_t row_stride, int M, int V, const fl
  * What a score is before the softmax (verify_attn_masked, attn_mass).  For row r
  * = cu_q[b] + i at position p = L_b + i, head h and key j:
  *   x = scale * q . K_j
- *   x = softcap * tanh(x / softcap)              (softcap > 0; 0: off)
+ *   x = softcap * tanh(x / softcap)              (softcap > 0; 0: off.  At most 2^127, with
+ *                                                scale / softcap in [2^-126, 2^125])
  *   x = x - slopes[h] * |p - j|                  (slopes [Hq] float; NULL: off)
  * over the keys  max(first_key[r], p - window + 1, 0) <= j < end_key[r]  and
  * j < L_b + k_b:
  *   window            keys that a row sees at most, its own the last of them (0: off)
  *   first_key [T] int32   e.g. where the row's document begins (NULL: 0)
  *   end_key [T] int32     e.g. the end of a prefix that sees itself whole (NULL: p + 1)
- * A row may be left without keys.
+ * A row may be left without keys.  Scores are fp32; up to a softcap of 64 bf16 calls hold a
+ * capped one to 2^-22 of softcap, with larger ones to 2^-20 of itself.
  */
 
 /* Workspace bytes verify_attn_masked needs (0 if the arguments are invalid).
@@ -753,7 +755,7 @@ size_t ipdv_attn_masked_workspace_size(int n_seq, int Hq, int Hkv, int D, int ma
  * max_q * Hq / Hkv may be 2^20 in any case, and more where the keys are few.
  *
  * Errors: IPDV_EINVAL (also: softcap negative or not finite, window < 0),
- * IPDV_EUNSUPPORTED (D, page_size, dtype, alignment, sizes), IPDV_EWORKSPACE, IPDV_EHIP.
+ * IPDV_EUNSUPPORTED (D, page_size, dtype, softcap, alignment, sizes), IPDV_EWORKSPACE, IPDV_EHIP.
  */
 int verify_attn_masked(const void* q, int64_t q_row_stride, const void* k_new, const void* v_new,
                        void* k_cache, void* v_cache,

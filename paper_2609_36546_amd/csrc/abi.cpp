@@ -734,11 +734,14 @@ size_t ipdv_attn_masked_workspace_size(int n_seq, int Hq, int Hkv, int D, int ma
 // What verify_attn_masked and attn_mass check alike.
 static int masked_call_check(const void* q, int64_t q_stride, const void* k_cache, const int32_t* page_table,
                              const int32_t* ctx_lens, const int32_t* cu_q, int n_seq, int Hq, int Hkv, int D,
-                             int num_pages, float scale, int dtype) {
+                             int num_pages, float scale, float softcap, int dtype) {
   if (dtype != IPDV_F32 && dtype != IPDV_BF16) return fail(IPDV_EUNSUPPORTED, "dtype %d", dtype);
   if (num_pages < 1) return fail(IPDV_EINVAL, "num_pages must be >= 1 (got %d)", num_pages);
   if ((int64_t)num_pages * Hkv >= (int64_t)1 << 31) return fail(IPDV_EUNSUPPORTED, "num_pages * Hkv exceeds 2^31 - 1");
   if (!std::isfinite(scale) || !(scale > 0.f)) return fail(IPDV_EINVAL, "scale must be positive and finite");
+  // the kernels' factors, 1.44 softcap and 2.89 scale / softcap, are normal fp32 numbers
+  if (softcap > 0.f && !(softcap <= 0x1p127f && std::isnormal(scale / softcap) && scale / softcap <= 0x1p125f))
+    return fail(IPDV_EUNSUPPORTED, "softcap %g is too large or too small for scale %g", softcap, scale);
   if (q_stride < (int64_t)Hq * D) return fail(IPDV_EINVAL, "a row stride is shorter than the row");
   if (n_seq > 0 && (!q || !k_cache || !page_table || !ctx_lens || !cu_q)) return fail(IPDV_EINVAL, "null required pointer");
   const int size = dtype == IPDV_BF16 ? 2 : 4;
@@ -758,7 +761,8 @@ int verify_attn_masked(const void* q, int64_t q_stride, const void* k_new, const
   if (st != IPDV_OK) return st;
   st = masked_shape_check(n_seq, Hq, Hkv, D, max_q, max_pages, page_size, m.window, m.end_key != nullptr);
   if (st != IPDV_OK) return st;
-  st = masked_call_check(q, q_stride, k_cache, page_table, ctx_lens, cu_q, n_seq, Hq, Hkv, D, num_pages, scale, dtype);
+  st = masked_call_check(q, q_stride, k_cache, page_table, ctx_lens, cu_q, n_seq, Hq, Hkv, D, num_pages, scale, softcap,
+                         dtype);
   if (st != IPDV_OK) return st;
   if (n_seq == 0) return ok();
   if (!v_cache || !out) return fail(IPDV_EINVAL, "null required pointer");
@@ -789,7 +793,8 @@ int attn_mass(const void* q, int64_t q_stride, const void* k_cache, const float*
   if (st != IPDV_OK) return st;
   if ((int64_t)max_pages * page_size + max_q > 1 << 22)
     return fail(IPDV_EUNSUPPORTED, "max_pages_per_seq * page_size + max_q exceeds 2^22");
-  st = masked_call_check(q, q_stride, k_cache, page_table, ctx_lens, cu_q, n_seq, Hq, Hkv, D, num_pages, scale, dtype);
+  st = masked_call_check(q, q_stride, k_cache, page_table, ctx_lens, cu_q, n_seq, Hq, Hkv, D, num_pages, scale, softcap,
+                         dtype);
   if (st != IPDV_OK) return st;
   if (!std::isfinite(decay) || decay < 0.f) return fail(IPDV_EINVAL, "decay must be >= 0 and finite");
   if (n_seq == 0) return ok();

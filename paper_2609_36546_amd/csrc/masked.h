@@ -256,24 +256,52 @@ __device__ __forceinline__ void scores(const F& f, const Queries<DT, D, QT>& Q, 
   }
 }
 
+// tanh(z ln 2 / 2), to 8 2^-24 of itself: near 0 the series up to z^13 (1.8e-7 left out at the seam),
+// else 1 - 2 / (2^z + 1).
+__device__ __forceinline__ float tanh_of(float z) {
+#pragma clang fp contract(off)                   // an fma of two constants holds one in a register of the callers' loops
+  constexpr double h = 0.34657359027997264, h2 = h * h;
+  const float z2 = z * z;
+  float near = z2 * (float)(h * h2 * h2 * h2 * h2 * h2 * h2 * 21844. / 6081075.) - (float)(h * h2 * h2 * h2 * h2 * h2 * 1382. / 155925.);
+  near = fmaf(z2, near, (float)(h * h2 * h2 * h2 * h2 * 62. / 2835.));
+  near = fmaf(z2, near, (float)(h * h2 * h2 * h2 * -17. / 315.));
+  near = fmaf(z2, near, (float)(h * h2 * h2 * 2. / 15.));
+  near = fmaf(z2, near, (float)(h * h2 * -1. / 3.));
+  near = fmaf(z2, near, (float)h) * z;
+  asm volatile("" : "+v"(near), "+v"(z));        // one after the other: the callers have no registers for both
+  const float far = fmaf(__builtin_amdgcn_rcpf(fast_exp2(z) + 1.f), -2.f, 1.f);
+  return fabsf(z) < 1.4426950f ? near : far;
+}
+// Caps (by log2(e)) up to which bf16 calls take 1 - 2 / (e^2y + 1) everywhere: off by 2^-22 of the cap
+// near 0, 2e-5 in a score; with larger ones that would reach every probability (0.09 at a cap of 10^6).
+constexpr float kNearCap = 64.f * 1.4426950408889634f;
+
 // Raw products to modified scores in log2 units, plus a number per row.
 template <typename DT, int QT>
 __device__ __forceinline__ void modify(const WindowParams& a, const RowInfo (&row)[QT], const float (&plus)[QT], int k0, floatx4 (&s)[QT][2]) {
-  if (a.cap2 != 0.f) {
-    // tanh x = 1 - 2 / (e^2x + 1): infinities give +-1.  Off by 2^-23 of the cap near 0, which
-    // fp32 calls do not have.
+  if (sizeof(DT) == 2 && a.cap2 != 0.f && a.cap2 <= kNearCap) {
+    // tanh x = 1 - 2 / (e^2x + 1): infinities give +-1
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       const float top = a.cap2 + plus[t];
 #pragma unroll
+      for (int i = 0; i < 8; ++i)
+        s[t][i >> 2][i & 3] =
+            fmaf(__builtin_amdgcn_rcpf(fast_exp2(s[t][i >> 2][i & 3] * a.scale2) + 1.f), -2.f * a.cap2, top);
+    }
+  } else if (a.cap2 != 0.f) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float x = s[t][i >> 2][i & 3];
-        if constexpr (sizeof(DT) == 2)
-          s[t][i >> 2][i & 3] = fmaf(__builtin_amdgcn_rcpf(fast_exp2(x * a.scale2) + 1.f), -2.f * a.cap2, top);
-        else
+        if constexpr (sizeof(DT) == 2) {
+          s[t][i >> 2][i & 3] = fmaf(a.cap2, tanh_of(x * a.scale2), plus[t]);
+          __builtin_amdgcn_sched_barrier(0);           // one after the other: no registers for more
+        } else {
           s[t][i >> 2][i & 3] = fmaf(a.cap2, tanhf(x * a.cap_scale), plus[t]);
+        }
       }
-    }
   } else {
 #pragma unroll
     for (int t = 0; t < QT; ++t)

@@ -1,0 +1,59 @@
+"""Caps that scores stay far below, against 64-bit plain forms; caps that are refused."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_36546_amd import ops
+from tests import masked_reference as ref
+from tests.masked_reference import BF16, F32, Batch, check_attention, f64, limits
+from tests.test_gpu_masked import c_attn, run
+from tests.test_gpu_mass_evict import c_mass
+
+STEP = 2.0 ** -24
+
+
+def weights(q, K, lse, L, scale, lo, hi, cap):
+    """ref.weights, whose bound allows the cap's roundings, with the bound of uncapped scores: theirs
+    are not smaller, so it allows a capped one its own roundings."""
+    k, Hq, _ = q.shape
+    n, Hkv = K.shape[:2]
+    out, err = np.zeros((n, Hkv)), np.zeros((n, Hkv))
+    for h in range(Hq):
+        x, e = ref.scores(q, K, L, scale, cap, None, h)[0], ref.scores(q, K, L, scale, 0.0, None, h)[1]
+        for i in range(k):
+            at = slice(lo[i], hi[i])
+            w = np.exp(x[i, at] - lse[i, h])
+            out[at, h * Hkv // Hq] += w
+            err[at, h * Hkv // Hq] += w * (e[i, at] + 4 * STEP * (np.abs(lse[i, h]) + 4 + k * Hq // Hkv)) + 2.0 ** -126
+    return out, err
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("windows,Hq,Hkv,D", [([(700, 1), (40, 2)], 4, 2, 64), ([(300, 4), (5, 9)], 8, 2, 128),
+                                              ([(0, 150), (333, 40)], 16, 2, 128), ([(90, 70)], 4, 1, 64)])
+@pytest.mark.parametrize("cap", [65.0, 1e4, 1e6, 1e12, 2.0 ** 100])
+def test_a_cap_far_above_the_scores_changes_nothing(dt, windows, Hq, Hkv, D, cap):
+    """Attention and masses: the error of a score does not grow with the cap."""
+    b = Batch(windows, Hq, Hkv, D, 16, dt, seed=D, spread=1.5)
+    out, lse = run(b, softcap=cap)
+    pool = torch.zeros(b.kc.shape[0], Hkv, 16, device="cuda")
+    mass = f64(ops.attn_mass(b.q.cuda(), b.kc, lse, *b.args, out=pool, softcap=cap))
+    rounded = dt == BF16 and b.max_q * Hq // Hkv > 16
+    for i, (L, k) in enumerate(windows):
+        r, at = b.rows(i), limits(L, k)
+        given = f64(b.q[r]), b.K[i], b.V[i], L, b.scale, *at
+        want = (*ref.attention(*given, cap)[:3], ref.attention(*given)[3])
+        check_attention(out[r], lse[r], want, dt, L + k, rounded)
+        w, e = weights(f64(b.q[r]), b.K[i], f64(lse[r]), L, b.scale, *at, cap)
+        for p in range(L + k):
+            assert (np.abs(mass[int(b.table[i, p // 16]), :, p % 16] - w[p]) <= e[p] + 2 * STEP * w[p]).all()
+
+
+# --- refusals (no GPU) ---
+
+@pytest.mark.parametrize("kw", [dict(cap=3e38), dict(cap=1e-44), dict(cap=1e38, scale=0.1), dict(cap=1e-20, scale=1e20),
+                                dict(cap=1e12, scale=1e-30)])
+def test_caps_that_fp32_cannot_hold_are_refused(kw):
+    assert c_attn(**kw) == -2 and c_mass(**kw) == -2
+    assert b"softcap" in ops.lib().ipdv_last_error()
