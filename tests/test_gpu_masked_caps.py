@@ -1,4 +1,5 @@
-"""Caps that scores stay far below, against 64-bit plain forms; caps that are refused."""
+"""Caps that scores stay far below, and scores far beyond the cap, against 64-bit plain forms;
+caps that are refused."""
 import numpy as np
 import pytest
 import torch
@@ -48,6 +49,32 @@ def test_a_cap_far_above_the_scores_changes_nothing(dt, windows, Hq, Hkv, D, cap
         w, e = weights(f64(b.q[r]), b.K[i], f64(lse[r]), L, b.scale, *at, cap)
         for p in range(L + k):
             assert (np.abs(mass[int(b.table[i, p // 16]), :, p % 16] - w[p]) <= e[p] + 2 * STEP * w[p]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("windows,Hq,D", [([(300, 2)], 2, 64), ([(100, 40)], 8, 128)])
+@pytest.mark.parametrize("cap", [1.0, 50.0, 70.0, 1000.0])
+def test_scores_far_beyond_the_cap(dt, windows, Hq, D, cap):
+    """Scores of either sign, hundreds of caps and more: all are +-cap, also where e^2x has left fp32."""
+    b = Batch(windows, Hq, 2, D, 16, dt, seed=5)
+    (L, k), = windows
+    sign = np.where(np.random.default_rng(1).random((L + k, 2, 1)) < 0.5, -1.0, 1.0)
+    K = sign * (1 + 0.25 * np.abs(b.K[0]))
+    K = f64(torch.from_numpy(K).to(dt))
+    for p in range(L + k):
+        key = torch.from_numpy(K[p]).to(dt)
+        if p < L:
+            b.kc[b.table[0, p // 16], :, :, p % 16, :] = key.view(2, -1, 32).cuda()
+        else:
+            b.k_new[p - L] = key
+    b.q = torch.full_like(b.q, 1e5)
+    x = b.scale * np.einsum("rhd,nhd->rhn", f64(b.q)[:, :2], K)
+    assert (np.abs(x) > 200 * cap).all() and (x > 0).any() and (x < 0).any()
+    out, lse = run(b, softcap=cap)
+    want = ref.attention(f64(b.q), K, b.V[0], L, b.scale, *limits(L, k), cap)
+    # tanh is +-1 to the last bit: the cap's own factors and the roundings of the sums are left
+    check_attention(out, lse, (*want[:3], np.full_like(want[3], 4 * STEP * cap)), dt, L + k, dt == BF16 and k * Hq // 2 > 16)
 
 
 # --- refusals (no GPU) ---
