@@ -773,7 +773,8 @@ int verify_attn_masked(const void* q, int64_t q_row_stride, const void* k_new, c
  * with x and the rows' keys as in verify_attn_masked, whose lse the call takes.  j runs
  * over all positions below L_b + k_b, also those that no row sees; those of the window
  * itself (j >= L_b) start at 0, and so do all where mass_in is NULL.  Slots of other
- * positions are left as they are.  The window must be in the cache.
+ * positions are left as they are.  The window must be in the cache.  q and lse may both be
+ * NULL: no sequence has rows then, whatever cu_q holds.
  *
  * q, k_cache, the scores' and the batch's arguments as in verify_attn_masked; lse [T,
  * Hq] float; mass_in, mass_out [num_pages, Hkv, page_size] float, the same array or

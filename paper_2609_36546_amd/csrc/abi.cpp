@@ -793,14 +793,15 @@ int attn_mass(const void* q, int64_t q_stride, const void* k_cache, const float*
   if (st != IPDV_OK) return st;
   if ((int64_t)max_pages * page_size + max_q > 1 << 22)
     return fail(IPDV_EUNSUPPORTED, "max_pages_per_seq * page_size + max_q exceeds 2^22");
-  st = masked_call_check(q, q_stride, k_cache, page_table, ctx_lens, cu_q, n_seq, Hq, Hkv, D, num_pages, scale, softcap,
-                         dtype);
+  const bool no_rows = !q && !lse;       // of empty arrays: masses decay all the same
+  st = masked_call_check(no_rows ? k_cache : q, q_stride, k_cache, page_table, ctx_lens, cu_q, n_seq, Hq, Hkv, D, num_pages,
+                         scale, softcap, dtype);
   if (st != IPDV_OK) return st;
   if (!std::isfinite(decay) || decay < 0.f) return fail(IPDV_EINVAL, "decay must be >= 0 and finite");
   if (n_seq == 0) return ok();
-  if (!lse || !mass_out) return fail(IPDV_EINVAL, "null required pointer");
+  if ((!lse && !no_rows) || !mass_out) return fail(IPDV_EINVAL, "null required pointer");
   ipdv::AttnMaskedLaunch L{q, q_stride, nullptr, nullptr, const_cast<void*>(k_cache), nullptr, page_table, max_pages,
-                           ctx_lens, cu_q, seq_ids, n_seq, max_q, m, nullptr, const_cast<float*>(lse), Hq, Hkv, D,
+                           ctx_lens, cu_q, seq_ids, n_seq, no_rows ? 0 : max_q, m, nullptr, const_cast<float*>(lse), Hq, Hkv, D,
                            page_size, num_pages, scale, dtype == IPDV_BF16, nullptr, mass_in, mass_out, decay};
   hipError_t e = ipdv::launch_attn_mass(L, reinterpret_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return hip_fail("attn_mass launch", e);

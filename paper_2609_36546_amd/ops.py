@@ -1126,6 +1126,8 @@ def attn_mass(q, k_cache, lse, page_table, ctx_lens, cu_q, max_q: int, mass=None
     if validate:
         check_page_table(page_table, ctx_lens, cu_q, max_q, ps, P, seq_ids=seq_ids, n_seq=n_seq,
                          rows=T)
+    if T == 0:                        # no rows: the masses decay
+        qp = lp = None
     st = lib().attn_mass(qp, qs, kc, lp, table, max_pages, ctx, cu, ids, n_seq, max_q,
                          softcap, window, slopes_p, first_p, end_p,
                          None if mass is None else mass.data_ptr(), decay, mp, Hq, Hkv, D, ps, P,
