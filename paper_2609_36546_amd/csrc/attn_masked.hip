@@ -736,7 +736,7 @@ Plan plan_of(int n_seq, int Hq, int Hkv, int max_q, long slots, int window, bool
   long units = p.tiles;
   if (p.cut) {
     const long few = std::min((long)p.tiles, std::max(1L, (long)p.walk / p.per));
-    units = std::max(units, few * ((nb + p.walk - 1) / p.walk));
+    units = std::max(units, few * ((nb + least - 1) / least));
     if (p.tiles > few) units = p.tiles + nb / p.per + 1;
   }
   p.units = (int)units;
