@@ -846,7 +846,8 @@ size_t ipdv_verify_drafts_workspace_size(int T, int V, int B, int target_filtere
  *   token[b]     the token behind them, -1 for none (all accepted, or the window ended by EOS
  *                or by a row that cannot be drawn from)
  *   finished[b]  1 if the last of these is eos_id
- *   p_accept[r]  min(1, p(x) / q(x)), of every row; 0 where x < 0, and where p(x) = q(x) = 0
+ *   p_accept[r]  min(1, p(x) / q(x)), of every row of a window, also behind the one that ends it;
+ *                0 where x < 0, and where p(x) = q(x) = 0.  Rows outside every window are left
  *   logp[b]      ln p(token[b]), NaN without one (optional; NULL)
  * A row whose target logits (or, with a draft, its draft logits) hold NaN or +inf or nothing
  * above -inf, or whose temperature is negative or NaN, ends its window without a token; its

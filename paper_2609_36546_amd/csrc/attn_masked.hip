@@ -579,7 +579,10 @@ template <int D, bool WIDE> struct Loader {
   }
 };
 
-// NT: the ring's loads go past the caches' order of use.
+// NT: the ring's loads go past the caches' order of use.  A probability is rounded to bf16 once (outputs off
+// by 0.0020 to 0.0023 of their size, of which their own rounding is 0.0016); in two terms, as decode rows have
+// it, products take twice as long: 64 windows of eight 138 and 146 us, documents 58 and 63, packed prompts 80
+// and 96.
 template <int D, bool WIDE, int QT, bool NT>
 __global__ __launch_bounds__(256, 3) void masked_tile_kernel(MaskedParams a) {
   typedef Loader<D, WIDE> Load;

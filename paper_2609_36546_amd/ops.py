@@ -1176,8 +1176,8 @@ def kv_evict(k_cache, v_cache, mass, page_table, dst_table, ctx_lens, keep, n_si
     slots = (B, Hkv, max_dst * ps)
     if new_lens is None:
         new_lens = torch.empty(B, dtype=torch.int32, device=dev)
-    elif _sized(new_lens, "new_lens", torch.int32, dev, B) is None:
-        raise ValueError("new_lens must be [B]")
+    else:
+        _sized(new_lens, "new_lens", torch.int32, dev, B)
     if kept is None:
         kept = torch.empty(*slots, dtype=torch.int32, device=dev)
     else:
@@ -1236,7 +1236,8 @@ def verify_drafts(target_logits, draft_logits, prop_tok, cu_q, u_accept, u_draw,
     cu_q [B+1] int32, u_accept [T] and u_draw [B] float32 in [0, 1); the target's
     and the draft's filters per row, as in sample_logits.  Returns dict n_acc,
     token [B] int32, finished [B] uint8, p_accept [T] float32, logp [B] float32
-    (`outs` may hold these to be written)."""
+    (`outs` may hold these to be written).  p_accept of rows outside every window is
+    not written: in a new tensor it may be anything."""
     dev, dt = target_logits.device, target_logits.dtype
     code = _dtype_code(dt)
     tp, ts, (T, V) = _rows(target_logits, "target_logits", dt, dev, 2)
