@@ -808,8 +808,8 @@ int attn_mass(const void* q, int64_t q_row_stride, const void* k_cache, const fl
  * k_cache, v_cache as in verify_attn_paged (dtype, in/out), mass [num_pages, Hkv,
  * page_size] float (in/out); page_table [B, max_pages_per_seq], dst_table [B,
  * max_dst_pages] int32; ctx_lens, keep [B] int32; seq_ids [n_seq] int32 or NULL;
- * new_lens [B], kept [B, Hkv, max_dst_pages * page_size] int32 (entries of other sequences
- * are left).  The pages that dst_table names for positions 0 .. n - 1 must belong to no
+ * new_lens [B], which may be ctx_lens or keep itself, kept [B, Hkv, max_dst_pages * page_size]
+ * int32 (entries of other sequences are left).  The pages that dst_table names for positions 0 .. n - 1 must belong to no
  * other sequence and hold nothing that the call reads: not the sequence's own, either.
  * Slots behind position n - 1 are left as they are.
  * Requirements: D in {64, 128}; both tables times page_size <= 2^22; num_pages *

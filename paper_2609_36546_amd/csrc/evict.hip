@@ -100,7 +100,6 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictParams a) {
     for (int i = 0; i < kRun / 4; ++i) early[i] = ld16<f32x4>(m + 4 * i);
   }
   const Seq s = seq_of(a, slot);
-  if (g == 0 && tid == 0) a.new_lens[s.b] = s.n;
   int32_t* kept = a.kept + ((size_t)s.b * a.Hkv + g) * (unsigned)a.dst_slots;
   for (int i = s.n + tid; i < a.dst_slots; i += kThreads) kept[i] = -1;
   if (s.n == 0) return;
@@ -206,6 +205,9 @@ __global__ __launch_bounds__(256, 4) void evict_move_kernel(EvictParams a) {
   if (tid < kMove && i0 + tid < a.dst_slots)
     p = a.kept[((size_t)(a.seq_ids ? a.seq_ids[slot] : slot) * a.Hkv + g) * (unsigned)a.dst_slots + i0 + tid];
   const Seq s = seq_of(a, slot);
+  // Not before the selection has ended: new_lens may be ctx_lens or keep, and n stays the same with
+  // itself in the place of either.
+  if (i0 == 0 && g == 0 && tid == 0) a.new_lens[s.b] = s.n;
   const int n = min(s.n - i0, kMove);
   if (n <= 0) return;
   const int ps = a.page_size;
