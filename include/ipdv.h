@@ -860,7 +860,8 @@ size_t ipdv_verify_drafts_workspace_size(int T, int V, int B, int target_filtere
  *
  * target_logits, draft_logits [T, V] (dtype), *_row_stride elements from one row to the next
  * (>= V); prop_tok [T], cu_q [B+1] int32 (cu_q[B] <= T); u_accept [T], u_draw [B] float in [0,
- * 1); temperature ... draft_min_p [T], each NULL for off (as in sample_logits).
+ * 1); temperature ... draft_min_p [T], each NULL for off (as in sample_logits).  Outputs and
+ * inputs may not overlap, except that logp may be u_draw.
  * Requirements: 0 <= T < 2^22, 0 <= B < 2^22, 1 <= V <= 262144, T * V and B * V < 2^35;
  * workspace on a 16-byte boundary, written by the call: two calls that may overlap need one each.
  *

@@ -865,6 +865,12 @@ int verify_drafts(const void* target, int64_t target_stride, const void* draft, 
   if (!workspace || workspace_bytes < need)
     return fail(IPDV_EWORKSPACE, "workspace of %zu bytes needed (got %zu)", need, workspace ? workspace_bytes : (size_t)0);
   if (!on16(workspace)) return fail(IPDV_EUNSUPPORTED, "workspace must start on a 16-byte boundary");
+  // a sequence's first workgroup writes these while its others read the inputs
+  for (const void* out : {(const void*)n_acc, (const void*)token, (const void*)p_accept})
+    for (const void* in : {(const void*)prop_tok, (const void*)cu_q, (const void*)u_accept, (const void*)tf.temperature,
+                           (const void*)tf.top_k, (const void*)tf.top_p, (const void*)tf.min_p, (const void*)df.temperature,
+                           (const void*)df.top_k, (const void*)df.top_p, (const void*)df.min_p})
+      if (out && out == in) return fail(IPDV_EINVAL, "n_acc, token and p_accept may not be inputs of the call");
   ipdv::DraftLaunch L{target, target_stride, draft, draft_stride, T, V, B, prop_tok, cu_q, u_accept, u_draw, tf, df,
                       eos_id, n_acc, token, finished, p_accept, logp, dtype == IPDV_BF16, workspace};
   hipError_t e = ipdv::launch_verify_drafts(L, reinterpret_cast<hipStream_t>(hip_stream));
