@@ -262,7 +262,8 @@ __device__ __forceinline__ float tanh_of(float z) {
 #pragma clang fp contract(off)                   // an fma of two constants holds one in a register of the callers' loops
   constexpr double h = 0.34657359027997264, h2 = h * h;
   const float z2 = z * z;
-  float near = z2 * (float)(h * h2 * h2 * h2 * h2 * h2 * h2 * 21844. / 6081075.) - (float)(h * h2 * h2 * h2 * h2 * h2 * 1382. / 155925.);
+  float near = z2 * (float)(h * h2 * h2 * h2 * h2 * h2 * h2 * 21844. / 6081075.);
+  near = near - (float)(h * h2 * h2 * h2 * h2 * h2 * 1382. / 155925.);
   near = fmaf(z2, near, (float)(h * h2 * h2 * h2 * h2 * 62. / 2835.));
   near = fmaf(z2, near, (float)(h * h2 * h2 * h2 * -17. / 315.));
   near = fmaf(z2, near, (float)(h * h2 * h2 * 2. / 15.));

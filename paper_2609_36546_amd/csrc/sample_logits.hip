@@ -273,7 +273,8 @@ __device__ __forceinline__ void chunk_work(const SampleLogitsLaunch& p, int n_ch
     s_at[tid] = rec.start[tid] = cum - count;
     bool fits = cum <= kList;
     if (r.k > 0) fits &= cum - count < r.k;
-    if (r.min_p > 0.f && !(r.k > 0 && r.top_p < 1.f)) fits &= (float)tid <= 2.f - (CUTS ? (float)(r.width * r.temp) : (float)kWidth) * __logf(r.min_p);
+    const float per = CUTS ? (float)(r.width * r.temp) : (float)kWidth;      // bins of a factor of e
+    if (r.min_p > 0.f && !(r.k > 0 && r.top_p < 1.f)) fits &= (float)tid <= 2.f - per * __logf(r.min_p);
     const u64 first = __ballot(fits);             // all three hold for the first bins
     if (lane == 0) atomicAdd(&s_cover, __popcll(first));
   }

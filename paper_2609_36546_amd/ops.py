@@ -1144,8 +1144,8 @@ def kv_evict(k_cache, v_cache, mass, page_table, dst_table, ctx_lens, keep, n_si
 
     k_cache [P,Hkv,D/32,ps,32], v_cache [P,Hkv,D,ps] (bf16 or fp32), mass
     [P,Hkv,ps] float32, page_table [B,maxp], dst_table [B,maxd], ctx_lens and keep
-    [B] int32.  validate=True first checks both tables on host copies.  Returns
-    (new_lens [B], kept [B,Hkv,maxd*ps]) int32."""
+    [B] int32; new_lens may be ctx_lens or keep.  validate=True first checks both
+    tables on host copies.  Returns (new_lens [B], kept [B,Hkv,maxd*ps]) int32."""
     dev, dt = k_cache.device, k_cache.dtype
     code = _dtype_code(dt)
     ctx = _at(ctx_lens, "ctx_lens", torch.int32, dev, 1)
